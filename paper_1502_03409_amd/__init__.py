@@ -6,3 +6,4 @@ this package is its thin Python binding.  PyTorch only provides device memory an
 """
 from .binding import *  # noqa: F401,F403
 from .binding import lib, LcError, LcGeom, geom, geom_derive, workspace_bytes, plan_query, l2pool_lcn_plan_query  # noqa: F401
+from .head import *  # noqa: F401,F403

@@ -36,7 +36,7 @@ def _compile(src: Path) -> Path:
 def build(force: bool = True, jobs: int = 8, verbose: bool = False) -> Path:
     """Compile every ``csrc/*.hip`` for gfx950 and link ``liblc.so``."""
     srcs = sources()
-    deps = srcs + list(CSRC.glob("*.hpp")) + [HERE.parent / "include" / "lc.h"]
+    deps = srcs + list(CSRC.glob("*.hpp")) + list((HERE.parent / "include").glob("*.h"))
     if not force and LIB.exists() and all(LIB.stat().st_mtime >= d.stat().st_mtime for d in deps):
         return LIB
     OBJ.mkdir(exist_ok=True)

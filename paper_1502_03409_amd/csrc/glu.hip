@@ -1,0 +1,268 @@
+// Gated hidden layer: h = act(x wg^T) * (x wu^T) in one product kernel, and its gradients.
+//
+// Forward: a tile of the product covers the same outputs of both weight matrices (blocks of 32 rows of wg and wu alternate), so
+// the activation and the product happen on the accumulators.  Backward: one pass over dh and the saved g, u leaves both
+// gradients side by side, [N][2F] and transposed, and two products finish: dx = [dg du] [wg; wu] and [dwg; dwu] = [dg du]^T x.
+#include "head_gemm.hpp"
+#include "head_planes.hpp"
+
+namespace lc {
+namespace head {
+namespace {
+
+template <int ACT>
+__device__ __forceinline__ float act_value(float g) {
+    if constexpr (ACT == LC_ACT_GELU) return 0.5f * g * erfcf(-0.70710678118654752f * g);
+    const float sg = 1.f / (1.f + expf(-g));
+    return ACT == LC_ACT_SIGMOID ? sg : g * sg;
+}
+// act(g) and act'(g)
+template <int ACT>
+__device__ __forceinline__ void act_both(float g, float &a, float &da) {
+    if constexpr (ACT == LC_ACT_GELU) {
+        const float phi = 0.5f * erfcf(-0.70710678118654752f * g);
+        a = g * phi;
+        da = phi + g * (0.39894228040143268f * expf(-0.5f * g * g));
+    } else {
+        const float sg = 1.f / (1.f + expf(-g));
+        a = ACT == LC_ACT_SIGMOID ? sg : g * sg;
+        da = ACT == LC_ACT_SIGMOID ? sg * (1.f - sg) : sg * (1.f + g * (1.f - sg));
+    }
+}
+
+// What the forward pass leaves of g and u for the backward pass.  fp32 operands: the values.  bf16 operands: 16 bits each, of which
+// the first two are the sign and a mark: 0, five bits of exponent and nine of fraction for magnitudes from 2^-16 up to 2^16; 1, the eight
+// bits of the fp32 exponent and six of fraction for all others, zero, infinities and NaN among them.  bf16's eight significant bits
+// would show in the gradients (each would be rounded four times in all instead of twice); these ten do not.
+__device__ __forceinline__ float saved_value(float v) { return v; }
+__device__ __forceinline__ float saved_value(bf16_t c) {
+    const unsigned sign = (unsigned)(c & 0x8000u) << 16;
+    const unsigned near = ((unsigned)(c & 0x3fffu) << 14) + (111u << 23), far = (unsigned)(c & 0x3fffu) << 17;
+    return __builtin_bit_cast(float, sign | ((c & 0x4000u) ? far : near));
+}
+template <typename T> __device__ __forceinline__ T save_value(float v);
+template <> __device__ __forceinline__ float save_value<float>(float v) { return v; }
+template <> __device__ __forceinline__ bf16_t save_value<bf16_t>(float v) {
+    const unsigned u = __builtin_bit_cast(unsigned, v), sign = (u >> 16) & 0x8000u, mag = u & 0x7fffffffu;
+    const unsigned near = (mag + 0x1fffu + ((mag >> 14) & 1u)) >> 14;   // nearest, ties to even; a carry moves to the next exponent
+    if (near >= (111u << 9) && near < (143u << 9)) return (bf16_t)(sign | (near - (111u << 9)));
+    const unsigned far = mag > 0x7f800000u ? (mag >> 17) | 0x20u          // NaN
+                                           : (mag + 0xffffu + ((mag >> 17) & 1u)) >> 17;
+    return (bf16_t)(sign | 0x4000u | far);
+}
+template <typename T>
+__device__ __forceinline__ void save4(T *row, int n, int width, bool vec, const float (&v)[4]) {
+    if constexpr (sizeof(T) == 4) {
+        store4(row, n, width, vec, v);
+    } else {
+        const u16x4 c = {save_value<T>(v[0]), save_value<T>(v[1]), save_value<T>(v[2]), save_value<T>(v[3])};
+        if (vec && n + 3 < width) {
+            *(u16x4 *)(row + n) = c;
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (n + r < width) row[n + r] = c[r];
+        }
+    }
+}
+
+// blocks j = 0, 2, .. of a wave are g, blocks 1, 3, .. the u of the same outputs
+template <typename T, int ACT>
+struct GluEpi {
+    T *h, *gu;   // gu may be null
+    int F;
+    template <int MT, int NT>
+    __device__ __forceinline__ void run(const f32x16 (&acc)[MT][NT], int m0, int n0, int lane, int M, int) const {
+        static_assert(NT % 2 == 0, "g and u of an output sit in neighbouring blocks");
+        const bool vec = F % 4 == 0;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            const int m = m0 + 32 * i + (lane & 31);
+            if (m >= M) continue;
+#pragma unroll
+            for (int j = 0; j < NT; j += 2)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int f = n0 / 2 + 16 * j + 8 * q + 4 * (lane >> 5);
+                    float g[4], u[4], v[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        g[r] = acc[i][j][4 * q + r];
+                        u[r] = acc[i][j + 1][4 * q + r];
+                        v[r] = act_value<ACT>(g[r]) * u[r];
+                    }
+                    store4(h + (long long)m * F, f, F, vec, v);
+                    if (gu) {
+                        save4(gu + (long long)m * 2 * F, f, F, vec, g);
+                        save4(gu + (long long)m * 2 * F + F, f, F, vec, u);
+                    }
+                }
+        }
+    }
+};
+
+// column c < Fp: dg, column c >= Fp: du (zeros where a half is padded)
+template <typename T, int ACT>
+struct GluGrad {
+    const T *dh, *gu;
+    int N, F, Fp;
+    __device__ bool idle(int) const { return false; }
+    __device__ float operator()(int r, int c) const {
+        const bool second = c >= Fp;
+        const int f = second ? c - Fp : c;
+        if (r >= N || f >= F) return 0.f;
+        const float d = widen<T>(dh[(long long)r * F + f]), g = saved_value(gu[(long long)r * 2 * F + f]);
+        float a, da;
+        act_both<ACT>(g, a, da);
+        return second ? d * a : d * saved_value(gu[(long long)r * 2 * F + F + f]) * da;
+    }
+};
+
+template <typename T>
+__global__ __launch_bounds__(256) void fill_zero_kernel(T *p, long long n) {
+    for (long long i = blockIdx.x * 256LL + threadIdx.x; i < n; i += gridDim.x * 256LL) p[i] = 0;
+}
+template <typename T>
+int launch_fill_zero(T *p, long long n, hipStream_t s) {
+    const LaunchPlan pl = make_plan("glu_fill", {}, {}, dim3((unsigned)std::min<long long>((n + 255) / 256, 4096)), 256, 0);
+    LC_LAUNCH(pl, "glu_bwd (no rows)", (fill_zero_kernel<T>), s, p, n);
+    return LC_OK;
+}
+
+template <typename T>
+struct GluScratch {
+    static constexpr int PL = Planes<T>::N;
+    int Np, Dp, Fp;
+    bool direct;   // the operands of the forward product are used where they are
+    bf16_t *x, *w, *wT, *xT, *dgu, *dguT;
+    GluScratch(Scratch &sc, int N, int D, int F, bool backward) {
+        Np = (int)round_up(N, kStep), Dp = (int)round_up(D, kStep), Fp = (int)round_up(F, kStep);
+        direct = PL == 1 && D == Dp;
+        x = direct ? nullptr : sc.take<bf16_t>((long long)PL * N * Dp);
+        w = direct ? nullptr : sc.take<bf16_t>((long long)PL * 2 * F * Dp);
+        if (!backward) return;
+        wT = sc.take<bf16_t>((long long)PL * D * 2 * Fp);
+        xT = sc.take<bf16_t>((long long)PL * D * Np);
+        dgu = sc.take<bf16_t>((long long)PL * N * 2 * Fp);
+        dguT = sc.take<bf16_t>((long long)PL * 2 * Fp * Np);
+    }
+};
+
+template <typename T, int ACT>
+int glu_forward(const T *x, const T *wg, const T *wu, T *h, T *gu, int N, int D, int F, void *ws, hipStream_t s) {
+    constexpr int PL = Planes<T>::N;
+    Scratch sc(ws);
+    const GluScratch<T> g(sc, N, D, F, false);
+    Operand A = {(const bf16_t *)x, (const bf16_t *)x, D, 0, N}, B = {(const bf16_t *)wg, (const bf16_t *)wu, D, 0, F};
+    if (!g.direct) {
+        const long long px = (long long)N * g.Dp, pw = 2LL * F * g.Dp;
+        if (int rc = launch_planes<PL>("glu_fwd (x)", Stored<T>{x, D, N, D, nullptr, nullptr}, PlanesOut{g.x, g.Dp, px}, N, D, N, 0, s))
+            return rc;
+        for (int k = 0; k < 2; ++k)
+            if (int rc = launch_planes<PL>("glu_fwd (w)", Stored<T>{k ? wu : wg, D, F, D, nullptr, nullptr},
+                                           PlanesOut{g.w + (long long)k * F * g.Dp, g.Dp, pw}, F, D, F, 0, s))
+                return rc;
+        A = {g.x, g.x, g.Dp, px, N};
+        B = {g.w, g.w + (long long)F * g.Dp, g.Dp, pw, F};
+    }
+    const Shape sh = {N, 2 * (int)round_up(F, 32), g.Dp, nullptr, 0, nullptr, 0};
+    return launch_gemm<PL, true>("glu_fwd", A, B, sh, GluEpi<T, ACT>{h, gu, F}, s);
+}
+
+template <typename T, int ACT>
+int glu_backward(const T *x, const T *wg, const T *wu, const T *gu, const T *dh, T *dx, T *dwg, T *dwu, int N, int D, int F,
+                 void *ws, hipStream_t s) {
+    constexpr int PL = Planes<T>::N;
+    if (N == 0) {
+        if (int rc = launch_fill_zero(dwg, (long long)F * D, s)) return rc;
+        return launch_fill_zero(dwu, (long long)F * D, s);
+    }
+    Scratch sc(ws);
+    const GluScratch<T> g(sc, N, D, F, true);
+    const int F2 = 2 * g.Fp;
+    const long long pd = (long long)N * F2, pdT = (long long)F2 * g.Np, pxT = (long long)D * g.Np, pwT = (long long)D * F2;
+    if (int rc = launch_planes<PL>("glu_bwd (gradients)", GluGrad<T, ACT>{dh, gu, N, F, g.Fp},
+                                   PlanesOut{g.dgu, F2, pd, g.dguT, g.Np, pdT}, N, F2, N, F2, s))
+        return rc;
+    if (int rc = launch_planes<PL>("glu_bwd (x)", Stored<T>{x, D, N, D, nullptr, nullptr}, PlanesOut{nullptr, 0, 0, g.xT, g.Np, pxT},
+                                   N, D, 0, D, s))
+        return rc;
+    if (dx) {
+        for (int k = 0; k < 2; ++k)
+            if (int rc = launch_planes<PL>("glu_bwd (w)", Stored<T>{k ? wu : wg, D, F, D, nullptr, nullptr},
+                                           PlanesOut{nullptr, 0, 0, g.wT + (long long)k * g.Fp, F2, pwT}, F, D, 0, D, s))
+                return rc;
+        const Shape sh = {N, D, F2, nullptr, 0, nullptr, 0};
+        if (int rc = launch_gemm<PL, false>("glu_bwd (dx)", Operand{g.dgu, g.dgu, F2, pd, N}, Operand{g.wT, g.wT, F2, pwT, D}, sh,
+                                            StoreEpi<T>{dx, nullptr, 0x7fffffff, N, 0, D, nullptr, nullptr, nullptr}, s))
+            return rc;
+    }
+    const Shape sh = {F2, D, g.Np, nullptr, 0, nullptr, 0};
+    return launch_gemm<PL, false>("glu_bwd (dw)", Operand{g.dguT, g.dguT, g.Np, pdT, F2}, Operand{g.xT, g.xT, g.Np, pxT, D}, sh,
+                                  StoreEpi<T>{dwg, dwu, g.Fp, F, F, D, nullptr, nullptr, nullptr}, s);
+}
+
+template <typename Fn>
+int by_act(int act, const Fn &fn) {
+    switch (act) {
+        case LC_ACT_SIGMOID: return fn(std::integral_constant<int, LC_ACT_SIGMOID>());
+        case LC_ACT_SILU: return fn(std::integral_constant<int, LC_ACT_SILU>());
+        default: return fn(std::integral_constant<int, LC_ACT_GELU>());
+    }
+}
+
+bool glu_sizes(int32_t N, int32_t D, int32_t F, int dtype) {
+    return head_rows(N) && head_width(D) && head_width(F) && (dtype == LC_F32 || dtype == LC_BF16);
+}
+
+}  // namespace
+}  // namespace head
+}  // namespace lc
+
+using namespace lc;
+using namespace lc::head;
+
+extern "C" {
+
+size_t glu_workspace_bytes(int32_t N, int32_t D, int32_t F, int dtype, int backward) {
+    if (!glu_sizes(N, D, F, dtype)) return 0;
+    Scratch sc(nullptr);
+    if (dtype == LC_BF16) (void)GluScratch<bf16_t>(sc, N, D, F, backward != 0);
+    else (void)GluScratch<float>(sc, N, D, F, backward != 0);
+    return sc.used;
+}
+
+int glu_fwd(const void *x, const void *wg, const void *wu, void *h, void *gu, int32_t N, int32_t D, int32_t F, int act,
+            int dtype, void *ws, size_t ws_bytes, void *hip_stream) {
+    if (!glu_sizes(N, D, F, dtype) || act < LC_ACT_SIGMOID || act > LC_ACT_GELU) return LC_EINVAL;
+    if (!wg || !wu || (N && (!x || !h))) return LC_ENULL;
+    for (const void *p : {x, wg, wu, (const void *)h, (const void *)gu, (const void *)ws})
+        if (!ptr_aligned16(p)) return LC_EALIGN;
+    if (!ws || ws_bytes < glu_workspace_bytes(N, D, F, dtype, 0)) return LC_EWORKSPACE;
+    if (N == 0) return LC_OK;
+    return by_act(act, [&](auto a) {
+        hipStream_t s = (hipStream_t)hip_stream;
+        if (dtype == LC_BF16)
+            return glu_forward<bf16_t, a>((const bf16_t *)x, (const bf16_t *)wg, (const bf16_t *)wu, (bf16_t *)h, (bf16_t *)gu, N, D, F, ws, s);
+        return glu_forward<float, a>((const float *)x, (const float *)wg, (const float *)wu, (float *)h, (float *)gu, N, D, F, ws, s);
+    });
+}
+
+int glu_bwd(const void *x, const void *wg, const void *wu, const void *gu, const void *dh, void *dx, void *dwg, void *dwu,
+            int32_t N, int32_t D, int32_t F, int act, int dtype, void *ws, size_t ws_bytes, void *hip_stream) {
+    if (!glu_sizes(N, D, F, dtype) || act < LC_ACT_SIGMOID || act > LC_ACT_GELU) return LC_EINVAL;
+    if (!wg || !wu || !dwg || !dwu || (N && (!x || !gu || !dh))) return LC_ENULL;
+    for (const void *p : {x, wg, wu, gu, dh, (const void *)dx, (const void *)dwg, (const void *)dwu, (const void *)ws})
+        if (!ptr_aligned16(p)) return LC_EALIGN;
+    if (!ws || ws_bytes < glu_workspace_bytes(N, D, F, dtype, 1)) return LC_EWORKSPACE;
+    return by_act(act, [&](auto a) {
+        hipStream_t s = (hipStream_t)hip_stream;
+        if (dtype == LC_BF16)
+            return glu_backward<bf16_t, a>((const bf16_t *)x, (const bf16_t *)wg, (const bf16_t *)wu, (const bf16_t *)gu, (const bf16_t *)dh,
+                                           (bf16_t *)dx, (bf16_t *)dwg, (bf16_t *)dwu, N, D, F, ws, s);
+        return glu_backward<float, a>((const float *)x, (const float *)wg, (const float *)wu, (const float *)gu, (const float *)dh, (float *)dx,
+                                      (float *)dwg, (float *)dwu, N, D, F, ws, s);
+    });
+}
+
+}  // extern "C"

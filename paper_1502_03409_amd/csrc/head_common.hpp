@@ -1,0 +1,95 @@
+// What the kernels of the supervised head share: operand planes, bf16 conversion, workspaces, host checks.
+#pragma once
+#include "../../include/lc_head.h"
+#include <algorithm>
+#include <type_traits>
+
+#include "lc_common.hpp"
+
+namespace lc {
+namespace head {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4v __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned short u16x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ bf16_t to_bf16(float v) { return __builtin_bit_cast(bf16_t, (__bf16)v); }   // nearest, ties to even
+__device__ __forceinline__ float from_bf16(bf16_t v) { return bf16_lo(v); }
+template <typename T> __device__ __forceinline__ float widen(T v);
+template <> __device__ __forceinline__ float widen<float>(float v) { return v; }
+template <> __device__ __forceinline__ float widen<bf16_t>(bf16_t v) { return from_bf16(v); }
+template <typename T> __device__ __forceinline__ T narrow(float v);
+template <> __device__ __forceinline__ float narrow<float>(float v) { return v; }
+template <> __device__ __forceinline__ bf16_t narrow<bf16_t>(float v) { return to_bf16(v); }
+
+// The three bf16 parts of an fp32 value: v = p[0] + p[1] + p[2] exactly, down to bits of 2^-133, the smallest that bf16 has.  Each part is the nearest bf16 to what remains, so the remainders have eight bits less each time; the first part of
+// a value that would round to infinity is cut instead.  An infinity or NaN is its own first part, the others zero.
+__device__ __forceinline__ void split3(float v, bf16_t (&p)[3]) {
+    const unsigned u = __builtin_bit_cast(unsigned, v);
+    if ((u & 0x7f800000u) == 0x7f800000u) {
+        p[0] = (bf16_t)((u >> 16) | ((u & 0xffffu) ? 0x40u : 0u));   // a NaN whose payload lies in the low half stays one
+        p[1] = p[2] = 0;
+        return;
+    }
+    p[0] = to_bf16(v);
+    if ((p[0] & 0x7f80u) == 0x7f80u) p[0] = (bf16_t)(u >> 16);
+    float r = v - from_bf16(p[0]);
+    p[1] = to_bf16(r);
+    r -= from_bf16(p[1]);
+    p[2] = to_bf16(r);
+}
+
+// Number of bf16 planes that hold an operand of storage type T, and of plane pairs whose products count.
+template <typename T> struct Planes;
+template <> struct Planes<bf16_t> { static constexpr int N = 1, PAIRS = 1; };
+template <> struct Planes<float> { static constexpr int N = 3, PAIRS = 6; };
+
+// Rows of bf16 values contiguous along the contraction, whose length is a multiple of kStep with zeros at the end: row r of
+// plane q starts at p0 + q * plane + r * ld.  With two matrices side by side (pair), see pair_row().
+constexpr int kStep = 64;
+struct Operand {
+    const bf16_t *p0, *p1;
+    long long ld, plane;
+    int rows;   // rows that exist (of each matrix)
+};
+// Virtual rows of a pair: blocks of 32 rows of the first matrix alternate with the same 32 rows of the second, so that any
+// tile of 64 or more holds both values of every output it covers.
+__device__ __host__ __forceinline__ int pair_row(int v, int *second) {
+    *second = (v >> 5) & 1;
+    return (v >> 6) * 32 + (v & 31);
+}
+template <bool PAIR>
+__device__ __forceinline__ const bf16_t *operand_row(const Operand &o, int r) {   // rows beyond the last read the last
+    if constexpr (PAIR) {
+        int second;
+        const int f = pair_row(r, &second);
+        return (second ? o.p1 : o.p0) + (long long)min(f, o.rows - 1) * o.ld;
+    } else {
+        return o.p0 + (long long)min(r, o.rows - 1) * o.ld;
+    }
+}
+
+inline long long round_up(long long a, long long b) { return (a + b - 1) / b * b; }
+
+// Hands out 256-byte aligned pieces of a workspace; with a null base it only counts.
+struct Scratch {
+    char *base;
+    size_t used = 0;
+    explicit Scratch(void *ws) : base((char *)ws) {}
+    template <typename T>
+    T *take(long long n) {
+        T *p = base ? (T *)(base + used) : nullptr;
+        used += ((size_t)n * sizeof(T) + 255) / 256 * 256;
+        return p;
+    }
+};
+
+// Sizes of a head's matrices: widths 1 .. 2^20, rows 0 .. 2^24, so that every index within a row or a tile has 31 bits and
+// every product of two sizes is formed in 64.
+inline bool head_width(long long v) { return v >= 1 && v <= (1 << 20); }
+inline bool head_rows(long long v) { return v >= 0 && v <= (1 << 24); }
+
+}  // namespace head
+}  // namespace lc

@@ -1,0 +1,369 @@
+// Softmax cross entropy over a vocabulary, projection included, with its gradients.
+//
+// The scores l = x w^T are never stored as such: each tile of the product leaves, per row, its largest score and the sum of
+// the exponentials below it, and a small kernel joins the tiles.  The target's own score is kept out of both and apart: with z the
+// logarithm of the other words' sum minus the target's score, loss = log(1 + e^z) and p(target) - 1 = -1 / (1 + e^-z), neither of
+// which cancels in rows that are already learned.  With gradients a tile also leaves the
+// exponentials themselves (bf16 operands: relative to the tile's largest score, in fp16 times 2^15, which holds eleven bits of
+// all above 2^-29, so that the one rounding to bf16 that follows is the only one that shows; fp32: the scores), for a bounded number of rows at a time; one pass turns them into d[n][v] = s[n] (p[n][v] - [v = t]) in
+// place and transposed, and two products give dx = d w and dw = d^T x.
+//
+// Masked rows take no part: the rows that count are gathered first, and every kernel runs over as many as there are.
+#include "head_gemm.hpp"
+#include "head_planes.hpp"
+
+namespace lc {
+namespace head {
+namespace {
+
+constexpr int kWaveCols = 64;               // columns of the vocabulary that share one entry of the row statistics
+constexpr long long kBlockBytes = 2LL << 30;   // exponentials kept at a time
+
+struct Rows {
+    int *count;
+    int *index, *target;   // by position among the rows that count
+    float *scale, *tl;     // weight in the cost, but for the factor *unit; the target's score
+    float *unit;           // 1 / count for the mean, else 1: the results' factor, so that d = p - [v = t] is what is rounded
+    float *lse, *dt, *loss;   // logsumexp; p(target) - 1; loss
+};
+
+// Positions of the rows that count, in order; loss 0 where masked.  One workgroup: a scan over 1024 rows at a time.
+__global__ __launch_bounds__(1024) void rows_kernel(const int64_t *target, const float *scale, float *loss, int N, int V, Rows o) {
+    __shared__ int part[16];
+    __shared__ int total;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (threadIdx.x == 0) total = 0;
+    __syncthreads();
+    for (int n0 = 0; n0 < N; n0 += 1024) {
+        const int n = n0 + threadIdx.x;
+        const long long t = n < N ? target[n] : -1;
+        const bool in = t >= 0;
+        const unsigned long long mask = __ballot(in);
+        if (lane == 0) part[wave] = __popcll(mask);
+        __syncthreads();
+        int at = total;
+        for (int w = 0; w < wave; ++w) at += part[w];
+        at += __popcll(mask & ((1ull << lane) - 1));
+        if (in) {
+            o.index[at] = n;
+            o.target[at] = t < V ? (int)t : -1;
+            o.tl[at] = __builtin_nanf("");      // stays where no column is the target
+            o.scale[at] = t >= V ? __builtin_nanf("") : scale ? scale[n] : 1.f;
+        } else if (n < N) {
+            loss[n] = 0.f;
+        }
+        __syncthreads();
+        if (threadIdx.x == 0)
+            for (int w = 0; w < 16; ++w) total += part[w];
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) {
+        *o.count = total;
+        *o.unit = scale ? 1.f : 1.f / (float)max(total, 1);
+    }
+}
+
+template <typename T> struct Kept;   // what a tile leaves for the gradient
+template <> struct Kept<float> { typedef float V; };
+template <> struct Kept<bf16_t> { typedef _Float16 V; };
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ void keep4(float *row, int n, const float (&v)[4]) {
+    *(f32x4 *)(row + n) = (f32x4){v[0], v[1], v[2], v[3]};
+}
+__device__ __forceinline__ void keep4(_Float16 *row, int n, const float (&v)[4]) {
+    *(f16x4 *)(row + n) = (f16x4){(_Float16)(v[0] * 32768.f), (_Float16)(v[1] * 32768.f), (_Float16)(v[2] * 32768.f), (_Float16)(v[3] * 32768.f)};
+}
+
+// Per wave and row: the largest score, the sum of exponentials (both without the target), the target's score, and with KEEP what
+// the gradient needs.
+template <typename T, bool KEEP>
+struct XentEpi {
+    float2 *stats;       // [tile of kWaveCols columns][stats_ld]
+    long long stats_ld;
+    const int *target;
+    float *tl;
+    typename Kept<T>::V *keep;   // [M][ld], ld a multiple of 64 that holds all columns: exponentials (bf16) or scores (fp32)
+    long long ld;
+    template <int MT, int NT>
+    __device__ __forceinline__ void run(const f32x16 (&acc)[MT][NT], int m0, int n0, int lane, int M, int V) const {
+        static_assert(NT * 32 == kWaveCols, "one entry of the statistics per wave");
+        const int h = lane >> 5;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            const int m = m0 + 32 * i + (lane & 31);
+            const int t = m < M ? target[m] : -1;
+            float top = -__builtin_inff();
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int n = n0 + 32 * j + 8 * (e >> 2) + 4 * h + (e & 3);
+                    if (n == t) tl[m] = acc[i][j][e];
+                    else if (n < V) top = fmaxf(top, acc[i][j][e]);
+                }
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float base = top == -__builtin_inff() ? 0.f : top;   // all scores -inf: exponentials of 0, not of NaN
+            float sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int n = n0 + 32 * j + 8 * q + 4 * h;
+                    float v[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float l = acc[i][j][4 * q + r];
+                        const float e = sizeof(T) == 4 ? expf(l - base) : __expf(l - base);
+                        if (n + r < V && n + r != t) sum += e;
+                        v[r] = sizeof(T) == 4 ? l : e;
+                    }
+                    if (KEEP && m < M && n < ld) keep4(keep + m * ld, n, v);
+                }
+            sum += __shfl_xor(sum, 32);
+            if (m < M && h == 0) stats[(n0 / kWaveCols) * stats_ld + m] = make_float2(top, sum);
+        }
+    }
+};
+
+// Joins the tiles of 16 rows: 16 threads a row, each over every 16th tile, in a fixed order.
+__global__ __launch_bounds__(256) void lse_kernel(const float2 *stats, long long stats_ld, int tiles, Rows o, int first, int most,
+                                                  float *loss) {
+    const int M = live(most, o.count, first);
+    const int m = blockIdx.x * 16 + (threadIdx.x & 15), part = threadIdx.x >> 4;
+    __shared__ float tops[16][17], sums[16][17];
+    float top = -__builtin_inff(), sum = 0.f;
+    if (m < M) {
+        for (int t = part; t < tiles; t += 16) {
+            const float2 s = stats[t * stats_ld + m];
+            if (s.x > top) {
+                sum = sum * expf(top - s.x) + s.y;
+                top = s.x;
+            } else if (s.x != -__builtin_inff()) {
+                sum += s.y * expf(s.x - top);
+            } else {
+                sum += s.y * 0.f;   // nothing, unless it is NaN
+            }
+        }
+    }
+    tops[part][threadIdx.x & 15] = top;
+    sums[part][threadIdx.x & 15] = sum;
+    __syncthreads();
+    if (part == 0 && m < M) {
+        for (int p = 1; p < 16; ++p) top = fmaxf(top, tops[p][threadIdx.x]);
+        sum = 0.f;
+        for (int p = 0; p < 16; ++p) {
+            const float tp = tops[p][threadIdx.x];
+            sum += sums[p][threadIdx.x] * (tp == -__builtin_inff() ? 0.f : expf(tp - top));
+        }
+        const float tl = o.tl[first + m];
+        const float z = top == -__builtin_inff() && sum == 0.f ? top : top + logf(sum) - tl;
+        const float e = expf(-fabsf(z));
+        float v = fmaxf(z, 0.f) + log1pf(e), dt = -(z > 0.f ? 1.f : e) / (1.f + e);
+        if (!(z == z) || !(tl < __builtin_inff())) v = dt = __builtin_nanf("");   // as in inf - inf
+        o.lse[first + m] = tl + v;
+        o.dt[first + m] = dt;
+        o.loss[first + m] = v;
+        loss[o.index[first + m]] = v;
+    }
+}
+
+__global__ __launch_bounds__(1024) void cost_kernel(Rows o, float *cost) {
+    __shared__ double part[1024];
+    double s = 0.0;
+    const int n = *o.count;
+    for (int m = threadIdx.x; m < n; m += 1024) s += (double)o.scale[m] * (double)o.loss[m];
+    part[threadIdx.x] = s;
+    __syncthreads();
+    for (int w = 512; w; w >>= 1) {
+        if (threadIdx.x < w) part[threadIdx.x] += part[threadIdx.x + w];
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) *cost = (float)(part[0] * (double)*o.unit);
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void zero_masked_kernel(const int64_t *target, T *dx, int D) {
+    const int n = blockIdx.x;
+    if (target[n] >= 0) return;
+    for (int d = threadIdx.x; d < D; d += 256) dx[(long long)n * D + d] = 0;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void zero_kernel(T *p, long long n, float *cost) {
+    if (cost && blockIdx.x == 0 && threadIdx.x == 0) *cost = 0.f;
+    for (long long i = blockIdx.x * 256LL + threadIdx.x; i < n; i += gridDim.x * 256LL) p[i] = 0;
+}
+
+// d[m][v] of the rows first .. of the block
+template <typename T>
+struct XentGrad {
+    const typename Kept<T>::V *keep;
+    long long ld;
+    const float2 *stats;
+    long long stats_ld;
+    Rows o;
+    int first, most, V;
+    __device__ bool idle(int r0) const { return r0 >= (live(most, o.count, first) + 63) / 64 * 64; }
+    __device__ float operator()(int m, int v) const {
+        if (v >= V || m >= live(most, o.count, first)) return 0.f;
+        const int r = first + m;
+        const float lse = o.lse[r], s = o.scale[r];
+        if (v == o.target[r]) return s * o.dt[r];
+        const float k = keep[m * ld + v];
+        if constexpr (sizeof(T) == 4) return s * expf(k - lse);
+        else return s * (k * (__expf(stats[(v / kWaveCols) * stats_ld + m].x - lse) * 0x1p-15f));
+    }
+};
+
+template <typename T>
+struct XentScratch {
+    static constexpr int PL = Planes<T>::N;
+    int Np, Dp, Vp, tiles, block, blocks;   // rows of a block (a multiple of 64), number of blocks
+    bool direct;                            // w is used where it is
+    Rows rows;
+    bf16_t *x, *w, *wT, *xT, *d, *dT;
+    float2 *stats;
+    float *scores, *sum;
+    XentScratch(Scratch &sc, int N, int D, int V, bool grads) {
+        Np = (int)round_up(N, kStep), Dp = (int)round_up(D, kStep), Vp = (int)round_up(V, kStep);
+        direct = PL == 1 && D == Dp;
+        tiles = Vp / kWaveCols;
+        block = Np;
+        if (grads) block = (int)std::min<long long>(Np, std::max<long long>(kStep, kBlockBytes / ((long long)Vp * sizeof(T)) / 256 * 256));
+        blocks = Np ? (Np + block - 1) / block : 0;
+        rows.count = sc.take<int>(1);
+        rows.unit = sc.take<float>(1);
+        rows.index = sc.take<int>(N);
+        rows.target = sc.take<int>(N);
+        rows.scale = sc.take<float>(N);
+        rows.tl = sc.take<float>(N);
+        rows.lse = sc.take<float>(N);
+        rows.dt = sc.take<float>(N);
+        rows.loss = sc.take<float>(N);
+        x = sc.take<bf16_t>((long long)PL * N * Dp);
+        w = direct ? nullptr : sc.take<bf16_t>((long long)PL * V * Dp);
+        stats = sc.take<float2>((long long)tiles * block);
+        if (!grads) return;
+        wT = sc.take<bf16_t>((long long)PL * D * Vp);
+        xT = sc.take<bf16_t>((long long)PL * D * Np);
+        d = sc.take<bf16_t>((long long)PL * block * Vp);
+        dT = sc.take<bf16_t>((long long)PL * V * block);
+        scores = PL == 3 ? sc.take<float>((long long)block * Vp) : nullptr;
+        sum = blocks > 1 ? sc.take<float>((long long)V * D) : nullptr;
+    }
+};
+
+template <typename T>
+int xent(const T *x, const T *w, const int64_t *target, const float *scale, float *loss, float *cost, T *dx, T *dw, int N, int D, int V,
+         bool grads, void *ws, hipStream_t s) {
+    constexpr int PL = Planes<T>::N;
+    Scratch sc(ws);
+    const XentScratch<T> g(sc, N, D, V, grads);
+    if (N == 0) {
+        const long long n = grads ? (long long)V * D : 0;
+        const LaunchPlan p = make_plan("xent_zero", {}, {}, dim3((unsigned)std::min<long long>((n + 256) / 256, 4096)), 256, 0);
+        LC_LAUNCH(p, "xent (no rows)", (zero_kernel<T>), s, dw, n, cost);
+        return LC_OK;
+    }
+    const LaunchPlan one = make_plan("xent_rows", {}, {N}, dim3(1), 1024, 0);
+    LC_LAUNCH(one, "xent (rows)", rows_kernel, s, target, scale, loss, N, V, g.rows);
+    const long long px = (long long)N * g.Dp, pw = (long long)V * g.Dp, pwT = (long long)D * g.Vp, pxT = (long long)D * g.Np;
+    if (int rc = launch_planes<PL>("xent (x)", Stored<T>{x, D, N, D, g.rows.index, g.rows.count},
+                                   PlanesOut{g.x, g.Dp, px, grads ? g.xT : nullptr, g.Np, pxT}, N, D, N, D, s))
+        return rc;
+    if (!g.direct || grads)
+        if (int rc = launch_planes<PL>("xent (w)", Stored<T>{w, D, V, D, nullptr, nullptr},
+                                       PlanesOut{g.w, g.Dp, pw, grads && dx ? g.wT : nullptr, g.Vp, pwT}, V, D, V, D, s))
+            return rc;
+    const Operand W = g.direct ? Operand{(const bf16_t *)w, (const bf16_t *)w, D, 0, V} : Operand{g.w, g.w, g.Dp, pw, V};
+    if (grads && dx) {
+        const LaunchPlan p = make_plan("xent_zero_masked", {}, {N}, dim3(N), 256, 0);
+        LC_LAUNCH(p, "xent (masked rows)", (zero_masked_kernel<T>), s, target, dx, D);
+    }
+    for (int b = 0; b < g.blocks; ++b) {
+        const int first = b * g.block, most = std::min(g.block, N - first);
+        const Operand X = {g.x + (long long)first * g.Dp, g.x, g.Dp, px, most};
+        const Shape sh = {most, V, g.Dp, g.rows.count, first, nullptr, 0};
+        int rc;
+        if (!grads)
+            rc = launch_gemm<PL, false>("xent", X, W, sh, XentEpi<T, false>{g.stats, g.block, g.rows.target + first, g.rows.tl + first, nullptr, 0}, s);
+        else
+            rc = launch_gemm<PL, false>("xent", X, W, sh,
+                                        XentEpi<T, true>{g.stats, g.block, g.rows.target + first, g.rows.tl + first,
+                                                         (typename Kept<T>::V *)(PL == 3 ? (void *)g.scores : (void *)g.d), g.Vp}, s);
+        if (rc) return rc;
+        const LaunchPlan p = make_plan("xent_lse", {}, {most}, dim3((most + 15) / 16), 256, 0);
+        LC_LAUNCH(p, "xent (logsumexp)", lse_kernel, s, g.stats, (long long)g.block, g.tiles, g.rows, first, most, loss);
+        if (!grads) continue;
+        const long long pd = (long long)g.block * g.Vp, pdT = (long long)V * g.block;
+        if ((rc = launch_planes<PL>("xent (d)",
+                                    XentGrad<T>{(typename Kept<T>::V *)(PL == 3 ? (void *)g.scores : (void *)g.d), g.Vp, g.stats, g.block, g.rows, first, most, V},
+                                    PlanesOut{g.d, g.Vp, pd, g.dT, g.block, pdT}, most, V, most, V, s)))
+            return rc;
+        if (dx) {
+            const Shape shx = {most, D, g.Vp, g.rows.count, first, nullptr, 0};
+            if ((rc = launch_gemm<PL, false>("xent (dx)", Operand{g.d, g.d, g.Vp, pd, most}, Operand{g.wT, g.wT, g.Vp, pwT, D}, shx,
+                                             StoreEpi<T>{dx, nullptr, 0x7fffffff, most, 0, D, g.rows.index + first, nullptr, g.rows.unit}, s)))
+                return rc;
+        }
+        const Shape shw = {V, D, (int)round_up(most, kStep), nullptr, 0, g.rows.count, first};
+        const Operand dT = {g.dT, g.dT, g.block, pdT, V}, xT = {g.xT + first, g.xT, g.Np, pxT, D};
+        const float *add = b ? g.sum : nullptr;
+        if (b + 1 < g.blocks)
+            rc = launch_gemm<PL, false>("xent (dw)", dT, xT, shw, StoreEpi<float>{g.sum, nullptr, 0x7fffffff, V, 0, D, nullptr, add, nullptr}, s);
+        else
+            rc = launch_gemm<PL, false>("xent (dw)", dT, xT, shw, StoreEpi<T>{dw, nullptr, 0x7fffffff, V, 0, D, nullptr, add, g.rows.unit}, s);
+        if (rc) return rc;
+    }
+    const LaunchPlan p = make_plan("xent_cost", {}, {N}, dim3(1), 1024, 0);
+    LC_LAUNCH(p, "xent (cost)", cost_kernel, s, g.rows, cost);
+    return LC_OK;
+}
+
+bool xent_sizes(int32_t N, int32_t D, int32_t V, int dtype) {
+    return head_rows(N) && head_width(D) && head_width(V) && (dtype == LC_F32 || dtype == LC_BF16);
+}
+
+int xent_checked(const void *x, const void *w, const int64_t *target, const float *scale, float *loss, float *cost, void *dx, void *dw,
+                 int32_t N, int32_t D, int32_t V, int dtype, bool grads, void *ws, size_t ws_bytes, void *hip_stream) {
+    if (!xent_sizes(N, D, V, dtype)) return LC_EINVAL;
+    if (!w || !cost || (grads && !dw) || (N && (!x || !target || !loss))) return LC_ENULL;
+    for (const void *p : {x, w, (const void *)dx, (const void *)dw, (const void *)ws, (const void *)target, (const void *)scale,
+                          (const void *)loss, (const void *)cost})
+        if (!ptr_aligned16(p)) return LC_EALIGN;
+    if (!ws || ws_bytes < xent_workspace_bytes(N, D, V, dtype, grads)) return LC_EWORKSPACE;
+    hipStream_t s = (hipStream_t)hip_stream;
+    if (dtype == LC_BF16)
+        return xent<bf16_t>((const bf16_t *)x, (const bf16_t *)w, target, scale, loss, cost, (bf16_t *)dx, (bf16_t *)dw, N, D, V, grads, ws, s);
+    return xent<float>((const float *)x, (const float *)w, target, scale, loss, cost, (float *)dx, (float *)dw, N, D, V, grads, ws, s);
+}
+
+}  // namespace
+}  // namespace head
+}  // namespace lc
+
+using namespace lc;
+using namespace lc::head;
+
+extern "C" {
+
+size_t xent_workspace_bytes(int32_t N, int32_t D, int32_t V, int dtype, int grads) {
+    if (!xent_sizes(N, D, V, dtype)) return 0;
+    Scratch sc(nullptr);
+    if (dtype == LC_BF16) (void)XentScratch<bf16_t>(sc, N, D, V, grads != 0);
+    else (void)XentScratch<float>(sc, N, D, V, grads != 0);
+    return sc.used;
+}
+
+int xent_fwd(const void *x, const void *w, const int64_t *target, const float *scale, float *loss, float *cost, int32_t N, int32_t D,
+             int32_t V, int dtype, void *ws, size_t ws_bytes, void *hip_stream) {
+    return xent_checked(x, w, target, scale, loss, cost, nullptr, nullptr, N, D, V, dtype, false, ws, ws_bytes, hip_stream);
+}
+
+int xent_fwd_bwd(const void *x, const void *w, const int64_t *target, const float *scale, float *loss, float *cost, void *dx, void *dw,
+                 int32_t N, int32_t D, int32_t V, int dtype, void *ws, size_t ws_bytes, void *hip_stream) {
+    return xent_checked(x, w, target, scale, loss, cost, dx, dw, N, D, V, dtype, true, ws, ws_bytes, hip_stream);
+}
+
+}  // extern "C"

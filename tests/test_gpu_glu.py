@@ -1,0 +1,176 @@
+"""glu_fwd / glu_bwd against the definitions in 64 bits."""
+import pytest
+import torch
+
+import head_ref as ref
+import paper_1502_03409_amd as lc
+
+pytestmark = pytest.mark.gpu
+
+CODE = {"sigmoid": lc.LC_ACT_SIGMOID, "silu": lc.LC_ACT_SILU, "gelu": lc.LC_ACT_GELU}
+SIZES = [(1, 1, 1), (1, 64, 64), (2, 8, 200), (3, 65, 33), (16, 256, 96), (17, 200, 130), (33, 130, 31), (64, 64, 32), (70, 320, 260),
+         (129, 257, 65), (200, 1000, 300), (257, 512, 513), (300, 72, 1100)]
+
+
+def dtypes(f):
+    return pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])(f)
+
+
+def code(dtype):
+    return lc.LC_BF16 if dtype == torch.bfloat16 else lc.LC_F32
+
+
+def inputs(N, D, F, dtype, seed=0, std=1.0):
+    gen = torch.Generator().manual_seed(seed)
+    x, wg, wu, dh = (torch.randn(s, generator=gen) for s in ((N, D), (F, D), (F, D), (N, F)))
+    return tuple(t.to(dtype).cuda() for t in (x * std, wg * D ** -0.5, wu * D ** -0.5, dh / N))
+
+
+def scratch(nbytes):
+    return torch.full((nbytes // 4 + 64,), float("nan"), device="cuda")
+
+
+def saved(codes):
+    """The values of a 16-bit code of g or u (fp32: the values themselves)."""
+    if codes.dtype == torch.float32:
+        return codes.double()
+    c = codes.contiguous().view(torch.int16).int() & 0xffff
+    bits = torch.where((c & 0x4000) != 0, (c & 0x3fff) << 17, ((c & 0x3fff) << 14) + (111 << 23))
+    return (bits | ((c >> 15) << 31)).view(torch.float32).double()
+
+
+def forward(x, wg, wu, name, save=True, ws=None):
+    (N, D), F = x.shape, wg.shape[0]
+    h = torch.full((N, F), float("nan"), dtype=x.dtype, device="cuda")
+    gu = torch.full((N, 2, F), float("nan"), dtype=x.dtype, device="cuda") if save else None
+    ws = scratch(lc.glu_workspace_bytes(N, D, F, code(x.dtype))) if ws is None else ws
+    lc.glu_fwd(x, wg, wu, h, gu, CODE[name], code(x.dtype), ws)
+    return h, gu
+
+
+def backward(x, wg, wu, gu, dh, name, want_dx=True):
+    (N, D), F = x.shape, wg.shape[0]
+    out = [torch.full_like(t, float("nan")) for t in (x, wg, wu)]
+    ws = scratch(lc.glu_workspace_bytes(N, D, F, code(x.dtype), True))
+    lc.glu_bwd(x, wg, wu, gu, dh, out[0] if want_dx else None, out[1], out[2], CODE[name], code(x.dtype), ws)
+    return out
+
+
+@dtypes
+@pytest.mark.parametrize("name", ref.ACTS)
+@pytest.mark.parametrize("N,D,F", SIZES)
+def test_values_and_gradients(N, D, F, name, dtype):
+    print(f"case glu {N} {D} {F} {name} {dtype}", flush=True)
+    x, wg, wu, dh = inputs(N, D, F, dtype)
+    h, gu = forward(x, wg, wu, name)
+    rh, rg, ru = ref.glu(x, wg, wu, name)
+    ref.check("h", h, rh, ref.tol(dtype, D, 1))
+    for k, r in ((0, rg), (1, ru)):
+        ref.check("gu", saved(gu[:, k]), r, ref.tol(dtype, D, 0) + (2.0 ** -10 if dtype == torch.bfloat16 else 0.0))
+    h2, _ = forward(x, wg, wu, name, save=False)
+    assert torch.equal(h, h2)
+    dx, dwg, dwu = backward(x, wg, wu, gu, dh, name)
+    rx, rwg, rwu = ref.glu_grads(x, wg, wu, dh, name)
+    # roundings to bf16: dg and the result's own; those of g (whose derivative act' follows within a factor of two) and u are a
+    # quarter of one each
+    ref.check("dx", dx, rx, ref.tol(dtype, D + 2 * F, 2.75))
+    ref.check("dwg", dwg, rwg, ref.tol(dtype, D + N, 2.75))
+    ref.check("dwu", dwu, rwu, ref.tol(dtype, D + N, 2.75))
+    _, dwg2, dwu2 = backward(x, wg, wu, gu, dh, name, want_dx=False)
+    assert torch.equal(dwg, dwg2) and torch.equal(dwu, dwu2)
+
+
+@pytest.mark.parametrize("name", ref.ACTS)
+def test_gradients_against_differences(name):
+    """Along a random direction of all three inputs: the kernels' gradients against the difference quotient of the cost in 64
+    bits.  With steps of 1e-5 the quotient is good to 1e-9; the gradients are held to their own bound, times the ratio of the norms
+    that a single inner product can lose."""
+    x, wg, wu, dh = inputs(40, 100, 70, torch.float32, seed=3)
+    _, gu = forward(x, wg, wu, name)
+    grads = backward(x, wg, wu, gu, dh, name)
+    gen = torch.Generator().manual_seed(5)
+    dirs = [torch.randn(t.shape, generator=gen, dtype=torch.float64).cuda() for t in (x, wg, wu)]
+
+    def cost(e):
+        h, _, _ = ref.glu(*(t.double() + e * d for t, d in zip((x, wg, wu), dirs)), name)
+        return float((h * dh.double()).sum())
+
+    quotient = (cost(1e-5) - cost(-1e-5)) / 2e-5
+    inner = sum(float((g.double() * d).sum()) for g, d in zip(grads, dirs))
+    size = sum(float(g.double().norm() * d.norm()) for g, d in zip(grads, dirs))
+    assert abs(inner - quotient) <= ref.tol(torch.float32, 240, 0) * size
+
+
+@dtypes
+def test_no_rows(dtype):
+    x, wg, wu, dh = inputs(0, 40, 24, dtype)[0], *inputs(1, 40, 24, dtype)[1:3], torch.empty(0, 24, dtype=dtype, device="cuda")
+    h, gu = forward(x, wg, wu, "silu")
+    assert h.shape == (0, 24)
+    _, dwg, dwu = backward(x, wg, wu, gu, dh, "silu")
+    assert not dwg.any() and not dwu.any()
+
+
+@dtypes
+def test_infinities_and_nan_stay_in_their_rows(dtype):
+    x, wg, wu, _ = inputs(70, 96, 64, dtype, seed=2)
+    x[3, 5], x[40, 7], x[69, 0] = float("inf"), float("nan"), float("-inf")
+    h, _ = forward(x, wg, wu, "silu")
+    rh, rg, ru = ref.glu(x, wg, wu, "silu")
+    bad = torch.zeros(70, dtype=torch.bool)
+    bad[[3, 40, 69]] = True
+    ref.check("other rows", h[~bad.cuda()], rh[~bad.cuda()], ref.tol(dtype, 96, 1))
+    _, gu = forward(x, wg, wu, "silu")
+    for k, r in ((0, rg), (1, ru)):      # a single infinite factor: infinities of the right sign, NaN where NaN went in
+        ref.check("projections", saved(gu[:, k]), r, ref.tol(dtype, 96, 1))
+
+
+def test_the_code_of_saved_values():
+    """Through a layer of one weight (g = u = x): ten bits between 2^-16 and 2^16, seven elsewhere, signs, infinities, NaN, zero."""
+    gen = torch.Generator().manual_seed(1)
+    x = torch.cat([torch.randn(3000, generator=gen) * 2.0 ** k for k in (-120, -40, -17, -15, -1, 0, 5, 15, 17, 60, 120)])
+    x = torch.cat([x, torch.tensor([0.0, float("inf"), float("-inf"), float("nan"), 65535.9, 65536.0, 2.0 ** -16, 3.4e38, 1e-39])])
+    x = x.bfloat16()[:, None].cuda()
+    w = torch.full((1, 1), 1.00390625, device="cuda").bfloat16() * 1.0078125      # products need more than eight bits
+    _, gu = forward(x, w, w, "silu")
+    want = (x.double() * w.double())[:, 0].float()
+    got = saved(gu[:, 0, 0])
+    fine = torch.isfinite(want)
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    near = fine & (want.abs() >= 2.0 ** -16) & (want.abs() < 65536.0 * (1 - 2.0 ** -11))
+    assert bool(((got - want.double()).abs()[near] <= 2.0 ** -10 * want.double().abs()[near]).all())
+    far = fine & ~near & (want.abs() < 3e38)
+    assert bool(((got - want.double()).abs()[far] <= 2.0 ** -7 * want.double().abs()[far] + 2.0 ** -132).all())
+    inf = torch.isinf(want)
+    assert torch.equal(got[inf].float(), want[inf]) and bool((got[far].sign() * want[far].sign() >= 0).all())
+    assert torch.equal(gu[:, 0].contiguous().view(torch.int16), gu[:, 1].contiguous().view(torch.int16))
+
+
+def test_small_and_large_fp32_operands():
+    """Operands at the ends of the exponent range: bits of 2^-133 and above count, so an operand is off by 2^-134 at most; sums that
+    overflow before they come back never become NaN."""
+    for std in (1e-33, 1e-37, 3e-41, 1e30):
+        x, wg, wu, _ = inputs(20, 70, 40, torch.float32, seed=4, std=std)
+        _, gu = forward(x, wg, wu, "sigmoid")
+        _, rg, ru = ref.glu(x, wg, wu, "sigmoid")
+        bound = ref.tol(torch.float32, 70, 0) + (2.0 ** -134 + 2.0 ** -149 * 70) / std
+        ref.check(f"g {std}", gu[:, 0], rg, bound)
+        ref.check(f"u {std}", gu[:, 1], ru, bound)
+    x = torch.full((3, 4), 3e38, device="cuda")
+    w = torch.tensor([[1.0, 1.0, -1.0, -0.5]], device="cuda")
+    _, gu = forward(x, w, w, "sigmoid")
+    assert not torch.isnan(gu).any()
+
+
+@dtypes
+def test_the_same_bits_every_time_on_any_stream(dtype):
+    x, wg, wu, dh = inputs(150, 200, 170, dtype, seed=6)
+    first = forward(x, wg, wu, "gelu")
+    gfirst = backward(x, wg, wu, first[1], dh, "gelu")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        again = forward(x, wg, wu, "gelu")
+        gagain = backward(x, wg, wu, again[1], dh, "gelu")
+    side.synchronize()
+    for a, b in zip((*first, *gfirst), (*again, *gagain)):
+        assert torch.equal(a, b)

@@ -1,0 +1,121 @@
+"""grad_norm / grad_clip against the definitions in 64 bits."""
+import math
+
+import pytest
+import torch
+
+import paper_1502_03409_amd as lc
+
+pytestmark = pytest.mark.gpu
+
+
+def make(sizes, kinds, seed=0, std=1.0, offset=0):
+    """Tensors of these sizes as slices of one buffer a type, each starting `offset` values after the end of the one before."""
+    gen = torch.Generator().manual_seed(seed)
+    out = []
+    for i, n in enumerate(sizes):
+        dt = kinds[i % len(kinds)]
+        buf = torch.zeros(n + offset, dtype=dt, device="cuda")
+        buf[offset:] = (torch.randn(n, generator=gen) * std).to(dt).cuda()
+        out.append(buf[offset:])
+    return out
+
+
+def scratch(tensors):
+    return torch.full((lc.grad_clip_workspace_bytes(tensors) // 4 + 8,), float("nan"), device="cuda")
+
+
+def norm64(tensors):
+    return math.sqrt(sum(float((t.double() ** 2).sum()) for t in tensors))
+
+
+def check(tensors, max_norm, in_place):
+    norm = torch.full((1,), float("nan"), device="cuda")
+    want = norm64(tensors)
+    k = max_norm / want if want > max_norm else 1.0
+    expect = [t.double() * k for t in tensors]
+    work = [t.clone() for t in tensors] if in_place else [torch.full_like(t, float("nan")) for t in tensors]
+    src = work if in_place else tensors
+    lc.grad_clip(src, None if in_place else work, max_norm, norm, scratch(tensors))
+    # the sum is formed in 64 bits and rounded once; the factor and the product are rounded to fp32, the result to its type
+    assert abs(float(norm) - want) <= 2.0 ** -23 * want
+    for a, b in zip(work, expect):
+        unit = 2.0 ** -8 if a.dtype == torch.bfloat16 else 2.0 ** -22
+        assert bool(((a.double() - b).abs() <= unit * b.abs() + 1e-44).all())
+        if k == 1.0:
+            assert torch.equal(a.double(), b)
+
+
+F, H = torch.float32, torch.bfloat16
+LISTS = [([1], [F]), ([1], [H]), ([5, 0, 7], [F, H, F]), ([16383, 16384, 16385], [F]), ([16385, 32768, 3], [H, F]), ([100003], [H]),
+         ([300 + 7 * i for i in range(300)], [F, H]), ([1 << 20, 17, 4096, 999999], [F, H, H])]
+
+
+@pytest.mark.parametrize("in_place", [False, True], ids=["elsewhere", "in_place"])
+@pytest.mark.parametrize("offset", [0, 1, 2, 3, 4, 5, 7])
+@pytest.mark.parametrize("sizes,kinds", LISTS, ids=[str(i) for i in range(len(LISTS))])
+def test_lists(sizes, kinds, offset, in_place):
+    tensors = make(sizes, kinds, offset=offset)
+    full = norm64(tensors)
+    check(tensors, 0.25 * full, in_place)
+    check(tensors, 2.0 * full, in_place)
+
+
+def test_source_and_destination_at_different_alignments():
+    for a in range(4):
+        for b in range(4):
+            src = make([5000, 333], [F, H], offset=a)
+            dst = make([5000, 333], [F, H], offset=b, seed=1)
+            norm = torch.empty(1, device="cuda")
+            lc.grad_clip(src, dst, 1.0, norm, scratch(src))
+            for s, d in zip(src, dst):
+                torch.testing.assert_close(d.double(), s.double() / norm64(src), rtol=2.0 ** -8 if d.dtype == H else 2.0 ** -22, atol=0)
+
+
+@pytest.mark.parametrize("std", [1e-30, 1e30, 3e-42])
+def test_squares_beyond_the_range_of_fp32(std):
+    tensors = make([4000, 50], [F], std=std)
+    want = norm64(tensors)
+    norm = torch.empty(1, device="cuda")
+    lc.grad_norm(tensors, norm, scratch(tensors))
+    assert abs(float(norm) - want) <= 2.0 ** -23 * want + 2.0 ** -149
+    if std == 1e30:
+        lc.grad_clip(tensors, None, 1.0, norm, scratch(tensors))
+        assert abs(norm64(tensors) - 1.0) < 1e-6
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+def test_a_norm_that_is_not_finite_changes_nothing(bad):
+    tensors = make([1000, 70000, 3], [F, H])
+    tensors[1][69999] = bad
+    before = [t.clone() for t in tensors]
+    norm = torch.zeros(1, device="cuda")
+    lc.grad_clip(tensors, None, 1.0, norm, scratch(tensors))
+    assert not torch.isfinite(norm).any()
+    out = [torch.zeros_like(t) for t in tensors]
+    lc.grad_clip(tensors, out, 1.0, norm, scratch(tensors))
+    for a, b, c in zip(tensors, before, out):
+        assert torch.equal(a.nan_to_num(7.0), b.nan_to_num(7.0)) and torch.equal(c.nan_to_num(7.0), b.nan_to_num(7.0))
+
+
+def test_nothing_to_sum():
+    norm = torch.full((1,), 5.0, device="cuda")
+    ws = torch.empty(64, device="cuda")
+    lc.grad_norm([], norm, ws)
+    assert float(norm) == 0.0
+    lc.grad_clip([torch.empty(0, device="cuda")], None, 1.0, norm, ws)
+    assert float(norm) == 0.0
+    z = torch.zeros(1000, device="cuda")
+    lc.grad_clip([z], None, 1.0, norm, ws)
+    assert float(norm) == 0.0 and not z.any()
+
+
+def test_nothing_beside_the_tensors_is_written():
+    for n in (1, 3, 5, 1000, 16384 + 3):
+        for dt in (F, H):
+            for offset in range(1, 9):
+                buf = torch.full((n + 24,), 3.0, dtype=dt, device="cuda")
+                t = buf[offset:offset + n]
+                norm = torch.empty(1, device="cuda")
+                lc.grad_clip([t], None, 0.5, norm, scratch([t]))
+                assert bool((buf[:offset] == 3.0).all()) and bool((buf[offset + n:] == 3.0).all()) and bool((t < 0.6).all())
