@@ -101,20 +101,38 @@ struct GluEpi {
     }
 };
 
-// column c < Fp: dg, column c >= Fp: du (zeros where a half is padded)
+// dg and du
 template <typename T, int ACT>
 struct GluGrad {
     const T *dh, *gu;
-    int N, F, Fp;
-    __device__ bool idle(int) const { return false; }
-    __device__ float operator()(int r, int c) const {
-        const bool second = c >= Fp;
-        const int f = second ? c - Fp : c;
-        if (r >= N || f >= F) return 0.f;
-        const float d = widen<T>(dh[(long long)r * F + f]), g = saved_value(gu[(long long)r * 2 * F + f]);
-        float a, da;
-        act_both<ACT>(g, a, da);
-        return second ? d * a : d * saved_value(gu[(long long)r * 2 * F + F + f]) * da;
+    int F;
+    __device__ bool skip(int) const { return false; }
+    __device__ void operator()(int r, int c, float (&v)[2][8]) const {
+        const bool vec = F % 8 == 0;
+        float d[8], g[8], u[8];
+        load8(dh + (long long)r * F, c, F, vec, d);
+        const T *p = gu + (long long)r * 2 * F;
+        if (vec && sizeof(T) == 2 && c + 8 <= F) {
+            const u32x4 a = *(const u32x4 *)(p + c), b = *(const u32x4 *)(p + F + c);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                g[e] = saved_value((bf16_t)(a[e >> 1] >> (16 * (e & 1))));
+                u[e] = saved_value((bf16_t)(b[e >> 1] >> (16 * (e & 1))));
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                g[e] = c + e < F ? saved_value(p[c + e]) : 0.f;
+                u[e] = c + e < F ? saved_value(p[F + c + e]) : 0.f;
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float a, da;
+            act_both<ACT>(g[e], a, da);
+            v[0][e] = d[e] * u[e] * da;
+            v[1][e] = d[e] * a;
+        }
     }
 };
 
@@ -132,19 +150,32 @@ int launch_fill_zero(T *p, long long n, hipStream_t s) {
 template <typename T>
 struct GluScratch {
     static constexpr int PL = Planes<T>::N;
-    int Np, Dp, Fp;
-    bool direct;   // the operands of the forward product are used where they are
-    bf16_t *x, *w, *wT, *xT, *dgu, *dguT;
+    int Dp, Fp;
+    bool direct;   // x and the weights are used where they are
+    bf16_t *x, *w, *d;
     GluScratch(Scratch &sc, int N, int D, int F, bool backward) {
-        Np = (int)round_up(N, kStep), Dp = (int)round_up(D, kStep), Fp = (int)round_up(F, kStep);
+        Dp = (int)round_up(D, 8), Fp = (int)round_up(F, kStep);
         direct = PL == 1 && D == Dp;
-        x = direct ? nullptr : sc.take<bf16_t>((long long)PL * N * Dp);
+        x = sc.take<bf16_t>(direct ? 8 : (long long)PL * N * Dp);
         w = direct ? nullptr : sc.take<bf16_t>((long long)PL * 2 * F * Dp);
-        if (!backward) return;
-        wT = sc.take<bf16_t>((long long)PL * D * 2 * Fp);
-        xT = sc.take<bf16_t>((long long)PL * D * Np);
-        dgu = sc.take<bf16_t>((long long)PL * N * 2 * Fp);
-        dguT = sc.take<bf16_t>((long long)PL * 2 * Fp * Np);
+        d = backward ? sc.take<bf16_t>((long long)PL * N * 2 * Fp) : nullptr;
+    }
+    // x and both weights as operands: laid out first unless they are where they can be used
+    int operands(const T *xs, const T *wg, const T *wu, int N, int D, int F, Operand *X, Operand *W, hipStream_t s) const {
+        if (direct) {
+            *X = {(const bf16_t *)xs, (const bf16_t *)xs, D, 0, N, 0, 0};
+            *W = {(const bf16_t *)wg, (const bf16_t *)wu, D, 0, F, 0, 0};
+            return LC_OK;
+        }
+        const long long px = (long long)N * Dp, pw = 2LL * F * Dp;
+        *X = {x, x, Dp, px, N, 0, 0};
+        *W = {w, w + (long long)F * Dp, Dp, pw, F, 0, 0};
+        if (int rc = launch_planes<PL, 1>("glu (x)", Stored<T>{xs, N, D, nullptr, nullptr}, x, Dp, px, N, Dp, 0, s)) return rc;
+        for (int k = 0; k < 2; ++k)
+            if (int rc = launch_planes<PL, 1>("glu (w)", Stored<T>{k ? wu : wg, F, D, nullptr, nullptr}, w + (long long)k * F * Dp, Dp, pw, F,
+                                              Dp, 0, s))
+                return rc;
+        return LC_OK;
     }
 };
 
@@ -153,20 +184,10 @@ int glu_forward(const T *x, const T *wg, const T *wu, T *h, T *gu, int N, int D,
     constexpr int PL = Planes<T>::N;
     Scratch sc(ws);
     const GluScratch<T> g(sc, N, D, F, false);
-    Operand A = {(const bf16_t *)x, (const bf16_t *)x, D, 0, N}, B = {(const bf16_t *)wg, (const bf16_t *)wu, D, 0, F};
-    if (!g.direct) {
-        const long long px = (long long)N * g.Dp, pw = 2LL * F * g.Dp;
-        if (int rc = launch_planes<PL>("glu_fwd (x)", Stored<T>{x, D, N, D, nullptr, nullptr}, PlanesOut{g.x, g.Dp, px}, N, D, N, 0, s))
-            return rc;
-        for (int k = 0; k < 2; ++k)
-            if (int rc = launch_planes<PL>("glu_fwd (w)", Stored<T>{k ? wu : wg, D, F, D, nullptr, nullptr},
-                                           PlanesOut{g.w + (long long)k * F * g.Dp, g.Dp, pw}, F, D, F, 0, s))
-                return rc;
-        A = {g.x, g.x, g.Dp, px, N};
-        B = {g.w, g.w + (long long)F * g.Dp, g.Dp, pw, F};
-    }
-    const Shape sh = {N, 2 * (int)round_up(F, 32), g.Dp, nullptr, 0, nullptr, 0};
-    return launch_gemm<PL, true>("glu_fwd", A, B, sh, GluEpi<T, ACT>{h, gu, F}, s);
+    Operand X, W;
+    if (int rc = g.operands(x, wg, wu, N, D, F, &X, &W, s)) return rc;
+    const Shape sh = {N, 2 * (int)round_up(F, 32), D, nullptr, 0, nullptr, 0};
+    return launch_gemm<PL, ROW, PAIR>("glu_fwd", X, W, sh, GluEpi<T, ACT>{h, gu, F}, s);
 }
 
 template <typename T, int ACT>
@@ -179,27 +200,23 @@ int glu_backward(const T *x, const T *wg, const T *wu, const T *gu, const T *dh,
     }
     Scratch sc(ws);
     const GluScratch<T> g(sc, N, D, F, true);
+    Operand X, W;
+    if (int rc = g.operands(x, wg, wu, N, D, F, &X, &W, s)) return rc;
     const int F2 = 2 * g.Fp;
-    const long long pd = (long long)N * F2, pdT = (long long)F2 * g.Np, pxT = (long long)D * g.Np, pwT = (long long)D * F2;
-    if (int rc = launch_planes<PL>("glu_bwd (gradients)", GluGrad<T, ACT>{dh, gu, N, F, g.Fp},
-                                   PlanesOut{g.dgu, F2, pd, g.dguT, g.Np, pdT}, N, F2, N, F2, s))
-        return rc;
-    if (int rc = launch_planes<PL>("glu_bwd (x)", Stored<T>{x, D, N, D, nullptr, nullptr}, PlanesOut{nullptr, 0, 0, g.xT, g.Np, pxT},
-                                   N, D, 0, D, s))
-        return rc;
+    const long long pd = (long long)N * F2;
+    const Operand dgu = {g.d, g.d, F2, pd, N, 0, 0};
+    if (int rc = launch_planes<PL, 2>("glu_bwd (gradients)", GluGrad<T, ACT>{dh, gu, F}, g.d, F2, pd, N, g.Fp, g.Fp, s)) return rc;
     if (dx) {
-        for (int k = 0; k < 2; ++k)
-            if (int rc = launch_planes<PL>("glu_bwd (w)", Stored<T>{k ? wu : wg, D, F, D, nullptr, nullptr},
-                                           PlanesOut{nullptr, 0, 0, g.wT + (long long)k * g.Fp, F2, pwT}, F, D, 0, D, s))
-                return rc;
-        const Shape sh = {N, D, F2, nullptr, 0, nullptr, 0};
-        if (int rc = launch_gemm<PL, false>("glu_bwd (dx)", Operand{g.dgu, g.dgu, F2, pd, N}, Operand{g.wT, g.wT, F2, pwT, D}, sh,
-                                            StoreEpi<T>{dx, nullptr, 0x7fffffff, N, 0, D, nullptr, nullptr, nullptr}, s))
+        W.depth = F, W.half = g.Fp, W.rows = g.Dp;
+        const Shape sh = {N, D, g.Fp + F, nullptr, 0, nullptr, 0};
+        if (int rc = launch_gemm<PL, ROW, COLPAIR>("glu_bwd (dx)", dgu, W, sh,
+                                                   StoreEpi<T>{dx, nullptr, 0x7fffffff, N, 0, D, nullptr, nullptr, nullptr}, s))
             return rc;
     }
-    const Shape sh = {F2, D, g.Np, nullptr, 0, nullptr, 0};
-    return launch_gemm<PL, false>("glu_bwd (dw)", Operand{g.dguT, g.dguT, g.Np, pdT, F2}, Operand{g.xT, g.xT, g.Np, pxT, D}, sh,
-                                  StoreEpi<T>{dwg, dwu, g.Fp, F, F, D, nullptr, nullptr, nullptr}, s);
+    Operand dT = dgu;
+    dT.rows = F2, X.rows = g.Dp;
+    const Shape sh = {F2, D, N, nullptr, 0, nullptr, 0};
+    return launch_gemm<PL, COL, COL>("glu_bwd (dw)", dT, X, sh, StoreEpi<T>{dwg, dwu, g.Fp, F, F, D, nullptr, nullptr, nullptr}, s);
 }
 
 template <typename Fn>

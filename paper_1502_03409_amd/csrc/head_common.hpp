@@ -46,29 +46,24 @@ template <typename T> struct Planes;
 template <> struct Planes<bf16_t> { static constexpr int N = 1, PAIRS = 1; };
 template <> struct Planes<float> { static constexpr int N = 3, PAIRS = 6; };
 
-// Rows of bf16 values contiguous along the contraction, whose length is a multiple of kStep with zeros at the end: row r of
-// plane q starts at p0 + q * plane + r * ld.  With two matrices side by side (pair), see pair_row().
-constexpr int kStep = 64;
+// An operand of a product, as bf16 planes: plane q starts at p0 + q * plane.  How the matrix lies (FORM):
+//   ROW      row r of the operand at r * ld, contiguous along the contraction
+//   PAIR     two such matrices (p0, p1) of `rows` rows each, blocks of 32 rows taken from them in turn, so that any tile of 64 rows
+//            or more holds both values of every output it covers
+//   COL      index k of the contraction at k * ld, contiguous along the operand's rows
+//   COLPAIR  two such matrices one after the other along the contraction: `depth` indices of the first from 0 on, as many of the
+//            second from `half` (a multiple of kStep) on
+enum { ROW = 0, PAIR = 1, COL = 2, COLPAIR = 3 };
+constexpr int kStep = 64;   // indices of the contraction a step
 struct Operand {
     const bf16_t *p0, *p1;
     long long ld, plane;
-    int rows;   // rows that exist (of each matrix)
+    int rows;          // rows that exist, COL: in whole 16-byte pieces
+    int depth, half;   // COLPAIR
 };
-// Virtual rows of a pair: blocks of 32 rows of the first matrix alternate with the same 32 rows of the second, so that any
-// tile of 64 or more holds both values of every output it covers.
 __device__ __host__ __forceinline__ int pair_row(int v, int *second) {
     *second = (v >> 5) & 1;
     return (v >> 6) * 32 + (v & 31);
-}
-template <bool PAIR>
-__device__ __forceinline__ const bf16_t *operand_row(const Operand &o, int r) {   // rows beyond the last read the last
-    if constexpr (PAIR) {
-        int second;
-        const int f = pair_row(r, &second);
-        return (second ? o.p1 : o.p0) + (long long)min(f, o.rows - 1) * o.ld;
-    } else {
-        return o.p0 + (long long)min(r, o.rows - 1) * o.ld;
-    }
 }
 
 inline long long round_up(long long a, long long b) { return (a + b - 1) / b * b; }

@@ -1,75 +1,83 @@
-// Laying out operands: a matrix given by a functor becomes bf16 planes, by rows and / or transposed, padded with zeros to
-// whole steps of the contraction.  Read once, written once; bound by HBM.
+// Laying out operands: a matrix given by a functor becomes rows of bf16 planes, padded with zeros to whole 16-byte pieces.  Read
+// once, written once, 16 bytes a thread and plane; bound by HBM.
 #pragma once
 #include "head_common.hpp"
 
 namespace lc {
 namespace head {
 
-// Where planes go: rows [..][ld] with ld the padded number of columns, and / or the transpose [..][ldT].
-struct PlanesOut {
-    bf16_t *rows = nullptr;    // may be null
-    long long ld = 0, plane = 0;
-    bf16_t *cols = nullptr;    // transposed; may be null
-    long long ldT = 0, planeT = 0;
-};
-
-// One workgroup per 64 x 64 block, blocks along the columns fastest.  get(r, c) is the value or 0 outside the matrix; the
-// transposed side has cols_out rows (those beyond are not written) and the row side rows_out.
-template <int PL, typename Get>
-__global__ __launch_bounds__(256) void planes_kernel(Get get, PlanesOut o, int rows_out, int cols_out, int cblocks) {
-    __shared__ bf16_t t[PL][64][66];
-    const int r0 = blockIdx.x / cblocks * 64, c0 = blockIdx.x % cblocks * 64;
-    const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
-    if (get.idle(r0)) return;
-#pragma unroll 4
-    for (int i = 0; i < 16; ++i) {
-        const int r = ty + 4 * i;
-        const float v = get(r0 + r, c0 + tx);
-        bf16_t p[3];
-        if constexpr (PL == 3) split3(v, p);
-        else p[0] = to_bf16(v);
+// get(r, c, v): v[o][0..7] are columns c .. c + 7 of row r of output o (0 outside the matrix); output o lies `apart` * o columns to
+// the right.  skip(r): rows that nobody reads.
+template <int PL, int OUT, typename Get>
+__global__ __launch_bounds__(256) void planes_kernel(Get get, bf16_t *dst, long long ld, long long plane, int rows, int pieces, int apart) {
+    const long long at = blockIdx.x * 256LL + threadIdx.x;
+    const int r = (int)(at / pieces), c = (int)(at - (long long)r * pieces) * 8;
+    if (r >= rows || get.skip(r)) return;
+    float v[OUT][8];
+    get(r, c, v);
+#pragma unroll
+    for (int o = 0; o < OUT; ++o) {
+        bf16_t p[8][3];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if constexpr (PL == 3) split3(v[o][e], p[e]);
+            else p[e][0] = to_bf16(v[o][e]);
+        }
 #pragma unroll
         for (int q = 0; q < PL; ++q) {
-            t[q][r][tx] = p[q];
-            if (o.rows && r0 + r < rows_out) o.rows[q * o.plane + (long long)(r0 + r) * o.ld + c0 + tx] = p[q];
-        }
-    }
-    if (!o.cols) return;
-    __syncthreads();
-#pragma unroll 4
-    for (int i = 0; i < 16; ++i) {
-        const int c = ty + 4 * i;
-        if (c0 + c < cols_out)
+            u32x4 w;
 #pragma unroll
-            for (int q = 0; q < PL; ++q) o.cols[q * o.planeT + (long long)(c0 + c) * o.ldT + r0 + tx] = t[q][tx][c];
+            for (int e = 0; e < 4; ++e) w[e] = (unsigned)p[2 * e][q] | (unsigned)p[2 * e + 1][q] << 16;
+            *(u32x4 *)(dst + q * plane + (long long)r * ld + c + (long long)o * apart) = w;
+        }
     }
 }
 
-// A stored matrix of R rows; `index` (nullable): row r is row index[r] of it, for r < *count
+// eight consecutive values of a row from column c on, zeros from column C on
+template <typename T>
+__device__ __forceinline__ void load8(const T *row, int c, int C, bool vec, float (&v)[8]) {
+    if (vec && c + 8 <= C) {
+        if constexpr (sizeof(T) == 4) {
+            const f32x4 a = *(const f32x4 *)(row + c), b = *(const f32x4 *)(row + c + 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = a[e], v[4 + e] = b[e];
+        } else {
+            const u32x4 a = *(const u32x4 *)(row + c);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = (e & 1) ? bf16_hi(a[e >> 1]) : bf16_lo(a[e >> 1]);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = c + e < C ? widen<T>(row[c + e]) : 0.f;
+    }
+}
+
+// A stored matrix of R rows; `index` (nullable): row r is row index[r] of it, for r < *count, and zeros behind
 template <typename T>
 struct Stored {
     const T *p;
-    long long ld;
     int R, C;
     const int *index, *count;
-    __device__ bool idle(int) const { return false; }
-    __device__ float operator()(int r, int c) const {
-        if (c >= C || r >= (index ? *count : R)) return 0.f;
-        return widen<T>(p[(long long)(index ? index[r] : r) * ld + c]);
+    __device__ bool skip(int) const { return false; }
+    __device__ void operator()(int r, int c, float (&v)[1][8]) const {
+        if (r >= (index ? *count : R)) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[0][e] = 0.f;
+            return;
+        }
+        load8(p + (long long)(index ? index[r] : r) * C, c, C, C % 8 == 0, v[0]);
     }
 };
 
-template <int PL, typename Get>
-int launch_planes(const char *name, const Get &get, const PlanesOut &o, int rows, int cols, int rows_out, int cols_out,
-                  hipStream_t s) {
-    const long long rb = (rows + 63) / 64, cb = (cols + 63) / 64;
-    if (rb * cb == 0) return LC_OK;
-    const LaunchPlan p = make_plan(name, {PL}, {rows, cols, rows_out, cols_out}, dim3((unsigned)(rb * cb)), 256, 0);
-    LC_PLAN_REQUIRE(p, rb * cb <= 0x7fffffffLL);
-    LC_PLAN_REQUIRE(p, !o.rows || o.ld >= cb * 64);
-    LC_PLAN_REQUIRE(p, !o.cols || o.ldT >= rb * 64);
-    LC_LAUNCH(p, name, (planes_kernel<PL, Get>), s, get, o, rows_out, cols_out, (int)cb);
+// rows x cols (cols: of one output, padded to whole pieces) at dst
+template <int PL, int OUT, typename Get>
+int launch_planes(const char *name, const Get &get, bf16_t *dst, long long ld, long long plane, int rows, int cols, int apart, hipStream_t s) {
+    const long long pieces = cols / 8, n = ((long long)rows * pieces + 255) / 256;
+    if (n == 0) return LC_OK;
+    const LaunchPlan p = make_plan(name, {PL, OUT}, {rows, cols, apart}, dim3((unsigned)n), 256, 0);
+    LC_PLAN_REQUIRE(p, n <= 0x7fffffffLL && cols % 8 == 0 && ld % 8 == 0 && plane % 8 == 0 && apart % 8 == 0);
+    LC_PLAN_REQUIRE(p, (long long)apart * (OUT - 1) + cols <= ld);
+    LC_LAUNCH(p, name, (planes_kernel<PL, OUT, Get>), s, get, dst, ld, plane, rows, (int)pieces, apart);
     return LC_OK;
 }
 

@@ -6,7 +6,7 @@
 // which cancels in rows that are already learned.  With gradients a tile also leaves the
 // exponentials themselves (bf16 operands: relative to the tile's largest score, in fp16 times 2^15, which holds eleven bits of
 // all above 2^-29, so that the one rounding to bf16 that follows is the only one that shows; fp32: the scores), for a bounded number of rows at a time; one pass turns them into d[n][v] = s[n] (p[n][v] - [v = t]) in
-// place and transposed, and two products give dx = d w and dw = d^T x.
+// place, and two products give dx = d w and dw = d^T x.
 //
 // Masked rows take no part: the rows that count are gathered first, and every kernel runs over as many as there are.
 #include "head_gemm.hpp"
@@ -195,7 +195,7 @@ __global__ __launch_bounds__(256) void zero_kernel(T *p, long long n, float *cos
     for (long long i = blockIdx.x * 256LL + threadIdx.x; i < n; i += gridDim.x * 256LL) p[i] = 0;
 }
 
-// d[m][v] of the rows first .. of the block
+// d[m][v] of the rows first .. of the block (bf16: over the exponentials themselves)
 template <typename T>
 struct XentGrad {
     const typename Kept<T>::V *keep;
@@ -204,34 +204,46 @@ struct XentGrad {
     long long stats_ld;
     Rows o;
     int first, most, V;
-    __device__ bool idle(int r0) const { return r0 >= (live(most, o.count, first) + 63) / 64 * 64; }
-    __device__ float operator()(int m, int v) const {
-        if (v >= V || m >= live(most, o.count, first)) return 0.f;
-        const int r = first + m;
+    __device__ bool skip(int m) const { return m >= live(most, o.count, first); }
+    __device__ void operator()(int m, int c, float (&v)[1][8]) const {
+        const int r = first + m, t = o.target[r];
         const float lse = o.lse[r], s = o.scale[r];
-        if (v == o.target[r]) return s * o.dt[r];
-        const float k = keep[m * ld + v];
-        if constexpr (sizeof(T) == 4) return s * expf(k - lse);
-        else return s * (k * (__expf(stats[(v / kWaveCols) * stats_ld + m].x - lse) * 0x1p-15f));
+        if constexpr (sizeof(T) == 4) {
+            const f32x4 *k = (const f32x4 *)(keep + m * ld + c);
+            const f32x4 a = k[0], b = k[1];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[0][e] = s * expf((e < 4 ? a[e & 3] : b[e & 3]) - lse);
+        } else {
+            typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+            const f16x8 k = *(const f16x8 *)(keep + m * ld + c);
+            const float f = __expf(stats[(c / kWaveCols) * stats_ld + m].x - lse) * 0x1p-15f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[0][e] = s * ((float)k[e] * f);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (c + e == t) v[0][e] = s * o.dt[r];
+            if (c + e >= V) v[0][e] = 0.f;
+        }
     }
 };
 
 template <typename T>
 struct XentScratch {
     static constexpr int PL = Planes<T>::N;
-    int Np, Dp, Vp, tiles, block, blocks;   // rows of a block (a multiple of 64), number of blocks
+    int Dp, Vp, tiles, block, blocks;   // rows of a block, number of blocks
     bool direct;                            // w is used where it is
     Rows rows;
-    bf16_t *x, *w, *wT, *xT, *d, *dT;
+    bf16_t *x, *w, *d;
     float2 *stats;
     float *scores, *sum;
     XentScratch(Scratch &sc, int N, int D, int V, bool grads) {
-        Np = (int)round_up(N, kStep), Dp = (int)round_up(D, kStep), Vp = (int)round_up(V, kStep);
+        Dp = (int)round_up(D, 8), Vp = (int)round_up(V, kWaveCols);
         direct = PL == 1 && D == Dp;
         tiles = Vp / kWaveCols;
-        block = Np;
-        if (grads) block = (int)std::min<long long>(Np, std::max<long long>(kStep, kBlockBytes / ((long long)Vp * sizeof(T)) / 256 * 256));
-        blocks = Np ? (Np + block - 1) / block : 0;
+        block = (int)round_up(N, 8);
+        if (grads) block = (int)std::min<long long>(block, std::max<long long>(kStep, kBlockBytes / ((long long)Vp * sizeof(T)) / 256 * 256));
+        blocks = N ? (N + block - 1) / block : 0;
         rows.count = sc.take<int>(1);
         rows.unit = sc.take<float>(1);
         rows.index = sc.take<int>(N);
@@ -245,10 +257,7 @@ struct XentScratch {
         w = direct ? nullptr : sc.take<bf16_t>((long long)PL * V * Dp);
         stats = sc.take<float2>((long long)tiles * block);
         if (!grads) return;
-        wT = sc.take<bf16_t>((long long)PL * D * Vp);
-        xT = sc.take<bf16_t>((long long)PL * D * Np);
         d = sc.take<bf16_t>((long long)PL * block * Vp);
-        dT = sc.take<bf16_t>((long long)PL * V * block);
         scores = PL == 3 ? sc.take<float>((long long)block * Vp) : nullptr;
         sum = blocks > 1 ? sc.take<float>((long long)V * D) : nullptr;
     }
@@ -268,52 +277,47 @@ int xent(const T *x, const T *w, const int64_t *target, const float *scale, floa
     }
     const LaunchPlan one = make_plan("xent_rows", {}, {N}, dim3(1), 1024, 0);
     LC_LAUNCH(one, "xent (rows)", rows_kernel, s, target, scale, loss, N, V, g.rows);
-    const long long px = (long long)N * g.Dp, pw = (long long)V * g.Dp, pwT = (long long)D * g.Vp, pxT = (long long)D * g.Np;
-    if (int rc = launch_planes<PL>("xent (x)", Stored<T>{x, D, N, D, g.rows.index, g.rows.count},
-                                   PlanesOut{g.x, g.Dp, px, grads ? g.xT : nullptr, g.Np, pxT}, N, D, N, D, s))
-        return rc;
-    if (!g.direct || grads)
-        if (int rc = launch_planes<PL>("xent (w)", Stored<T>{w, D, V, D, nullptr, nullptr},
-                                       PlanesOut{g.w, g.Dp, pw, grads && dx ? g.wT : nullptr, g.Vp, pwT}, V, D, V, D, s))
-            return rc;
-    const Operand W = g.direct ? Operand{(const bf16_t *)w, (const bf16_t *)w, D, 0, V} : Operand{g.w, g.w, g.Dp, pw, V};
+    const long long px = (long long)N * g.Dp, pw = (long long)V * g.Dp;
+    if (int rc = launch_planes<PL, 1>("xent (x)", Stored<T>{x, N, D, g.rows.index, g.rows.count}, g.x, g.Dp, px, N, g.Dp, 0, s)) return rc;
+    if (!g.direct)
+        if (int rc = launch_planes<PL, 1>("xent (w)", Stored<T>{w, V, D, nullptr, nullptr}, g.w, g.Dp, pw, V, g.Dp, 0, s)) return rc;
+    const Operand W = g.direct ? Operand{(const bf16_t *)w, (const bf16_t *)w, D, 0, V, 0, 0} : Operand{g.w, g.w, g.Dp, pw, V, 0, 0};
     if (grads && dx) {
         const LaunchPlan p = make_plan("xent_zero_masked", {}, {N}, dim3(N), 256, 0);
         LC_LAUNCH(p, "xent (masked rows)", (zero_masked_kernel<T>), s, target, dx, D);
     }
     for (int b = 0; b < g.blocks; ++b) {
         const int first = b * g.block, most = std::min(g.block, N - first);
-        const Operand X = {g.x + (long long)first * g.Dp, g.x, g.Dp, px, most};
-        const Shape sh = {most, V, g.Dp, g.rows.count, first, nullptr, 0};
+        Operand X = {g.x + (long long)first * g.Dp, g.x, g.Dp, px, most, 0, 0}, Wc = W;
+        const Shape sh = {most, V, D, g.rows.count, first, nullptr, 0};
+        typename Kept<T>::V *keep = (typename Kept<T>::V *)(PL == 3 ? (void *)g.scores : (void *)g.d);
         int rc;
         if (!grads)
-            rc = launch_gemm<PL, false>("xent", X, W, sh, XentEpi<T, false>{g.stats, g.block, g.rows.target + first, g.rows.tl + first, nullptr, 0}, s);
+            rc = launch_gemm<PL, ROW, ROW>("xent", X, W, sh, XentEpi<T, false>{g.stats, g.block, g.rows.target + first, g.rows.tl + first, nullptr, 0}, s);
         else
-            rc = launch_gemm<PL, false>("xent", X, W, sh,
-                                        XentEpi<T, true>{g.stats, g.block, g.rows.target + first, g.rows.tl + first,
-                                                         (typename Kept<T>::V *)(PL == 3 ? (void *)g.scores : (void *)g.d), g.Vp}, s);
+            rc = launch_gemm<PL, ROW, ROW>("xent", X, W, sh, XentEpi<T, true>{g.stats, g.block, g.rows.target + first, g.rows.tl + first, keep, g.Vp}, s);
         if (rc) return rc;
         const LaunchPlan p = make_plan("xent_lse", {}, {most}, dim3((most + 15) / 16), 256, 0);
         LC_LAUNCH(p, "xent (logsumexp)", lse_kernel, s, g.stats, (long long)g.block, g.tiles, g.rows, first, most, loss);
         if (!grads) continue;
-        const long long pd = (long long)g.block * g.Vp, pdT = (long long)V * g.block;
-        if ((rc = launch_planes<PL>("xent (d)",
-                                    XentGrad<T>{(typename Kept<T>::V *)(PL == 3 ? (void *)g.scores : (void *)g.d), g.Vp, g.stats, g.block, g.rows, first, most, V},
-                                    PlanesOut{g.d, g.Vp, pd, g.dT, g.block, pdT}, most, V, most, V, s)))
+        const long long pd = (long long)g.block * g.Vp;
+        if ((rc = launch_planes<PL, 1>("xent (d)", XentGrad<T>{keep, g.Vp, g.stats, g.block, g.rows, first, most, V}, g.d, g.Vp, pd, most, g.Vp, 0, s)))
             return rc;
+        Operand d = {g.d, g.d, g.Vp, pd, most, 0, 0};
+        Wc.rows = X.rows = g.Dp;
         if (dx) {
-            const Shape shx = {most, D, g.Vp, g.rows.count, first, nullptr, 0};
-            if ((rc = launch_gemm<PL, false>("xent (dx)", Operand{g.d, g.d, g.Vp, pd, most}, Operand{g.wT, g.wT, g.Vp, pwT, D}, shx,
-                                             StoreEpi<T>{dx, nullptr, 0x7fffffff, most, 0, D, g.rows.index + first, nullptr, g.rows.unit}, s)))
+            const Shape shx = {most, D, V, g.rows.count, first, nullptr, 0};
+            if ((rc = launch_gemm<PL, ROW, COL>("xent (dx)", d, Wc, shx,
+                                                StoreEpi<T>{dx, nullptr, 0x7fffffff, most, 0, D, g.rows.index + first, nullptr, g.rows.unit}, s)))
                 return rc;
         }
-        const Shape shw = {V, D, (int)round_up(most, kStep), nullptr, 0, g.rows.count, first};
-        const Operand dT = {g.dT, g.dT, g.block, pdT, V}, xT = {g.xT + first, g.xT, g.Np, pxT, D};
+        const Shape shw = {V, D, most, nullptr, 0, g.rows.count, first};
+        d.rows = g.Vp;
         const float *add = b ? g.sum : nullptr;
         if (b + 1 < g.blocks)
-            rc = launch_gemm<PL, false>("xent (dw)", dT, xT, shw, StoreEpi<float>{g.sum, nullptr, 0x7fffffff, V, 0, D, nullptr, add, nullptr}, s);
+            rc = launch_gemm<PL, COL, COL>("xent (dw)", d, X, shw, StoreEpi<float>{g.sum, nullptr, 0x7fffffff, V, 0, D, nullptr, add, nullptr}, s);
         else
-            rc = launch_gemm<PL, false>("xent (dw)", dT, xT, shw, StoreEpi<T>{dw, nullptr, 0x7fffffff, V, 0, D, nullptr, add, g.rows.unit}, s);
+            rc = launch_gemm<PL, COL, COL>("xent (dw)", d, X, shw, StoreEpi<T>{dw, nullptr, 0x7fffffff, V, 0, D, nullptr, add, g.rows.unit}, s);
         if (rc) return rc;
     }
     const LaunchPlan p = make_plan("xent_cost", {}, {N}, dim3(1), 1024, 0);
