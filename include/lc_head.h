@@ -74,8 +74,8 @@ typedef struct {
     int32_t dtype;
 } lc_tensor_t;
 
-/* Host only.  Scratch for grad_norm and grad_clip of a list of `count` tensors that hold `values` values together; 0 for
- * invalid arguments. */
+/* Host only.  Scratch for grad_norm and grad_clip of a list of `count` tensors that hold at most `values` values together; 0
+ * for invalid arguments. */
 size_t grad_clip_workspace_bytes(int64_t values, int32_t count);
 
 /* norm[0] = sqrt(sum of the squares of all values of all tensors), summed in 64 bits.  dst is not looked at. */
