@@ -3,7 +3,7 @@
 // Forward: a tile of the product covers the same outputs of both weight matrices (blocks of 32 rows of wg and wu alternate), so
 // the activation and the product happen on the accumulators.  Backward: one pass over dh and the saved g, u leaves both
 // gradients side by side, [N][2F] and transposed, and two products finish: dx = [dg du] [wg; wu] and [dwg; dwu] = [dg du]^T x.
-#include "head_gemm.hpp"
+#include "head_few.hpp"
 #include "head_planes.hpp"
 
 namespace lc {
@@ -50,54 +50,44 @@ template <> __device__ __forceinline__ bf16_t save_value<bf16_t>(float v) {
                                            : (mag + 0xffffu + ((mag >> 17) & 1u)) >> 17;
     return (bf16_t)(sign | 0x4000u | far);
 }
-template <typename T>
-__device__ __forceinline__ void save4(T *row, int n, int width, bool vec, const float (&v)[4]) {
-    if constexpr (sizeof(T) == 4) {
-        store4(row, n, width, vec, v);
-    } else {
-        const u16x4 c = {save_value<T>(v[0]), save_value<T>(v[1]), save_value<T>(v[2]), save_value<T>(v[3])};
-        if (vec && n + 3 < width) {
-            *(u16x4 *)(row + n) = c;
-        } else {
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (n + r < width) row[n + r] = c[r];
-        }
-    }
-}
-
-// blocks j = 0, 2, .. of a wave are g, blocks 1, 3, .. the u of the same outputs
-template <typename T, int ACT>
+// EACH 32: blocks j = 0, 2, .. of a wave are g, blocks 1, 3, .. the u of the same outputs; 16: every block holds both of 16 outputs.
+template <typename T, int ACT, int EACH = 32>
 struct GluEpi {
     T *h, *gu;   // gu may be null
     int F;
     template <int MT, int NT>
-    __device__ __forceinline__ void run(const f32x16 (&acc)[MT][NT], int m0, int n0, int lane, int M, int) const {
-        static_assert(NT % 2 == 0, "g and u of an output sit in neighbouring blocks");
-        const bool vec = F % 4 == 0;
+    __device__ __forceinline__ void run(f32x16 (&acc)[MT][NT], int m0, int n0, int lane, int M, int, int, char *lds) const {
+        static_assert(EACH == 16 || NT % 2 == 0, "g and u of an output sit in neighbouring blocks or in one");
+        const RowStage<T, NT * 16> stage = {lds, lane};
+        const int f0 = n0 / 2;
+        // what: 0 h, 1 g, 2 u
+        auto send = [&](auto block, auto what, T *out, int ld) __attribute__((always_inline)) {
+            constexpr int i = decltype(block)::value, W = decltype(what)::value;
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            const int m = m0 + 32 * i + (lane & 31);
-            if (m >= M) continue;
+            for (int j = 0; j < NT; j += EACH / 16)
 #pragma unroll
-            for (int j = 0; j < NT; j += 2)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int f = n0 / 2 + 16 * j + 8 * q + 4 * (lane >> 5);
-                    float g[4], u[4], v[4];
+                for (int q = 0; q < EACH / 8; ++q) {
+                    T v[4];
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        g[r] = acc[i][j][4 * q + r];
-                        u[r] = acc[i][j + 1][4 * q + r];
-                        v[r] = act_value<ACT>(g[r]) * u[r];
+                        const float g = acc[i][j][4 * q + r];
+                        const float u = EACH == 16 ? acc[i][j][(8 + 4 * q + r) & 15] : acc[i][j + EACH / 32][4 * q + r];
+                        v[r] = W == 0 ? narrow<T>(act_value<ACT>(g) * u) : save_value<T>(W == 1 ? g : u);
                     }
-                    store4(h + (long long)m * F, f, F, vec, v);
-                    if (gu) {
-                        save4(gu + (long long)m * 2 * F, f, F, vec, g);
-                        save4(gu + (long long)m * 2 * F + F, f, F, vec, u);
-                    }
+                    stage.put(16 * j + 8 * q + 4 * (lane >> 5), v);
                 }
-        }
+            stage.take([&](int r, int c, const u32x4 &w) {
+                const int m = m0 + 32 * i + r;
+                if (m < M) store_piece(out + (long long)m * ld, f0 + c, F, w);
+            });
+        };
+        for_blocks<MT>([&](auto block) __attribute__((always_inline)) {
+            send(block, std::integral_constant<int, 0>(), h, F);
+            if (gu) {
+                send(block, std::integral_constant<int, 1>(), gu, 2 * F);
+                send(block, std::integral_constant<int, 2>(), gu + F, 2 * F);
+            }
+        });
     }
 };
 
@@ -108,12 +98,12 @@ struct GluGrad {
     int F;
     __device__ bool skip(int) const { return false; }
     __device__ void operator()(int r, int c, float (&v)[2][8]) const {
-        const bool vec = F % 8 == 0;
         float d[8], g[8], u[8];
-        load8(dh + (long long)r * F, c, F, vec, d);
+        load8(dh + (long long)r * F, c, F, d);
         const T *p = gu + (long long)r * 2 * F;
-        if (vec && sizeof(T) == 2 && c + 8 <= F) {
-            const u32x4 a = *(const u32x4 *)(p + c), b = *(const u32x4 *)(p + F + c);
+        if (sizeof(T) == 2 && c + 8 <= F) {
+            typedef u32x4 any __attribute__((aligned(2)));
+            const u32x4 a = *(const any *)(p + c), b = *(const any *)(p + F + c);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 g[e] = saved_value((bf16_t)(a[e >> 1] >> (16 * (e & 1))));
@@ -153,12 +143,15 @@ struct GluScratch {
     int Dp, Fp;
     bool direct;   // x and the weights are used where they are
     bf16_t *x, *w, *d;
+    float *part;   // one product at a time
     GluScratch(Scratch &sc, int N, int D, int F, bool backward) {
         Dp = (int)round_up(D, 8), Fp = (int)round_up(F, kStep);
         direct = PL == 1 && D == Dp;
         x = sc.take<bf16_t>(direct ? 8 : (long long)PL * N * Dp);
         w = direct ? nullptr : sc.take<bf16_t>((long long)PL * 2 * F * Dp);
         d = backward ? sc.take<bf16_t>((long long)PL * N * 2 * Fp) : nullptr;
+        const int pairs = Planes<T>::PAIRS;
+        part = backward ? sc.take<float>(std::max(part_floats(N, D, Fp + F, pairs), part_floats(2 * Fp, D, N, pairs))) : nullptr;
     }
     // x and both weights as operands: laid out first unless they are where they can be used
     int operands(const T *xs, const T *wg, const T *wu, int N, int D, int F, Operand *X, Operand *W, hipStream_t s) const {
@@ -182,6 +175,9 @@ struct GluScratch {
 template <typename T, int ACT>
 int glu_forward(const T *x, const T *wg, const T *wu, T *h, T *gu, int N, int D, int F, void *ws, hipStream_t s) {
     constexpr int PL = Planes<T>::N;
+    if (N <= kFewRows)
+        return launch_few<T, PAIR>("glu_fwd (few rows)", FewOperand<T>{x, x, D, N, nullptr}, FewOperand<T>{wg, wu, D, F, nullptr}, N, nullptr,
+                                   2 * (int)round_up(F, 16), D, GluEpi<T, ACT, 16>{h, gu, F}, s);
     Scratch sc(ws);
     const GluScratch<T> g(sc, N, D, F, false);
     Operand X, W;
@@ -209,14 +205,14 @@ int glu_backward(const T *x, const T *wg, const T *wu, const T *gu, const T *dh,
     if (dx) {
         W.depth = F, W.half = g.Fp, W.rows = g.Dp;
         const Shape sh = {N, D, g.Fp + F, nullptr, 0, nullptr, 0};
-        if (int rc = launch_gemm<PL, ROW, COLPAIR>("glu_bwd (dx)", dgu, W, sh,
-                                                   StoreEpi<T>{dx, nullptr, 0x7fffffff, N, 0, D, nullptr, nullptr, nullptr}, s))
+        if (int rc = launch_product<PL, ROW, COLPAIR>("glu_bwd (dx)", dgu, W, sh,
+                                                   StoreEpi<T>{dx, nullptr, 0x7fffffff, N, 0, D, nullptr, nullptr, nullptr}, g.part, s))
             return rc;
     }
     Operand dT = dgu;
     dT.rows = F2, X.rows = g.Dp;
     const Shape sh = {F2, D, N, nullptr, 0, nullptr, 0};
-    return launch_gemm<PL, COL, COL>("glu_bwd (dw)", dT, X, sh, StoreEpi<T>{dwg, dwu, g.Fp, F, F, D, nullptr, nullptr, nullptr}, s);
+    return launch_product<PL, COL, COL>("glu_bwd (dw)", dT, X, sh, StoreEpi<T>{dwg, dwu, g.Fp, F, F, D, nullptr, nullptr, nullptr}, g.part, s);
 }
 
 template <typename Fn>

@@ -2,6 +2,7 @@
 #pragma once
 #include "../../include/lc_head.h"
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "lc_common.hpp"
@@ -61,9 +62,9 @@ struct Operand {
     int rows;          // rows that exist, COL: in whole 16-byte pieces
     int depth, half;   // COLPAIR
 };
-__device__ __host__ __forceinline__ int pair_row(int v, int *second) {
-    *second = (v >> 5) & 1;
-    return (v >> 6) * 32 + (v & 31);
+__device__ __host__ __forceinline__ int pair_row(int v, int each, int *second) {   // each: rows taken in turn
+    *second = v / each & 1;
+    return v / (2 * each) * each + v % each;
 }
 
 inline long long round_up(long long a, long long b) { return (a + b - 1) / b * b; }

@@ -18,6 +18,15 @@ __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
+// fn(0), fn(1), .. with the numbers as types: the accumulators may only be indexed by constants, however long fn is
+template <int N, int I = 0, typename Fn>
+__device__ __forceinline__ void for_blocks(const Fn &fn) {
+    if constexpr (I < N) {
+        fn(std::integral_constant<int, I>());
+        for_blocks<N, I + 1>(fn);
+    }
+}
+
 // What a product needs besides its operands.  rows_dev (nullable): the rows of A that count, minus first_row, at most M.
 // k_dev (nullable): the same for the contraction.  Both are read on the device.
 struct Shape {
@@ -31,149 +40,189 @@ __device__ __forceinline__ int live(int most, const int *dev, int first) {
     return dev ? max(0, min(most, *dev - first)) : most;
 }
 
-// Adds the exact products of a wave's rows with the fp32 matrix instruction: lane l brings eight consecutive k of its row.
+// Value k of row r of an operand: its planes added up; 0 from k_end on.
+template <int FORM>
+__device__ __forceinline__ float whole_value(const Operand &o, int r, int k, int k_end) {
+    const bf16_t *p;
+    bool in = k < k_end;
+    if constexpr (FORM == PAIR) {
+        int second;
+        const int f = min(pair_row(r, 32, &second), o.rows - 1);
+        p = (second ? o.p1 : o.p0) + f * o.ld + k;
+    } else if constexpr (FORM == ROW) {
+        p = o.p0 + min(r, o.rows - 1) * o.ld + k;
+    } else {
+        const bool second = FORM == COLPAIR && k >= o.half;
+        const int d = k - (second ? o.half : 0);
+        if (FORM == COLPAIR) in &= d < o.depth;
+        p = (second ? o.p1 : o.p0) + d * o.ld + min(r, o.rows - 1);
+    }
+    return in ? from_bf16(p[2 * o.plane]) + from_bf16(p[o.plane]) + from_bf16(p[0]) : 0.f;
+}
+
+// The products of a wave's rows with the fp32 matrix instruction.  Rare, so one block and one value at a time: it must not take
+// registers from the rest.
 template <int MT, int NT, int FA, int FB>
-__device__ __forceinline__ void product_exact(const Operand &A, const Operand &B, int m0, int n0, int K, int lane,
-                                           f32x16 (&acc)[MT][NT]) {
+__device__ __forceinline__ void product_exact(const Operand &A, const Operand &B, int m0, int n0, int k_first, int k_end, int lane,
+                                              f32x16 (&acc)[MT][NT]) {
     const int l32 = lane & 31, h = lane >> 5;
-    auto whole = [&](const Operand &o, auto form, int r, int k, float (&v)[8]) {
-        constexpr int FORM = decltype(form)::value;
-        for (int e = 0; e < 8; ++e) {
-            const bf16_t *p;
-            bool in = k + e < K;
-            if constexpr (FORM == PAIR) {
-                int second;
-                const int f = min(pair_row(r, &second), o.rows - 1);
-                p = (second ? o.p1 : o.p0) + f * o.ld + k + e;
-            } else if constexpr (FORM == ROW) {
-                p = o.p0 + min(r, o.rows - 1) * o.ld + k + e;
-            } else {
-                const bool second = FORM == COLPAIR && k + e >= o.half;
-                const int d = k + e - (second ? o.half : 0);
-                if (FORM == COLPAIR) in &= d < o.depth;
-                p = (second ? o.p1 : o.p0) + d * o.ld + min(r, o.rows - 1);
-            }
-            float s = 0.f;
-            for (int q = 2; q >= 0; --q)
-                if (in) s += from_bf16(p[q * o.plane]);
-            v[e] = s;
-        }
-    };
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {   // one block at a time: this is rare, and must not take registers from the rest
+        for (int j = 0; j < NT; ++j) {
             f32x16 c = {};
 #pragma unroll 1
-            for (int k = 0; k < K; k += 16) {
-                float a[8], b[8];
-                whole(A, std::integral_constant<int, FA>(), m0 + 32 * i + l32, k + 8 * h, a);
-                whole(B, std::integral_constant<int, FB>(), n0 + 32 * j + l32, k + 8 * h, b);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(b[e], a[e], c, 0, 0, 0);
-            }
+            for (int k = k_first; k < k_end; k += 2)
+                c = __builtin_amdgcn_mfma_f32_32x32x2f32(whole_value<FB>(B, n0 + 32 * j + l32, k + h, k_end),
+                                                         whole_value<FA>(A, m0 + 32 * i + l32, k + h, k_end), c, 0, 0, 0);
             acc[i][j] = c;
         }
 }
 
+// whether the sums of all rows that count are finite (operands may hold anything in rows behind them)
 template <int MT, int NT>
-__device__ __forceinline__ bool all_finite(const f32x16 (&acc)[MT][NT]) {
+__device__ __forceinline__ bool all_finite(const f32x16 (&acc)[MT][NT], int rows, int lane) {
     bool ok = true;
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+    for (int i = 0; i < MT; ++i) {
+        bool fine = true;
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) ok &= __builtin_isfinite(acc[i][j][e]);
+            for (int e = 0; e < 16; ++e) fine &= __builtin_isfinite(acc[i][j][e]);
+        ok &= fine || 32 * i + (lane & 31) >= rows;
+    }
     return __all(ok);
 }
 
-// Tile order: groups of kGroup tiles along m share their tiles along n, and an XCD walks a contiguous range, so that the
+// Tile order: rows that do not count have no tiles (their workgroups are the last ones); groups of kGroup tiles along m share their tiles along n, and an XCD walks a contiguous range, so that the
 // workgroups that run at once on one XCD share operand rows in its L2.
 constexpr int kGroup = 8;
-__device__ __forceinline__ void tile_of(int wg, int mt, int nt, int *tm, int *tn) {
-    const int id = remap_xcd(wg, mt * nt);
+__device__ __forceinline__ bool tile_of(int wg, int mt, int nt, int splits, int *tm, int *tn, int *split) {
+    if (wg >= mt * nt * splits) return false;
+    int id = remap_xcd(wg, mt * nt * splits);
+    *split = id / (mt * nt);
+    id -= *split * (mt * nt);
     const int group = id / (kGroup * nt), first = group * kGroup, size = min(kGroup, mt - first);
     const int in = id - group * kGroup * nt;
     *tm = first + in % size;
     *tn = in / size;
+    return true;
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------
-// The tiled product.  BM x BN of the result per workgroup, WM x WN waves, steps of 64 along the contraction through two LDS
-// buffers that are filled by loads which go straight there; one barrier a step: behind it the other buffer is free (every wave
-// has read it) and this one is full (every wave has waited for its loads), so a step's loads have a whole step to arrive.
+// The tiled product.  BM x BN of the result per workgroup of 2 x 2 waves, steps of 64 along the contraction, through LDS buffers that
+// are filled by loads which go straight there: three for A, two for B (all 160 KB for 256 x 256).  A long contraction over few tiles is
+// cut into `splits` parts, whose sums are added up by a kernel of their own.
 //
-// An operand's tile is kept as it lies in memory.  By rows (ROW, PAIR): 128 bytes a row, its eight 16-byte pieces exchanged by
-// the row's low bits so that the 32 rows a fragment reads fall on all banks.  By columns (COL, COLPAIR): 64 rows of
-// BM or BN values, 64-byte pieces exchanged by the row's bits, read with the transposing LDS load, which hands lane i of 16 the
-// four k of column i from four rows of 32 bytes.
+// An operand's tile is kept as it lies in memory.  By rows (ROW, PAIR): 128 bytes a row (whole lines: half lines at a time come at half the
+// rate, 15 against 25 TB/s from the L2 caches), whose eight 16-byte pieces are exchanged by bits of the row so that 16 rows read at
+// once fall on all 64 banks.  By columns (COL, COLPAIR): 64 rows of BM or BN values, 64-byte pieces exchanged by the row's bits, read with
+// the transposing LDS load, which hands lane i of 16 the four k of column i from four rows of 32 bytes.
+//
+// Order of a step: its quarters of 16 indices; while one is multiplied, the fragments of the next are read, between the matrix
+// instructions.  In the last quarter, after the first few products have been issued, comes the step's one barrier: behind it the next
+// step is there for everybody (each wave has waited for its own loads) and this step's buffers are free (each wave has read them).
+// Loads go out evenly: the address unit takes one every 18 clocks, and a wave that waits for it cannot issue matrix instructions.  Between
+// two barriers the B of the step after next comes first, half of it still in the last quarter, then the A of the step behind that, which
+// may stay in flight across the next barrier.
 template <int N>
 __device__ __forceinline__ int col_swizzle(int k) {   // N columns: N / 32 pieces of 64 bytes
     return ((k & 3) | ((k >> 3) & 1) << 2) & (N / 32 - 1);
 }
 
-template <int FORM, int N, int NW>
+constexpr int kWaves = 4;
+
+// Brings an operand's tile of N rows, one step after the other.  A wave can issue about six other instructions per matrix instruction, so
+// what a step needs is kept running: one base for all of a wave's loads, which moves along, and one offset per load.
+template <int FORM, int N, int PL>
 struct Stager {
     static constexpr bool COLS = FORM == COL || FORM == COLPAIR;
-    static constexpr int Q = N / 8 / NW;   // load instructions of a wave a step, 1024 bytes each
+    static constexpr int Q = N / 8 / kWaves;   // load instructions of a wave a step, 1024 bytes each
+    static constexpr int PAIRS = PL == 3 ? 6 : 1;
     unsigned off[Q];
-    gbyte_ptr base[FORM == PAIR ? Q : FORM == COLPAIR ? 2 : 1];
-    long long ld2, plane2;                 // bytes
-    int wave, lane, depth, half;
-    __device__ __forceinline__ void init(const Operand &o, int r0, int wave_, int lane_) {
-        wave = wave_, lane = lane_;
-        ld2 = o.ld * 2, plane2 = o.plane * 2;
+    gbyte_ptr base, base2;                     // of the current kStep indices; the second matrix (PAIR: of these indices, COLPAIR: its start)
+    long long move, plane, at;                 // bytes: to the next kStep indices, to the next plane, to the current plane
+    unsigned ld2, planes;                      // planes of the six products, the next one's lowest
+    int wave, lane, K, depth, half, kt, pair;
+    bool trimmed;
+    __device__ __forceinline__ void init(const Operand &o, int r0, int kt_, int K_, unsigned planes_, int wave_, int lane_) {
+        wave = wave_, lane = lane_, K = K_, kt = kt_, pair = 0, planes = planes_, at = 0;
+        const long long ld = o.ld * 2;
+        ld2 = (unsigned)ld, plane = o.plane * 2;
         depth = o.depth, half = o.half;
+        move = COLS ? kStep * ld : kStep * 2;
+        // load q of this wave brings rows 8 (q kWaves + wave) on: of a pair, those of the first matrix for even q
+        int second;
+        const int top = min(FORM == PAIR ? pair_row(r0, 32, &second) : r0, o.rows - 1);
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
-            const int g = q * NW + wave;   // this kilobyte of the tile
             if constexpr (COLS) {
                 const int pc = lane % (N / 8);
                 const int c = ((pc / 4) ^ col_swizzle<N>(first_k(q))) * 4 + pc % 4;
-                off[q] = (unsigned)((long long)first_k(q) * ld2) + (unsigned)(min(r0 + 8 * c, o.rows - 8) - r0) * 2;
+                off[q] = (unsigned)first_k(q) * ld2 + (unsigned)(min(r0 + 8 * c, o.rows - 8) - r0) * 2;
             } else {
-                int f0 = r0 + 8 * g, second = 0;
-                if constexpr (FORM == PAIR) f0 = pair_row(f0, &second);
-                const int top = min(f0, o.rows - 1);
-                const int rel = min(f0 + lane / 8, o.rows - 1) - (FORM == PAIR ? top : r0);
-                if constexpr (FORM == PAIR) base[q] = (gbyte_ptr)((second ? o.p1 : o.p0) + (long long)top * o.ld);
-                off[q] = (unsigned)((long long)rel * ld2) + first_k(q) * 2;
+                int f = r0 + 8 * (q * kWaves + wave), s;
+                if constexpr (FORM == PAIR) f = pair_row(f, 32, &s);
+                off[q] = (unsigned)(min(f + lane / 8, o.rows - 1) - top) * ld2 + first_k(q) * 2;
             }
         }
-        if constexpr (FORM == ROW) base[0] = (gbyte_ptr)(o.p0 + (long long)r0 * o.ld);
-        if constexpr (COLS) base[0] = (gbyte_ptr)(o.p0 + r0);
-        if constexpr (FORM == COLPAIR) base[1] = (gbyte_ptr)(o.p1 + r0);
+        if constexpr (COLS) base = (gbyte_ptr)(o.p0 + r0), base2 = (gbyte_ptr)(o.p1 + r0);
+        else base = (gbyte_ptr)(o.p0 + (long long)top * o.ld), base2 = (gbyte_ptr)(o.p1 + (long long)top * o.ld) + kt * move;
+        if (FORM == COLPAIR && kt * kStep >= half) base = base2, base += (kt - half / kStep) * move;
+        else base += kt * move;
+        trimmed = false;
+        trim();
     }
     // the index within the step of the first value (by columns: of all values) of this lane's 16 bytes of load q
     __device__ __forceinline__ int first_k(int q) const {
-        if constexpr (COLS) return (q * NW + wave) * (512 / N) + lane / (N / 8);
-        else return ((lane % 8) ^ (lane / 8)) * 8;
+        if constexpr (COLS) return (q * kWaves + wave) * (512 / N) + lane / (N / 8);
+        else return ((lane % 8) ^ (4 * (wave & 1) + lane / 16)) * 8;
     }
-    // indices from k0 on that exist, of K in all (by rows: in whole 16-byte pieces)
-    __device__ __forceinline__ int left(int k0, int K) const {
+    // indices from this step on that exist (by rows: in whole 16-byte pieces)
+    __device__ __forceinline__ int left(int step) const {
+        const int k0 = step * kStep;
         if constexpr (FORM == COLPAIR) return depth - (k0 >= half ? k0 - half : k0);
         else return COLS ? K - k0 : (K - k0 + 7) & ~7;
     }
-    // The step from k0 on into LDS.  Where less than a step is left, lanes beyond it read its start; clear() follows.
-    __device__ __forceinline__ void load(unsigned lds, int k0, int K, int pl) const {
-        const int n = left(k0, K);
-        const bool second = FORM == COLPAIR && k0 >= half;
-        const int k1 = second ? k0 - half : k0;
-        const long long at = (COLS ? k1 * ld2 : k1 * 2LL) + pl * plane2;
+    // Where less than a step is left, lanes beyond it read its start; clear() follows.
+    __device__ __forceinline__ void trim() {
+        const int n = left(kt);
+        if (trimmed || n < kStep) {
 #pragma unroll
-        for (int q = 0; q < Q; ++q) {
-            unsigned o = off[q];
-            if (n < kStep && first_k(q) >= n) o -= COLS ? (unsigned)((long long)first_k(q) * ld2) : first_k(q) * 2;
-            load_lds16((FORM == PAIR ? base[q] : FORM == COLPAIR ? (second ? base[1] : base[0]) : base[0]) + at, o,
-                       lds + (q * NW + wave) * 1024);
+            for (int q = 0; q < Q; ++q) {
+                const unsigned by = first_k(q) * (COLS ? ld2 : 2u);
+                const int was = FORM == COLPAIR ? depth % kStep : 0;   // only the end of the first matrix has something behind it
+                if (trimmed && first_k(q) >= was) off[q] += by;
+                if (n < kStep && first_k(q) >= n) off[q] -= by;
+            }
+            trimmed = n < kStep;
         }
     }
-    // zeros for what is beyond the `n` indices left of this step (the same bytes this lane brought)
+    __device__ __forceinline__ void next() {   // on to the next step: the next pair of planes, or the next indices
+        if constexpr (PL == 3) {
+            if (++pair < PAIRS) {
+                at = (planes >> (4 * pair) & 0xf) * plane;
+                return;
+            }
+            pair = 0, at = 0;
+        }
+        ++kt;
+        base += move;
+        if (FORM == PAIR) base2 += move;
+        if (FORM == COLPAIR && kt * kStep == half) base = base2;
+        if (kt * kStep < K) trim();
+    }
+    template <int q>
+    __device__ __forceinline__ void load(unsigned lds) const {
+        const gbyte_ptr p = FORM == PAIR && q % 2 ? base2 : base;
+        load_lds16(PL == 1 ? p : p + at, off[q], lds + q * kWaves * 1024);
+    }
+    // zeros for what is beyond the `n` indices left of a step (the same bytes this lane brought)
     __device__ __forceinline__ void clear(char *lds, int n) const {
 #pragma unroll
         for (int q = 0; q < Q; ++q)
-            if (first_k(q) >= n) *(u32x4 *)(lds + (q * NW + wave) * 1024 + lane * 16) = (u32x4){0, 0, 0, 0};
+            if (first_k(q) >= n) *(u32x4 *)(lds + (q * kWaves + wave) * 1024 + lane * 16) = (u32x4){0, 0, 0, 0};
     }
 };
 
@@ -181,146 +230,250 @@ struct Stager {
 template <int FORM, int N, int T>
 struct Reader {
     static constexpr bool COLS = FORM == COL || FORM == COLPAIR;
-    unsigned at[COLS ? T : 4];
-    __device__ __forceinline__ void init(int r0, int lane) {
+    unsigned at[COLS ? T : 4], high[COLS ? T : 4];   // high: 64 KB further, an instruction's offset has 16 bits
+    __device__ __forceinline__ void init(unsigned lds, int r0, int lane) {
         if constexpr (COLS) {
             const int s = lane % 16, g = lane / 16;
             const int k = 8 * (g >> 1) + s / 4;
 #pragma unroll
             for (int i = 0; i < T; ++i)
-                at[i] = k * (2 * N) + (((r0 / 32 + i) ^ col_swizzle<N>(k)) * 64) + (g & 1) * 32 + (s % 4) * 8;
+                at[i] = lds + k * (2 * N) + (((r0 / 32 + i) ^ col_swizzle<N>(k)) * 64) + (g & 1) * 32 + (s % 4) * 8;
         } else {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) at[c] = (r0 + (lane & 31)) * 128 + (((2 * c + (lane >> 5)) ^ (lane & 7)) * 16);
+            for (int c = 0; c < 4; ++c) at[c] = lds + (r0 + (lane & 31)) * 128 + (((2 * c + (lane >> 5)) ^ ((lane >> 1) & 7)) * 16);
+        }
+#pragma unroll
+        for (int i = 0; i < (COLS ? T : 4); ++i) {
+            high[i] = at[i] + 65536;
+            asm volatile("" : "+v"(at[i]), "+v"(high[i]));   // held, not formed anew for every read
         }
     }
-    __device__ __forceinline__ u32x4 read(unsigned lds, int c, int i) const {
+    template <int AT>   // offset of the buffer
+    __device__ __forceinline__ u32x4 read(int c, int i) const {
+        typedef const __attribute__((address_space(3))) char *p1;
         typedef __attribute__((address_space(3))) u32x4 *p4;
+        constexpr int REST = AT & 0xffff;
+        const int k = COLS ? i : c;
+        const p1 p = (p1)(size_t)(AT >= 65536 ? high[k] : at[k]);
         if constexpr (COLS) {
             typedef short s16x4 __attribute__((ext_vector_type(4)));
             typedef __attribute__((address_space(3))) s16x4 *p2;
-            const unsigned a = lds + at[i] + c * (16 * 2 * N);
-            const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((p2)(size_t)a));
-            const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((p2)(size_t)(a + 4 * 2 * N)));
+            const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((p2)(p + REST + c * (16 * 2 * N))));
+            const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((p2)(p + REST + c * (16 * 2 * N) + 4 * 2 * N)));
             return (u32x4){lo[0], lo[1], hi[0], hi[1]};
         } else {
-            return *(p4)(size_t)(lds + at[c] + i * (32 * 128));
+            return *(p4)(p + REST + i * (32 * 128));
         }
     }
 };
 
-template <int PL, int FA, int FB, int BM, int BN, int WM, int WN, typename Epi>
-__global__ __launch_bounds__(64 * WM * WN, 2) void gemm_kernel(Operand A, Operand B, Shape sh, int mt, int nt, Epi epi) {
-    constexpr int NW = WM * WN, MT = BM / WM / 32, NT = BN / WN / 32, PAIRS = PL == 3 ? 6 : 1;
+// LDS of a wave's epilogue: one block of 32 rows on its way to whole 16-byte pieces.
+template <int NT> constexpr int kEpiBytes = 32 * (NT * 32 * 4 + 16);
+
+template <int PL, int FA, int FB, int BM, int BN, typename Epi>
+__global__ __launch_bounds__(64 * kWaves, BM == 256 ? 1 : 2) void gemm_kernel(Operand A, Operand B, Shape sh, int nt, int splits, Epi epi) {
+    constexpr int MT = BM / 64, NT = BN / 64, PAIRS = PL == 3 ? 6 : 1;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    int tm, tn;
-    tile_of(blockIdx.x, mt, nt, &tm, &tn);
     const int M = live(sh.M, sh.rows_dev, sh.rows_first);
     const int K = live(sh.K, sh.k_dev, sh.k_first);
-    if (tm * BM >= M) return;
-    Stager<FA, BM, NW> sa;
-    Stager<FB, BN, NW> sb;
-    sa.init(A, tm * BM, wave, lane);
-    sb.init(B, tn * BN, wave, lane);
+    int tm, tn, split;
+    if (!tile_of(blockIdx.x, (M + BM - 1) / BM, nt, splits, &tm, &tn, &split)) return;
+    const int wm = wave / 2, wn = wave % 2;
+    constexpr unsigned ABYTES = BM * 128, BBYTES = BN * 128, B0 = 3 * ABYTES;   // A's buffers, then B's
+    const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) char *)smem;
     Reader<FA, BM, MT> ra;
     Reader<FB, BN, NT> rb;
-    const int wm = wave / WN, wn = wave % WN;
-    ra.init(wm * MT * 32, lane);
-    rb.init(wn * NT * 32, lane);
-    constexpr unsigned ABYTES = BM * 128, STAGE = (BM + BN) * 128;
-    const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) char *)smem;
+    ra.init(lds0, wm * MT * 32, lane);
+    rb.init(lds0 + B0, wn * NT * 32, lane);
     f32x16 acc[MT][NT] = {};
-    const int steps = (K + kStep - 1) / kStep * PAIRS;
-    auto stage = [&](int st) {
-        const int kt = PAIRS == 1 ? st : st / PAIRS, s = PAIRS == 1 ? 0 : st - kt * PAIRS;
-        const unsigned l = lds0 + (st & 1) * STAGE;
-        // planes of A and B in the six products: 00 10 01 11 02 20
-        const int pa = PL == 1 ? 0 : (0x010102 >> (4 * (5 - s))) & 0xf, pb = PL == 1 ? 0 : (0x001120 >> (4 * (5 - s))) & 0xf;
-        sa.load(l, kt * kStep, K, pa);
-        sb.load(l + ABYTES, kt * kStep, K, pb);
+    // parts are whole steps of the contraction at its longest; what is beyond its actual end is left out
+    const int per = ((sh.K + kStep - 1) / kStep + splits - 1) / splits;
+    const int kt0 = split * per, kt1 = min((K + kStep - 1) / kStep, kt0 + per), steps = max(0, kt1 - kt0) * PAIRS;
+    Stager<FA, BM, PL> sa;
+    Stager<FB, BN, PL> sb;
+    // planes of A and B in the six products: 00 10 01 11 02 20
+    sa.init(A, tm * BM, kt0, K, 0x201010, wave, lane);
+    sb.init(B, tn * BN, kt0, K, 0x021100, wave, lane);
+    constexpr int QA = Stager<FA, BM, PL>::Q, QB = Stager<FB, BN, PL>::Q;
+    const unsigned lds_wave = lds0 + wave * 1024;
+    auto load_a = [&](auto buf, auto number) __attribute__((always_inline)) {
+        sa.template load<decltype(number)::value>(lds_wave + decltype(buf)::value % 3 * ABYTES);
     };
-    if (steps) stage(0);
-    for (int st = 0; st < steps; ++st) {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (st + 1 < steps) stage(st + 1);
-        const unsigned l = lds0 + (st & 1) * STAGE;
-        {
-            const int k0 = (PAIRS == 1 ? st : st / PAIRS) * kStep;
-            const int la = sa.left(k0, K), lb = sb.left(k0, K);
-            if (la < kStep || lb < kStep) {
-                sa.clear(smem + (st & 1) * STAGE, la);
-                sb.clear(smem + (st & 1) * STAGE + ABYTES, lb);
-                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            }
+    auto load_b = [&](auto buf, auto number) __attribute__((always_inline)) {
+        sb.template load<decltype(number)::value>(lds_wave + B0 + decltype(buf)::value % 2 * BBYTES);
+    };
+    int akt = kt0, as = 0;   // the step that arrives next
+    // The next step is there and everybody may read it: its loads have landed (`ahead` that were issued later stay in flight), all waves
+    // have read what they need of the step before, and what lies beyond the contraction is zero.
+    auto arrive = [&](auto buf, auto ahead) __attribute__((always_inline)) {
+        constexpr int U = decltype(buf)::value;
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(decltype(ahead)::value) : "memory");
+        const int la = sa.left(akt), lb = sb.left(akt);
+        if (__builtin_expect(min(la, lb) < kStep, 0)) {
+            sa.clear(smem + U % 3 * ABYTES, la);
+            sb.clear(smem + B0 + U % 2 * BBYTES, lb);
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         }
-        u32x4 a[2][MT], b[2][NT];
+        if (PAIRS == 1 || ++as == PAIRS) as = 0, ++akt;
+    };
+    u32x4 a[2][MT], b[2][NT];
+    auto fetch = [&](auto buf, int c, int r) __attribute__((always_inline)) {   // read r of the MT + NT of quarter c, in the order the products need them
+        constexpr int U = decltype(buf)::value;
+        if (r == 0) a[c & 1][0] = ra.template read<U % 3 * ABYTES>(c, 0);
+        else if (r <= NT) b[c & 1][r - 1] = rb.template read<U % 2 * BBYTES>(c, r - 1);
+        else a[c & 1][r - NT] = ra.template read<U % 3 * ABYTES>(c, r - NT);
+    };
+    constexpr int P = MT * NT, R = MT + NT;
+    constexpr int BAR = P / 4;   // products of the last quarter in front of the barrier
+    // Step U of six (after which all buffers have had their turn).  left: steps from this one on, which FULL says are more than two.
+    auto step = [&](auto number, auto full, int left) __attribute__((always_inline)) {
+        constexpr int U = decltype(number)::value;
+        constexpr bool FULL = decltype(full)::value;
+        const std::integral_constant<int, U> now;
+        const std::integral_constant<int, U + 1> next;
+        const std::integral_constant<int, U + 2> second;
+        const bool has_next = FULL || left > 1, has_second = FULL || left > 2;
+        for_blocks<4>([&](auto quarter) __attribute__((always_inline)) {
+            constexpr int c = decltype(quarter)::value;
+            for_blocks<P>([&](auto product) __attribute__((always_inline)) {
+                constexpr int p = decltype(product)::value;
+                if constexpr (c == 3 && p == BAR) {
+                    if (has_next) {
+                        if (has_second) arrive(next, std::integral_constant<int, QA>());
+                        else arrive(next, std::integral_constant<int, 0>());
+                    }
+                }
+                acc[p / NT][p % NT] = mfma32(b[c & 1][p % NT], a[c & 1][p / NT], acc[p / NT][p % NT]);
+                if constexpr (c < 3) {
 #pragma unroll
-        for (int i = 0; i < MT; ++i) a[0][i] = ra.read(l, 0, i);
+                    for (int r = p * R / P; r < (p + 1) * R / P; ++r) fetch(now, c + 1, r);
+                } else if constexpr (p >= BAR) {
+                    constexpr int S = P - BAR;
+                    if (has_next) {
 #pragma unroll
-        for (int j = 0; j < NT; ++j) b[0][j] = rb.read(l + ABYTES, 0, j);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            if (c < 3) {
-#pragma unroll
-                for (int i = 0; i < MT; ++i) a[(c + 1) & 1][i] = ra.read(l, c + 1, i);
-#pragma unroll
-                for (int j = 0; j < NT; ++j) b[(c + 1) & 1][j] = rb.read(l + ABYTES, c + 1, j);
-            }
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = mfma32(b[c & 1][j], a[c & 1][i], acc[i][j]);
+                        for (int r = (p - BAR) * R / S; r < (p - BAR + 1) * R / S; ++r) fetch(next, 0, r);
+                    }
+                    // the first half of B's step after next, into this step's buffer
+                    if (has_second)
+                        for_blocks<(p - BAR + 1) * (QB / 2) / S - (p - BAR) * (QB / 2) / S>([&](auto k) __attribute__((always_inline)) {
+                            load_b(second, std::integral_constant<int, (p - BAR) * (QB / 2) / S + decltype(k)::value>());
+                        });
+                }
+                // the other half of B's next step, then A's step after next
+                if constexpr (c == 0) {
+                    if (has_next)
+                        for_blocks<(p + 1) * (QB / 2) / P - p * (QB / 2) / P>([&](auto k) __attribute__((always_inline)) {
+                            load_b(next, std::integral_constant<int, QB / 2 + p * (QB / 2) / P + decltype(k)::value>());
+                        });
+                    if (p == P - 1 && has_next) sb.next();
+                } else if constexpr (c < 3) {
+                    if (has_second)
+                        for_blocks<(p + 1) * (QA / 2) / P - p * (QA / 2) / P>([&](auto k) __attribute__((always_inline)) {
+                            load_a(second, std::integral_constant<int, (c - 1) * (QA / 2) + p * (QA / 2) / P + decltype(k)::value>());
+                        });
+                    if (c == 2 && p == P - 1 && has_second) sa.next();
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        });
+    };
+    if (steps) {
+        const std::integral_constant<int, 0> zero;
+        const std::integral_constant<int, 1> one;
+        for_blocks<QA>([&](auto q) __attribute__((always_inline)) { load_a(zero, q); });
+        sa.next();
+        for_blocks<QB>([&](auto q) __attribute__((always_inline)) { load_b(zero, q); });
+        sb.next();
+        if (steps > 1) {
+            for_blocks<QA>([&](auto q) __attribute__((always_inline)) { load_a(one, q); });
+            sa.next();
+            for_blocks<QB / 2>([&](auto q) __attribute__((always_inline)) { load_b(one, q); });
+            arrive(zero, std::integral_constant<int, QA + QB / 2>());
+        } else {
+            arrive(zero, zero);
         }
+#pragma unroll
+        for (int r = 0; r < R; ++r) fetch(zero, 0, r);
     }
+    int left = steps;
+    for (; left > 7; left -= 6) for_blocks<6>([&](auto u) __attribute__((always_inline)) { step(u, std::true_type(), 3); });
+    for_blocks<7>([&](auto u) __attribute__((always_inline)) {
+        if (left > decltype(u)::value) step(u, std::false_type(), left - decltype(u)::value);
+    });
     const int m0 = tm * BM + wm * MT * 32, n0 = tn * BN + wn * NT * 32;
-    if (m0 >= M || n0 >= sh.Nn) return;
     if constexpr (PL == 3) {
-        if (!all_finite(acc)) product_exact<MT, NT, FA, FB>(A, B, m0, n0, K, lane, acc);
+        if (m0 < M && n0 < sh.Nn && !all_finite(acc, M - m0, lane))
+            product_exact<MT, NT, FA, FB>(A, B, m0, n0, kt0 * kStep, min(K, kt1 * kStep), lane, acc);
     }
-    epi.run(acc, m0, n0, lane, M, sh.Nn);
+    __syncthreads();   // the buffers are free for the epilogue
+    if (m0 >= M || n0 >= sh.Nn) return;
+    epi.run(acc, m0, n0, lane, M, sh.Nn, split, smem + wave * kEpiBytes<NT>);
 }
 
-template <int PL, int FA, int FB, int BM, int BN, int WM, int WN, typename Epi>
-int launch_tiles(const char *name, const Operand &A, const Operand &B, const Shape &sh, const Epi &epi, hipStream_t s) {
+template <int PL, int FA, int FB, int BM, int BN, typename Epi>
+int launch_tiles(const char *name, const Operand &A, const Operand &B, const Shape &sh, int splits, const Epi &epi, hipStream_t s) {
     const int mt = ceil_div(sh.M, BM), nt = ceil_div(sh.Nn, BN);
-    const LaunchPlan p = make_plan(name, {PL, FA, FB, BM, BN}, {sh.M, sh.Nn, sh.K}, dim3((unsigned)((long long)mt * nt)), 64 * WM * WN,
-                                   2 * (BM + BN) * 128);
-    LC_PLAN_REQUIRE(p, (long long)mt * nt <= 0x7fffffffLL);
+    constexpr int LDS = (3 * BM + 2 * BN) * 128;
+    static_assert(kWaves * kEpiBytes<BN / 64> <= LDS, "the epilogue's LDS is that of the buffers");
+    const LaunchPlan p = make_plan(name, {PL, FA, FB, BM, BN}, {sh.M, sh.Nn, sh.K, splits}, dim3((unsigned)((long long)mt * nt * splits)),
+                                   64 * kWaves, LDS);
+    LC_PLAN_REQUIRE(p, (long long)mt * nt * splits <= 0x7fffffffLL && splits >= 1);
     LC_PLAN_REQUIRE(p, A.ld % 8 == 0 && B.ld % 8 == 0 && A.plane % 8 == 0 && B.plane % 8 == 0);
     constexpr bool CA = FA == COL || FA == COLPAIR, CB = FB == COL || FB == COLPAIR;
     LC_PLAN_REQUIRE(p, CA ? A.rows % 8 == 0 && A.ld >= A.rows && A.rows >= sh.M : A.rows >= sh.M && A.ld >= sh.K);
     LC_PLAN_REQUIRE(p, CB ? B.rows % 8 == 0 && B.ld >= B.rows && B.rows >= sh.Nn : B.rows >= (FB == PAIR ? 1 : sh.Nn) && B.ld >= sh.K);
     LC_PLAN_REQUIRE(p, FA != PAIR && FA != COLPAIR && (FB != PAIR || sh.Nn == 64 * ceil_div(B.rows, 32)));
-    LC_PLAN_REQUIRE(p, FB != COLPAIR || (B.half % kStep == 0 && B.depth >= 1 && B.depth <= B.half && sh.K == B.half + B.depth));
+    LC_PLAN_REQUIRE(p, FB != COLPAIR || (B.half % kStep == 0 && B.depth >= 1 && B.half - B.depth < kStep && B.depth <= B.half &&
+                                         sh.K == B.half + B.depth));
     LC_PLAN_REQUIRE(p, A.ld <= (1 << 22) && B.ld <= (1 << 22));   // 256 rows' offsets stay below 2^31 bytes
     LC_PLAN_REQUIRE(p, ptr_aligned16(A.p0) && ptr_aligned16(B.p0) && ptr_aligned16(B.p1));
-    LC_LAUNCH(p, name, (gemm_kernel<PL, FA, FB, BM, BN, WM, WN, Epi>), s, A, B, sh, mt, nt, epi);
+    LC_LAUNCH(p, name, (gemm_kernel<PL, FA, FB, BM, BN, Epi>), s, A, B, sh, nt, splits, epi);
     return LC_OK;
 }
 
-// A workgroup per 256 x 256 of the result where that fills the chip, per 128 x 128 (two at a time on a compute unit) where not.
-template <int PL, int FA, int FB, typename Epi>
-int launch_gemm(const char *name, const Operand &A, const Operand &B, const Shape &sh, const Epi &epi, hipStream_t s) {
-    if (sh.M == 0 || sh.Nn == 0) return LC_OK;
-    if ((long long)ceil_div(sh.M, 256) * ceil_div(sh.Nn, 256) >= kComputeUnits)
-        return launch_tiles<PL, FA, FB, 256, 256, 2, 4>(name, A, B, sh, epi, s);
-    return launch_tiles<PL, FA, FB, 128, 128, 2, 2>(name, A, B, sh, epi, s);
-}
+// ---------------------------------------------------------------------------------------------------------------------------
+// Epilogues.  A lane's values of one row lie 32 columns apart, four at a time; through LDS they become whole 16-byte pieces of rows, so
+// that a wave's store covers lines.
 
-// four consecutive values of one row; n counts from the row's start and may run past its end at `width`
-template <typename T>
-__device__ __forceinline__ void store4(T *row, int n, int width, bool vec, const float (&v)[4]) {
-    if (vec && n + 3 < width) {
-        if constexpr (sizeof(T) == 4) {
-            *(f32x4 *)(row + n) = (f32x4){v[0], v[1], v[2], v[3]};
-        } else {
-            *(u16x4 *)(row + n) = (u16x4){to_bf16(v[0]), to_bf16(v[1]), to_bf16(v[2]), to_bf16(v[3])};
+// 32 rows of COLS values of type V on their way; the pitch spreads rows over the banks.
+template <typename V, int COLS>
+struct RowStage {
+    static constexpr int PITCH = COLS * (int)sizeof(V) + 16, PIECES = COLS * (int)sizeof(V) / 16, EACH = 16 / (int)sizeof(V);
+    char *lds;
+    int lane;
+    // four values of this lane's row from column c on
+    __device__ __forceinline__ void put(int c, const V (&v)[4]) const {
+        typedef V V4 __attribute__((ext_vector_type(4)));
+        *(V4 *)(lds + (lane & 31) * PITCH + c * (int)sizeof(V)) = (V4){v[0], v[1], v[2], v[3]};
+    }
+    // each(row, column, piece) for all pieces; LDS serves a wave in order
+    template <typename Each>
+    __device__ __forceinline__ void take(const Each &each) const {
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int p = 0; p < 32 * PIECES / 64; ++p) {
+            const int at = p * 64 + lane, row = at / PIECES, piece = at % PIECES;
+            each(row, piece * EACH, *(const u32x4 *)(lds + row * PITCH + piece * 16));
         }
+        __builtin_amdgcn_wave_barrier();
+    }
+};
+
+// a piece of a row of `width` values from column n on, at any alignment
+template <typename V>
+__device__ __forceinline__ void store_piece(V *row, int n, int width, const u32x4 &w) {
+    constexpr int EACH = 16 / sizeof(V);
+    if (n + EACH <= width) {
+        __builtin_memcpy(row + n, &w, 16);
     } else {
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-            if (n + r < width) row[n + r] = narrow<T>(v[r]);
+        for (int e = 0; e < EACH; ++e)
+            if (n + e < width) {
+                const unsigned x = w[e * sizeof(V) / 4];
+                if constexpr (sizeof(V) == 4) ((unsigned *)row)[n + e] = x;
+                else ((unsigned short *)row)[n + e] = (unsigned short)(x >> (16 * (e & 1)));
+            }
     }
 }
 
@@ -329,39 +482,161 @@ __device__ __forceinline__ void store4(T *row, int n, int width, bool vec, const
 template <typename T>
 struct StoreEpi {
     T *out0, *out1;
-    int second, width0rows, width1rows;   // rows that exist of each
+    int second, rows0, rows1;   // rows that exist of each
     int width;
     const int *index;
     const float *add, *factor;
+    // where row m goes; null: nowhere
+    __device__ __forceinline__ T *row(int m) const {
+        const bool up = m >= second;
+        const int r = up ? m - second : m;
+        if (r >= (up ? rows1 : rows0)) return nullptr;
+        return (up ? out1 : out0) + (long long)(index ? index[r] : r) * width;
+    }
+    __device__ __forceinline__ void finish(int m, int n, float f, float (&v)[4], T (&o)[4]) const {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            if (add && n + r < width) v[r] += add[(long long)m * width + n + r];
+            o[r] = narrow<T>(v[r] * f);
+        }
+    }
     template <int MT, int NT>
-    __device__ __forceinline__ void run(const f32x16 (&acc)[MT][NT], int m0, int n0, int lane, int M, int Nn) const {
-        const bool vec = width % 4 == 0;
+    __device__ __forceinline__ void run(f32x16 (&acc)[MT][NT], int m0, int n0, int lane, int M, int, int, char *lds) const {
+        const RowStage<T, NT * 32> stage = {lds, lane};
         const float f = factor ? *factor : 1.f;
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             const int m = m0 + 32 * i + (lane & 31);
-            if (m >= M) continue;
-            const bool up = m >= second;
-            const int row = up ? m - second : m;
-            if (row >= (up ? width1rows : width0rows)) continue;
-            T *o = (up ? out1 : out0) + (long long)(index ? index[row] : row) * width;
 #pragma unroll
             for (int j = 0; j < NT; ++j)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const int n = n0 + 32 * j + 8 * q + 4 * (lane >> 5);
-                    float v[4];
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        v[r] = acc[i][j][4 * q + r];
-                        if (add && n + r < width) v[r] += add[(long long)m * width + n + r];
-                        v[r] *= f;
-                    }
-                    store4(o, n, width, vec, v);
+                    const int c = 32 * j + 8 * q + 4 * (lane >> 5);
+                    float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                    T o[4];
+                    finish(min(m, M - 1), n0 + c, f, v, o);
+                    stage.put(c, o);
                 }
+            stage.take([&](int r, int c, const u32x4 &w) {
+                const int to = m0 + 32 * i + r;
+                T *o = to < M ? row(to) : nullptr;
+                if (o) store_piece(o, n0 + c, width, w);
+            });
         }
     }
 };
+
+// The sums of one part of the contraction, as they are: [split][M][ld] floats, ld a multiple of 4.
+struct PartEpi {
+    float *part;
+    long long ld;
+    int M;
+    template <int MT, int NT>
+    __device__ __forceinline__ void run(f32x16 (&acc)[MT][NT], int m0, int n0, int lane, int live_rows, int, int split, char *lds) const {
+        const RowStage<float, NT * 32> stage = {lds, lane};
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                    stage.put(32 * j + 8 * q + 4 * (lane >> 5), v);
+                }
+            stage.take([&](int r, int c, const u32x4 &w) {
+                const int m = m0 + 32 * i + r;
+                if (m < live_rows && n0 + c < ld) *(u32x4 *)(part + ((long long)split * M + m) * ld + n0 + c) = w;
+            });
+        }
+    }
+};
+
+// Adds the parts up in their order and stores the sums, four columns a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void join_parts_kernel(const float *part, long long ld, int splits, Shape sh, StoreEpi<T> epi) {
+    const long long at = blockIdx.x * 256LL + threadIdx.x, quads = ld / 4;
+    const int m = (int)(at / quads), n = (int)(at - m * quads) * 4;
+    if (m >= live(sh.M, sh.rows_dev, sh.rows_first)) return;
+    T *row = epi.row(m);
+    if (!row) return;
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < splits; ++i) s += *(const f32x4 *)(part + ((long long)i * sh.M + m) * ld + n);
+    float v[4] = {s[0], s[1], s[2], s[3]};
+    T o[4];
+    epi.finish(m, n, epi.factor ? *epi.factor : 1.f, v, o);
+    if (n + 4 <= epi.width) {
+        __builtin_memcpy(row + n, o, sizeof(o));
+    } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (n + r < epi.width) row[n + r] = o[r];
+    }
+}
+
+// How a product is cut: into tiles of 256 x 256, one on a compute unit, or of 128 x 128, two on one; and its contraction into parts.
+struct Cut {
+    bool large;
+    int splits;
+};
+// The cut that takes least by an estimate in microseconds from measured times: a step of a large tile 1.7, of two small ones that share
+// a compute unit 0.82, of one that has it for itself 0.56, and what begins and ends a tile; joining parts moves 8 bytes a value at 4 TB/s.
+// From four rounds of large tiles on these are taken in any case: they bring half the bytes into LDS per product, and the chip runs
+// at the clock its power allows (8192 x 128000 x 4096 6.8 against 8.0 ms).  Both cuts at other sizes: 192 x 16384 x 4096 85 us large
+// and 40 small; 1000 x 768 x 30011 in fp32 3330 and 1572, in 16 parts 256 and 265.
+inline Cut choose_cut(int M, int Nn, int K, int pairs, bool may_split) {
+    const double large = (double)ceil_div(M, 256) * ceil_div(Nn, 256), small = (double)ceil_div(M, 128) * ceil_div(Nn, 128);
+    if (large >= 4 * kComputeUnits) return Cut{true, 1};
+    const int steps = ceil_div(K, kStep);
+    Cut best = {false, 1};
+    double least = 1e30;
+    for (int s = 1; s <= 32 && s <= std::max(1, steps / 2) && (s == 1 || may_split); ++s) {
+        const double part = (double)ceil_div(steps, s) * pairs;
+        const double join = s > 1 ? 4 + 8e-6 * s * (double)M * Nn / 4 : 0;
+        const double rounds = std::ceil(large * s / kComputeUnits), wgs = small * s;
+        const double tl = rounds * (part * 1.7 + 15) + join;
+        const double ts = (wgs <= kComputeUnits ? part * 0.56 + 4 : std::max(1.0, wgs / (2 * kComputeUnits) + 0.25) * (part * 0.82 + 6)) + join;
+        if (tl < least) best = {true, s}, least = tl;
+        if (ts < least) best = {false, s}, least = ts;
+    }
+    return best;
+}
+
+template <int PL, int FA, int FB, typename Epi>
+int launch_cut(const char *name, const Operand &A, const Operand &B, const Shape &sh, const Cut &c, const Epi &epi, hipStream_t s) {
+    if (c.large) return launch_tiles<PL, FA, FB, 256, 256>(name, A, B, sh, c.splits, epi, s);
+    return launch_tiles<PL, FA, FB, 128, 128>(name, A, B, sh, c.splits, epi, s);
+}
+
+// columns of a wave in such a product
+inline int product_wave_cols(int M, int Nn, int K, int pairs) { return choose_cut(M, Nn, K, pairs, false).large ? 128 : 64; }
+
+// A product whose epilogue needs whole sums.
+template <int PL, int FA, int FB, typename Epi>
+int launch_gemm(const char *name, const Operand &A, const Operand &B, const Shape &sh, const Epi &epi, hipStream_t s) {
+    if (sh.M == 0 || sh.Nn == 0) return LC_OK;
+    return launch_cut<PL, FA, FB>(name, A, B, sh, choose_cut(sh.M, sh.Nn, sh.K, PL == 3 ? 6 : 1, false), epi, s);
+}
+
+// Floats that launch_product() needs for the parts of a product of this size.
+inline long long part_floats(int M, int Nn, int K, int pairs) {
+    const Cut c = choose_cut(M, Nn, K, pairs, true);
+    return c.splits > 1 ? (long long)c.splits * M * round_up(Nn, 4) : 0;
+}
+
+// A product that is stored, cut along its contraction where that helps.
+template <int PL, int FA, int FB, typename T>
+int launch_product(const char *name, const Operand &A, const Operand &B, const Shape &sh, const StoreEpi<T> &epi, float *part, hipStream_t s) {
+    if (sh.M == 0 || sh.Nn == 0) return LC_OK;
+    const Cut c = choose_cut(sh.M, sh.Nn, sh.K, PL == 3 ? 6 : 1, true);
+    if (c.splits == 1) return launch_cut<PL, FA, FB>(name, A, B, sh, c, epi, s);
+    const long long ld = round_up(sh.Nn, 4);
+    if (int rc = launch_cut<PL, FA, FB>(name, A, B, sh, c, PartEpi{part, ld, sh.M}, s)) return rc;
+    const long long blocks = ((long long)sh.M * (ld / 4) + 255) / 256;
+    const LaunchPlan p = make_plan(name, {}, {sh.M, sh.Nn, c.splits}, dim3((unsigned)blocks), 256, 0);
+    LC_PLAN_REQUIRE(p, blocks <= 0x7fffffffLL && part);
+    LC_LAUNCH(p, name, (join_parts_kernel<T>), s, part, ld, c.splits, sh, epi);
+    return LC_OK;
+}
 
 }  // namespace head
 }  // namespace lc

@@ -33,16 +33,18 @@ __global__ __launch_bounds__(256) void planes_kernel(Get get, bf16_t *dst, long 
     }
 }
 
-// eight consecutive values of a row from column c on, zeros from column C on
+// eight consecutive values of a row from column c on (any alignment), zeros from column C on
 template <typename T>
-__device__ __forceinline__ void load8(const T *row, int c, int C, bool vec, float (&v)[8]) {
-    if (vec && c + 8 <= C) {
+__device__ __forceinline__ void load8(const T *row, int c, int C, float (&v)[8]) {
+    if (c + 8 <= C) {
         if constexpr (sizeof(T) == 4) {
-            const f32x4 a = *(const f32x4 *)(row + c), b = *(const f32x4 *)(row + c + 4);
+            typedef f32x4 any __attribute__((aligned(4)));
+            const f32x4 a = *(const any *)(row + c), b = *(const any *)(row + c + 4);
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = a[e], v[4 + e] = b[e];
         } else {
-            const u32x4 a = *(const u32x4 *)(row + c);
+            typedef u32x4 any __attribute__((aligned(2)));
+            const u32x4 a = *(const any *)(row + c);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = (e & 1) ? bf16_hi(a[e >> 1]) : bf16_lo(a[e >> 1]);
         }
@@ -65,7 +67,7 @@ struct Stored {
             for (int e = 0; e < 8; ++e) v[0][e] = 0.f;
             return;
         }
-        load8(p + (long long)(index ? index[r] : r) * C, c, C, C % 8 == 0, v[0]);
+        load8(p + (long long)(index ? index[r] : r) * C, c, C, v[0]);
     }
 };
 

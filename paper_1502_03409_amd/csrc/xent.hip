@@ -9,14 +9,13 @@
 // place, and two products give dx = d w and dw = d^T x.
 //
 // Masked rows take no part: the rows that count are gathered first, and every kernel runs over as many as there are.
-#include "head_gemm.hpp"
+#include "head_few.hpp"
 #include "head_planes.hpp"
 
 namespace lc {
 namespace head {
 namespace {
 
-constexpr int kWaveCols = 64;               // columns of the vocabulary that share one entry of the row statistics
 constexpr long long kBlockBytes = 2LL << 30;   // exponentials kept at a time
 
 struct Rows {
@@ -66,42 +65,43 @@ __global__ __launch_bounds__(1024) void rows_kernel(const int64_t *target, const
 template <typename T> struct Kept;   // what a tile leaves for the gradient
 template <> struct Kept<float> { typedef float V; };
 template <> struct Kept<bf16_t> { typedef _Float16 V; };
-typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
-
-__device__ __forceinline__ void keep4(float *row, int n, const float (&v)[4]) {
-    *(f32x4 *)(row + n) = (f32x4){v[0], v[1], v[2], v[3]};
-}
-__device__ __forceinline__ void keep4(_Float16 *row, int n, const float (&v)[4]) {
-    *(f16x4 *)(row + n) = (f16x4){(_Float16)(v[0] * 32768.f), (_Float16)(v[1] * 32768.f), (_Float16)(v[2] * 32768.f), (_Float16)(v[3] * 32768.f)};
-}
+__device__ __forceinline__ float kept(float, float l, float) { return l; }                                     // score l
+__device__ __forceinline__ _Float16 kept(_Float16, float, float e) { return (_Float16)(e * 32768.f); }         // exponential e
 
 // Per wave and row: the largest score, the sum of exponentials (both without the target), the target's score, and with KEEP what
 // the gradient needs.
 template <typename T, bool KEEP>
 struct XentEpi {
-    float2 *stats;       // [tile of kWaveCols columns][stats_ld]
+    float2 *stats;       // [wave's columns][stats_ld]
     long long stats_ld;
     const int *target;
     float *tl;
     typename Kept<T>::V *keep;   // [M][ld], ld a multiple of 64 that holds all columns: exponentials (bf16) or scores (fp32)
     long long ld;
     template <int MT, int NT>
-    __device__ __forceinline__ void run(const f32x16 (&acc)[MT][NT], int m0, int n0, int lane, int M, int V) const {
-        static_assert(NT * 32 == kWaveCols, "one entry of the statistics per wave");
+    __device__ __forceinline__ void run(f32x16 (&acc)[MT][NT], int m0, int n0, int lane, int M, int V, int, char *lds) const {
+        typedef typename Kept<T>::V K;
+        const RowStage<K, NT * 32> stage = {lds, lane};
         const int h = lane >> 5;
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
+        for_blocks<MT>([&](auto block) __attribute__((always_inline)) {
+            constexpr int i = decltype(block)::value;
             const int m = m0 + 32 * i + (lane & 31);
-            const int t = m < M ? target[m] : -1;
-            float top = -__builtin_inff();
+            // columns of this wave that exist, and the target's, as this lane counts: 0 .. 3, 8 .. 11, ..
+            int end = V - n0 - 4 * h, at = (m < M ? target[m] : -1) - n0 - 4 * h;
+            asm volatile("" : "+v"(end), "+v"(at));   // compared anew for every block of rows: the masks of all would not fit
+            float top = -__builtin_inff(), own = 0.f;
 #pragma unroll
             for (int j = 0; j < NT; ++j)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const int n = n0 + 32 * j + 8 * (e >> 2) + 4 * h + (e & 3);
-                    if (n == t) tl[m] = acc[i][j][e];
-                    else if (n < V) top = fmaxf(top, acc[i][j][e]);
+                    const int c = 32 * j + 8 * (e >> 2) + (e & 3);
+                    const float l = acc[i][j][e];
+                    own = c == at ? l : own;
+                    const float rest = c == at || c >= end ? -__builtin_inff() : l;
+                    acc[i][j][e] = rest;
+                    top = fmaxf(top, rest);
                 }
+            if (m < M && at >= 0 && at < NT * 32 && (at & 4) == 0) tl[m] = own;
             top = fmaxf(top, __shfl_xor(top, 32));
             const float base = top == -__builtin_inff() ? 0.f : top;   // all scores -inf: exponentials of 0, not of NaN
             float sum = 0.f;
@@ -109,53 +109,63 @@ struct XentEpi {
             for (int j = 0; j < NT; ++j)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const int n = n0 + 32 * j + 8 * q + 4 * h;
-                    float v[4];
+                    K v[4];
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const float l = acc[i][j][4 * q + r];
                         const float e = sizeof(T) == 4 ? expf(l - base) : __expf(l - base);
-                        if (n + r < V && n + r != t) sum += e;
-                        v[r] = sizeof(T) == 4 ? l : e;
+                        sum += e;
+                        v[r] = kept(K(), l, e);
                     }
-                    if (KEEP && m < M && n < ld) keep4(keep + m * ld, n, v);
+                    if (KEEP) stage.put(32 * j + 8 * q + 4 * h, v);
                 }
+            if (KEEP)
+                stage.take([&](int r, int c, const u32x4 &w) {
+                    const int to = m0 + 32 * i + r;
+                    if (to < M && n0 + c < ld) *(u32x4 *)(keep + to * ld + n0 + c) = w;
+                });
             sum += __shfl_xor(sum, 32);
-            if (m < M && h == 0) stats[(n0 / kWaveCols) * stats_ld + m] = make_float2(top, sum);
-        }
+            if (m < M && h == 0) stats[(n0 / (NT * 32)) * stats_ld + m] = make_float2(top, sum);
+        });
     }
 };
 
-// Joins the tiles of 16 rows: 16 threads a row, each over every 16th tile, in a fixed order.
+// Joins the tiles of R rows: 256 / R threads a row, each over its share of the tiles, in a fixed order.  16 rows read whole lines of
+// the statistics; with few rows the share of a thread matters more (one row of 1563 tiles: 4 instead of 38 us).
+template <int R>
 __global__ __launch_bounds__(256) void lse_kernel(const float2 *stats, long long stats_ld, int tiles, Rows o, int first, int most,
                                                   float *loss) {
+    constexpr int P = 256 / R;
     const int M = live(most, o.count, first);
-    const int m = blockIdx.x * 16 + (threadIdx.x & 15), part = threadIdx.x >> 4;
-    __shared__ float tops[16][17], sums[16][17];
+    const int row = threadIdx.x % R, part = threadIdx.x / R, m = blockIdx.x * R + row;
+    __shared__ float tops[P][R + 1], sums[P][R + 1];
     float top = -__builtin_inff(), sum = 0.f;
-    if (m < M) {
-        for (int t = part; t < tiles; t += 16) {
+    auto join = [&](float t, float s) {
+        if (t > top) {
+            sum = sum * expf(top - t) + s;
+            top = t;
+        } else if (t != -__builtin_inff()) {
+            sum += s * expf(t - top);
+        } else {
+            sum += s * 0.f;   // nothing, unless it is NaN
+        }
+    };
+    if (m < M)
+        for (int t = part; t < tiles; t += P) {
             const float2 s = stats[t * stats_ld + m];
-            if (s.x > top) {
-                sum = sum * expf(top - s.x) + s.y;
-                top = s.x;
-            } else if (s.x != -__builtin_inff()) {
-                sum += s.y * expf(s.x - top);
-            } else {
-                sum += s.y * 0.f;   // nothing, unless it is NaN
-            }
+            join(s.x, s.y);
+        }
+    tops[part][row] = top;
+    sums[part][row] = sum;
+    for (int w = P / 2; w; w >>= 1) {
+        __syncthreads();
+        if (part < w) {
+            join(tops[part + w][row], sums[part + w][row]);
+            tops[part][row] = top;
+            sums[part][row] = sum;
         }
     }
-    tops[part][threadIdx.x & 15] = top;
-    sums[part][threadIdx.x & 15] = sum;
-    __syncthreads();
     if (part == 0 && m < M) {
-        for (int p = 1; p < 16; ++p) top = fmaxf(top, tops[p][threadIdx.x]);
-        sum = 0.f;
-        for (int p = 0; p < 16; ++p) {
-            const float tp = tops[p][threadIdx.x];
-            sum += sums[p][threadIdx.x] * (tp == -__builtin_inff() ? 0.f : expf(tp - top));
-        }
         const float tl = o.tl[first + m];
         const float z = top == -__builtin_inff() && sum == 0.f ? top : top + logf(sum) - tl;
         const float e = expf(-fabsf(z));
@@ -203,7 +213,7 @@ struct XentGrad {
     const float2 *stats;
     long long stats_ld;
     Rows o;
-    int first, most, V;
+    int first, most, V, wave_cols;
     __device__ bool skip(int m) const { return m >= live(most, o.count, first); }
     __device__ void operator()(int m, int c, float (&v)[1][8]) const {
         const int r = first + m, t = o.target[r];
@@ -216,7 +226,7 @@ struct XentGrad {
         } else {
             typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
             const f16x8 k = *(const f16x8 *)(keep + m * ld + c);
-            const float f = __expf(stats[(c / kWaveCols) * stats_ld + m].x - lse) * 0x1p-15f;
+            const float f = __expf(stats[(c / wave_cols) * stats_ld + m].x - lse) * 0x1p-15f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[0][e] = s * ((float)k[e] * f);
         }
@@ -231,19 +241,21 @@ struct XentGrad {
 template <typename T>
 struct XentScratch {
     static constexpr int PL = Planes<T>::N;
-    int Dp, Vp, tiles, block, blocks;   // rows of a block, number of blocks
+    int Dp, Vp, block, blocks;   // rows of a block, number of blocks
+    int wave_cols, tiles;        // columns that share an entry of the statistics; entries of a row
     bool direct;                            // w is used where it is
     Rows rows;
     bf16_t *x, *w, *d;
     float2 *stats;
-    float *scores, *sum;
+    float *scores, *sum, *part;
     XentScratch(Scratch &sc, int N, int D, int V, bool grads) {
-        Dp = (int)round_up(D, 8), Vp = (int)round_up(V, kWaveCols);
+        Dp = (int)round_up(D, 8), Vp = (int)round_up(V, 64);
         direct = PL == 1 && D == Dp;
-        tiles = Vp / kWaveCols;
         block = (int)round_up(N, 8);
         if (grads) block = (int)std::min<long long>(block, std::max<long long>(kStep, kBlockBytes / ((long long)Vp * sizeof(T)) / 256 * 256));
         blocks = N ? (N + block - 1) / block : 0;
+        wave_cols = N <= kFewRows ? 64 : product_wave_cols(block, V, D, Planes<T>::PAIRS);
+        tiles = (V + wave_cols - 1) / wave_cols;
         rows.count = sc.take<int>(1);
         rows.unit = sc.take<float>(1);
         rows.index = sc.take<int>(N);
@@ -259,6 +271,7 @@ struct XentScratch {
         if (!grads) return;
         d = sc.take<bf16_t>((long long)PL * block * Vp);
         scores = PL == 3 ? sc.take<float>((long long)block * Vp) : nullptr;
+        part = sc.take<float>(std::max(part_floats(block, D, V, Planes<T>::PAIRS), part_floats(V, D, block, Planes<T>::PAIRS)));
         sum = blocks > 1 ? sc.take<float>((long long)V * D) : nullptr;
     }
 };
@@ -278,8 +291,10 @@ int xent(const T *x, const T *w, const int64_t *target, const float *scale, floa
     const LaunchPlan one = make_plan("xent_rows", {}, {N}, dim3(1), 1024, 0);
     LC_LAUNCH(one, "xent (rows)", rows_kernel, s, target, scale, loss, N, V, g.rows);
     const long long px = (long long)N * g.Dp, pw = (long long)V * g.Dp;
-    if (int rc = launch_planes<PL, 1>("xent (x)", Stored<T>{x, N, D, g.rows.index, g.rows.count}, g.x, g.Dp, px, N, g.Dp, 0, s)) return rc;
-    if (!g.direct)
+    const bool few = N <= kFewRows;   // the scores of few rows need neither x nor w laid out
+    if (!few || grads)
+        if (int rc = launch_planes<PL, 1>("xent (x)", Stored<T>{x, N, D, g.rows.index, g.rows.count}, g.x, g.Dp, px, N, g.Dp, 0, s)) return rc;
+    if (!g.direct && (!few || grads))
         if (int rc = launch_planes<PL, 1>("xent (w)", Stored<T>{w, V, D, nullptr, nullptr}, g.w, g.Dp, pw, V, g.Dp, 0, s)) return rc;
     const Operand W = g.direct ? Operand{(const bf16_t *)w, (const bf16_t *)w, D, 0, V, 0, 0} : Operand{g.w, g.w, g.Dp, pw, V, 0, 0};
     if (grads && dx) {
@@ -292,32 +307,43 @@ int xent(const T *x, const T *w, const int64_t *target, const float *scale, floa
         const Shape sh = {most, V, D, g.rows.count, first, nullptr, 0};
         typename Kept<T>::V *keep = (typename Kept<T>::V *)(PL == 3 ? (void *)g.scores : (void *)g.d);
         int rc;
+        auto scores = [&](auto epi) {
+            if (few)
+                return launch_few<T, ROW>("xent (few rows)", FewOperand<T>{x, x, D, N, g.rows.index}, FewOperand<T>{w, w, D, V, nullptr}, N,
+                                          g.rows.count, V, D, epi, s);
+            return launch_cut<PL, ROW, ROW>("xent", X, W, sh, choose_cut(g.block, V, D, Planes<T>::PAIRS, false), epi, s);
+        };
         if (!grads)
-            rc = launch_gemm<PL, ROW, ROW>("xent", X, W, sh, XentEpi<T, false>{g.stats, g.block, g.rows.target + first, g.rows.tl + first, nullptr, 0}, s);
+            rc = scores(XentEpi<T, false>{g.stats, g.block, g.rows.target + first, g.rows.tl + first, nullptr, 0});
         else
-            rc = launch_gemm<PL, ROW, ROW>("xent", X, W, sh, XentEpi<T, true>{g.stats, g.block, g.rows.target + first, g.rows.tl + first, keep, g.Vp}, s);
+            rc = scores(XentEpi<T, true>{g.stats, g.block, g.rows.target + first, g.rows.tl + first, keep, g.Vp});
         if (rc) return rc;
-        const LaunchPlan p = make_plan("xent_lse", {}, {most}, dim3((most + 15) / 16), 256, 0);
-        LC_LAUNCH(p, "xent (logsumexp)", lse_kernel, s, g.stats, (long long)g.block, g.tiles, g.rows, first, most, loss);
+        if (most >= 2048) {
+            const LaunchPlan p = make_plan("xent_lse", {16}, {most}, dim3((most + 15) / 16), 256, 0);
+            LC_LAUNCH(p, "xent (logsumexp)", lse_kernel<16>, s, g.stats, (long long)g.block, g.tiles, g.rows, first, most, loss);
+        } else {
+            const LaunchPlan p = make_plan("xent_lse", {1}, {most}, dim3(most), 256, 0);
+            LC_LAUNCH(p, "xent (logsumexp)", lse_kernel<1>, s, g.stats, (long long)g.block, g.tiles, g.rows, first, most, loss);
+        }
         if (!grads) continue;
         const long long pd = (long long)g.block * g.Vp;
-        if ((rc = launch_planes<PL, 1>("xent (d)", XentGrad<T>{keep, g.Vp, g.stats, g.block, g.rows, first, most, V}, g.d, g.Vp, pd, most, g.Vp, 0, s)))
+        if ((rc = launch_planes<PL, 1>("xent (d)", XentGrad<T>{keep, g.Vp, g.stats, g.block, g.rows, first, most, V, g.wave_cols}, g.d, g.Vp, pd, most, g.Vp, 0, s)))
             return rc;
         Operand d = {g.d, g.d, g.Vp, pd, most, 0, 0};
         Wc.rows = X.rows = g.Dp;
         if (dx) {
             const Shape shx = {most, D, V, g.rows.count, first, nullptr, 0};
-            if ((rc = launch_gemm<PL, ROW, COL>("xent (dx)", d, Wc, shx,
-                                                StoreEpi<T>{dx, nullptr, 0x7fffffff, most, 0, D, g.rows.index + first, nullptr, g.rows.unit}, s)))
+            if ((rc = launch_product<PL, ROW, COL>("xent (dx)", d, Wc, shx,
+                                                StoreEpi<T>{dx, nullptr, 0x7fffffff, most, 0, D, g.rows.index + first, nullptr, g.rows.unit}, g.part, s)))
                 return rc;
         }
         const Shape shw = {V, D, most, nullptr, 0, g.rows.count, first};
         d.rows = g.Vp;
         const float *add = b ? g.sum : nullptr;
         if (b + 1 < g.blocks)
-            rc = launch_gemm<PL, COL, COL>("xent (dw)", d, X, shw, StoreEpi<float>{g.sum, nullptr, 0x7fffffff, V, 0, D, nullptr, add, nullptr}, s);
+            rc = launch_product<PL, COL, COL>("xent (dw)", d, X, shw, StoreEpi<float>{g.sum, nullptr, 0x7fffffff, V, 0, D, nullptr, add, nullptr}, g.part, s);
         else
-            rc = launch_gemm<PL, COL, COL>("xent (dw)", d, X, shw, StoreEpi<T>{dw, nullptr, 0x7fffffff, V, 0, D, nullptr, add, g.rows.unit}, s);
+            rc = launch_product<PL, COL, COL>("xent (dw)", d, X, shw, StoreEpi<T>{dw, nullptr, 0x7fffffff, V, 0, D, nullptr, add, g.rows.unit}, g.part, s);
         if (rc) return rc;
     }
     const LaunchPlan p = make_plan("xent_cost", {}, {N}, dim3(1), 1024, 0);
