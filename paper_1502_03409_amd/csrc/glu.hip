@@ -10,21 +10,27 @@ namespace lc {
 namespace head {
 namespace {
 
-template <int ACT>
+// 1 / (1 + e^-g).  bf16 results: by the hardware's exponential and reciprocal, whose errors of 2^-22 vanish in the rounding.
+template <typename T>
+__device__ __forceinline__ float sigmoid(float g) {
+    if constexpr (sizeof(T) == 4) return 1.f / (1.f + expf(-g));
+    else return __builtin_amdgcn_rcpf(1.f + __expf(-g));
+}
+template <typename T, int ACT>
 __device__ __forceinline__ float act_value(float g) {
     if constexpr (ACT == LC_ACT_GELU) return 0.5f * g * erfcf(-0.70710678118654752f * g);
-    const float sg = 1.f / (1.f + expf(-g));
+    const float sg = sigmoid<T>(g);
     return ACT == LC_ACT_SIGMOID ? sg : g * sg;
 }
 // act(g) and act'(g)
-template <int ACT>
+template <typename T, int ACT>
 __device__ __forceinline__ void act_both(float g, float &a, float &da) {
     if constexpr (ACT == LC_ACT_GELU) {
         const float phi = 0.5f * erfcf(-0.70710678118654752f * g);
         a = g * phi;
         da = phi + g * (0.39894228040143268f * expf(-0.5f * g * g));
     } else {
-        const float sg = 1.f / (1.f + expf(-g));
+        const float sg = sigmoid<T>(g);
         a = ACT == LC_ACT_SIGMOID ? sg : g * sg;
         da = ACT == LC_ACT_SIGMOID ? sg * (1.f - sg) : sg * (1.f + g * (1.f - sg));
     }
@@ -72,7 +78,7 @@ struct GluEpi {
                     for (int r = 0; r < 4; ++r) {
                         const float g = acc[i][j][4 * q + r];
                         const float u = EACH == 16 ? acc[i][j][(8 + 4 * q + r) & 15] : acc[i][j + EACH / 32][4 * q + r];
-                        v[r] = W == 0 ? narrow<T>(act_value<ACT>(g) * u) : save_value<T>(W == 1 ? g : u);
+                        v[r] = W == 0 ? narrow<T>(act_value<T, ACT>(g) * u) : save_value<T>(W == 1 ? g : u);
                     }
                     stage.put(16 * j + 8 * q + 4 * (lane >> 5), v);
                 }
@@ -119,7 +125,7 @@ struct GluGrad {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             float a, da;
-            act_both<ACT>(g[e], a, da);
+            act_both<T, ACT>(g[e], a, da);
             v[0][e] = d[e] * u[e] * da;
             v[1][e] = d[e] * a;
         }

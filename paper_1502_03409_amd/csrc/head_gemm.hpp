@@ -112,8 +112,8 @@ __device__ __forceinline__ bool tile_of(int wg, int mt, int nt, int splits, int 
 
 // ---------------------------------------------------------------------------------------------------------------------------
 // The tiled product.  BM x BN of the result per workgroup of 2 x 2 waves, steps of 64 along the contraction, through LDS buffers that
-// are filled by loads which go straight there: three for A, two for B (all 160 KB for 256 x 256).  A long contraction over few tiles is
-// cut into `splits` parts, whose sums are added up by a kernel of their own.
+// are filled by loads which go straight there: NA for A, NB for B (three and two are all 160 KB for 256 x 256).  A long contraction over
+// few tiles is cut into `splits` parts, whose sums are added up by a kernel of their own.
 //
 // An operand's tile is kept as it lies in memory.  By rows (ROW, PAIR): 128 bytes a row (whole lines: half lines at a time come at half the
 // rate, 15 against 25 TB/s from the L2 caches), whose eight 16-byte pieces are exchanged by bits of the row so that 16 rows read at
@@ -124,8 +124,8 @@ __device__ __forceinline__ bool tile_of(int wg, int mt, int nt, int splits, int 
 // instructions.  In the last quarter, after the first few products have been issued, comes the step's one barrier: behind it the next
 // step is there for everybody (each wave has waited for its own loads) and this step's buffers are free (each wave has read them).
 // Loads go out evenly: the address unit takes one every 18 clocks, and a wave that waits for it cannot issue matrix instructions.  Between
-// two barriers the B of the step after next comes first, half of it still in the last quarter, then the A of the step behind that, which
-// may stay in flight across the next barrier.
+// two barriers the B comes first whose buffer the barrier has freed, half of it still in the last quarter, then such an A; with three and
+// two buffers that A may stay in flight across the next barrier, with five of each all of three steps.
 template <int N>
 __device__ __forceinline__ int col_swizzle(int k) {   // N columns: N / 32 pieces of 64 bytes
     return ((k & 3) | ((k >> 3) & 1) << 2) & (N / 32 - 1);
@@ -230,39 +230,38 @@ struct Stager {
 template <int FORM, int N, int T>
 struct Reader {
     static constexpr bool COLS = FORM == COL || FORM == COLPAIR;
-    unsigned at[COLS ? T : 4], high[COLS ? T : 4];   // high: 64 KB further, an instruction's offset has 16 bits
+    unsigned first[COLS ? T : 4], at[COLS ? T : 4];   // in the first buffer, in the current one
     __device__ __forceinline__ void init(unsigned lds, int r0, int lane) {
         if constexpr (COLS) {
             const int s = lane % 16, g = lane / 16;
             const int k = 8 * (g >> 1) + s / 4;
 #pragma unroll
             for (int i = 0; i < T; ++i)
-                at[i] = lds + k * (2 * N) + (((r0 / 32 + i) ^ col_swizzle<N>(k)) * 64) + (g & 1) * 32 + (s % 4) * 8;
+                first[i] = lds + k * (2 * N) + (((r0 / 32 + i) ^ col_swizzle<N>(k)) * 64) + (g & 1) * 32 + (s % 4) * 8;
         } else {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) at[c] = lds + (r0 + (lane & 31)) * 128 + (((2 * c + (lane >> 5)) ^ ((lane >> 1) & 7)) * 16);
-        }
-#pragma unroll
-        for (int i = 0; i < (COLS ? T : 4); ++i) {
-            high[i] = at[i] + 65536;
-            asm volatile("" : "+v"(at[i]), "+v"(high[i]));   // held, not formed anew for every read
+            for (int c = 0; c < 4; ++c) first[c] = lds + (r0 + (lane & 31)) * 128 + (((2 * c + (lane >> 5)) ^ ((lane >> 1) & 7)) * 16);
         }
     }
-    template <int AT>   // offset of the buffer
+    __device__ __forceinline__ void turn(unsigned buffer) {
+#pragma unroll
+        for (int i = 0; i < (COLS ? T : 4); ++i) {
+            at[i] = first[i] + buffer;
+            asm volatile("" : "+v"(at[i]));   // held, not formed anew for every read
+        }
+    }
     __device__ __forceinline__ u32x4 read(int c, int i) const {
         typedef const __attribute__((address_space(3))) char *p1;
         typedef __attribute__((address_space(3))) u32x4 *p4;
-        constexpr int REST = AT & 0xffff;
-        const int k = COLS ? i : c;
-        const p1 p = (p1)(size_t)(AT >= 65536 ? high[k] : at[k]);
+        const p1 p = (p1)(size_t)at[COLS ? i : c];
         if constexpr (COLS) {
             typedef short s16x4 __attribute__((ext_vector_type(4)));
             typedef __attribute__((address_space(3))) s16x4 *p2;
-            const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((p2)(p + REST + c * (16 * 2 * N))));
-            const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((p2)(p + REST + c * (16 * 2 * N) + 4 * 2 * N)));
+            const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((p2)(p + c * (16 * 2 * N))));
+            const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((p2)(p + c * (16 * 2 * N) + 4 * 2 * N)));
             return (u32x4){lo[0], lo[1], hi[0], hi[1]};
         } else {
-            return *(p4)(p + REST + i * (32 * 128));
+            return *(p4)(p + i * (32 * 128));
         }
     }
 };
@@ -270,8 +269,8 @@ struct Reader {
 // LDS of a wave's epilogue: one block of 32 rows on its way to whole 16-byte pieces.
 template <int NT> constexpr int kEpiBytes = 32 * (NT * 32 * 4 + 16);
 
-template <int PL, int FA, int FB, int BM, int BN, typename Epi>
-__global__ __launch_bounds__(64 * kWaves, BM == 256 ? 1 : 2) void gemm_kernel(Operand A, Operand B, Shape sh, int nt, int splits, Epi epi) {
+template <int PL, int FA, int FB, int BM, int BN, int NA, int NB, typename Epi>
+__global__ __launch_bounds__(64 * kWaves, (NA * BM + NB * BN) * 128 > 81920 ? 1 : 2) void gemm_kernel(Operand A, Operand B, Shape sh, int nt, int splits, Epi epi) {
     constexpr int MT = BM / 64, NT = BN / 64, PAIRS = PL == 3 ? 6 : 1;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -280,7 +279,7 @@ __global__ __launch_bounds__(64 * kWaves, BM == 256 ? 1 : 2) void gemm_kernel(Op
     int tm, tn, split;
     if (!tile_of(blockIdx.x, (M + BM - 1) / BM, nt, splits, &tm, &tn, &split)) return;
     const int wm = wave / 2, wn = wave % 2;
-    constexpr unsigned ABYTES = BM * 128, BBYTES = BN * 128, B0 = 3 * ABYTES;   // A's buffers, then B's
+    constexpr unsigned ABYTES = BM * 128, BBYTES = BN * 128, B0 = NA * ABYTES;   // A's buffers, then B's
     const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) char *)smem;
     Reader<FA, BM, MT> ra;
     Reader<FB, BN, NT> rb;
@@ -297,110 +296,109 @@ __global__ __launch_bounds__(64 * kWaves, BM == 256 ? 1 : 2) void gemm_kernel(Op
     sb.init(B, tn * BN, kt0, K, 0x021100, wave, lane);
     constexpr int QA = Stager<FA, BM, PL>::Q, QB = Stager<FB, BN, PL>::Q;
     const unsigned lds_wave = lds0 + wave * 1024;
-    auto load_a = [&](auto buf, auto number) __attribute__((always_inline)) {
-        sa.template load<decltype(number)::value>(lds_wave + decltype(buf)::value % 3 * ABYTES);
-    };
-    auto load_b = [&](auto buf, auto number) __attribute__((always_inline)) {
-        sb.template load<decltype(number)::value>(lds_wave + B0 + decltype(buf)::value % 2 * BBYTES);
-    };
+    auto load_a = [&](unsigned buffer, auto number) __attribute__((always_inline)) { sa.template load<decltype(number)::value>(lds_wave + buffer); };
+    auto load_b = [&](unsigned buffer, auto number) __attribute__((always_inline)) { sb.template load<decltype(number)::value>(lds_wave + B0 + buffer); };
+    // buffers of this step, of the one before (which is free) and of the next
+    unsigned ao = 0, aprev = (NA - 1) * ABYTES, anext = ABYTES, bo = 0, bprev = (NB - 1) * BBYTES, bnext = BBYTES;
     int akt = kt0, as = 0;   // the step that arrives next
-    // The next step is there and everybody may read it: its loads have landed (`ahead` that were issued later stay in flight), all waves
-    // have read what they need of the step before, and what lies beyond the contraction is zero.
-    auto arrive = [&](auto buf, auto ahead) __attribute__((always_inline)) {
-        constexpr int U = decltype(buf)::value;
+    // The step in these buffers is there and everybody may read it: its loads have landed (`ahead` that were issued later stay in flight),
+    // all waves have read what they need of the step before, and what lies beyond the contraction is zero.
+    auto arrive = [&](unsigned a_at, unsigned b_at, auto ahead) __attribute__((always_inline)) {
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(decltype(ahead)::value) : "memory");
         const int la = sa.left(akt), lb = sb.left(akt);
         if (__builtin_expect(min(la, lb) < kStep, 0)) {
-            sa.clear(smem + U % 3 * ABYTES, la);
-            sb.clear(smem + B0 + U % 2 * BBYTES, lb);
+            sa.clear(smem + a_at, la);
+            sb.clear(smem + B0 + b_at, lb);
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         }
         if (PAIRS == 1 || ++as == PAIRS) as = 0, ++akt;
     };
     u32x4 a[2][MT], b[2][NT];
-    auto fetch = [&](auto buf, int c, int r) __attribute__((always_inline)) {   // read r of the MT + NT of quarter c, in the order the products need them
-        constexpr int U = decltype(buf)::value;
-        if (r == 0) a[c & 1][0] = ra.template read<U % 3 * ABYTES>(c, 0);
-        else if (r <= NT) b[c & 1][r - 1] = rb.template read<U % 2 * BBYTES>(c, r - 1);
-        else a[c & 1][r - NT] = ra.template read<U % 3 * ABYTES>(c, r - NT);
+    auto fetch = [&](int c, int r) __attribute__((always_inline)) {   // read r of the MT + NT of quarter c, as the products need them
+        if (r == 0) a[c & 1][0] = ra.read(c, 0);
+        else if (r <= NT) b[c & 1][r - 1] = rb.read(c, r - 1);
+        else a[c & 1][r - NT] = ra.read(c, r - NT);
     };
     constexpr int P = MT * NT, R = MT + NT;
     constexpr int BAR = P / 4;   // products of the last quarter in front of the barrier
-    // Step U of six (after which all buffers have had their turn).  left: steps from this one on, which FULL says are more than two.
-    auto step = [&](auto number, auto full, int left) __attribute__((always_inline)) {
-        constexpr int U = decltype(number)::value;
+    constexpr int FAR = NA - 1 > NB ? NA - 1 : NB, BEHIND = (NA - 2) * QA + (NB - 2) * QB;
+    // One step.  left: steps from this one on; FULL: more than FAR.
+    auto step = [&](auto full, int left) __attribute__((always_inline)) {
         constexpr bool FULL = decltype(full)::value;
-        const std::integral_constant<int, U> now;
-        const std::integral_constant<int, U + 1> next;
-        const std::integral_constant<int, U + 2> second;
-        const bool has_next = FULL || left > 1, has_second = FULL || left > 2;
+        const bool has_next = FULL || left > 1;
         for_blocks<4>([&](auto quarter) __attribute__((always_inline)) {
             constexpr int c = decltype(quarter)::value;
             for_blocks<P>([&](auto product) __attribute__((always_inline)) {
                 constexpr int p = decltype(product)::value;
                 if constexpr (c == 3 && p == BAR) {
                     if (has_next) {
-                        if (has_second) arrive(next, std::integral_constant<int, QA>());
-                        else arrive(next, std::integral_constant<int, 0>());
+                        if (FULL || left > FAR) arrive(anext, bnext, std::integral_constant<int, BEHIND>());
+                        else arrive(anext, bnext, std::integral_constant<int, 0>());
+                        ra.turn(anext);
+                        rb.turn(bnext);
                     }
                 }
                 acc[p / NT][p % NT] = mfma32(b[c & 1][p % NT], a[c & 1][p / NT], acc[p / NT][p % NT]);
                 if constexpr (c < 3) {
 #pragma unroll
-                    for (int r = p * R / P; r < (p + 1) * R / P; ++r) fetch(now, c + 1, r);
+                    for (int r = p * R / P; r < (p + 1) * R / P; ++r) fetch(c + 1, r);
                 } else if constexpr (p >= BAR) {
                     constexpr int S = P - BAR;
                     if (has_next) {
 #pragma unroll
-                        for (int r = (p - BAR) * R / S; r < (p - BAR + 1) * R / S; ++r) fetch(next, 0, r);
+                        for (int r = (p - BAR) * R / S; r < (p - BAR + 1) * R / S; ++r) fetch(0, r);
                     }
-                    // the first half of B's step after next, into this step's buffer
-                    if (has_second)
+                    if (FULL || left > NB)   // the first half of a B, into this step's buffer
                         for_blocks<(p - BAR + 1) * (QB / 2) / S - (p - BAR) * (QB / 2) / S>([&](auto k) __attribute__((always_inline)) {
-                            load_b(second, std::integral_constant<int, (p - BAR) * (QB / 2) / S + decltype(k)::value>());
+                            load_b(bo, std::integral_constant<int, (p - BAR) * (QB / 2) / S + decltype(k)::value>());
                         });
                 }
-                // the other half of B's next step, then A's step after next
-                if constexpr (c == 0) {
-                    if (has_next)
+                if constexpr (c == 0) {          // the second half of the one before
+                    if (FULL || left > NB - 1)
                         for_blocks<(p + 1) * (QB / 2) / P - p * (QB / 2) / P>([&](auto k) __attribute__((always_inline)) {
-                            load_b(next, std::integral_constant<int, QB / 2 + p * (QB / 2) / P + decltype(k)::value>());
+                            load_b(bprev, std::integral_constant<int, QB / 2 + p * (QB / 2) / P + decltype(k)::value>());
                         });
-                    if (p == P - 1 && has_next) sb.next();
-                } else if constexpr (c < 3) {
-                    if (has_second)
+                    if (p == P - 1 && (FULL || left > NB - 1)) sb.next();
+                } else if constexpr (c < 3) {    // an A, into the buffer of the step before
+                    if (FULL || left > NA - 1)
                         for_blocks<(p + 1) * (QA / 2) / P - p * (QA / 2) / P>([&](auto k) __attribute__((always_inline)) {
-                            load_a(second, std::integral_constant<int, (c - 1) * (QA / 2) + p * (QA / 2) / P + decltype(k)::value>());
+                            load_a(aprev, std::integral_constant<int, (c - 1) * (QA / 2) + p * (QA / 2) / P + decltype(k)::value>());
                         });
-                    if (c == 2 && p == P - 1 && has_second) sa.next();
+                    if (c == 2 && p == P - 1 && (FULL || left > NA - 1)) sa.next();
                 }
                 __builtin_amdgcn_sched_barrier(0);
             });
         });
+        aprev = ao, ao = anext, anext = anext == (NA - 1) * ABYTES ? 0 : anext + ABYTES;
+        bprev = bo, bo = bnext, bnext = bnext == (NB - 1) * BBYTES ? 0 : bnext + BBYTES;
     };
-    if (steps) {
-        const std::integral_constant<int, 0> zero;
-        const std::integral_constant<int, 1> one;
-        for_blocks<QA>([&](auto q) __attribute__((always_inline)) { load_a(zero, q); });
-        sa.next();
-        for_blocks<QB>([&](auto q) __attribute__((always_inline)) { load_b(zero, q); });
-        sb.next();
-        if (steps > 1) {
-            for_blocks<QA>([&](auto q) __attribute__((always_inline)) { load_a(one, q); });
-            sa.next();
-            for_blocks<QB / 2>([&](auto q) __attribute__((always_inline)) { load_b(one, q); });
-            arrive(zero, std::integral_constant<int, QA + QB / 2>());
-        } else {
-            arrive(zero, zero);
-        }
+    if (steps) {   // what earlier steps would have sent for
+        for_blocks<(NA > NB ? NA : NB) - 1>([&](auto s) __attribute__((always_inline)) {
+            constexpr int at = decltype(s)::value;
+            if (at < steps) {
+                if constexpr (at < NA - 1) {
+                    for_blocks<QA>([&](auto q) __attribute__((always_inline)) { load_a(at * ABYTES, q); });
+                    sa.next();
+                }
+                if constexpr (at < NB - 1) {
+                    for_blocks<QB>([&](auto q) __attribute__((always_inline)) { load_b(at * BBYTES, q); });
+                    sb.next();
+                }
+            }
+        });
+        if (steps > NB - 1) for_blocks<QB / 2>([&](auto q) __attribute__((always_inline)) { load_b((NB - 1) * BBYTES, q); });
+        if (steps > FAR) arrive(0, 0, std::integral_constant<int, BEHIND + QB / 2>());
+        else arrive(0, 0, std::integral_constant<int, 0>());
+        ra.turn(0);
+        rb.turn(0);
 #pragma unroll
-        for (int r = 0; r < R; ++r) fetch(zero, 0, r);
+        for (int r = 0; r < R; ++r) fetch(0, r);
     }
     int left = steps;
-    for (; left > 7; left -= 6) for_blocks<6>([&](auto u) __attribute__((always_inline)) { step(u, std::true_type(), 3); });
-    for_blocks<7>([&](auto u) __attribute__((always_inline)) {
-        if (left > decltype(u)::value) step(u, std::false_type(), left - decltype(u)::value);
-    });
+#pragma unroll 1
+    for (; left > FAR; --left) step(std::true_type(), 0);
+#pragma unroll 1
+    for (; left > 0; --left) step(std::false_type(), left);
     const int m0 = tm * BM + wm * MT * 32, n0 = tn * BN + wn * NT * 32;
     if constexpr (PL == 3) {
         if (m0 < M && n0 < sh.Nn && !all_finite(acc, M - m0, lane))
@@ -411,12 +409,12 @@ __global__ __launch_bounds__(64 * kWaves, BM == 256 ? 1 : 2) void gemm_kernel(Op
     epi.run(acc, m0, n0, lane, M, sh.Nn, split, smem + wave * kEpiBytes<NT>);
 }
 
-template <int PL, int FA, int FB, int BM, int BN, typename Epi>
+template <int PL, int FA, int FB, int BM, int BN, int NA, int NB, typename Epi>
 int launch_tiles(const char *name, const Operand &A, const Operand &B, const Shape &sh, int splits, const Epi &epi, hipStream_t s) {
     const int mt = ceil_div(sh.M, BM), nt = ceil_div(sh.Nn, BN);
-    constexpr int LDS = (3 * BM + 2 * BN) * 128;
+    constexpr int LDS = (NA * BM + NB * BN) * 128;
     static_assert(kWaves * kEpiBytes<BN / 64> <= LDS, "the epilogue's LDS is that of the buffers");
-    const LaunchPlan p = make_plan(name, {PL, FA, FB, BM, BN}, {sh.M, sh.Nn, sh.K, splits}, dim3((unsigned)((long long)mt * nt * splits)),
+    const LaunchPlan p = make_plan(name, {PL, FA, FB, BM, BN, NA, NB}, {sh.M, sh.Nn, sh.K, splits}, dim3((unsigned)((long long)mt * nt * splits)),
                                    64 * kWaves, LDS);
     LC_PLAN_REQUIRE(p, (long long)mt * nt * splits <= 0x7fffffffLL && splits >= 1);
     LC_PLAN_REQUIRE(p, A.ld % 8 == 0 && B.ld % 8 == 0 && A.plane % 8 == 0 && B.plane % 8 == 0);
@@ -428,7 +426,7 @@ int launch_tiles(const char *name, const Operand &A, const Operand &B, const Sha
                                          sh.K == B.half + B.depth));
     LC_PLAN_REQUIRE(p, A.ld <= (1 << 22) && B.ld <= (1 << 22));   // 256 rows' offsets stay below 2^31 bytes
     LC_PLAN_REQUIRE(p, ptr_aligned16(A.p0) && ptr_aligned16(B.p0) && ptr_aligned16(B.p1));
-    LC_LAUNCH(p, name, (gemm_kernel<PL, FA, FB, BM, BN, Epi>), s, A, B, sh, nt, splits, epi);
+    LC_LAUNCH(p, name, (gemm_kernel<PL, FA, FB, BM, BN, NA, NB, Epi>), s, A, B, sh, nt, splits, epi);
     return LC_OK;
 }
 
@@ -573,42 +571,46 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const float *part, long
     }
 }
 
-// How a product is cut: into tiles of 256 x 256, one on a compute unit, or of 128 x 128, two on one; and its contraction into parts.
+// How a product is cut: into tiles of 256 x 256, one on a compute unit, or of 128 x 128, two on one or, with more buffers, one; and its
+// contraction into parts.
 struct Cut {
-    bool large;
+    enum Tile { LARGE, SMALL, DEEP } tile;
     int splits;
 };
 // The cut that takes least by an estimate in microseconds from measured times: a step of a large tile 1.7, of two small ones that share
-// a compute unit 0.82, of one that has it for itself 0.56, and what begins and ends a tile; joining parts moves 8 bytes a value at 4 TB/s.
+// a compute unit 0.82, of one that has it for itself and so five buffers 0.5 (192 rows of 4096 with weights from HBM: 44 us, 55 with the
+// usual buffers), and what begins and ends a tile; joining parts moves 8 bytes a value at 4 TB/s.
 // From four rounds of large tiles on these are taken in any case: they bring half the bytes into LDS per product, and the chip runs
 // at the clock its power allows (8192 x 128000 x 4096 6.8 against 8.0 ms).  Both cuts at other sizes: 192 x 16384 x 4096 85 us large
 // and 40 small; 1000 x 768 x 30011 in fp32 3330 and 1572, in 16 parts 256 and 265.
 inline Cut choose_cut(int M, int Nn, int K, int pairs, bool may_split) {
     const double large = (double)ceil_div(M, 256) * ceil_div(Nn, 256), small = (double)ceil_div(M, 128) * ceil_div(Nn, 128);
-    if (large >= 4 * kComputeUnits) return Cut{true, 1};
+    if (large >= 4 * kComputeUnits) return Cut{Cut::LARGE, 1};
     const int steps = ceil_div(K, kStep);
-    Cut best = {false, 1};
+    Cut best = {Cut::SMALL, 1};
     double least = 1e30;
     for (int s = 1; s <= 32 && s <= std::max(1, steps / 2) && (s == 1 || may_split); ++s) {
         const double part = (double)ceil_div(steps, s) * pairs;
         const double join = s > 1 ? 4 + 8e-6 * s * (double)M * Nn / 4 : 0;
         const double rounds = std::ceil(large * s / kComputeUnits), wgs = small * s;
         const double tl = rounds * (part * 1.7 + 15) + join;
-        const double ts = (wgs <= kComputeUnits ? part * 0.56 + 4 : std::max(1.0, wgs / (2 * kComputeUnits) + 0.25) * (part * 0.82 + 6)) + join;
-        if (tl < least) best = {true, s}, least = tl;
-        if (ts < least) best = {false, s}, least = ts;
+        const bool deep = wgs <= kComputeUnits;
+        const double ts = (deep ? part * 0.5 + 4 : std::max(1.0, wgs / (2 * kComputeUnits) + 0.25) * (part * 0.82 + 6)) + join;
+        if (tl < least) best = {Cut::LARGE, s}, least = tl;
+        if (ts < least) best = {deep ? Cut::DEEP : Cut::SMALL, s}, least = ts;
     }
     return best;
 }
 
 template <int PL, int FA, int FB, typename Epi>
 int launch_cut(const char *name, const Operand &A, const Operand &B, const Shape &sh, const Cut &c, const Epi &epi, hipStream_t s) {
-    if (c.large) return launch_tiles<PL, FA, FB, 256, 256>(name, A, B, sh, c.splits, epi, s);
-    return launch_tiles<PL, FA, FB, 128, 128>(name, A, B, sh, c.splits, epi, s);
+    if (c.tile == Cut::LARGE) return launch_tiles<PL, FA, FB, 256, 256, 3, 2>(name, A, B, sh, c.splits, epi, s);
+    if (c.tile == Cut::SMALL) return launch_tiles<PL, FA, FB, 128, 128, 3, 2>(name, A, B, sh, c.splits, epi, s);
+    return launch_tiles<PL, FA, FB, 128, 128, 5, 5>(name, A, B, sh, c.splits, epi, s);
 }
 
 // columns of a wave in such a product
-inline int product_wave_cols(int M, int Nn, int K, int pairs) { return choose_cut(M, Nn, K, pairs, false).large ? 128 : 64; }
+inline int product_wave_cols(int M, int Nn, int K, int pairs) { return choose_cut(M, Nn, K, pairs, false).tile == Cut::LARGE ? 128 : 64; }
 
 // A product whose epilogue needs whole sums.
 template <int PL, int FA, int FB, typename Epi>
