@@ -202,7 +202,8 @@ struct Stager {
     __device__ __forceinline__ void next() {   // on to the next step: the next pair of planes, or the next indices
         if constexpr (PL == 3) {
             if (++pair < PAIRS) {
-                at = (planes >> (4 * pair) & 0xf) * plane;
+                const unsigned q = planes >> (4 * pair);
+                at = q & 1 ? plane : q & 2 ? 2 * plane : 0;
                 return;
             }
             pair = 0, at = 0;

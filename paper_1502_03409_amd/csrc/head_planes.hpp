@@ -6,31 +6,36 @@
 namespace lc {
 namespace head {
 
+// eight values as planes at p: 16 bytes each
+template <int PL>
+__device__ __forceinline__ void put_planes(bf16_t *to, long long plane, const float (&v)[8]) {
+    bf16_t p[8][3];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if constexpr (PL == 3) split3(v[e], p[e]);
+        else p[e][0] = to_bf16(v[e]);
+    }
+#pragma unroll
+    for (int q = 0; q < PL; ++q) {
+        u32x4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = (unsigned)p[2 * e][q] | (unsigned)p[2 * e + 1][q] << 16;
+        *(u32x4 *)(to + q * plane) = w;
+    }
+}
+
 // get(r, c, v): v[o][0..7] are columns c .. c + 7 of row r of output o (0 outside the matrix); output o lies `apart` * o columns to
-// the right.  skip(r): rows that nobody reads.
+// the right.  skip(r): rows that nobody reads.  beside(): something small that the first workgroup does as well.
 template <int PL, int OUT, typename Get>
 __global__ __launch_bounds__(256) void planes_kernel(Get get, bf16_t *dst, long long ld, long long plane, int rows, int pieces, int apart) {
+    if (blockIdx.x == 0) get.beside();
     const long long at = blockIdx.x * 256LL + threadIdx.x;
     const int r = (int)(at / pieces), c = (int)(at - (long long)r * pieces) * 8;
     if (r >= rows || get.skip(r)) return;
     float v[OUT][8];
     get(r, c, v);
 #pragma unroll
-    for (int o = 0; o < OUT; ++o) {
-        bf16_t p[8][3];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if constexpr (PL == 3) split3(v[o][e], p[e]);
-            else p[e][0] = to_bf16(v[o][e]);
-        }
-#pragma unroll
-        for (int q = 0; q < PL; ++q) {
-            u32x4 w;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = (unsigned)p[2 * e][q] | (unsigned)p[2 * e + 1][q] << 16;
-            *(u32x4 *)(dst + q * plane + (long long)r * ld + c + (long long)o * apart) = w;
-        }
-    }
+    for (int o = 0; o < OUT; ++o) put_planes<PL>(dst + (long long)r * ld + c + (long long)o * apart, plane, v[o]);
 }
 
 // eight consecutive values of a row from column c on (any alignment), zeros from column C on
@@ -54,21 +59,14 @@ __device__ __forceinline__ void load8(const T *row, int c, int C, float (&v)[8])
     }
 }
 
-// A stored matrix of R rows; `index` (nullable): row r is row index[r] of it, for r < *count, and zeros behind
+// A stored matrix of R rows
 template <typename T>
 struct Stored {
     const T *p;
     int R, C;
-    const int *index, *count;
+    __device__ void beside() const {}
     __device__ bool skip(int) const { return false; }
-    __device__ void operator()(int r, int c, float (&v)[1][8]) const {
-        if (r >= (index ? *count : R)) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[0][e] = 0.f;
-            return;
-        }
-        load8(p + (long long)(index ? index[r] : r) * C, c, C, v[0]);
-    }
+    __device__ void operator()(int r, int c, float (&v)[1][8]) const { load8(p + (long long)r * C, c, C, v[0]); }
 };
 
 // rows x cols (cols: of one output, padded to whole pieces) at dst
