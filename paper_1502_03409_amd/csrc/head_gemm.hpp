@@ -123,9 +123,9 @@ __device__ __forceinline__ bool tile_of(int wg, int mt, int nt, int splits, int 
 // Order of a step: its quarters of 16 indices; while one is multiplied, the fragments of the next are read, between the matrix
 // instructions.  In the last quarter, after the first few products have been issued, comes the step's one barrier: behind it the next
 // step is there for everybody (each wave has waited for its own loads) and this step's buffers are free (each wave has read them).
-// Loads go out evenly: the address unit takes one every 18 clocks, and a wave that waits for it cannot issue matrix instructions.  Between
-// two barriers the B comes first whose buffer the barrier has freed, half of it still in the last quarter, then such an A; with three and
-// two buffers that A may stay in flight across the next barrier, with five of each all of three steps.
+// Loads go out evenly: the address unit takes one every 18 clocks, and a wave that waits for it cannot issue matrix instructions.  Behind
+// a barrier comes first the B whose buffer it has freed, still in the last quarter, then, over the second and third quarter that follow,
+// such an A; with three and two buffers that A may stay in flight across the next barrier, with five of each all of three steps.
 template <int N>
 __device__ __forceinline__ int col_swizzle(int k) {   // N columns: N / 32 pieces of 64 bytes
     return ((k & 3) | ((k >> 3) & 1) << 2) & (N / 32 - 1);
@@ -299,8 +299,8 @@ __global__ __launch_bounds__(64 * kWaves, (NA * BM + NB * BN) * 128 > 81920 ? 1 
     const unsigned lds_wave = lds0 + wave * 1024;
     auto load_a = [&](unsigned buffer, auto number) __attribute__((always_inline)) { sa.template load<decltype(number)::value>(lds_wave + buffer); };
     auto load_b = [&](unsigned buffer, auto number) __attribute__((always_inline)) { sb.template load<decltype(number)::value>(lds_wave + B0 + buffer); };
-    // buffers of this step, of the one before (which is free) and of the next
-    unsigned ao = 0, aprev = (NA - 1) * ABYTES, anext = ABYTES, bo = 0, bprev = (NB - 1) * BBYTES, bnext = BBYTES;
+    // buffers of this step, of the next, and A's of the one before, which is free
+    unsigned ao = 0, aprev = (NA - 1) * ABYTES, anext = ABYTES, bo = 0, bnext = BBYTES;
     int akt = kt0, as = 0;   // the step that arrives next
     // The step in these buffers is there and everybody may read it: its loads have landed (`ahead` that were issued later stay in flight),
     // all waves have read what they need of the step before, and what lies beyond the contraction is zero.
@@ -349,18 +349,13 @@ __global__ __launch_bounds__(64 * kWaves, (NA * BM + NB * BN) * 128 > 81920 ? 1 
 #pragma unroll
                         for (int r = (p - BAR) * R / S; r < (p - BAR + 1) * R / S; ++r) fetch(0, r);
                     }
-                    if (FULL || left > NB)   // the first half of a B, into this step's buffer
-                        for_blocks<(p - BAR + 1) * (QB / 2) / S - (p - BAR) * (QB / 2) / S>([&](auto k) __attribute__((always_inline)) {
-                            load_b(bo, std::integral_constant<int, (p - BAR) * (QB / 2) / S + decltype(k)::value>());
+                    if (FULL || left > NB)   // a B, into this step's buffer
+                        for_blocks<(p - BAR + 1) * QB / S - (p - BAR) * QB / S>([&](auto k) __attribute__((always_inline)) {
+                            load_b(bo, std::integral_constant<int, (p - BAR) * QB / S + decltype(k)::value>());
                         });
+                    if (p == P - 1 && (FULL || left > NB)) sb.next();
                 }
-                if constexpr (c == 0) {          // the second half of the one before
-                    if (FULL || left > NB - 1)
-                        for_blocks<(p + 1) * (QB / 2) / P - p * (QB / 2) / P>([&](auto k) __attribute__((always_inline)) {
-                            load_b(bprev, std::integral_constant<int, QB / 2 + p * (QB / 2) / P + decltype(k)::value>());
-                        });
-                    if (p == P - 1 && (FULL || left > NB - 1)) sb.next();
-                } else if constexpr (c < 3) {    // an A, into the buffer of the step before
+                if constexpr (c == 1 || c == 2) {   // an A, into the buffer of the step before
                     if (FULL || left > NA - 1)
                         for_blocks<(p + 1) * (QA / 2) / P - p * (QA / 2) / P>([&](auto k) __attribute__((always_inline)) {
                             load_a(aprev, std::integral_constant<int, (c - 1) * (QA / 2) + p * (QA / 2) / P + decltype(k)::value>());
@@ -371,24 +366,23 @@ __global__ __launch_bounds__(64 * kWaves, (NA * BM + NB * BN) * 128 > 81920 ? 1 
             });
         });
         aprev = ao, ao = anext, anext = anext == (NA - 1) * ABYTES ? 0 : anext + ABYTES;
-        bprev = bo, bo = bnext, bnext = bnext == (NB - 1) * BBYTES ? 0 : bnext + BBYTES;
+        bo = bnext, bnext = bnext == (NB - 1) * BBYTES ? 0 : bnext + BBYTES;
     };
     if (steps) {   // what earlier steps would have sent for
-        for_blocks<(NA > NB ? NA : NB) - 1>([&](auto s) __attribute__((always_inline)) {
+        for_blocks<(NA - 1 > NB ? NA - 1 : NB)>([&](auto s) __attribute__((always_inline)) {
             constexpr int at = decltype(s)::value;
             if (at < steps) {
                 if constexpr (at < NA - 1) {
                     for_blocks<QA>([&](auto q) __attribute__((always_inline)) { load_a(at * ABYTES, q); });
                     sa.next();
                 }
-                if constexpr (at < NB - 1) {
+                if constexpr (at < NB) {
                     for_blocks<QB>([&](auto q) __attribute__((always_inline)) { load_b(at * BBYTES, q); });
                     sb.next();
                 }
             }
         });
-        if (steps > NB - 1) for_blocks<QB / 2>([&](auto q) __attribute__((always_inline)) { load_b((NB - 1) * BBYTES, q); });
-        if (steps > FAR) arrive(0, 0, std::integral_constant<int, BEHIND + QB / 2>());
+        if (steps > FAR) arrive(0, 0, std::integral_constant<int, BEHIND + QB>());
         else arrive(0, 0, std::integral_constant<int, 0>());
         ra.turn(0);
         rb.turn(0);

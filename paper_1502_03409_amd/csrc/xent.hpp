@@ -91,21 +91,28 @@ struct XentEpi {
             // columns of this wave that exist, and the target's, as this lane counts: 0 .. 3, 8 .. 11, ..
             int end = V - n0 - 4 * h, at = (m < M ? target[m] : -1) - n0 - 4 * h;
             asm volatile("" : "+v"(end), "+v"(at));   // compared anew for every block of rows: the masks of all would not fit
-            float top = -__builtin_inff(), own = 0.f;
+            // the target and what lies beyond the vocabulary are taken out, where there is any of it
+            if (__any(end < NT * 32 || (at >= 0 && at < NT * 32))) {
+                float own = 0.f;
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int c = 32 * j + 8 * (e >> 2) + (e & 3);
+                        const float l = acc[i][j][e];
+                        own = c == at ? l : own;
+                        acc[i][j][e] = c == at || c >= end ? -__builtin_inff() : l;
+                    }
+                if (m < M && at >= 0 && at < NT * 32 && (at & 4) == 0) tl[m] = own;
+            }
+            float top = -__builtin_inff();
 #pragma unroll
             for (int j = 0; j < NT; ++j)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int c = 32 * j + 8 * (e >> 2) + (e & 3);
-                    const float l = acc[i][j][e];
-                    own = c == at ? l : own;
-                    const float rest = c == at || c >= end ? -__builtin_inff() : l;
-                    acc[i][j][e] = rest;
-                    top = fmaxf(top, rest);
-                }
-            if (m < M && at >= 0 && at < NT * 32 && (at & 4) == 0) tl[m] = own;
+                for (int e = 0; e < 16; ++e) top = fmaxf(top, acc[i][j][e]);
             top = fmaxf(top, __shfl_xor(top, 32));
             const float base = top == -__builtin_inff() ? 0.f : top;   // all scores -inf: exponentials of 0, not of NaN
+            const float base2 = base * 1.44269504f;   // bf16: e^(l - base) = 2^(l log2 e - base log2 e), good to 2^-24 |l|
             float sum = 0.f;
 #pragma unroll
             for (int j = 0; j < NT; ++j)
@@ -115,7 +122,7 @@ struct XentEpi {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const float l = acc[i][j][4 * q + r];
-                        const float e = sizeof(T) == 4 ? expf(l - base) : __expf(l - base);
+                        const float e = sizeof(T) == 4 ? expf(l - base) : __builtin_amdgcn_exp2f(__builtin_fmaf(l, 1.44269504f, -base2));
                         sum += e;
                         v[r] = kept(K(), l, e);
                     }
