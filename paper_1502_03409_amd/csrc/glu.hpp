@@ -2,7 +2,7 @@
 //
 // Forward: a tile of the product covers the same outputs of both weight matrices (blocks of 32 rows of wg and wu alternate), so
 // the activation and the product happen on the accumulators.  Backward: one pass over dh and the saved g, u leaves both
-// gradients side by side, [N][2F] and transposed, and two products finish: dx = [dg du] [wg; wu] and [dwg; dwu] = [dg du]^T x.
+// gradients side by side, [N][2F], and two products finish: dx = [dg du] [wg; wu] and [dwg; dwu] = [dg du]^T x.
 #pragma once
 #include "head_few.hpp"
 #include "head_planes.hpp"
@@ -144,6 +144,19 @@ int launch_fill_zero(T *p, long long n, hipStream_t s) {
     return LC_OK;
 }
 
+// the rows of x, wg and wu, one below the other
+template <typename T>
+struct Stacked {
+    const T *x, *wg, *wu;
+    int N, F, D;
+    __device__ void beside() const {}
+    __device__ bool skip(int) const { return false; }
+    __device__ void operator()(int r, int c, float (&v)[1][8]) const {
+        const T *p = r < N ? x + (long long)r * D : r - N < F ? wg + (long long)(r - N) * D : wu + (long long)(r - N - F) * D;
+        load8(p, c, D, v[0]);
+    }
+};
+
 template <typename T>
 struct GluScratch {
     static constexpr int PL = Planes<T>::N;
@@ -154,8 +167,8 @@ struct GluScratch {
     GluScratch(Scratch &sc, int N, int D, int F, bool backward) {
         Dp = (int)round_up(D, 8), Fp = (int)round_up(F, kStep);
         direct = PL == 1 && D == Dp;
-        x = sc.take<bf16_t>(direct ? 8 : (long long)PL * N * Dp);
-        w = direct ? nullptr : sc.take<bf16_t>((long long)PL * 2 * F * Dp);
+        x = sc.take<bf16_t>(direct ? 8 : PL * ((long long)N + 2LL * F) * Dp);
+        w = x ? x + (long long)N * Dp : nullptr;   // behind x in each plane, so that one launch lays all three out
         d = backward ? sc.take<bf16_t>((long long)PL * N * 2 * Fp) : nullptr;
         const int pairs = Planes<T>::PAIRS;
         part = backward ? sc.take<float>(std::max(part_floats(N, D, Fp + F, pairs), part_floats(2 * Fp, D, N, pairs))) : nullptr;
@@ -167,15 +180,10 @@ struct GluScratch {
             *W = {(const bf16_t *)wg, (const bf16_t *)wu, D, 0, F, 0, 0};
             return LC_OK;
         }
-        const long long px = (long long)N * Dp, pw = 2LL * F * Dp;
-        *X = {x, x, Dp, px, N, 0, 0};
-        *W = {w, w + (long long)F * Dp, Dp, pw, F, 0, 0};
-        if (int rc = launch_planes<PL, 1>("glu (x)", Stored<T>{xs, N, D}, x, Dp, px, N, Dp, 0, s)) return rc;
-        for (int k = 0; k < 2; ++k)
-            if (int rc = launch_planes<PL, 1>("glu (w)", Stored<T>{k ? wu : wg, F, D}, w + (long long)k * F * Dp, Dp, pw, F,
-                                              Dp, 0, s))
-                return rc;
-        return LC_OK;
+        const long long plane = ((long long)N + 2LL * F) * Dp;
+        *X = {x, x, Dp, plane, N, 0, 0};
+        *W = {w, w + (long long)F * Dp, Dp, plane, F, 0, 0};
+        return launch_planes<PL, 1>("glu (x, w)", Stacked<T>{xs, wg, wu, N, F, D}, x, Dp, plane, N + 2 * F, Dp, 0, s);
     }
 };
 

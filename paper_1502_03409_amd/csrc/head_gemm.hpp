@@ -544,16 +544,25 @@ struct PartEpi {
     }
 };
 
-// Adds the parts up in their order and stores the sums, four columns a thread.
+// Adds the parts up in their order and stores the sums, four columns a thread.  Bound by the latency of the loads where the result
+// is small, so kJoin parts are in flight at a time.
+constexpr int kJoin = 8;
 template <typename T>
 __global__ __launch_bounds__(256) void join_parts_kernel(const float *part, long long ld, int splits, Shape sh, StoreEpi<T> epi) {
     const long long at = blockIdx.x * 256LL + threadIdx.x, quads = ld / 4;
     const int m = (int)(at / quads), n = (int)(at - m * quads) * 4;
+    if (m >= sh.M) return;
+    f32x4 s = {0.f, 0.f, 0.f, 0.f}, p[kJoin];
+    for (int i = 0; i < splits; i += kJoin) {
+#pragma unroll
+        for (int k = 0; k < kJoin; ++k) p[k] = *(const f32x4 *)(part + ((long long)min(i + k, splits - 1) * sh.M + m) * ld + n);
+#pragma unroll
+        for (int k = 0; k < kJoin; ++k)
+            if (i + k < splits) s += p[k];
+    }
     if (m >= live(sh.M, sh.rows_dev, sh.rows_first)) return;
     T *row = epi.row(m);
     if (!row) return;
-    f32x4 s = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < splits; ++i) s += *(const f32x4 *)(part + ((long long)i * sh.M + m) * ld + n);
     float v[4] = {s[0], s[1], s[2], s[3]};
     T o[4];
     epi.finish(m, n, epi.factor ? *epi.factor : 1.f, v, o);
