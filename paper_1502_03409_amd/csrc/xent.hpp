@@ -8,6 +8,9 @@
 // all above 2^-29, so that the one rounding to bf16 that follows is the only one that shows; fp32: the scores), for a bounded number of rows at a time; one pass turns them into d[n][v] = s[n] (p[n][v] - [v = t]) in
 // place, and two products give dx = d w and dw = d^T x.
 //
+// 8192 rows of 4096 over 128000 words in bf16, a tenth masked: scores 6.4 ms, statistics 0.02, d 0.74, dx 6.3, dw 6.5; three products of 7.7
+// TFLOP each, bound as large products are.
+//
 // Masked rows take no part: the rows that count are gathered first, and every kernel runs over as many as there are.
 #pragma once
 #include "head_few.hpp"
@@ -27,7 +30,8 @@ struct Rows {
     float *lse, *dt, *loss;   // logsumexp; p(target) - 1; loss
 };
 
-// Positions of the rows that count, in order; loss 0 where masked.  One workgroup: a scan over 1024 rows at a time.
+// Positions of the rows that count, in order; loss 0 where masked.  One workgroup: a scan over 1024 rows at a time
+// (2 us, a launch's latency, up to that many).
 static __global__ __launch_bounds__(1024) void rows_kernel(const int64_t *target, const float *scale, float *loss, int N, int V, Rows o) {
     __shared__ int part[16];
     __shared__ int total;
@@ -140,7 +144,8 @@ struct XentEpi {
 };
 
 // Joins the tiles of R rows: 256 / R threads a row, each over its share of the tiles, in a fixed order.  16 rows read whole lines of
-// the statistics; with few rows the share of a thread matters more (one row of 1563 tiles: 4 instead of 38 us).
+// the statistics; with few rows the share of a thread matters more (one row of 1563 tiles: 4 instead of 38 us).  Bound by latency: 5 us for
+// 192 rows of 313 tiles, 24 for 8192 rows of 1000.
 template <int R>
 static __global__ __launch_bounds__(256) void lse_kernel(const float2 *stats, long long stats_ld, int tiles, Rows o, int first, int most,
                                                   float *loss) {
@@ -207,7 +212,8 @@ __device__ __forceinline__ void write_cost(const Rows &o, float *cost) {
 }
 static __global__ __launch_bounds__(256) void cost_kernel(Rows o, float *cost) { write_cost(o, cost); }
 
-// The rows that count, gathered as planes; zeros in the masked rows of dx (nullable).  Eight columns a thread.
+// The rows that count, gathered as planes; zeros in the masked rows of dx (nullable).  Eight columns a thread; bound by
+// HBM: 8192 rows of 4096 in bf16, 134 MB, 25 us.
 template <typename T>
 __global__ __launch_bounds__(256) void gather_kernel(const T *x, bf16_t *dst, T *dx, Rows o, int N, int D, int pieces) {
     constexpr int PL = Planes<T>::N;
@@ -233,7 +239,8 @@ __global__ __launch_bounds__(256) void zero_kernel(T *p, long long n, float *cos
     for (long long i = blockIdx.x * 256LL + threadIdx.x; i < n; i += gridDim.x * 256LL) p[i] = 0;
 }
 
-// d[m][v] of the rows first .. of the block (bf16: over the exponentials themselves)
+// d[m][v] of the rows first .. of the block (bf16: over the exponentials themselves).  Bound by HBM: 7400 x 128000 in bf16 move 3.8 GB in
+// 0.74 ms.
 template <typename T>
 struct XentGrad {
     const typename Kept<T>::V *keep;
