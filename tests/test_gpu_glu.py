@@ -1,4 +1,5 @@
 """glu_fwd / glu_bwd against the definitions in 64 bits."""
+import numpy
 import pytest
 import torch
 
@@ -143,6 +144,33 @@ def test_the_code_of_saved_values():
     inf = torch.isinf(want)
     assert torch.equal(got[inf].float(), want[inf]) and bool((got[far].sign() * want[far].sign() >= 0).all())
     assert torch.equal(gu[:, 0].contiguous().view(torch.int16), gu[:, 1].contiguous().view(torch.int16))
+
+
+@pytest.mark.parametrize("N", [5, 150])
+def test_saved_values_bit_by_bit(N):
+    """Neighbouring outputs on both sides of the marked form's border, in kernels for few rows and in tiles.  Products of two bf16
+    numbers are exact in fp32, so the code of each is known."""
+    gen = torch.Generator().manual_seed(7)
+    F = 150
+    x = torch.randn(N, 1, generator=gen).bfloat16()
+    x[1] = 0
+    x[2, 0], x[3, 0], x[4, 0] = float("inf"), float("nan"), -0.0
+    exponent = torch.randint(-40, 40, (F, 1), generator=gen) * (torch.rand(F, 1, generator=gen) < 0.3)
+    w = (torch.randn(F, 1, generator=gen) * 2.0 ** exponent).bfloat16()
+    x[0, 0] = 1
+    w[:6, 0] = torch.tensor([65280.0, 65536.0, 2.0 ** -16, 2.0 ** -17, 1.9921875 * 2.0 ** 15, -1.9921875 * 2.0 ** -17])
+    v = (x.float() * w.float().T).numpy().view("uint32").astype("int64")
+    sign, mag = (v >> 16) & 0x8000, v & 0x7FFFFFFF
+    near = ((mag + 0x1FFF + ((mag >> 14) & 1)) >> 14) - (111 << 9)
+    far = (mag + 0xFFFF + ((mag >> 17) & 1)) >> 17
+    nan = mag > 0x7F800000
+    want = sign | numpy.where((near >= 0) & (near < 32 << 9), near, 0x4000 | far)
+    _, gu = forward(x.cuda(), w.cuda(), w.cuda(), "sigmoid")
+    for k in (0, 1):
+        got = gu[:, k].cpu().contiguous().view(torch.int16).numpy().astype("int64") & 0xFFFF
+        assert (got[~nan] == want[~nan])[mag[~nan] != 0].all()
+        assert ((got[~nan] & 0x7FFF) == (want[~nan] & 0x7FFF)).all()      # a zero may lose its sign in a sum
+        assert ((got[nan] & 0x7FE0) == 0x7FE0).all()
 
 
 def test_small_and_large_fp32_operands():
