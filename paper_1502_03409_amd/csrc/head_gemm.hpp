@@ -484,13 +484,13 @@ struct StoreEpi {
     int width;
     const int *index;
     const float *add, *factor;
-    // where row m goes; null: nowhere
-    __device__ __forceinline__ T *row(int m) const {
+    // which row of its matrix row m goes to; -1: nowhere
+    __device__ __forceinline__ int place(int m) const {
         const bool up = m >= second;
         const int r = up ? m - second : m;
-        if (r >= (up ? rows1 : rows0)) return nullptr;
-        return (up ? out1 : out0) + (long long)(index ? index[r] : r) * width;
+        return r >= (up ? rows1 : rows0) ? -1 : index ? index[r] : r;
     }
+    __device__ __forceinline__ T *row(int m, int place) const { return (m >= second ? out1 : out0) + (long long)place * width; }
     __device__ __forceinline__ void finish(int m, int n, float f, float (&v)[4], T (&o)[4]) const {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
@@ -502,6 +502,13 @@ struct StoreEpi {
     __device__ __forceinline__ void run(f32x16 (&acc)[MT][NT], int m0, int n0, int lane, int M, int, int, char *lds) const {
         const RowStage<T, NT * 32> stage = {lds, lane};
         const float f = factor ? *factor : 1.f;
+        // by the lane of the row in its block, all before the first store: a load behind a store waits until that has reached memory
+        int places[MT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            const int m = m0 + 32 * i + (lane & 31);
+            places[i] = m < M ? place(m) : -1;
+        }
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             const int m = m0 + 32 * i + (lane & 31);
@@ -517,8 +524,8 @@ struct StoreEpi {
                 }
             stage.take([&](int r, int c, const u32x4 &w) {
                 const int to = m0 + 32 * i + r;
-                T *o = to < M ? row(to) : nullptr;
-                if (o) store_piece(o, n0 + c, width, w);
+                const int at = __shfl(places[i], r);
+                if (at >= 0) store_piece(row(to, at), n0 + c, width, w);
             });
         }
     }
@@ -554,8 +561,8 @@ struct PartEpi {
 constexpr int kJoin = 8;
 template <typename T>
 __global__ __launch_bounds__(256) void join_parts_kernel(const float *part, long long ld, int splits, Shape sh, StoreEpi<T> epi) {
-    const long long at = blockIdx.x * 256LL + threadIdx.x, quads = ld / 4;
-    const int m = (int)(at / quads), n = (int)(at - m * quads) * 4;
+    const long long id = blockIdx.x * 256LL + threadIdx.x, quads = ld / 4;
+    const int m = (int)(id / quads), n = (int)(id - m * quads) * 4;
     if (m >= sh.M) return;
     f32x4 s = {0.f, 0.f, 0.f, 0.f}, p[kJoin];
     for (int i = 0; i < splits; i += kJoin) {
@@ -566,8 +573,9 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const float *part, long
             if (i + k < splits) s += p[k];
     }
     if (m >= live(sh.M, sh.rows_dev, sh.rows_first)) return;
-    T *row = epi.row(m);
-    if (!row) return;
+    const int at = epi.place(m);
+    if (at < 0) return;
+    T *const row = epi.row(m, at);
     float v[4] = {s[0], s[1], s[2], s[3]};
     T o[4];
     epi.finish(m, n, epi.factor ? *epi.factor : 1.f, v, o);

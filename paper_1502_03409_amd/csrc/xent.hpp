@@ -89,11 +89,17 @@ struct XentEpi {
         typedef typename Kept<T>::V K;
         const RowStage<K, NT * 32> stage = {lds, lane};
         const int h = lane >> 5;
+        int targets[MT];   // all before the first store: a load behind a store waits until that has reached memory
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            const int m = m0 + 32 * i + (lane & 31);
+            targets[i] = m < M ? target[m] : -1;
+        }
         for_blocks<MT>([&](auto block) __attribute__((always_inline)) {
             constexpr int i = decltype(block)::value;
             const int m = m0 + 32 * i + (lane & 31);
             // columns of this wave that exist, and the target's, as this lane counts: 0 .. 3, 8 .. 11, ..
-            int end = V - n0 - 4 * h, at = (m < M ? target[m] : -1) - n0 - 4 * h;
+            int end = V - n0 - 4 * h, at = targets[i] - n0 - 4 * h;
             asm volatile("" : "+v"(end), "+v"(at));   // compared anew for every block of rows: the masks of all would not fit
             // the target and what lies beyond the vocabulary are taken out, where there is any of it
             if (__any(end < NT * 32 || (at >= 0 && at < NT * 32))) {
