@@ -1,5 +1,5 @@
 /*
- * lc_plan.h - host-only introspection of the launch plans behind lc.h's layer primitives.
+ * lc_plan.h - host-only introspection of the launch plans behind lc.h's layer primitives and lc_head.h's operators.
  *
  * Every launcher of the library first writes down the launch it is about to make (kernel family,
  * compile-time tile parameters, the scalars that fix the kernel's indexing, grid, block and LDS bytes),
@@ -44,6 +44,15 @@ int lc_plan_query(const lc_geom_t *g, int op, int dtype, lc_launch_t *out, int32
  * kernels one after the other (those keep no plan records).  Returns LC_OK, LC_EINVAL or LC_EINTERNAL. */
 int l2pool_lcn_plan_query(int32_t B, int32_t H, int32_t W, int32_t C, int32_t pool_ksize, int32_t pool_stride,
                           int32_t lcn_ksize, float gauss_sigma, lc_launch_t *out, int32_t max_out, int32_t *n_out);
+
+/* Operators of lc_head.h, for head_plan_query. */
+enum lc_head_op { LC_HEAD_GLU_FWD = 0, LC_HEAD_GLU_BWD = 1, LC_HEAD_XENT_FWD = 2, LC_HEAD_XENT_FWD_BWD = 3 };
+
+/* Host only.  The launches of an operator of lc_head.h for N rows of D values and `width` outputs (F or V), planned and
+ * checked as in a call that has every optional argument and exactly the scratch that the operator's workspace function
+ * gives.  *n_out and out as in lc_plan_query.  Returns LC_OK, LC_EINVAL or LC_EINTERNAL. */
+int head_plan_query(int op, int32_t N, int32_t D, int32_t width, int dtype, lc_launch_t *out, int32_t max_out,
+                    int32_t *n_out);
 
 #ifdef __cplusplus
 }

@@ -21,13 +21,15 @@ LIB_PATH = _HERE / "liblc.so"
 LC_OK, LC_EINVAL, LC_ENULL, LC_EALIGN, LC_EWORKSPACE, LC_EUNSUPPORTED, LC_EHIP, LC_EINTERNAL = 0, -1, -2, -3, -4, -5, -6, -7
 LC_F32, LC_BF16 = 0, 1
 LC_OP_FORWARD, LC_OP_BACKWARD_DATA, LC_OP_BACKWARD_WEIGHTS, LC_OP_SAE_STEP = 0, 1, 2, 3
+LC_HEAD_GLU_FWD, LC_HEAD_GLU_BWD, LC_HEAD_XENT_FWD, LC_HEAD_XENT_FWD_BWD = 0, 1, 2, 3
 LC_SAE_PROJECT_ROWS, LC_SAE_LEARN_ALPHA = 1, 2
 _STATUS = {0: "LC_OK", -1: "LC_EINVAL", -2: "LC_ENULL", -3: "LC_EALIGN", -4: "LC_EWORKSPACE",
            -5: "LC_EUNSUPPORTED", -6: "LC_EHIP", -7: "LC_EINTERNAL"}
 
 EXPORTS = ("lc_geom_derive", "lc_workspace_bytes", "lc_forward", "lc_forward_dev_scale", "lc_backward_data", "lc_backward_weights",
            "l2pool_fwd", "l2pool_bwd", "lcn_fwd", "lcn_bwd", "l2pool_lcn_fwd", "lcn_l2pool_bwd", "lcn_variant_workspace_bytes", "lcn_variant_fwd",
-           "lcn_variant_bwd", "lcn_variant_bwd_static", "sae_step", "lc_last_error", "lc_plan_query", "l2pool_lcn_plan_query")
+           "lcn_variant_bwd", "lcn_variant_bwd_static", "sae_step", "lc_last_error", "lc_plan_query", "l2pool_lcn_plan_query",
+           "head_plan_query")
 
 
 class LcGeom(C.Structure):
@@ -81,6 +83,7 @@ def lib() -> C.CDLL:
         L.lc_last_error.restype = C.c_char_p
         L.lc_plan_query.argtypes = [G, C.c_int, C.c_int, C.POINTER(LcLaunch), i32, C.POINTER(i32)]
         L.l2pool_lcn_plan_query.argtypes = [i32, i32, i32, i32, i32, i32, i32, f32, C.POINTER(LcLaunch), i32, C.POINTER(i32)]
+        L.head_plan_query.argtypes = [C.c_int, i32, i32, i32, C.c_int, C.POINTER(LcLaunch), i32, C.POINTER(i32)]
         for name in EXPORTS:
             if name not in ("lc_workspace_bytes", "lc_last_error"):
                 getattr(L, name).restype = C.c_int
@@ -129,9 +132,22 @@ def plan_query(g: LcGeom, op: int, dtype: int = LC_F32, max_out: int = 16):
     _check("lc_plan_query", lib().lc_plan_query(C.byref(g), op, dtype, out, max_out, C.byref(n)))
     if n.value > max_out:
         return plan_query(g, op, dtype, n.value)
-    return [{"kernel": out[i].kernel.decode(), "tparam": list(out[i].tparam), "arg": list(out[i].arg),
-             "grid": tuple(out[i].grid), "block": int(out[i].block), "lds_bytes": int(out[i].lds_bytes)}
-            for i in range(n.value)]
+    return [_launch(out[i]) for i in range(n.value)]
+
+
+def _launch(p: LcLaunch) -> dict:
+    return {"kernel": p.kernel.decode(), "tparam": list(p.tparam), "arg": list(p.arg), "grid": tuple(p.grid),
+            "block": int(p.block), "lds_bytes": int(p.lds_bytes)}
+
+
+def head_plan_query(op: int, N: int, D: int, width: int, dtype: int = LC_F32, max_out: int = 64):
+    """The launches an operator of the supervised head would make, as a list of dicts (host only; nothing is launched)."""
+    out = (LcLaunch * max_out)()
+    n = C.c_int32()
+    _check("head_plan_query", lib().head_plan_query(op, N, D, width, dtype, out, max_out, C.byref(n)))
+    if n.value > max_out:
+        return head_plan_query(op, N, D, width, dtype, n.value)
+    return [_launch(out[i]) for i in range(n.value)]
 
 
 def l2pool_lcn_plan_query(shape, pool_ksize: int, pool_stride: int, lcn_ksize: int, gauss_sigma: float = 1.0):
@@ -144,8 +160,7 @@ def l2pool_lcn_plan_query(shape, pool_ksize: int, pool_stride: int, lcn_ksize: i
                                                                 gauss_sigma, out, 1, C.byref(n)))
     if n.value == 0:
         return None
-    return {"kernel": out[0].kernel.decode(), "tparam": list(out[0].tparam), "arg": list(out[0].arg),
-            "grid": tuple(out[0].grid), "block": int(out[0].block), "lds_bytes": int(out[0].lds_bytes)}
+    return _launch(out[0])
 
 
 # The current stream's handle without building a Stream object (which costs as much as the launch itself).  A torch without

@@ -187,7 +187,7 @@ struct GluScratch {
     int Dp, Fp;
     bool direct;   // x and the weights are used where they are
     bf16_t *x, *w, *d;
-    float *part;   // one product at a time
+    Parts part = {};   // one product at a time
     GluScratch(Scratch &sc, int N, int D, int F, bool backward) {
         Dp = (int)round_up(D, 8), Fp = (int)round_up(F, kStep);
         direct = PL == 1 && D == Dp;
@@ -195,7 +195,9 @@ struct GluScratch {
         w = x ? x + (long long)N * Dp : nullptr;   // behind x in each plane, so that one launch lays all three out
         d = backward ? sc.take<bf16_t>((long long)PL * N * 2 * Fp) : nullptr;
         const int pairs = Planes<T>::PAIRS;
-        part = backward ? sc.take<float>(std::max(part_floats(N, D, Fp + F, pairs), part_floats(2 * Fp, D, N, pairs))) : nullptr;
+        if (!backward) return;
+        part.floats = std::max(part_floats(N, D, Fp + F, pairs), part_floats(2 * Fp, D, N, pairs));
+        part.at = sc.take<float>(part.floats);
     }
     // x and both weights as operands: laid out first unless they are where they can be used
     int operands(const T *xs, const T *wg, const T *wu, int N, int D, int F, Operand *X, Operand *W, hipStream_t s) const {

@@ -644,18 +644,24 @@ inline long long part_floats(int M, int Nn, int K, int pairs) {
     return c.splits > 1 ? (long long)c.splits * M * round_up(Nn, 4) : 0;
 }
 
+// Scratch for the sums of parts: as many floats as were set aside.
+struct Parts {
+    float *at;
+    long long floats;
+};
+
 // A product that is stored, cut along its contraction where that helps.
 template <int PL, int FA, int FB, typename T>
-int launch_product(const char *name, const Operand &A, const Operand &B, const Shape &sh, const StoreEpi<T> &epi, float *part, hipStream_t s) {
+int launch_product(const char *name, const Operand &A, const Operand &B, const Shape &sh, const StoreEpi<T> &epi, const Parts &part, hipStream_t s) {
     if (sh.M == 0 || sh.Nn == 0) return LC_OK;
     const Cut c = choose_cut(sh.M, sh.Nn, sh.K, PL == 3 ? 6 : 1, true);
     if (c.splits == 1) return launch_cut<PL, FA, FB>(name, A, B, sh, c, epi, s);
     const long long ld = round_up(sh.Nn, 4);
-    if (int rc = launch_cut<PL, FA, FB>(name, A, B, sh, c, PartEpi{part, ld, sh.M}, s)) return rc;
     const long long blocks = ((long long)sh.M * (ld / 4) + 255) / 256;
     const LaunchPlan p = make_plan(name, {}, {sh.M, sh.Nn, c.splits}, dim3((unsigned)blocks), 256, 0);
-    LC_PLAN_REQUIRE(p, blocks <= 0x7fffffffLL && part);
-    LC_LAUNCH(p, name, (join_parts_kernel<T>), s, part, ld, c.splits, sh, epi);
+    LC_PLAN_REQUIRE(p, blocks <= 0x7fffffffLL && part.at && c.splits * sh.M * ld <= part.floats);
+    if (int rc = launch_cut<PL, FA, FB>(name, A, B, sh, c, PartEpi{part.at, ld, sh.M}, s)) return rc;
+    LC_LAUNCH(p, name, (join_parts_kernel<T>), s, part.at, ld, c.splits, sh, epi);
     return LC_OK;
 }
 

@@ -7,6 +7,7 @@
 #include <utility>
 #include <vector>
 
+#include "../../include/lc_head.h"
 #include "lc_common.hpp"
 
 namespace lc {
@@ -185,6 +186,32 @@ int lc_plan_query(const lc_geom_t *g, int op, int dtype, lc_launch_t *out, int32
                               : launch_backward_weights_f32(q, ff, ff, nullptr, nullptr, 0.f, 1.f, ff, s);
     } else if (op == LC_OP_SAE_STEP) {
         rc = launch_sae_step(q, ff, ff, ff, ff, 0.1f, 1e-6f, 1e-3f, LC_SAE_PROJECT_ROWS | LC_SAE_LEARN_ALPHA, ff, ff, fake, s);
+    }
+    g_capture = nullptr;
+    if (rc != LC_OK) return rc;
+    *n_out = (int32_t)plans.size();
+    for (int32_t k = 0; k < max_out && k < (int32_t)plans.size(); ++k) out[k] = plans[k];
+    return LC_OK;
+}
+
+int head_plan_query(int op, int32_t N, int32_t D, int32_t width, int dtype, lc_launch_t *out, int32_t max_out, int32_t *n_out) {
+    if (max_out < 0 || (max_out > 0 && !out) || !n_out) return LC_EINVAL;
+    char *f = (char *)(uintptr_t)0x100000;      // never dereferenced: nothing is launched
+    const float *cf = (const float *)f;
+    float *ff = (float *)f;
+    const int64_t *t = (const int64_t *)f;
+    const int grads = op == LC_HEAD_GLU_BWD || op == LC_HEAD_XENT_FWD_BWD;
+    std::vector<LaunchPlan> plans;
+    int rc = LC_EINVAL;
+    g_capture = &plans;
+    if (op == LC_HEAD_GLU_FWD || op == LC_HEAD_GLU_BWD) {
+        const size_t ws = glu_workspace_bytes(N, D, width, dtype, grads);
+        rc = grads ? glu_bwd(f, f, f, f, f, f, f, f, N, D, width, LC_ACT_SILU, dtype, f, ws, nullptr)
+                   : glu_fwd(f, f, f, f, f, N, D, width, LC_ACT_SILU, dtype, f, ws, nullptr);
+    } else if (op == LC_HEAD_XENT_FWD || op == LC_HEAD_XENT_FWD_BWD) {
+        const size_t ws = xent_workspace_bytes(N, D, width, dtype, grads);
+        rc = grads ? xent_fwd_bwd(f, f, t, cf, ff, ff, f, f, N, D, width, dtype, f, ws, nullptr)
+                   : xent_fwd(f, f, t, cf, ff, ff, N, D, width, dtype, f, ws, nullptr);
     }
     g_capture = nullptr;
     if (rc != LC_OK) return rc;

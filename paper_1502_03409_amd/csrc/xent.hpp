@@ -292,7 +292,8 @@ struct XentScratch {
     Rows rows;
     bf16_t *x, *w, *d;
     float2 *stats;
-    float *scores, *sum, *part;
+    float *scores, *sum;
+    Parts part = {};
     XentScratch(Scratch &sc, int N, int D, int V, bool grads) {
         Dp = (int)round_up(D, 8), Vp = (int)round_up(V, 64);
         direct = PL == 1 && D == Dp;
@@ -317,7 +318,10 @@ struct XentScratch {
         if (!grads) return;
         d = sc.take<bf16_t>((long long)PL * block * Vp);
         scores = PL == 3 ? sc.take<float>((long long)block * Vp) : nullptr;
-        part = sc.take<float>(std::max(part_floats(block, D, V, Planes<T>::PAIRS), part_floats(V, D, block, Planes<T>::PAIRS)));
+        // the last block may have fewer rows than the others, and its products more parts
+        for (const int rows : {block, N - (blocks - 1) * block})
+            if (N) part.floats = std::max({part.floats, part_floats(rows, D, V, Planes<T>::PAIRS), part_floats(V, D, rows, Planes<T>::PAIRS)});
+        part.at = sc.take<float>(part.floats);
         sum = blocks > 1 ? sc.take<float>((long long)V * D) : nullptr;
     }
 };
