@@ -29,7 +29,7 @@ extern "C" {
 enum lc_act { LC_ACT_SIGMOID = 0, LC_ACT_SILU = 1, LC_ACT_GELU = 2 };
 
 /* Host only.  Scratch for glu_fwd (backward = 0), or for glu_fwd and glu_bwd (backward = 1); 0 for invalid arguments.
- * Both calls of one step may be given the same scratch. */
+ * Both calls of one step may be given the same scratch.  What is enough for N rows is enough for fewer. */
 size_t glu_workspace_bytes(int32_t N, int32_t D, int32_t F, int dtype, int backward);
 
 /* Gated layer: g = x wg^T, u = x wu^T, h = act(g) * u.
@@ -46,7 +46,8 @@ int glu_bwd(const void *x, const void *wg, const void *wu, const void *gu, const
             void *dwu, int32_t N, int32_t D, int32_t F, int act, int dtype, void *ws, size_t ws_bytes,
             void *hip_stream);
 
-/* Host only.  Scratch for xent_fwd (grads = 0) or xent_fwd_bwd (grads = 1); 0 for invalid arguments.  It holds no
+/* Host only.  Scratch for xent_fwd (grads = 0) or xent_fwd_bwd (grads = 1); 0 for invalid arguments.  What is enough for N
+ * rows is enough for fewer, with gradients also for the loss alone.  It holds no
  * [N][V] array without bound: the exponentials of at most 2 GiB worth of rows at a time with gradients, none without. */
 size_t xent_workspace_bytes(int32_t N, int32_t D, int32_t V, int dtype, int grads);
 

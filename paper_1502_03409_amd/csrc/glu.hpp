@@ -194,9 +194,8 @@ struct GluScratch {
         x = sc.take<bf16_t>(direct ? 8 : PL * ((long long)N + 2LL * F) * Dp);
         w = x ? x + (long long)N * Dp : nullptr;   // behind x in each plane, so that one launch lays all three out
         d = backward ? sc.take<bf16_t>((long long)PL * N * 2 * Fp) : nullptr;
-        const int pairs = Planes<T>::PAIRS;
         if (!backward) return;
-        part.floats = std::max(part_floats(N, D, Fp + F, pairs), part_floats(2 * Fp, D, N, pairs));
+        part.floats = std::max(part_floats(N, D, Fp + F), part_floats(2 * Fp, D, N));
         part.at = sc.take<float>(part.floats);
     }
     // x and both weights as operands: laid out first unless they are where they can be used

@@ -602,13 +602,18 @@ struct Cut {
 // From four rounds of large tiles on these are taken in any case: they bring half the bytes into LDS per product, and the chip runs
 // at the clock its power allows (8192 x 128000 x 4096 6.8 against 8.0 ms).  Both cuts at other sizes: 192 x 16384 x 4096 85 us large
 // and 40 small; 1000 x 768 x 30011 in fp32 3330 and 1572, in 16 parts 256 and 265.
+// Parts take no more than kMostParts floats, as many as the largest result that is cut at all: of 19000 products drawn from the ranges of
+// gradients of up to 8192 rows two lose by it, 0.1 % by the estimate.
+constexpr int kMostSplits = 32;
+constexpr long long kMostParts = 1LL << 26;
 inline Cut choose_cut(int M, int Nn, int K, int pairs, bool may_split) {
     const double large = (double)ceil_div(M, 256) * ceil_div(Nn, 256), small = (double)ceil_div(M, 128) * ceil_div(Nn, 128);
     if (large >= 4 * kComputeUnits) return Cut{Cut::LARGE, 1};
     const int steps = ceil_div(K, kStep);
     Cut best = {Cut::SMALL, 1};
     double least = 1e30;
-    for (int s = 1; s <= 32 && s <= std::max(1, steps / 2) && (s == 1 || may_split); ++s) {
+    const long long result = M * round_up(Nn, 4);
+    for (int s = 1; s == 1 || (may_split && s <= kMostSplits && s <= steps / 2 && s * result <= kMostParts); ++s) {
         const double part = (double)ceil_div(steps, s) * pairs;
         const double join = s > 1 ? 4 + 8e-6 * s * (double)M * Nn / 4 : 0;
         const double rounds = std::ceil(large * s / kComputeUnits), wgs = small * s;
@@ -638,10 +643,10 @@ int launch_gemm(const char *name, const Operand &A, const Operand &B, const Shap
     return launch_cut<PL, FA, FB>(name, A, B, sh, choose_cut(sh.M, sh.Nn, sh.K, PL == 3 ? 6 : 1, false), epi, s);
 }
 
-// Floats that launch_product() needs for the parts of a product of this size.
-inline long long part_floats(int M, int Nn, int K, int pairs) {
-    const Cut c = choose_cut(M, Nn, K, pairs, true);
-    return c.splits > 1 ? (long long)c.splits * M * round_up(Nn, 4) : 0;
+// Floats that are enough for the parts of any product of up to M rows and up to K indices: a shorter product may be cut into more parts.
+inline long long part_floats(int M, int Nn, int K) {
+    const int most = std::min(kMostSplits, ceil_div(K, kStep) / 2);
+    return most > 1 ? std::min(kMostParts, most * M * round_up(Nn, 4)) : 0;
 }
 
 // Scratch for the sums of parts: as many floats as were set aside.

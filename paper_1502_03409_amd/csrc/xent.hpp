@@ -314,13 +314,11 @@ struct XentScratch {
         rows.loss = sc.take<float>(N);
         x = sc.take<bf16_t>((long long)PL * N * Dp);
         w = direct ? nullptr : sc.take<bf16_t>((long long)PL * V * Dp);
-        stats = sc.take<float2>((long long)tiles * block);
+        stats = sc.take<float2>((V + 63) / 64 * (long long)block);   // as for the smaller tiles that fewer rows may take
         if (!grads) return;
         d = sc.take<bf16_t>((long long)PL * block * Vp);
         scores = PL == 3 ? sc.take<float>((long long)block * Vp) : nullptr;
-        // the last block may have fewer rows than the others, and its products more parts
-        for (const int rows : {block, N - (blocks - 1) * block})
-            if (N) part.floats = std::max({part.floats, part_floats(rows, D, V, Planes<T>::PAIRS), part_floats(V, D, rows, Planes<T>::PAIRS)});
+        part.floats = std::max(part_floats(block, D, V), part_floats(V, D, block));
         part.at = sc.take<float>(part.floats);
         sum = blocks > 1 ? sc.take<float>((long long)V * D) : nullptr;
     }

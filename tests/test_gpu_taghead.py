@@ -68,3 +68,24 @@ def test_features_are_one_row_an_image():
     g = lc.geom(5, 32, 32, 3, 8, 4, 16)
     f = features(g, torch.randn(5, 32, 32, 3, device="cuda"), torch.randn(7, 7, 192, 16, device="cuda"))
     assert f.shape == (5, 5 * 5 * 16) and bool(torch.isfinite(f).all())
+
+
+@pytest.mark.parametrize("D,F,V,batch,N,dtype", [(1024, 2048, 20011, 192, 128, torch.bfloat16), (400, 256, 1000, 512, 486, torch.bfloat16),
+                                                 (400, 256, 1000, 512, 300, torch.float32)])
+def test_the_last_batch_of_an_epoch(D, F, V, batch, N, dtype):
+    """Smaller batches whose products are cut into more parts than the largest one's, through the scratch of the largest."""
+    print(f"case tag head {D} {F} {V} {batch} {N} {dtype}", flush=True)
+    head = TagHead(D, F, V, batch, dtype=dtype)
+    gen = torch.Generator().manual_seed(2)
+    x = torch.randn(N, D, generator=gen).to(dtype).cuda()
+    t = torch.randint(0, V, (N,), generator=gen).cuda()
+    head.gradients(x, t)
+    wg, wu, wv = (w.double() for w in head.params)
+    h, _, _ = ref.glu(x, wg, wu, "silu")
+    _, cost, dh, dwv = ref.xent(h, wv, t)
+    _, dwg, dwu = ref.glu_grads(x, wg, wu, dh, "silu")
+    # as in the test of a step
+    bound = 7 * 2.0 ** -8 if dtype == torch.bfloat16 else ref.tol(dtype, D + F + V, 0) * 4
+    assert abs(float(head.cost) - float(cost)) <= bound * max(1.0, abs(float(cost)))
+    for got, want in zip(head.grads, (dwg, dwu, dwv)):
+        ref.check("gradient", got, want, bound)

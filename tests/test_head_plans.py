@@ -74,6 +74,22 @@ def test_any_size_passes_the_host_checks_and_fits_its_scratch(dtype):
         assert used <= lc.glu_workspace_bytes(N, D, F, dtype, True), (N, D, F)
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
+def test_scratch_for_a_batch_is_enough_for_smaller_ones(dtype):
+    """The last batch of an epoch, through the scratch of the others; fewer rows are cut into more parts."""
+    rng = random.Random(6)
+    sizes = [(1024, 2048, 192), (2048, 20011, 192), (400, 256, 512), (256, 1000, 512), (1024, 4096, 1024), (4096, 20011, 1024),
+             (4096, 8192, 512), (8192, 20011, 512)]
+    sizes += [(log_int(rng, 1, 8192), log_int(rng, 1, 200000), log_int(rng, 2, 8192)) for _ in range(150)]
+    for D, width, N in sizes:
+        for size in (lc.glu_workspace_bytes, lc.xent_workspace_bytes):
+            for grads in (False, True):
+                enough = size(N, D, width, dtype, grads)
+                fewer = range(0, N) if N <= 1024 else [rng.randrange(N) for _ in range(200)] + list(range(N - 300, N))
+                assert all(size(n, D, width, dtype, grads) <= enough for n in fewer), (size.__name__, D, width, N, grads)
+            assert size(N, D, width, dtype, False) <= size(N, D, width, dtype, True)
+
+
 def test_refusals():
     for op, sizes, dtype in ((9, (4, 4, 4), 0), (0, (-1, 4, 4), 0), (2, (4, 0, 4), 0), (3, (4, 4, 1 << 21), 1), (1, (4, 4, 4), 5)):
         with pytest.raises(lc.LcError) as e:
