@@ -191,7 +191,7 @@ static __global__ __launch_bounds__(256) void lse_kernel(const float2 *stats, lo
     }
     if (part == 0 && m < M) {
         const float tl = o.tl[first + m];
-        const float z = top == -__builtin_inff() && sum == 0.f ? top : top + logf(sum) - tl;
+        const float z = top + logf(sum) - tl;   // -inf where there is no other word, NaN where the target's score is -inf as well
         const float e = expf(-fabsf(z));
         float v = fmaxf(z, 0.f) + log1pf(e), dt = -(z > 0.f ? 1.f : e) / (1.f + e);
         if (!(z == z) || !(tl < __builtin_inff())) v = dt = __builtin_nanf("");   // as in inf - inf

@@ -230,3 +230,18 @@ def test_the_same_bits_on_another_stream_and_in_a_graph(dtype):
         torch.cuda.synchronize()
         for a, b in zip(first, (loss, cost, dx, dw)):
             assert torch.equal(a, b)
+
+
+@dtypes
+@pytest.mark.parametrize("N", [5, 70])
+def test_a_row_whose_scores_are_all_minus_infinity_is_loud(N, dtype):
+    """The logarithm of nothing less the logarithm of nothing: NaN, for one word and for many."""
+    for V in (1, 150):
+        x, w, t = inputs(N, 33, V, dtype, seed=12, masked=0.0)
+        x[:, 0] = 1.0
+        w[:, 0] = float("-inf")
+        t[1] = -1
+        live = t >= 0
+        for grads in (False, True):
+            loss, cost = run(x, w, t, grads=grads)[:2]
+            assert torch.equal(torch.isnan(loss), live) and torch.isnan(cost).all()
