@@ -27,7 +27,10 @@ struct Rows {
     int *index, *target;   // by position
     float *scale, *tl;     // weight in the cost, but for the factor *unit; the target's score
     float *unit;           // 1 / count for the mean, else 1: the results' factor, so that d = p - [v = t] is what is rounded
-    float *lse, *dt, *loss;   // logsumexp; p(target) - 1; loss
+    // p = exp((l - base) - log_sum): the largest score, and the logarithm of the sum of the exponentials relative to it.  As one number
+    // their sum would be rounded at the scores' size, and all of a row's probabilities with it.
+    float *base, *log_sum;
+    float *dt, *loss;      // p(target) - 1; loss
 };
 
 // Positions of the rows that count, in order; loss 0 where masked.  One workgroup: a scan over 1024 rows at a time
@@ -191,11 +194,13 @@ static __global__ __launch_bounds__(256) void lse_kernel(const float2 *stats, lo
     }
     if (part == 0 && m < M) {
         const float tl = o.tl[first + m];
-        const float z = top + logf(sum) - tl;   // -inf where there is no other word, NaN where the target's score is -inf as well
+        const float z = (top - tl) + logf(sum);   // -inf where there is no other word, NaN where the target's score is -inf as well
         const float e = expf(-fabsf(z));
         float v = fmaxf(z, 0.f) + log1pf(e), dt = -(z > 0.f ? 1.f : e) / (1.f + e);
         if (!(z == z) || !(tl < __builtin_inff())) v = dt = __builtin_nanf("");   // as in inf - inf
-        o.lse[first + m] = tl + v;
+        const float base = fmaxf(top, tl);
+        o.base[first + m] = base;
+        o.log_sum[first + m] = logf(sum * expf(top - base) + expf(tl - base));
         o.dt[first + m] = dt;
         o.loss[first + m] = v;
         loss[o.index[first + m]] = v;
@@ -262,16 +267,16 @@ struct XentGrad {
     __device__ bool skip(int m) const { return m >= live(most, o.count, first); }
     __device__ void operator()(int m, int c, float (&v)[1][8]) const {
         const int r = first + m, t = o.target[r];
-        const float lse = o.lse[r], s = o.scale[r];
+        const float base = o.base[r], log_sum = o.log_sum[r], s = o.scale[r];
         if constexpr (sizeof(T) == 4) {
             const f32x4 *k = (const f32x4 *)(keep + m * ld + c);
             const f32x4 a = k[0], b = k[1];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[0][e] = s * expf((e < 4 ? a[e & 3] : b[e & 3]) - lse);
+            for (int e = 0; e < 8; ++e) v[0][e] = s * expf(((e < 4 ? a[e & 3] : b[e & 3]) - base) - log_sum);
         } else {
             typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
             const f16x8 k = *(const f16x8 *)(keep + m * ld + c);
-            const float f = __expf(stats[(c / wave_cols) * stats_ld + m].x - lse) * 0x1p-15f;
+            const float f = __expf((stats[(c / wave_cols) * stats_ld + m].x - base) - log_sum) * 0x1p-15f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[0][e] = s * ((float)k[e] * f);
         }
@@ -309,7 +314,8 @@ struct XentScratch {
         rows.target = sc.take<int>(N);
         rows.scale = sc.take<float>(N);
         rows.tl = sc.take<float>(N);
-        rows.lse = sc.take<float>(N);
+        rows.base = sc.take<float>(N);
+        rows.log_sum = sc.take<float>(N);
         rows.dt = sc.take<float>(N);
         rows.loss = sc.take<float>(N);
         x = sc.take<bf16_t>((long long)PL * N * Dp);

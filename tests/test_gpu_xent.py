@@ -245,3 +245,63 @@ def test_a_row_whose_scores_are_all_minus_infinity_is_loud(N, dtype):
         for grads in (False, True):
             loss, cost = run(x, w, t, grads=grads)[:2]
             assert torch.equal(torch.isnan(loss), live) and torch.isnan(cost).all()
+
+
+@dtypes
+@pytest.mark.parametrize("low", [-1e5, float("-inf")])
+@pytest.mark.parametrize("N", [5, 70])
+def test_a_target_far_below_the_other_words(N, low, dtype):
+    """The other words' probabilities are as exact as their own scores.  The target's score is `low`, its gradient -1 times the row's
+    weight; the cost of an impossible target is infinite, its gradients by words are finite."""
+    x, w, t = inputs(N, 33, 150, dtype, seed=13, masked=0.1)
+    x[:, 0] = 1.0
+    w[:, 0] = 0.0
+    w[77] = 0.0
+    w[77, 0] = low
+    t[0], t[3], t[4] = 77, 77, 78
+    loss, cost, dx, dw = run(x, w, t)
+    rl, rc, rx, rw = ref.xent(x, w, t)
+    others = torch.arange(150, device="cuda") != 77
+    b = loss_bound(x.float(), w[others])
+    impossible = torch.isinf(rl)
+    assert torch.equal(torch.isinf(loss), impossible) and bool((impossible == ((t == 77) & (low < -1e30))).all())
+    near = ~impossible
+    assert float((loss.double() - rl)[near].abs().max()) <= b + 2.0 ** -23 * float(rl[near].abs().max())
+    assert torch.isinf(cost).all() if low < -1e30 else abs(float(cost) - float(rc)) <= b + 2.0 ** -22 * float(rc)
+    bound = ref.tol(dtype, N, 2.25) + b
+    ref.check("dw", dw[others], rw[others], bound)
+    ref.check("dw of the target", dw[77], rw[77], bound)
+    live = t >= 0      # a masked row's dx is zero, whatever the words are
+    ref.check("dx", dx[live], rx[live], ref.tol(dtype, 150, 2.25) + b)
+    assert not dx[~live].any()
+
+
+def check_equal_scores(N, dtype, size):
+    """Half of the words share the score `size`, up to the row's sign, the others have its half: one product each, so all scores are
+    exact, and the probabilities are those of a draw among the largest."""
+    x = torch.full((N, 1), size, device="cuda").to(dtype)
+    x[1::2] *= -1
+    w = torch.ones((150, 1), device="cuda").to(dtype)
+    w[::2] = 0.5
+    t = torch.arange(N, device="cuda") * 2 % 150 + (torch.arange(N, device="cuda") + 1) % 2      # among the largest
+    t[2] = -1
+    loss, cost, dx, dw = run(x, w, t)
+    live = t >= 0
+    # the exponentials, their sum and its logarithm
+    bound = 2.0 ** -20 * math.log(75)
+    assert float((loss.double() - math.log(75) * live).abs().max()) <= bound
+    assert abs(float(cost) - math.log(75)) <= bound
+    d = torch.zeros((N, 150), dtype=torch.float64, device="cuda")
+    d[0::2, 1::2] = d[1::2, 0::2] = 1 / 75
+    d.scatter_add_(1, t.clamp(min=0)[:, None], torch.full((N, 1), -1.0, dtype=torch.float64, device="cuda"))
+    d = d * live[:, None] / int(live.sum())
+    # a word's gradient adds up terms of size * p of either sign: its bound is that of the sum of their magnitudes, of which it is a part
+    want, total = d.t() @ x.double(), d.abs().t() @ x.double().abs()
+    assert bool(((dw.double() - want).abs() <= (ref.tol(dtype, N, 2.25) + bound) * total).all())
+    assert torch.isfinite(dx).all() and not dx[~live].any()
+
+
+@pytest.mark.parametrize("size", [1e4, 1e8, 1e30, 1e38])
+@pytest.mark.parametrize("N", [5, 70])
+def test_equal_scores_of_any_size(N, size):
+    check_equal_scores(N, torch.float32, size)
