@@ -125,7 +125,6 @@ struct XentEpi {
                 for (int e = 0; e < 16; ++e) top = fmaxf(top, acc[i][j][e]);
             top = fmaxf(top, __shfl_xor(top, 32));
             const float base = top == -__builtin_inff() ? 0.f : top;   // all scores -inf: exponentials of 0, not of NaN
-            const float base2 = base * 1.44269504f;   // bf16: e^(l - base) = 2^(l log2 e - base log2 e), good to 2^-24 |l|
             float sum = 0.f;
 #pragma unroll
             for (int j = 0; j < NT; ++j)
@@ -135,7 +134,7 @@ struct XentEpi {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const float l = acc[i][j][4 * q + r];
-                        const float e = sizeof(T) == 4 ? expf(l - base) : __builtin_amdgcn_exp2f(__builtin_fmaf(l, 1.44269504f, -base2));
+                        const float e = sizeof(T) == 4 ? expf(l - base) : __builtin_amdgcn_exp2f((l - base) * 1.44269504f);
                         sum += e;
                         v[r] = kept(K(), l, e);
                     }

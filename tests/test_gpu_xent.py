@@ -305,3 +305,9 @@ def check_equal_scores(N, dtype, size):
 @pytest.mark.parametrize("N", [5, 70])
 def test_equal_scores_of_any_size(N, size):
     check_equal_scores(N, torch.float32, size)
+
+
+@pytest.mark.parametrize("size", [1e4, 1e8, 1e30, 1e38])
+@pytest.mark.parametrize("N", [5, 70])
+def test_equal_scores_of_any_size_in_bf16(N, size):
+    check_equal_scores(N, torch.bfloat16, size)
