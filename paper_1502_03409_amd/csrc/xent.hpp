@@ -4,9 +4,9 @@
 // the exponentials below it, and a small kernel joins the tiles.  The target's own score is kept out of both and apart: with z the
 // logarithm of the other words' sum minus the target's score, loss = log(1 + e^z) and p(target) - 1 = -1 / (1 + e^-z), neither of
 // which cancels in rows that are already learned.  With gradients a tile also leaves the
-// exponentials themselves (bf16 operands: relative to the tile's largest score, in fp16 times 2^15, which holds eleven bits of
-// all above 2^-29, so that the one rounding to bf16 that follows is the only one that shows; fp32: the scores), for a bounded number of rows at a time; one pass turns them into d[n][v] = s[n] (p[n][v] - [v = t]) in
-// place, and two products give dx = d w and dw = d^T x.
+// exponentials themselves (bf16 operands: relative to the tile's largest score, in 16 bits, ten of them significant, over the whole range of
+// fp32: a quarter of the rounding to bf16 that follows, and no word is too rare; fp32: the scores), for a bounded number of rows at a
+// time; one pass turns them into d[n][v] = s[n] (p[n][v] - [v = t]) in place, and two products give dx = d w and dw = d^T x.
 //
 // 8192 rows of 4096 over 128000 words in bf16, a tenth masked: scores 6.4 ms, statistics 0.02, d 0.74, dx 6.3, dw 6.5; three products of 7.7
 // TFLOP each, bound as large products are.
@@ -73,9 +73,13 @@ static __global__ __launch_bounds__(1024) void rows_kernel(const int64_t *target
 
 template <typename T> struct Kept;   // what a tile leaves for the gradient
 template <> struct Kept<float> { typedef float V; };
-template <> struct Kept<bf16_t> { typedef _Float16 V; };
+template <> struct Kept<bf16_t> { typedef unsigned short V; };
 __device__ __forceinline__ float kept(float, float l, float) { return l; }                                     // score l
-__device__ __forceinline__ _Float16 kept(_Float16, float, float e) { return (_Float16)(e * 32768.f); }         // exponential e
+// exponential e, 0 to 1: sign and first bit of fp32's exponent are zero, the next sixteen are kept, to nearest (NaN: the row's statistics
+// have it)
+__device__ __forceinline__ unsigned short kept(unsigned short, float, float e) {
+    return (unsigned short)((__builtin_bit_cast(unsigned, e) + 0x2000u) >> 14);
+}
 
 // Per wave and row: the largest score, the sum of exponentials (both without the target), the target's score, and with KEEP what
 // the gradient needs.
@@ -273,11 +277,10 @@ struct XentGrad {
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[0][e] = s * expf(((e < 4 ? a[e & 3] : b[e & 3]) - base) - log_sum);
         } else {
-            typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-            const f16x8 k = *(const f16x8 *)(keep + m * ld + c);
-            const float f = __expf((stats[(c / wave_cols) * stats_ld + m].x - base) - log_sum) * 0x1p-15f;
+            const u32x4 k = *(const u32x4 *)(keep + m * ld + c);
+            const float f = __expf((stats[(c / wave_cols) * stats_ld + m].x - base) - log_sum);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[0][e] = s * ((float)k[e] * f);
+            for (int e = 0; e < 8; ++e) v[0][e] = s * (__builtin_bit_cast(float, ((e & 1) ? k[e >> 1] >> 2 : k[e >> 1] << 14) & 0x3fffc000u) * f);
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {

@@ -311,3 +311,24 @@ def test_equal_scores_of_any_size(N, size):
 @pytest.mark.parametrize("N", [5, 70])
 def test_equal_scores_of_any_size_in_bf16(N, size):
     check_equal_scores(N, torch.bfloat16, size)
+
+
+@dtypes
+@pytest.mark.parametrize("N", [5, 70])
+def test_words_that_hardly_count_have_their_gradients(N, dtype):
+    """Words whose scores lie 30 to 60 below the largest, beside it in a tile and in tiles of their own: probabilities down to 10^-26 are
+    as exact as others, relative to their own size.  One product a score, so the scores' rounding is that of their size."""
+    gen = torch.Generator().manual_seed(14)
+    V = 300
+    x = (1.0 + 0.1 * torch.rand(N, 1, generator=gen)).to(dtype).cuda()
+    w = (-30.0 - 25.0 * torch.rand(V, 1, generator=gen)).to(dtype).cuda()
+    w[5] = 0.0
+    t = torch.full((N,), 5, device="cuda")
+    t[1] = -1
+    loss, cost, dx, dw = run(x, w, t)
+    _, _, rx, rw = ref.xent(x, w, t)
+    others = torch.arange(V, device="cuda") != 5
+    bound = ref.tol(dtype, N, 2.25) + 4 * 2.0 ** -24 * 60
+    worst = float(((dw.double() - rw).abs() / rw.abs())[others].max())
+    assert worst <= bound, (worst, bound)
+    ref.check("dx", dx, rx, bound)
