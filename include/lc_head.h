@@ -54,7 +54,8 @@ size_t xent_workspace_bytes(int32_t N, int32_t D, int32_t V, int dtype, int grad
 /* Softmax cross entropy over a vocabulary of V words, projection included:
  *   l[n][v] = sum_d x[n][d] w[v][d];  loss[n] = log sum_v exp(l[n][v]) - l[n][target[n]] for target[n] >= 0, else 0;
  *   cost = sum_n s[n] loss[n], s[n] = scale[n], or 1 / (number of targets >= 0) if scale is NULL.
- * x [N][D], w [V][D], target [N] int64, scale NULL or [N] fp32; loss [N] and cost [1] fp32.
+ * x [N][D], w [V][D], target [N] int64 (8-byte aligned: any part of a longer list), scale NULL or [N] fp32; loss [N] and
+ * cost [1] fp32.
  * A row with a negative target is masked: its x and scale are not looked at.  With no row left the cost is 0.
  * A target >= V makes the loss of its row, the cost and the gradients it enters NaN. */
 int xent_fwd(const void *x, const void *w, const int64_t *target, const float *scale, float *loss, float *cost,

@@ -20,9 +20,10 @@ int xent_checked(const void *x, const void *w, const int64_t *target, const floa
                  int32_t N, int32_t D, int32_t V, int dtype, bool grads, void *ws, size_t ws_bytes, void *hip_stream) {
     if (!xent_sizes(N, D, V, dtype)) return LC_EINVAL;
     if (!w || !cost || (grads && !dw) || (N && (!x || !target || !loss))) return LC_ENULL;
-    for (const void *p : {x, w, (const void *)dx, (const void *)dw, (const void *)ws, (const void *)target, (const void *)scale,
-                          (const void *)loss, (const void *)cost})
+    for (const void *p : {x, w, (const void *)dx, (const void *)dw, (const void *)ws, (const void *)scale, (const void *)loss,
+                          (const void *)cost})
         if (!ptr_aligned16(p)) return LC_EALIGN;
+    if ((uintptr_t)target & 7u) return LC_EALIGN;   // read one at a time: a batch may start at any row of a list
     if (!ws || ws_bytes < xent_workspace_bytes(N, D, V, dtype, grads)) return LC_EWORKSPACE;
     hipStream_t s = (hipStream_t)hip_stream;
     if (dtype == LC_BF16)

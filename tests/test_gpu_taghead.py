@@ -89,3 +89,14 @@ def test_the_last_batch_of_an_epoch(D, F, V, batch, N, dtype):
     assert abs(float(head.cost) - float(cost)) <= bound * max(1.0, abs(float(cost)))
     for got, want in zip(head.grads, (dwg, dwu, dwv)):
         ref.check("gradient", got, want, bound)
+
+
+@pytest.mark.parametrize("at", [1, 2, 3])
+def test_batches_of_a_list_of_targets(at):
+    head = TagHead(40, 24, 50, 20)
+    x, t = torch.randn(20, 40, device="cuda"), torch.randint(0, 50, (30,), device="cuda")
+    head.gradients(x, t[at:at + 20].clone())
+    want = [a.clone() for a in (head.cost, head.loss, *head.grads)]
+    head.gradients(x, t[at:at + 20])
+    for a, b in zip(want, (head.cost, head.loss, *head.grads)):
+        assert torch.equal(a, b)

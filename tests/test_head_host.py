@@ -132,3 +132,10 @@ def test_the_binding_refuses():
         lc.grad_norm([torch.zeros(3, dtype=torch.float64)], torch.zeros(1))
     with pytest.raises(ValueError):
         lc.grad_norm([x], torch.zeros(1))
+
+
+def test_targets_may_start_at_any_row_of_a_list():
+    """Alignment comes before scratch among the checks: a target aligned to 8 bytes gets past it, an odd one does not."""
+    for target, code in ((P + 8, B.LC_EWORKSPACE), (P + 24, B.LC_EWORKSPACE), (P + 4, B.LC_EALIGN), (P + 1, B.LC_EALIGN)):
+        assert L().xent_fwd(P, P, target, None, P, P, 4, 4, 4, 0, P, 8, None) == code
+        assert L().xent_fwd_bwd(P, P, target, P, P, P, P, P, 4, 4, 4, 1, P, 8, None) == code
