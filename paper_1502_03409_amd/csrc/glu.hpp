@@ -191,7 +191,8 @@ struct GluScratch {
     GluScratch(Scratch &sc, int N, int D, int F, bool backward) {
         Dp = (int)round_up(D, 8), Fp = (int)round_up(F, kStep);
         direct = PL == 1 && D == Dp;
-        x = sc.take<bf16_t>(direct ? 8 : PL * ((long long)N + 2LL * F) * Dp);
+        // few rows: the forward pass takes everything where it is
+        x = sc.take<bf16_t>(direct || (N <= kFewRows && !backward) ? 8 : PL * ((long long)N + 2LL * F) * Dp);
         w = x ? x + (long long)N * Dp : nullptr;   // behind x in each plane, so that one launch lays all three out
         d = backward ? sc.take<bf16_t>((long long)PL * N * 2 * Fp) : nullptr;
         if (!backward) return;

@@ -320,8 +320,9 @@ struct XentScratch {
         rows.log_sum = sc.take<float>(N);
         rows.dt = sc.take<float>(N);
         rows.loss = sc.take<float>(N);
-        x = sc.take<bf16_t>((long long)PL * N * Dp);
-        w = direct ? nullptr : sc.take<bf16_t>((long long)PL * V * Dp);
+        const bool laid_out = grads || N > kFewRows;   // the scores of few rows need neither x nor w as planes
+        x = laid_out ? sc.take<bf16_t>((long long)PL * N * Dp) : nullptr;
+        w = direct || !laid_out ? nullptr : sc.take<bf16_t>((long long)PL * V * Dp);
         stats = sc.take<float2>((V + 63) / 64 * (long long)block);   // as for the smaller tiles that fewer rows may take
         if (!grads) return;
         d = sc.take<bf16_t>((long long)PL * block * Vp);

@@ -90,6 +90,16 @@ def test_scratch_for_a_batch_is_enough_for_smaller_ones(dtype):
             assert size(N, D, width, dtype, False) <= size(N, D, width, dtype, True)
 
 
+def test_few_rows_ask_for_no_copy_of_the_weights():
+    """Answers for up to 32 rows read the weights where they are; what is left are a few numbers for each row, and for each row and 64 words."""
+    for dtype in TYPES:
+        for N in (1, 5, 32):
+            for D in (4096, 4097, 100):
+                assert lc.glu_workspace_bytes(N, D, 8192, dtype) <= 4096
+                assert lc.xent_workspace_bytes(N, D, 100003, dtype) <= 8 * up(N, 8) * (100003 // 64 + 1) + 16384
+        assert lc.xent_workspace_bytes(33, 4097, 100003, dtype) > 100003 * 4097 * 2      # laid out from 33 rows on
+
+
 def test_refusals():
     for op, sizes, dtype in ((9, (4, 4, 4), 0), (0, (-1, 4, 4), 0), (2, (4, 0, 4), 0), (3, (4, 4, 1 << 21), 1), (1, (4, 4, 4), 5)):
         with pytest.raises(lc.LcError) as e:
