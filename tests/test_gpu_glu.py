@@ -202,3 +202,18 @@ def test_the_same_bits_every_time_on_any_stream(dtype):
     side.synchronize()
     for a, b in zip((*first, *gfirst), (*again, *gagain)):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("N", [3, 100])
+def test_large_saved_values_stay_finite(N):
+    """The largest numbers of bf16 lie above the largest seven bits: they are saved as that, not as infinities, which times a
+    gradient of zero would be NaN."""
+    x = torch.full((N, 1), torch.finfo(torch.bfloat16).max, dtype=torch.bfloat16, device="cuda")
+    x[1] *= -1
+    w = torch.ones((9, 1), dtype=torch.bfloat16, device="cuda")
+    _, gu = forward(x, w, w, "sigmoid")
+    want = x.double().expand(N, 9)
+    for k in (0, 1):
+        assert bool(((saved(gu[:, k]) - want).abs() <= 2.0 ** -7 * want.abs()).all())
+    for grad in backward(x, w, w, gu, torch.zeros((N, 9), dtype=torch.bfloat16, device="cuda"), "sigmoid"):
+        assert not grad.any()
