@@ -19,6 +19,14 @@ __device__ __forceinline__ float sigmoid(float g) {
     if constexpr (sizeof(T) == 4) return 1.f / (1.f + expf(-g));
     else return __builtin_amdgcn_rcpf(1.f + __expf(-g));
 }
+// 1 / (1 + e^-g) and 1 / (1 + e^g), which 1 minus the first would lose where a gate is open wide
+template <typename T>
+__device__ __forceinline__ void sigmoid_both(float g, float &s, float &rest) {
+    const float e = sizeof(T) == 4 ? expf(-fabsf(g)) : __expf(-fabsf(g));
+    const float more = sizeof(T) == 4 ? 1.f / (1.f + e) : __builtin_amdgcn_rcpf(1.f + e), less = e * more;
+    s = g < 0.f ? less : more;
+    rest = g < 0.f ? more : less;
+}
 template <typename T, int ACT>
 __device__ __forceinline__ float act_value(float g) {
     if constexpr (ACT == LC_ACT_GELU) return 0.5f * g * erfcf(-0.70710678118654752f * g);
@@ -33,9 +41,10 @@ __device__ __forceinline__ void act_both(float g, float &a, float &da) {
         a = g * phi;
         da = phi + g * (0.39894228040143268f * expf(-0.5f * g * g));
     } else {
-        const float sg = sigmoid<T>(g);
+        float sg, rest;
+        sigmoid_both<T>(g, sg, rest);
         a = ACT == LC_ACT_SIGMOID ? sg : g * sg;
-        da = ACT == LC_ACT_SIGMOID ? sg * (1.f - sg) : sg * (1.f + g * (1.f - sg));
+        da = ACT == LC_ACT_SIGMOID ? sg * rest : sg * (1.f + g * rest);
     }
 }
 

@@ -217,3 +217,21 @@ def test_large_saved_values_stay_finite(N):
         assert bool(((saved(gu[:, k]) - want).abs() <= 2.0 ** -7 * want.abs()).all())
     for grad in backward(x, w, w, gu, torch.zeros((N, 9), dtype=torch.bfloat16, device="cuda"), "sigmoid"):
         assert not grad.any()
+
+
+@dtypes
+@pytest.mark.parametrize("name", ["sigmoid", "silu"])
+def test_gates_that_are_open_wide_or_shut(name, dtype):
+    """The gate's derivative by itself (one row, x = u = dh = 1), relative to its own size: e^-|g| however small.  Gates in steps of 1/4
+    up to 16 are exact in every type on the way."""
+    g = torch.arange(-64, 65, device="cuda")[:, None] / 4
+    x, wg, wu, dh = (t.to(dtype) for t in (torch.ones((1, 1), device="cuda"), g, torch.ones_like(g), torch.ones((1, 129), device="cuda")))
+    _, gu = forward(x, wg, wu, name)
+    _, dwg, dwu = backward(x, wg, wu, gu, dh, name)
+    a, da = ref.act(name, g.double())
+    rest = torch.sigmoid(-g.double())
+    da = a * rest if name == "sigmoid" else torch.sigmoid(g.double()) * (1 + g * rest)
+    # SiLU's derivative crosses zero, as a sum of one and g (1 - s): an error of one rounding of the larger of both
+    size = da.abs() if name == "sigmoid" else torch.sigmoid(g.double()) * torch.maximum(torch.ones_like(g), (g * rest).abs())
+    assert bool(((dwg.double() - da).abs() <= ref.tol(dtype, 1, 2.75) * size).all())
+    assert bool(((dwu.double() - a).abs() <= ref.tol(dtype, 1, 2.75) * a.abs()).all())
