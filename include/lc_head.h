@@ -84,7 +84,8 @@ size_t grad_clip_workspace_bytes(int64_t values, int32_t count);
 int grad_norm(const lc_tensor_t *list, int32_t count, float *norm, void *ws, size_t ws_bytes, void *hip_stream);
 
 /* grad_norm, then every tensor times min(1, max_norm / norm) into its dst.  Where the norm is not finite in 64 bits (a
- * value is infinite or NaN) the factor is 1: norm[0] says so and nothing is spread.  max_norm > 0. */
+ * value is infinite or NaN) the factor is 1: norm[0] says so and nothing is spread.  A finite norm beyond fp32's range clips all
+ * the same, with norm[0] infinite.  max_norm > 0. */
 int grad_clip(const lc_tensor_t *list, int32_t count, float max_norm, float *norm, void *ws, size_t ws_bytes,
               void *hip_stream);
 

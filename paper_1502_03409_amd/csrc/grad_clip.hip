@@ -105,23 +105,32 @@ __global__ __launch_bounds__(256) void norm_kernel(const double *partial, int gr
     if (threadIdx.x == 0) *norm = (float)sqrt(s);
 }
 
-// c = 1 copies: an infinity or NaN stays as it is, bit for bit
+// A factor of 1 copies: an infinity or NaN stays as it is, bit for bit.  Factors below 2^-100, which fp32 would hold with fewer bits or
+// not at all, multiply in 64 bits.
+struct Factor {
+    double whole;
+    float c;
+    bool tiny;
+    __device__ __forceinline__ explicit Factor(double f) : whole(f), c((float)f), tiny(f < 0x1p-100) {}
+    __device__ __forceinline__ float times(float v) const { return tiny ? (float)((double)v * whole) : v * c; }
+};
 template <typename T>
-__device__ __forceinline__ void scale(const T *p, T *o, int n, float c) {
+__device__ __forceinline__ void scale(const T *p, T *o, int n, const Factor &f) {
     constexpr int W = 16 / sizeof(T);
-    const auto one = [&](int i) { o[i] = c == 1.f ? p[i] : narrow<T>(widen<T>(p[i]) * c); };
+    const bool copies = f.c == 1.f;
+    const auto one = [&](int i) { o[i] = copies ? p[i] : narrow<T>(f.times(widen<T>(p[i]))); };
     if (((uintptr_t)p ^ (uintptr_t)o) & 15) {   // no vector is aligned on both sides
         for (int i = threadIdx.x; i < n; i += 256) one(i);
         return;
     }
     walk<W>(n, head_of(p), one, [&](int i) {
         u32x4 a = *(const u32x4 *)(p + i);
-        if (c != 1.f)
+        if (!copies)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const unsigned w = a[e];
-                if constexpr (W == 4) a[e] = __builtin_bit_cast(unsigned, __builtin_bit_cast(float, w) * c);
-                else a[e] = (unsigned)to_bf16(bf16_lo(w) * c) | (unsigned)to_bf16(bf16_hi(w) * c) << 16;
+                if constexpr (W == 4) a[e] = __builtin_bit_cast(unsigned, f.times(__builtin_bit_cast(float, w)));
+                else a[e] = (unsigned)to_bf16(f.times(bf16_lo(w))) | (unsigned)to_bf16(f.times(bf16_hi(w))) << 16;
             }
         *(u32x4 *)(o + i) = a;
     });
@@ -131,14 +140,14 @@ __global__ __launch_bounds__(256) void scale_kernel(Batch t, const double *parti
     const double norm = sqrt(whole_sum(partial, groups));
     if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
     const bool clips = __builtin_isfinite(norm) && norm > (double)max_norm;
-    const float c = clips ? (float)((double)max_norm / norm) : 1.f;
+    const Factor f(clips ? (double)max_norm / norm : 1.0);
     for (int b = t.chunks - 1 - (int)blockIdx.x; b >= 0; b -= gridDim.x) {
         const int k = tensor_of(t, b);
         if (!clips && t.src[k] == t.dst[k]) continue;
         const long long i0 = (long long)(b - t.first[k]) * kChunk;
         const int n = (int)min((long long)kChunk, t.n[k] - i0);
-        if (t.bf16[k]) scale((const bf16_t *)t.src[k] + i0, (bf16_t *)t.dst[k] + i0, n, c);
-        else scale((const float *)t.src[k] + i0, (float *)t.dst[k] + i0, n, c);
+        if (t.bf16[k]) scale((const bf16_t *)t.src[k] + i0, (bf16_t *)t.dst[k] + i0, n, f);
+        else scale((const float *)t.src[k] + i0, (float *)t.dst[k] + i0, n, f);
     }
 }
 

@@ -119,3 +119,19 @@ def test_nothing_beside_the_tensors_is_written():
                 norm = torch.empty(1, device="cuda")
                 lc.grad_clip([t], None, 0.5, norm, scratch([t]))
                 assert bool((buf[:offset] == 3.0).all()) and bool((buf[offset + n:] == 3.0).all()) and bool((t < 0.6).all())
+
+
+@pytest.mark.parametrize("offset", [0, 1])
+@pytest.mark.parametrize("std,max_norm", [(1e36, 1e-3), (1e30, 1e-12), (3e37, 1.0)])
+def test_factors_below_the_range_of_fp32(std, max_norm, offset):
+    """Gradients so large that max_norm over their norm is subnormal in fp32, or so that the norm itself is beyond it: values are clipped
+    to the same bounds as any others."""
+    tensors = make([4500, 50], [F, H], std=std, offset=offset)
+    want = norm64(tensors)
+    norm = torch.empty(1, device="cuda")
+    out = [torch.empty_like(t) for t in tensors]
+    lc.grad_clip(tensors, out, max_norm, norm, scratch(tensors))
+    assert torch.isinf(norm).all() if want > 3.4028235e38 else abs(float(norm) - want) <= 2.0 ** -23 * want
+    for t, o in zip(tensors, out):
+        expect = t.double() * (max_norm / want)
+        assert bool(((o.double() - expect).abs() <= (2.0 ** -8 if o.dtype == H else 2.0 ** -22) * expect.abs()).all())
