@@ -135,3 +135,18 @@ def test_factors_below_the_range_of_fp32(std, max_norm, offset):
     for t, o in zip(tensors, out):
         expect = t.double() * (max_norm / want)
         assert bool(((o.double() - expect).abs() <= (2.0 ** -8 if o.dtype == H else 2.0 ** -22) * expect.abs()).all())
+
+
+# lists of which a workgroup takes several chunks of 4096 values: more than 2048 chunks in one launch, and more in each of three
+# launches than the 682 workgroups that each of them has
+LONG = [([9_000_005], [F]), ([9_000_005], [H]), ([5_000_001, 3, 4_200_000, 70_001], [H, F]), ([25_000 + 11 * i for i in range(300)], [F, H])]
+
+
+@pytest.mark.parametrize("in_place", [False, True], ids=["elsewhere", "in_place"])
+@pytest.mark.parametrize("offset", [0, 3])
+@pytest.mark.parametrize("sizes,kinds", LONG, ids=[str(i) for i in range(len(LONG))])
+def test_lists_of_several_chunks_a_workgroup(sizes, kinds, offset, in_place):
+    tensors = make(sizes, kinds, seed=1, offset=offset)
+    full = norm64(tensors)
+    check(tensors, 0.25 * full, in_place)
+    check(tensors, 2.0 * full, in_place)

@@ -332,3 +332,30 @@ def test_words_that_hardly_count_have_their_gradients(N, dtype):
     worst = float(((dw.double() - rw).abs() / rw.abs())[others].max())
     assert worst <= bound, (worst, bound)
     ref.check("dx", dx, rx, bound)
+
+
+@dtypes
+@pytest.mark.parametrize("N", [5, 70])
+def test_gradients_of_scores_far_apart(N, dtype):
+    """Two groups of words 3000 apart, each with a spread of a few: one product a score, so scores are exact and probabilities those of
+    the upper group, which is another for rows of the other sign."""
+    gen = torch.Generator().manual_seed(15)
+    x = torch.ones(N, 1)
+    x[1::2] = -1
+    w = torch.randn(150, 1, generator=gen) * 2 + 3000 * (torch.rand(150, 1, generator=gen) < 0.5)
+    t = torch.randint(0, 150, (N,), generator=gen)
+    t[2] = -1
+    x, w, t = x.to(dtype).cuda(), w.to(dtype).cuda(), t.cuda()
+    loss, cost, dx, dw = run(x, w, t)
+    rl, rc, rx, rw = ref.xent(x, w, t)
+    # the loss is rounded at its own size, the differences of scores within a group at theirs (below 64)
+    assert bool(((loss.double() - rl).abs() <= 2.0 ** -20 + 2.0 ** -22 * rl).all())
+    assert abs(float(cost) - float(rc)) <= 2.0 ** -20 + 2.0 ** -22 * float(rc)
+    bound = ref.tol(dtype, N, 2.25) + 4 * 2.0 ** -24 * 64
+    ref.check("dw", dw, rw, bound)
+    # dx adds up 150 words of up to 3000 with weights of either sign: its bound is that of the sum of magnitudes
+    live = t >= 0
+    d = torch.softmax(x.double() @ w.double().t(), dim=1) + torch.nn.functional.one_hot(t.clamp(min=0), 150)
+    total = d @ w.double().abs() / int(live.sum())
+    assert bool(((dx.double() - rx).abs() <= (ref.tol(dtype, 150, 2.25) + 4 * 2.0 ** -24 * 64) * total)[live].all())
+    assert not dx[~live].any()
