@@ -72,3 +72,19 @@ def test_infinite_weights_in_gradients_of_fp32():
     ref.check("dx", dx, dg @ wg2.double() + du @ wu.double(), ref.tol(torch.float32, 500, 0))
     ref.check("dwg", dwg, dg.t() @ x2.double(), ref.tol(torch.float32, 140, 0))
     ref.check("dwu", dwu, du.t() @ x2.double(), ref.tol(torch.float32, 140, 0))
+
+
+@G.dtypes
+@pytest.mark.parametrize("N,D,F", [(150, 61952, 70), (20, 93312, 40)])
+def test_features_of_whole_layers(N, D, F, dtype):
+    """As many features as the pooled responses of a layer have, e.g. 44 x 44 places of 32 filters: one long contraction forward, wide
+    gradients."""
+    print(f"case wide glu {N} {D} {F} {dtype}", flush=True)
+    x, wg, wu, dh = G.inputs(N, D, F, dtype, seed=5)
+    h, gu = G.forward(x, wg, wu, "silu")
+    ref.check("h", h, ref.glu(x, wg, wu, "silu")[0], ref.tol(dtype, D, 1))
+    dx, dwg, dwu = G.backward(x, wg, wu, gu, dh, "silu")
+    rx, rwg, rwu = ref.glu_grads(x, wg, wu, dh, "silu")
+    ref.check("dx", dx, rx, ref.tol(dtype, D + 2 * F, 2.75))
+    ref.check("dwg", dwg, rwg, ref.tol(dtype, D + N, 2.75))
+    ref.check("dwu", dwu, rwu, ref.tol(dtype, D + N, 2.75))
