@@ -35,16 +35,17 @@ __device__ __forceinline__ void for_blocks(const Fn &fn) {
 }
 
 // What a product needs besides its operands.  rows_dev (nullable): the rows of A that count, minus first_row, at most M.
-// k_dev (nullable): the same for the contraction.  Both are read on the device.
+// k_dev (nullable): the same for the contraction.  Both are read on the device, and count `times` times.
 struct Shape {
     int M, Nn, K;
     const int *rows_dev;
     int rows_first;
     const int *k_dev;
     int k_first;
+    int times = 1;
 };
-__device__ __forceinline__ int live(int most, const int *dev, int first) {
-    return dev ? max(0, min(most, *dev - first)) : most;
+__device__ __forceinline__ int live(int most, const int *dev, int first, int times = 1) {
+    return dev ? max(0, min(most, times * (*dev - first))) : most;
 }
 
 // Value k of row r of an operand: its planes added up; 0 from k_end on.
@@ -282,8 +283,8 @@ __global__ __launch_bounds__(64 * kWaves, (NA * BM + NB * BN) * 128 > 81920 ? 1 
     constexpr int MT = BM / 64, NT = BN / 64, PAIRS = PL == 3 ? 6 : 1;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int M = live(sh.M, sh.rows_dev, sh.rows_first);
-    const int K = live(sh.K, sh.k_dev, sh.k_first);
+    const int M = live(sh.M, sh.rows_dev, sh.rows_first, sh.times);
+    const int K = live(sh.K, sh.k_dev, sh.k_first, sh.times);
     int tm, tn, split;
     if (!tile_of(blockIdx.x, (M + BM - 1) / BM, nt, splits, &tm, &tn, &split)) return;
     const int wm = wave / 2, wn = wave % 2;
@@ -559,22 +560,33 @@ struct PartEpi {
 };
 
 // Adds the parts up in their order and stores the sums, four columns a thread.  Bound by the latency of the loads where the result
-// is small, so kJoin parts are in flight at a time: 16 parts of 192 x 1024 3.9 us, 6.8 one after the other.
+// is small, so kJoin parts are in flight at a time: 16 parts of 192 x 1024 3.9 us, 6.8 one after the other.  FOLD: the product's rows
+// are the first and then the second planes of half as many; a row that is not finite is that of its first plane (0 times infinity in the
+// second would make it NaN).
 constexpr int kJoin = 8;
-template <typename T>
+template <typename T, bool FOLD>
 __global__ __launch_bounds__(256) void join_parts_kernel(const float *part, long long ld, int splits, Shape sh, StoreEpi<T> epi) {
     const long long id = blockIdx.x * 256LL + threadIdx.x, quads = ld / 4;
     const int m = (int)(id / quads), n = (int)(id - m * quads) * 4;
-    if (m >= sh.M) return;
-    f32x4 s = {0.f, 0.f, 0.f, 0.f}, p[kJoin];
-    for (int i = 0; i < splits; i += kJoin) {
+    const int rows = live(sh.M, sh.rows_dev, sh.rows_first, sh.times) / (FOLD ? 2 : 1);
+    if (m >= rows) return;
+    const auto sum = [&](int row) {
+        f32x4 s = {0.f, 0.f, 0.f, 0.f}, p[kJoin];
+        for (int i = 0; i < splits; i += kJoin) {
 #pragma unroll
-        for (int k = 0; k < kJoin; ++k) p[k] = *(const f32x4 *)(part + ((long long)min(i + k, splits - 1) * sh.M + m) * ld + n);
+            for (int k = 0; k < kJoin; ++k) p[k] = *(const f32x4 *)(part + ((long long)min(i + k, splits - 1) * sh.M + row) * ld + n);
 #pragma unroll
-        for (int k = 0; k < kJoin; ++k)
-            if (i + k < splits) s += p[k];
+            for (int k = 0; k < kJoin; ++k)
+                if (i + k < splits) s += p[k];
+        }
+        return s;
+    };
+    f32x4 s = sum(m);
+    if constexpr (FOLD) {
+        const f32x4 low = sum(rows + m);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[r] += __builtin_isfinite(s[r]) ? low[r] : 0.f;
     }
-    if (m >= live(sh.M, sh.rows_dev, sh.rows_first)) return;
     const int at = epi.place(m);
     if (at < 0) return;
     T *const row = epi.row(m, at);
@@ -643,7 +655,8 @@ int launch_gemm(const char *name, const Operand &A, const Operand &B, const Shap
     return launch_cut<PL, FA, FB>(name, A, B, sh, choose_cut(sh.M, sh.Nn, sh.K, PL == 3 ? 6 : 1, false), epi, s);
 }
 
-// Floats that are enough for the parts of any product of up to M rows and up to K indices: a shorter product may be cut into more parts.
+// Floats that are enough for the parts of any product of up to M rows and up to K indices that is cut: a shorter product may be cut into more
+// parts.
 inline long long part_floats(int M, int Nn, int K) {
     const int most = std::min(kMostSplits, ceil_div(K, kStep) / 2);
     return most > 1 ? std::min(kMostParts, most * M * round_up(Nn, 4)) : 0;
@@ -655,18 +668,18 @@ struct Parts {
     long long floats;
 };
 
-// A product that is stored, cut along its contraction where that helps.
-template <int PL, int FA, int FB, typename T>
+// A product that is stored, cut along its contraction where that helps; FOLD: always through its parts.
+template <int PL, int FA, int FB, bool FOLD = false, typename T>
 int launch_product(const char *name, const Operand &A, const Operand &B, const Shape &sh, const StoreEpi<T> &epi, const Parts &part, hipStream_t s) {
     if (sh.M == 0 || sh.Nn == 0) return LC_OK;
     const Cut c = choose_cut(sh.M, sh.Nn, sh.K, PL == 3 ? 6 : 1, true);
-    if (c.splits == 1) return launch_cut<PL, FA, FB>(name, A, B, sh, c, epi, s);
+    if (!FOLD && c.splits == 1) return launch_cut<PL, FA, FB>(name, A, B, sh, c, epi, s);
     const long long ld = round_up(sh.Nn, 4);
-    const long long blocks = ((long long)sh.M * (ld / 4) + 255) / 256;
+    const long long blocks = ((long long)(FOLD ? sh.M / 2 : sh.M) * (ld / 4) + 255) / 256;
     const LaunchPlan p = make_plan(name, {}, {sh.M, sh.Nn, c.splits}, dim3((unsigned)blocks), 256, 0);
     LC_PLAN_REQUIRE(p, blocks <= 0x7fffffffLL && part.at && c.splits * sh.M * ld <= part.floats);
     if (int rc = launch_cut<PL, FA, FB>(name, A, B, sh, c, PartEpi{part.at, ld, sh.M}, s)) return rc;
-    LC_LAUNCH(p, name, (join_parts_kernel<T>), s, part.at, ld, c.splits, sh, epi);
+    LC_LAUNCH(p, name, (join_parts_kernel<T, FOLD>), s, part.at, ld, c.splits, sh, epi);
     return LC_OK;
 }
 

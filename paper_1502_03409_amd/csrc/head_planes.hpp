@@ -1,6 +1,7 @@
 // Laying out operands: a matrix given by a functor becomes rows of bf16 planes, padded with zeros to whole 16-byte pieces.  Read
 // once, written once, 16 bytes a thread and plane; bound by HBM: 30011 x 768 fp32 values into three planes, 230 MB, 36 us.  The one
-// rounding here is that of a single plane to bf16, for gradients that meet bf16 operands in the matrix unit; three planes lose nothing.
+// rounding here is that of a single plane to bf16, or of two to sixteen bits, for gradients that meet bf16 operands in the matrix unit; three
+// planes lose nothing.
 #pragma once
 #include "head_common.hpp"
 
@@ -13,7 +14,7 @@ __device__ __forceinline__ void put_planes(bf16_t *to, long long plane, const fl
     bf16_t p[8][3];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        if constexpr (PL == 3) split3(v[e], p[e]);
+        if constexpr (PL > 1) split3(v[e], p[e]);
         else p[e][0] = to_bf16(v[e]);
     }
 #pragma unroll
@@ -26,13 +27,15 @@ __device__ __forceinline__ void put_planes(bf16_t *to, long long plane, const fl
 }
 
 // get(r, c, v): v[o][0..7] are columns c .. c + 7 of row r of output o (0 outside the matrix); output o lies `apart` * o columns to
-// the right.  skip(r): rows that nobody reads.  beside(): something small that the first workgroup does as well.
+// the right.  skip(r): rows that nobody reads.  beside(): something small that the first workgroup does as well.  Two planes: the second
+// lies get.rows() rows behind the first, a number that only the device knows.
 template <int PL, int OUT, typename Get>
 __global__ __launch_bounds__(256) void planes_kernel(Get get, bf16_t *dst, long long ld, long long plane, int rows, int pieces, int apart) {
     if (blockIdx.x == 0) get.beside();
     const long long at = blockIdx.x * 256LL + threadIdx.x;
     const int r = (int)(at / pieces), c = (int)(at - (long long)r * pieces) * 8;
     if (r >= rows || get.skip(r)) return;
+    if constexpr (PL == 2) plane = get.rows() * ld;
     float v[OUT][8];
     get(r, c, v);
 #pragma unroll

@@ -12,6 +12,12 @@
 // TFLOP each, bound as large products are.
 //
 // Masked rows take no part: the rows that count are gathered first, and every kernel runs over as many as there are.
+//
+// d meets bf16 operands as bf16, one rounding more than the sums in fp32 would have.  Over many rows that is the rounding of as many numbers;
+// of few rows a few weights of rows decide what is lost (6 rows with weights of their own: 0.28 % of dx and dw, where their own rounding is
+// 0.17 %).  Up to kFewRows rows are therefore kept in two bf16 parts, sixteen bits, all second parts behind all first ones: as twice
+// the rows of dx's product, which its tiles of 128 have room for and whose halves are added up with its parts, and, with x twice as
+// well, as twice the indices of dw's, which its steps of 64 have room for.
 #pragma once
 #include "head_few.hpp"
 #include "head_planes.hpp"
@@ -228,8 +234,9 @@ static __global__ __launch_bounds__(256) void cost_kernel(Rows o, float *cost) {
 
 // The rows that count, gathered as planes; zeros in the masked rows of dx (nullable).  Eight columns a thread; bound by
 // HBM: 8192 rows of 4096 in bf16, 134 MB, 25 us.
+// twice: once more behind all of them.
 template <typename T>
-__global__ __launch_bounds__(256) void gather_kernel(const T *x, bf16_t *dst, T *dx, Rows o, int N, int D, int pieces) {
+__global__ __launch_bounds__(256) void gather_kernel(const T *x, bf16_t *dst, T *dx, Rows o, int N, int D, int pieces, bool twice) {
     constexpr int PL = Planes<T>::N;
     const long long at = blockIdx.x * 256LL + threadIdx.x;
     const int n = (int)(at / pieces), c = (int)(at - (long long)n * pieces) * 8;
@@ -239,6 +246,7 @@ __global__ __launch_bounds__(256) void gather_kernel(const T *x, bf16_t *dst, T 
         float v[8];
         load8(x + (long long)n * D, c, D, v);
         put_planes<PL>(dst + (long long)to * pieces * 8 + c, (long long)N * pieces * 8, v);
+        if (twice) put_planes<PL>(dst + (long long)(*o.count + to) * pieces * 8 + c, 0, v);
     } else if (dx) {
         T *row = dx + (long long)n * D + c;
 #pragma unroll
@@ -268,6 +276,7 @@ struct XentGrad {
         if (cost) write_cost(o, cost);
     }
     __device__ bool skip(int m) const { return m >= live(most, o.count, first); }
+    __device__ long long rows() const { return live(most, o.count, first); }
     __device__ void operator()(int m, int c, float (&v)[1][8]) const {
         const int r = first + m, t = o.target[r];
         const float base = o.base[r], log_sum = o.log_sum[r], s = o.scale[r];
@@ -321,13 +330,15 @@ struct XentScratch {
         rows.dt = sc.take<float>(N);
         rows.loss = sc.take<float>(N);
         const bool laid_out = grads || N > kFewRows;   // the scores of few rows need neither x nor w as planes
-        x = laid_out ? sc.take<bf16_t>((long long)PL * N * Dp) : nullptr;
+        // rows of d's two parts, for any number of rows up to N; x of as many
+        const int twice = PL == 1 && grads ? 2 * std::min(N, kFewRows) : 0;
+        x = laid_out ? sc.take<bf16_t>((long long)Dp * std::max(PL * N, twice)) : nullptr;
         w = direct || !laid_out ? nullptr : sc.take<bf16_t>((long long)PL * V * Dp);
         stats = sc.take<float2>((V + 63) / 64 * (long long)block);   // as for the smaller tiles that fewer rows may take
         if (!grads) return;
-        d = sc.take<bf16_t>((long long)PL * block * Vp);
+        d = sc.take<bf16_t>((long long)Vp * std::max(PL * block, twice));
         scores = PL == 3 ? sc.take<float>((long long)block * Vp) : nullptr;
-        part.floats = std::max(part_floats(block, D, V), part_floats(V, D, block));
+        part.floats = std::max({part_floats(std::max(block, twice), D, V), part_floats(V, D, std::max(block, twice)), twice * round_up(D, 4)});
         part.at = sc.take<float>(part.floats);
         sum = blocks > 1 ? sc.take<float>((long long)V * D) : nullptr;
     }
@@ -350,12 +361,13 @@ int xent(const T *x, const T *w, const int64_t *target, const float *scale, floa
     LC_LAUNCH(one, "xent (rows)", rows_kernel, s, target, scale, loss, N, V, g.rows);
     const long long px = (long long)N * g.Dp, pw = (long long)V * g.Dp;
     const bool few = N <= kFewRows;   // the scores of few rows need neither x nor w laid out
+    const bool fine = few && grads && PL == 1;   // d in two parts
     if (!few || grads) {
         const int pieces = g.Dp / 8;
         const long long blocks = ((long long)N * pieces + 255) / 256;
         const LaunchPlan p = make_plan("xent_gather", {PL}, {N, D}, dim3((unsigned)blocks), 256, 0);
         LC_PLAN_REQUIRE(p, blocks <= 0x7fffffffLL);
-        LC_LAUNCH(p, "xent (x)", (gather_kernel<T>), s, x, g.x, grads ? dx : nullptr, g.rows, N, D, pieces);
+        LC_LAUNCH(p, "xent (x)", (gather_kernel<T>), s, x, g.x, grads ? dx : nullptr, g.rows, N, D, pieces, fine);
     }
     if (!g.direct && (!few || grads))
         if (int rc = launch_planes<PL, 1>("xent (w)", Stored<T>{w, V, D}, g.w, g.Dp, pw, V, g.Dp, 0, s)) return rc;
@@ -385,6 +397,25 @@ int xent(const T *x, const T *w, const int64_t *target, const float *scale, floa
             LC_LAUNCH(p, "xent (logsumexp)", lse_kernel<1>, s, g.stats, (long long)g.block, g.tiles, g.rows, first, most, loss);
         }
         if (!grads) continue;
+        if constexpr (PL == 1)
+            if (fine) {   // one block
+                const int two = 2 * N;
+                if ((rc = launch_planes<2, 1>("xent (d)", XentGrad<T>{keep, g.Vp, g.stats, g.block, g.rows, 0, N, V, g.wave_cols, cost}, g.d, g.Vp, 0, N, g.Vp,
+                                              0, s)))
+                    return rc;
+                Operand d = {g.d, g.d, g.Vp, 0, two, 0, 0};
+                Wc.rows = X.rows = g.Dp;
+                if (dx) {
+                    const Shape shx = {two, D, V, g.rows.count, 0, nullptr, 0, 2};
+                    if ((rc = launch_product<PL, ROW, COL, true>("xent (dx)", d, Wc, shx,
+                                                                 StoreEpi<T>{dx, nullptr, 0x7fffffff, N, 0, D, g.rows.index, nullptr, g.rows.unit}, g.part, s)))
+                        return rc;
+                }
+                const Shape shw = {V, D, two, nullptr, 0, g.rows.count, 0, 2};
+                d.rows = g.Vp;
+                return launch_product<PL, COL, COL>("xent (dw)", d, X, shw, StoreEpi<T>{dw, nullptr, 0x7fffffff, V, 0, D, nullptr, nullptr, g.rows.unit}, g.part,
+                                                    s);
+            }
         const long long pd = (long long)g.block * g.Vp;
         if ((rc = launch_planes<PL, 1>("xent (d)", XentGrad<T>{keep, g.Vp, g.stats, g.block, g.rows, first, most, V, g.wave_cols,
                                                           b + 1 == g.blocks ? cost : nullptr},

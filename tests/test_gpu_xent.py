@@ -359,3 +359,24 @@ def test_gradients_of_scores_far_apart(N, dtype):
     total = d @ w.double().abs() / int(live.sum())
     assert bool(((dx.double() - rx).abs() <= (ref.tol(dtype, 150, 2.25) + 4 * 2.0 ** -24 * 64) * total)[live].all())
     assert not dx[~live].any()
+
+
+@dtypes
+@pytest.mark.parametrize("N", [1, 2, 9, 32])
+@pytest.mark.parametrize("masked", [0.0, 0.5])
+def test_weights_of_few_rows_are_not_rounded(N, masked, dtype):
+    """Rows with a weight half way between two bf16 numbers, the same for all: rounded to either, all gradients were 0.4 % too short or too
+    long.  Against the exact gradient, rounded once: what is off along it is what was off before that rounding, 2^-16 for d in two
+    parts and less for the probabilities' 2^-10 (a hundredth of the gradients' squares).  Results are a number times one of the 128 significands
+    that bf16 has, so those that cross from one bf16 number to the next do so a 128th, or 2^-15 of the gradient, at a time: 2^-11 is sixteen."""
+    D, V = 2000, 250
+    x, w, t = inputs(N, D, V, dtype, seed=16, masked=masked, std=0.5)
+    t[0] = 7
+    scale = torch.full((N,), 1.00390625, device="cuda")
+    loss, cost, dx, dw = run(x, w, t, scale)
+    rl, rc, rx, rw = ref.xent(x, w, t, torch.where(t >= 0, scale, 0.0))
+    for got, want in ((dx, rx), (dw, rw)):
+        along = float(((got.double() - want.to(dtype).double()) * want).sum() / (want * want).sum())
+        assert abs(along) <= (2.0 ** -11 if dtype == torch.bfloat16 else ref.tol(dtype, D, 0)), along
+    check_all(x, w, t, torch.where(t >= 0, scale, 0.0), (loss, cost, dx, dw))
+    assert not dx[t < 0].any()
