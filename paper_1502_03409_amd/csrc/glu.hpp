@@ -2,7 +2,8 @@
 //
 // Forward: a tile of the product covers the same outputs of both weight matrices (blocks of 32 rows of wg and wu alternate), so
 // the activation and the product happen on the accumulators.  Backward: one pass over dh and the saved g, u leaves both
-// gradients side by side, [N][2F], and two products finish: dx = [dg du] [wg; wu] and [dwg; dwu] = [dg du]^T x.
+// gradients side by side, [N][2F], and two products finish: dx = [dg du] [wg; wu] and [dwg; dwu] = [dg du]^T x.  bf16 operands: rounded to bf16,
+// up to kFewRows rows in two parts (as in xent.hpp; 1 row of 64 -> 64 was off by 0.26 %, where the results' own rounding is 0.17 %).
 //
 // 8192 x 4096 -> 8192 in bf16: forward 0.94 ms, the gradients' pass 0.12, dx 0.87, dw 0.94; each product is 1.1 TFLOP, bound as large
 // products are.  192 rows: 39 us, the 134 MB of weights come at 3.4 TB/s.  1537 x 1021 -> 2055 in fp32: 0.37 ms for all.
@@ -135,7 +136,8 @@ struct GluEpi {
 template <typename T, int ACT>
 struct GluGrad {
     const T *dh, *gu;
-    int F;
+    int F, N;
+    __device__ long long rows() const { return N; }
     __device__ void beside() const {}
     __device__ bool skip(int) const { return false; }
     __device__ void operator()(int r, int c, float (&v)[2][8]) const {
@@ -204,9 +206,11 @@ struct GluScratch {
         // few rows: the forward pass takes everything where it is
         x = sc.take<bf16_t>(direct || (N <= kFewRows && !backward) ? 8 : PL * ((long long)N + 2LL * F) * Dp);
         w = x ? x + (long long)N * Dp : nullptr;   // behind x in each plane, so that one launch lays all three out
-        d = backward ? sc.take<bf16_t>((long long)PL * N * 2 * Fp) : nullptr;
+        // rows of the gradients' two parts, for any number of rows up to N
+        const int twice = PL == 1 && backward ? 2 * std::min(N, kFewRows) : 0;
+        d = backward ? sc.take<bf16_t>(2LL * Fp * std::max(PL * N, twice)) : nullptr;
         if (!backward) return;
-        part.floats = std::max(part_floats(N, D, Fp + F), part_floats(2 * Fp, D, N));
+        part.floats = std::max({part_floats(std::max(N, twice), D, Fp + F), part_floats(2 * Fp, D, N), twice * round_up(D, 4)});
         part.at = sc.take<float>(part.floats);
     }
     // x and both weights as operands: laid out first unless they are where they can be used
@@ -251,8 +255,24 @@ int glu_backward(const T *x, const T *wg, const T *wu, const T *gu, const T *dh,
     if (int rc = g.operands(x, wg, wu, N, D, F, &X, &W, s)) return rc;
     const int F2 = 2 * g.Fp;
     const long long pd = (long long)N * F2;
+    if constexpr (PL == 1)
+        if (N <= kFewRows) {
+            const int two = 2 * N;
+            if (int rc = launch_planes<2, 2>("glu_bwd (gradients)", GluGrad<T, ACT>{dh, gu, F, N}, g.d, F2, 0, N, g.Fp, g.Fp, s)) return rc;
+            Operand d = {g.d, g.d, F2, 0, two, 0, 0};
+            if (dx) {
+                W.depth = F, W.half = g.Fp, W.rows = g.Dp;
+                const Shape sh = {two, D, g.Fp + F, nullptr, 0, nullptr, 0};
+                if (int rc = launch_product<PL, ROW, COLPAIR, true>("glu_bwd (dx)", d, W, sh,
+                                                                    StoreEpi<T>{dx, nullptr, 0x7fffffff, N, 0, D, nullptr, nullptr, nullptr}, g.part, s))
+                    return rc;
+            }
+            d.rows = F2, X.rows = g.Dp;
+            const Shape sh = {F2, D, two, nullptr, 0, nullptr, 0};
+            return launch_gemm<2, COL, COL>("glu_bwd (dw)", d, X, sh, StoreEpi<T>{dwg, dwu, g.Fp, F, F, D, nullptr, nullptr, nullptr}, s);
+        }
     const Operand dgu = {g.d, g.d, F2, pd, N, 0, 0};
-    if (int rc = launch_planes<PL, 2>("glu_bwd (gradients)", GluGrad<T, ACT>{dh, gu, F}, g.d, F2, pd, N, g.Fp, g.Fp, s)) return rc;
+    if (int rc = launch_planes<PL, 2>("glu_bwd (gradients)", GluGrad<T, ACT>{dh, gu, F, N}, g.d, F2, pd, N, g.Fp, g.Fp, s)) return rc;
     if (dx) {
         W.depth = F, W.half = g.Fp, W.rows = g.Dp;
         const Shape sh = {N, D, g.Fp + F, nullptr, 0, nullptr, 0};

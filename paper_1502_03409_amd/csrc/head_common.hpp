@@ -42,6 +42,16 @@ __device__ __forceinline__ void split3(float v, bf16_t (&p)[3]) {
     p[2] = to_bf16(r);
 }
 
+// Two bf16 parts of an fp32 value, sixteen bits.  Both have its sign and neither is zero unless the value is (the second is 2^-24 of a
+// value that the first has whole), so that times infinity they add up to infinity and not to NaN.
+__device__ __forceinline__ void split2(float v, bf16_t (&p)[3]) {
+    const unsigned u = __builtin_bit_cast(unsigned, v);
+    p[0] = (bf16_t)(u >> 16);
+    const float r = v - from_bf16(p[0]);
+    p[1] = to_bf16(r != 0.f ? r : v * 0x1p-24f);
+    if ((u & 0x7f800000u) == 0x7f800000u) p[0] = p[1] = (bf16_t)((u >> 16) | ((u & 0xffffu) ? 0x40u : 0u));   // a NaN stays one
+}
+
 // Number of bf16 planes that hold an operand of storage type T, and of plane pairs whose products count.
 template <typename T> struct Planes;
 template <> struct Planes<bf16_t> { static constexpr int N = 1, PAIRS = 1; };

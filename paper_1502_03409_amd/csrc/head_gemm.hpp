@@ -9,6 +9,9 @@
 // operand is infinite or NaN, or a sum overflowed on the way) forms its tile again with the fp32 instruction: planes add up to the
 // operand exactly.
 //
+// PL 2: one plane each, but A, by columns, is the second part of each value behind all first ones, along the contraction, and B's indices come
+// twice; all of it within one step.
+//
 // Large products are bound by the matrix unit, by waits for the operand with two buffers and by the clock that the chip's power allows:
 // 1.13 to 1.22 PFLOP/s in the three of 7373 x 128000 x 4096, with the unit busy 62 to 68 % of the cycles at 1.7 GHz and waves waiting
 // in 21 to 24 % (the library's plain products of these sizes reach 1.3 to 1.6).
@@ -154,7 +157,8 @@ struct Stager {
     unsigned ld2, planes;                      // planes of the six products, the next one's lowest
     int wave, lane, K, depth, half, kt, pair;
     bool trimmed;
-    __device__ __forceinline__ void init(const Operand &o, int r0, int kt_, int K_, unsigned planes_, int wave_, int lane_) {
+    // again: 0, or the indices that are there, which come twice within the one step (by columns)
+    __device__ __forceinline__ void init(const Operand &o, int r0, int kt_, int K_, unsigned planes_, int wave_, int lane_, int again = 0) {
         wave = wave_, lane = lane_, K = K_, kt = kt_, pair = 0, planes = planes_, at = 0;
         const long long ld = o.ld * 2;
         ld2 = (unsigned)ld, plane = o.plane * 2;
@@ -168,7 +172,8 @@ struct Stager {
             if constexpr (COLS) {
                 const int pc = lane % (N / 8);
                 const int c = ((pc / 4) ^ col_swizzle<N>(first_k(q))) * 4 + pc % 4;
-                off[q] = (unsigned)first_k(q) * ld2 + (unsigned)(min(r0 + 8 * c, o.rows - 8) - r0) * 2;
+                const int k = first_k(q) >= again && first_k(q) < 2 * again ? first_k(q) - again : first_k(q);
+                off[q] = (unsigned)k * ld2 + (unsigned)(min(r0 + 8 * c, o.rows - 8) - r0) * 2;
             } else {
                 int f = r0 + 8 * (q * kWaves + wave), s;
                 if constexpr (FORM == PAIR) f = pair_row(f, 32, &s);
@@ -302,7 +307,7 @@ __global__ __launch_bounds__(64 * kWaves, (NA * BM + NB * BN) * 128 > 81920 ? 1 
     Stager<FB, BN, PL> sb;
     // planes of A and B in the six products: 00 10 01 11 02 20
     sa.init(A, tm * BM, kt0, K, 0x201010, wave, lane);
-    sb.init(B, tn * BN, kt0, K, 0x021100, wave, lane);
+    sb.init(B, tn * BN, kt0, K, 0x021100, wave, lane, PL == 2 ? K / 2 : 0);
     constexpr int QA = Stager<FA, BM, PL>::Q, QB = Stager<FB, BN, PL>::Q;
     const unsigned lds_wave = lds0 + wave * 1024;
     auto load_a = [&](unsigned buffer, auto number) __attribute__((always_inline)) { sa.template load<decltype(number)::value>(lds_wave + buffer); };
@@ -424,6 +429,7 @@ int launch_tiles(const char *name, const Operand &A, const Operand &B, const Sha
     constexpr bool CA = FA == COL || FA == COLPAIR, CB = FB == COL || FB == COLPAIR;
     LC_PLAN_REQUIRE(p, CA ? A.rows % 8 == 0 && A.ld >= A.rows && A.rows >= sh.M : A.rows >= sh.M && A.ld >= sh.K);
     LC_PLAN_REQUIRE(p, CB ? B.rows % 8 == 0 && B.ld >= B.rows && B.rows >= sh.Nn : B.rows >= (FB == PAIR ? 1 : sh.Nn) && B.ld >= sh.K);
+    LC_PLAN_REQUIRE(p, PL != 2 || (FA == COL && FB == COL && splits == 1 && sh.K <= kStep && sh.K % 2 == 0));
     LC_PLAN_REQUIRE(p, FA != PAIR && FA != COLPAIR && (FB != PAIR || sh.Nn == 64 * ceil_div(B.rows, 32)));
     LC_PLAN_REQUIRE(p, FB != COLPAIR || (B.half % kStep == 0 && B.depth >= 1 && B.half - B.depth < kStep && B.depth <= B.half &&
                                          sh.K == B.half + B.depth));
@@ -561,8 +567,7 @@ struct PartEpi {
 
 // Adds the parts up in their order and stores the sums, four columns a thread.  Bound by the latency of the loads where the result
 // is small, so kJoin parts are in flight at a time: 16 parts of 192 x 1024 3.9 us, 6.8 one after the other.  FOLD: the product's rows
-// are the first and then the second planes of half as many; a row that is not finite is that of its first plane (0 times infinity in the
-// second would make it NaN).
+// are the first and then the second parts of half as many.
 constexpr int kJoin = 8;
 template <typename T, bool FOLD>
 __global__ __launch_bounds__(256) void join_parts_kernel(const float *part, long long ld, int splits, Shape sh, StoreEpi<T> epi) {
@@ -582,11 +587,7 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const float *part, long
         return s;
     };
     f32x4 s = sum(m);
-    if constexpr (FOLD) {
-        const f32x4 low = sum(rows + m);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) s[r] += __builtin_isfinite(s[r]) ? low[r] : 0.f;
-    }
+    if constexpr (FOLD) s += sum(rows + m);
     const int at = epi.place(m);
     if (at < 0) return;
     T *const row = epi.row(m, at);

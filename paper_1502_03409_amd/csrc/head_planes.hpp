@@ -14,7 +14,8 @@ __device__ __forceinline__ void put_planes(bf16_t *to, long long plane, const fl
     bf16_t p[8][3];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        if constexpr (PL > 1) split3(v[e], p[e]);
+        if constexpr (PL == 3) split3(v[e], p[e]);
+        else if constexpr (PL == 2) split2(v[e], p[e]);
         else p[e][0] = to_bf16(v[e]);
     }
 #pragma unroll
@@ -28,7 +29,7 @@ __device__ __forceinline__ void put_planes(bf16_t *to, long long plane, const fl
 
 // get(r, c, v): v[o][0..7] are columns c .. c + 7 of row r of output o (0 outside the matrix); output o lies `apart` * o columns to
 // the right.  skip(r): rows that nobody reads.  beside(): something small that the first workgroup does as well.  Two planes: the second
-// lies get.rows() rows behind the first, a number that only the device knows.
+// lies get.rows() rows behind the first, a number that the device may know alone.
 template <int PL, int OUT, typename Get>
 __global__ __launch_bounds__(256) void planes_kernel(Get get, bf16_t *dst, long long ld, long long plane, int rows, int pieces, int apart) {
     if (blockIdx.x == 0) get.beside();

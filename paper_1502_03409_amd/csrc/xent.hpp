@@ -16,8 +16,8 @@
 // d meets bf16 operands as bf16, one rounding more than the sums in fp32 would have.  Over many rows that is the rounding of as many numbers;
 // of few rows a few weights of rows decide what is lost (6 rows with weights of their own: 0.28 % of dx and dw, where their own rounding is
 // 0.17 %).  Up to kFewRows rows are therefore kept in two bf16 parts, sixteen bits, all second parts behind all first ones: as twice
-// the rows of dx's product, which its tiles of 128 have room for and whose halves are added up with its parts, and, with x twice as
-// well, as twice the indices of dw's, which its steps of 64 have room for.
+// the rows of dx's product, which its tiles of 128 have room for and whose halves are added up with its parts, and as twice the indices
+// of dw's, which its steps of 64 have room for.
 #pragma once
 #include "head_few.hpp"
 #include "head_planes.hpp"
@@ -234,9 +234,8 @@ static __global__ __launch_bounds__(256) void cost_kernel(Rows o, float *cost) {
 
 // The rows that count, gathered as planes; zeros in the masked rows of dx (nullable).  Eight columns a thread; bound by
 // HBM: 8192 rows of 4096 in bf16, 134 MB, 25 us.
-// twice: once more behind all of them.
 template <typename T>
-__global__ __launch_bounds__(256) void gather_kernel(const T *x, bf16_t *dst, T *dx, Rows o, int N, int D, int pieces, bool twice) {
+__global__ __launch_bounds__(256) void gather_kernel(const T *x, bf16_t *dst, T *dx, Rows o, int N, int D, int pieces) {
     constexpr int PL = Planes<T>::N;
     const long long at = blockIdx.x * 256LL + threadIdx.x;
     const int n = (int)(at / pieces), c = (int)(at - (long long)n * pieces) * 8;
@@ -246,7 +245,6 @@ __global__ __launch_bounds__(256) void gather_kernel(const T *x, bf16_t *dst, T 
         float v[8];
         load8(x + (long long)n * D, c, D, v);
         put_planes<PL>(dst + (long long)to * pieces * 8 + c, (long long)N * pieces * 8, v);
-        if (twice) put_planes<PL>(dst + (long long)(*o.count + to) * pieces * 8 + c, 0, v);
     } else if (dx) {
         T *row = dx + (long long)n * D + c;
 #pragma unroll
@@ -330,15 +328,15 @@ struct XentScratch {
         rows.dt = sc.take<float>(N);
         rows.loss = sc.take<float>(N);
         const bool laid_out = grads || N > kFewRows;   // the scores of few rows need neither x nor w as planes
-        // rows of d's two parts, for any number of rows up to N; x of as many
+        // rows of d's two parts, for any number of rows up to N
         const int twice = PL == 1 && grads ? 2 * std::min(N, kFewRows) : 0;
-        x = laid_out ? sc.take<bf16_t>((long long)Dp * std::max(PL * N, twice)) : nullptr;
+        x = laid_out ? sc.take<bf16_t>((long long)PL * N * Dp) : nullptr;
         w = direct || !laid_out ? nullptr : sc.take<bf16_t>((long long)PL * V * Dp);
         stats = sc.take<float2>((V + 63) / 64 * (long long)block);   // as for the smaller tiles that fewer rows may take
         if (!grads) return;
         d = sc.take<bf16_t>((long long)Vp * std::max(PL * block, twice));
         scores = PL == 3 ? sc.take<float>((long long)block * Vp) : nullptr;
-        part.floats = std::max({part_floats(std::max(block, twice), D, V), part_floats(V, D, std::max(block, twice)), twice * round_up(D, 4)});
+        part.floats = std::max({part_floats(std::max(block, twice), D, V), part_floats(V, D, block), twice * round_up(D, 4)});
         part.at = sc.take<float>(part.floats);
         sum = blocks > 1 ? sc.take<float>((long long)V * D) : nullptr;
     }
@@ -367,7 +365,7 @@ int xent(const T *x, const T *w, const int64_t *target, const float *scale, floa
         const long long blocks = ((long long)N * pieces + 255) / 256;
         const LaunchPlan p = make_plan("xent_gather", {PL}, {N, D}, dim3((unsigned)blocks), 256, 0);
         LC_PLAN_REQUIRE(p, blocks <= 0x7fffffffLL);
-        LC_LAUNCH(p, "xent (x)", (gather_kernel<T>), s, x, g.x, grads ? dx : nullptr, g.rows, N, D, pieces, fine);
+        LC_LAUNCH(p, "xent (x)", (gather_kernel<T>), s, x, g.x, grads ? dx : nullptr, g.rows, N, D, pieces);
     }
     if (!g.direct && (!few || grads))
         if (int rc = launch_planes<PL, 1>("xent (w)", Stored<T>{w, V, D}, g.w, g.Dp, pw, V, g.Dp, 0, s)) return rc;
@@ -413,8 +411,7 @@ int xent(const T *x, const T *w, const int64_t *target, const float *scale, floa
                 }
                 const Shape shw = {V, D, two, nullptr, 0, g.rows.count, 0, 2};
                 d.rows = g.Vp;
-                return launch_product<PL, COL, COL>("xent (dw)", d, X, shw, StoreEpi<T>{dw, nullptr, 0x7fffffff, V, 0, D, nullptr, nullptr, g.rows.unit}, g.part,
-                                                    s);
+                return launch_gemm<2, COL, COL>("xent (dw)", d, X, shw, StoreEpi<T>{dw, nullptr, 0x7fffffff, V, 0, D, nullptr, nullptr, g.rows.unit}, s);
             }
         const long long pd = (long long)g.block * g.Vp;
         if ((rc = launch_planes<PL, 1>("xent (d)", XentGrad<T>{keep, g.Vp, g.stats, g.block, g.rows, first, most, V, g.wave_cols,

@@ -235,3 +235,43 @@ def test_gates_that_are_open_wide_or_shut(name, dtype):
     size = da.abs() if name == "sigmoid" else torch.sigmoid(g.double()) * torch.maximum(torch.ones_like(g), (g * rest).abs())
     assert bool(((dwg.double() - da).abs() <= ref.tol(dtype, 1, 2.75) * size).all())
     assert bool(((dwu.double() - a).abs() <= ref.tol(dtype, 1, 2.75) * a.abs()).all())
+
+
+@dtypes
+@pytest.mark.parametrize("N", [1, 2, 9, 32])
+def test_gradients_of_few_rows_are_not_rounded(N, dtype):
+    """All dg the same and half way between two bf16 numbers (u = 3/2, dh = 1 + 2^-7, act' = 1/4): rounded to either, the gradient of wg
+    was 0.26 % too short or too long.  Against the exact gradient, rounded once; the bound is that of 16 crossings of one significand of
+    128 from one bf16 number to the next, each 2^-15 of the gradient, where 2^-16 of it is left of d in two parts."""
+    D, F = 2000, 70
+    gen = torch.Generator().manual_seed(8)
+    x = torch.randn(N, D, generator=gen)
+    x[:, 0] = 1.0
+    wg, wu = torch.zeros(F, D), torch.zeros(F, D)
+    wu[:, 0] = 1.5
+    dh = torch.full((N, F), 1.0078125)
+    x, wg, wu, dh = (t.to(dtype).cuda() for t in (x, wg, wu, dh))
+    _, gu = forward(x, wg, wu, "sigmoid")
+    dx, dwg, dwu = backward(x, wg, wu, gu, dh, "sigmoid")
+    rx, rwg, rwu = ref.glu_grads(x, wg, wu, dh, "sigmoid")
+    for what, got, want in (("dwg", dwg, rwg), ("dwu", dwu, rwu)):
+        along = float(((got.double() - want.to(dtype).double()) * want).sum() / (want * want).sum())
+        assert abs(along) <= (2.0 ** -11 if dtype == torch.bfloat16 else ref.tol(dtype, D, 0)), (what, along)
+    ref.check("dx", dx, rx, ref.tol(dtype, D + 2 * F, 2.75))
+
+
+@dtypes
+@pytest.mark.parametrize("N", [3, 32, 33])
+def test_infinities_in_gradients_of_few_rows(N, dtype):
+    """An infinite feature, an infinite weight and an infinite gradient: infinities and NaN where the formulas have them, nothing else."""
+    x, wg, wu, dh = inputs(N, 96, 200, dtype, seed=9)
+    _, gu = forward(x, wg, wu, "silu")
+    x[1, 11], wg[3, 5], dh[2, 7] = float("inf"), float("-inf"), float("inf")
+    dx, dwg, dwu = backward(x, wg, wu, gu, dh, "silu")
+    g, u = saved(gu[:, 0]), saved(gu[:, 1])
+    a, da = ref.act("silu", g)
+    dg, du = dh.double() * u * da, dh.double() * a
+    bound = ref.tol(dtype, 500, 2.75)
+    ref.check("dx", dx, dg @ wg.double() + du @ wu.double(), bound)
+    ref.check("dwg", dwg, dg.t() @ x.double(), bound)
+    ref.check("dwu", dwu, du.t() @ x.double(), bound)
