@@ -10,6 +10,10 @@
  *  - Matrices are row-major and contiguous.  Weights are [outputs][inputs], one output's weights contiguous.
  *  - `dtype` is the type of every matrix of a call, results and gradients included: each is an operand of the next
  *    call.  Sums are formed in fp32 and rounded once.  Losses, costs and norms are fp32.
+ *  - With bf16 operands three numbers inside a call are rounded as well.  g and u are kept for glu_bwd in 16 bits (see
+ *    glu_fwd), the softmax's exponentials in ten significant bits; and dg, du and the softmax's d meet the bf16 operands of
+ *    the last products as bf16, for up to 32 rows as sixteen bits, because the roundings of few numbers do not average out.
+ *  - Widths D, F and V are 1 to 2^20, N is 0 to 2^24 (LC_EINVAL otherwise).
  *  - A batch may have no rows (N = 0): weight gradients and costs are then zero; matrices without rows may be NULL.
  *  - Results do not depend on the workspace's contents and are the same bit for bit from call to call.
  *  - fp32 products are formed from three bf16 parts of each operand, which hold all of its bits down to 2^-133 (what an
@@ -48,7 +52,8 @@ int glu_bwd(const void *x, const void *wg, const void *wu, const void *gu, const
 
 /* Host only.  Scratch for xent_fwd (grads = 0) or xent_fwd_bwd (grads = 1); 0 for invalid arguments.  What is enough for N
  * rows is enough for fewer, with gradients also for the loss alone.  It holds no
- * [N][V] array without bound: the exponentials of at most 2 GiB worth of rows at a time with gradients, none without. */
+ * [N][V] array without bound: with gradients what is kept of at most 2 GiB worth of rows at a time (fp32: of their scores,
+ * with another 3 GiB of planes), none without. */
 size_t xent_workspace_bytes(int32_t N, int32_t D, int32_t V, int dtype, int grads);
 
 /* Softmax cross entropy over a vocabulary of V words, projection included:

@@ -5,8 +5,8 @@
 // gradients side by side, [N][2F], and two products finish: dx = [dg du] [wg; wu] and [dwg; dwu] = [dg du]^T x.  bf16 operands: rounded to bf16,
 // up to kFewRows rows in two parts (as in xent.hpp; 1 row of 64 -> 64 was off by 0.26 %, where the results' own rounding is 0.17 %).
 //
-// 8192 x 4096 -> 8192 in bf16: forward 0.94 ms, the gradients' pass 0.12, dx 0.87, dw 0.94; each product is 1.1 TFLOP, bound as large
-// products are.  192 rows: 39 us, the 134 MB of weights come at 3.4 TB/s.  1537 x 1021 -> 2055 in fp32: 0.37 ms for all.
+// 8192 x 4096 -> 8192 in bf16: forward 0.93 to 0.95 ms, the gradients' pass 0.12, dx 0.87 to 0.94, dw 0.97 to 0.99; each product is 1.1 TFLOP,
+// bound as large products are.  192 rows: 40 us, the 134 MB of weights come at 3.4 TB/s.  1537 x 1021 -> 2055 in fp32: 0.37 ms for all.
 #pragma once
 #include "head_few.hpp"
 #include "head_planes.hpp"

@@ -7,7 +7,7 @@
 // sum, and each workgroup of the second pass adds all of them up again in the same order instead of waiting for a kernel that does it
 // once.
 //
-// 10^5 values in three tensors 12 us, two launches; 5 10^7 in 60 tensors of both types, 172 MB, most of which the second pass finds in the
+// 10^5 values in three tensors 13 us, two launches; 5 10^7 in 60 tensors of both types, 172 MB, most of which the second pass finds in the
 // 256 MB behind the L2 caches, 107 us; 10^9 values, which move 11.7 GB over both passes, 2.1 ms: 5.6 TB/s.
 #include "head_common.hpp"
 

@@ -25,8 +25,9 @@ template <typename T> __device__ __forceinline__ T narrow(float v);
 template <> __device__ __forceinline__ float narrow<float>(float v) { return v; }
 template <> __device__ __forceinline__ bf16_t narrow<bf16_t>(float v) { return to_bf16(v); }
 
-// The three bf16 parts of an fp32 value: v = p[0] + p[1] + p[2] exactly, down to bits of 2^-133, the smallest that bf16 has.  Each part is the nearest bf16 to what remains, so the remainders have eight bits less each time; the first part of
-// a value that would round to infinity is cut instead.  An infinity or NaN is its own first part, the others zero.
+// The three bf16 parts of an fp32 value: v = p[0] + p[1] + p[2] exactly, down to bits of 2^-133, the smallest that bf16 has.  Each part is the
+// nearest bf16 to what remains, so the remainders have eight bits less each time; the first part of a value that would round to infinity is
+// cut instead.  An infinity or NaN is its own first part, the others zero.
 __device__ __forceinline__ void split3(float v, bf16_t (&p)[3]) {
     const unsigned u = __builtin_bit_cast(unsigned, v);
     if ((u & 0x7f800000u) == 0x7f800000u) {

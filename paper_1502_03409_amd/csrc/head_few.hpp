@@ -1,8 +1,8 @@
 // Products with at most 32 rows on the left (answers for a few images): the weights stream by once, from HBM to registers.
 //
 // Two kernels.  Where rows begin at 16-byte boundaries the weights pass through LDS, because whole lines can go there directly; rows
-// of any other alignment go straight to registers.  In both, a workgroup owns NB blocks of 32 columns of the result; its four waves take turns along the contraction, 64 indices (whole lines of the
-// weights) at a time, and add up through LDS.  Bound by HBM: what matters is how many loads are in flight, so each wave asks for its next
+// of any other alignment go straight to registers.  In both, a workgroup owns NB blocks of 32 columns of the result; its four waves take
+// turns along the contraction, 64 indices (whole lines of the weights) at a time, and add up through LDS.  Bound by HBM: what matters is how many loads are in flight, so each wave asks for its next
 // 16 vectors of weights before it uses the last ones.  A pair of matrices shares a block, 16 rows of each in turn, so that a
 // small layer can be cut into single blocks.  fp32 operands meet the fp32 matrix instruction, as they are: it keeps up with
 // HBM here, and needs no planes.

@@ -13,8 +13,10 @@
 // twice; all of it within one step.
 //
 // Large products are bound by the matrix unit, by waits for the operand with two buffers and by the clock that the chip's power allows:
-// 1.13 to 1.22 PFLOP/s in the three of 7373 x 128000 x 4096, with the unit busy 62 to 68 % of the cycles at 1.7 GHz and waves waiting
-// in 21 to 24 % (the library's plain products of these sizes reach 1.3 to 1.6).
+// 1.13 to 1.23 PFLOP/s in the three of 7373 x 128000 x 4096, with the unit busy 62 to 67 % of the cycles at 1.7 to 1.8 GHz and waves waiting
+// in 20 to 24 % (the library's plain products of these sizes reach 1.3 to 1.6).  What follows a 256 x 256 tile's loop overlaps nothing, as its
+// workgroup is alone on its compute unit, and is long: the gated forward kernels have 103 to 140 KB of code, beyond the instruction cache, and
+// those that store bf16 gradients keep 208 registers in scratch memory on the way.  The loops themselves have no spills.
 // In fp32 six products make one: 143 TFLOP/s of fp32 in 700 x 30011 x 768, where the unit of 128 x 128 tiles is busy 46 % and waves wait in
 // 30 % of the cycles; an order of the six that takes seven tiles from the L2 caches, not twelve, gained 4 % in a loop over all six and lost
 // 30 % to that loop's length.
@@ -106,8 +108,8 @@ __device__ __forceinline__ bool all_finite(const f32x16 (&acc)[MT][NT], int rows
     return __all(ok);
 }
 
-// Tile order: rows that do not count have no tiles (their workgroups are the last ones); groups of kGroup tiles along m share their tiles along n, and an XCD walks a contiguous range, so that the
-// workgroups that run at once on one XCD share operand rows in its L2.
+// Tile order: rows that do not count have no tiles (their workgroups are the last ones); groups of kGroup tiles along m share their tiles
+// along n, and an XCD walks a contiguous range, so that the workgroups that run at once on one XCD share operand rows in its L2.
 constexpr int kGroup = 8;
 __device__ __forceinline__ bool tile_of(int wg, int mt, int nt, int splits, int *tm, int *tn, int *split) {
     if (wg >= mt * nt * splits) return false;

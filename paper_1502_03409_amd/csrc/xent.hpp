@@ -8,8 +8,8 @@
 // fp32: a quarter of the rounding to bf16 that follows, and no word is too rare; fp32: the scores), for a bounded number of rows at a
 // time; one pass turns them into d[n][v] = s[n] (p[n][v] - [v = t]) in place, and two products give dx = d w and dw = d^T x.
 //
-// 8192 rows of 4096 over 128000 words in bf16, a tenth masked: scores 6.4 ms, statistics 0.02, d 0.74, dx 6.3, dw 6.5; three products of 7.7
-// TFLOP each, bound as large products are.
+// 8192 rows of 4096 over 128000 words in bf16, a tenth masked: scores 6.5 to 6.7 ms, statistics 0.03, d 0.76, dx 6.3 to 6.5, dw 6.6 to 6.8;
+// three products of 7.7 TFLOP each, bound as large products are.
 //
 // Masked rows take no part: the rows that count are gathered first, and every kernel runs over as many as there are.
 //
@@ -163,7 +163,7 @@ struct XentEpi {
 
 // Joins the tiles of R rows: 256 / R threads a row, each over its share of the tiles, in a fixed order.  16 rows read whole lines of
 // the statistics; with few rows the share of a thread matters more (one row of 1563 tiles: 4 instead of 38 us).  Bound by latency: 5 us for
-// 192 rows of 313 tiles, 24 for 8192 rows of 1000.
+// 192 rows of 313 tiles, 25 for 8192 rows of 1000.
 template <int R>
 static __global__ __launch_bounds__(256) void lse_kernel(const float2 *stats, long long stats_ld, int tiles, Rows o, int first, int most,
                                                   float *loss) {
@@ -260,7 +260,7 @@ __global__ __launch_bounds__(256) void zero_kernel(T *p, long long n, float *cos
 }
 
 // d[m][v] of the rows first .. of the block (bf16: over the exponentials themselves).  Bound by HBM: 7400 x 128000 in bf16 move 3.8 GB in
-// 0.74 ms.
+// 0.76 ms.
 template <typename T>
 struct XentGrad {
     const typename Kept<T>::V *keep;

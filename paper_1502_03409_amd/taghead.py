@@ -3,8 +3,9 @@
     features [N, D] -> gated hidden layer [N, F] -> scores of V tags -> softmax cross entropy
     gradients of all three weight matrices -> clipped by their common norm -> one step of gradient descent
 
-The features are those of a trained, frozen layer (`features`: forward pass, pooling, contrast normalisation), so no gradient
-reaches them.  All memory is allocated when the head is made, for a largest batch; a step only enqueues work on the current
+The features are those of a trained, frozen layer (`features`: forward pass, pooling, contrast normalisation, in fp32; a head
+of bf16 weights takes them cast to bf16), so no gradient reaches them.  What a head answers is a loss: of the tags given to
+`evaluate`, row by row.  All memory is allocated when the head is made, for a largest batch; a step only enqueues work on the current
 stream.  ``python -m paper_1502_03409_amd.taghead`` trains one on synthetic images and prints its cost.
 """
 from __future__ import annotations
