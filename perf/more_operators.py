@@ -102,7 +102,8 @@ def draw(rng):
 # ------------------------------------------------------------------------------------------------------------ inputs
 def _to_8_bits(w):
     """Rows of 8-bit whole numbers, padded with zeros to whole blocks of 128, and the value of one for each row."""
-    scale = (w.abs().amax(dim=1) / 127.0).clamp(min=2.0 ** -126)
+    scale = w.abs().amax(dim=1)
+    scale = (scale / torch.full_like(scale, 127.0)).clamp(min=2.0 ** -126)
     q = torch.zeros((w.shape[0], -(-w.shape[1] // 128) * 128), dtype=torch.int8, device=w.device)
     q[:, :w.shape[1]] = torch.round(w / scale[:, None]).clamp(-127, 127).to(torch.int8)
     return q, scale
@@ -212,7 +213,9 @@ def _plain_muon(c, s):
 
 def _plain_q8(c, s):
     x = s["x"].float()
-    scale = (x.abs().amax(dim=1, keepdim=True) / 127.0).clamp(min=2.0 ** -126)
+    scale = x.abs().amax(dim=1, keepdim=True)
+    # by a tensor: by a number, a multiplication with its rounded reciprocal would take the division's place
+    scale = (scale / torch.full_like(scale, 127.0)).clamp(min=2.0 ** -126)
     # halves are told from their neighbours in 64 bits
     q = torch.round(x.double() / scale.double()).clamp(-127, 127).float()
     y = [(q @ s["q" + k][:, :c["D"]].float().t()) * scale * s["s" + k] for k in ("a", "b") if "q" + k in s]
@@ -312,7 +315,8 @@ def exact(case, seed):
             out["dx"], out["dw"] = torch.autograd.grad(cost, (x, w))
         return out
     x = s["x"].double()
-    scale = torch.clamp((s["x"].float().abs().amax(dim=1) / 127.0).double(), min=2.0 ** -126)
+    amax = x.abs().amax(dim=1)
+    scale = torch.clamp((amax / torch.full_like(amax, 127.0)).float().double(), min=2.0 ** -126)
     q = torch.clamp(torch.round(x / scale[:, None]), -127, 127) * scale[:, None]
     y = [torch.nn.functional.linear(q, s["q" + k][:, :c["D"]].double() * s["s" + k].double()[:, None])
          for k in ("a", "b") if "q" + k in s]
