@@ -94,6 +94,29 @@ int grad_norm(const lc_tensor_t *list, int32_t count, float *norm, void *ws, siz
 int grad_clip(const lc_tensor_t *list, int32_t count, float max_norm, float *norm, void *ws, size_t ws_bytes,
               void *hip_stream);
 
+/* Weights of 8 bits.  A row of values x is held as whole numbers q, -127 to 127, and a scale s: s = max |x| / 127, but at least 2^-126; q = x / s,
+ * to nearest, ties to even; q s stands for x.  A row of q takes q8_row_bytes(D) bytes: D rounded up to whole blocks of 128, zeros behind the last
+ * value.  A row with an infinite or NaN value has scale NaN, and so have all results that it enters.
+ * Widths D of these operators are 1 to 2^17. */
+
+/* Host only.  Bytes of a row of D values; 0 for invalid D. */
+int q8_row_bytes(int32_t D);
+
+/* x [N][D] of type dtype to q [N][q8_row_bytes(D)] and scale [N] fp32: weights, once. */
+int q8_rows(const void *x, int8_t *q, float *scale, int32_t N, int32_t D, int dtype, void *hip_stream);
+
+/* Host only.  Scratch for q8_matmul and q8_glu_fwd; 0 for invalid arguments.  What is enough for N rows is enough for fewer. */
+size_t q8_workspace_bytes(int32_t N, int32_t D, int32_t F, int dtype);
+
+/* y[n][f] = s[n] scale[f] sum_d p[n][d] q[f][d], with p, s the 8-bit form of x, formed by the call.  x [N][D] and y [N][F] of type
+ * dtype, q [F][q8_row_bytes(D)], scale [F] as from q8_rows.  The sum is exact; it, and its product with each scale, is rounded to fp32. */
+int q8_matmul(const void *x, const int8_t *q, const float *scale, void *y, int32_t N, int32_t D, int32_t F, int dtype,
+              void *ws, size_t ws_bytes, void *hip_stream);
+
+/* glu_fwd with 8-bit weights: h = act(g) * u, with g and u as q8_matmul gives them in fp32, from qg, sg and qu, su. */
+int q8_glu_fwd(const void *x, const int8_t *qg, const float *sg, const int8_t *qu, const float *su, void *h, int32_t N,
+               int32_t D, int32_t F, int act, int dtype, void *ws, size_t ws_bytes, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

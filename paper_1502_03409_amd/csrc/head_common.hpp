@@ -72,6 +72,7 @@ struct Operand {
     long long ld, plane;
     int rows;          // rows that exist, COL: in whole 16-byte pieces
     int depth, half;   // COLPAIR
+    long long each = 0;   // values from one item of a stack to the next
 };
 __device__ __host__ __forceinline__ int pair_row(int v, int each, int *second) {   // each: rows taken in turn
     *second = v / each & 1;

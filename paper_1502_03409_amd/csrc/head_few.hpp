@@ -142,6 +142,10 @@ __global__ __launch_bounds__(256, 2) void few_kernel(FewOperand<T> A, FewOperand
     epi.run(acc, 0, n0, lane, M, Nn, 0, (char *)sums);
 }
 
+// The number format of an operand that comes in 16-byte pieces of one plane; 8-bit whole numbers (int8_t) only through LDS
+template <typename T> struct FewFormat : Format<1> {};
+template <> struct FewFormat<int8_t> : Format<BYTES> {};
+
 // The same through LDS: each wave has a ring of ST steps of its own and waits for nobody.  A load instruction brings whole lines, eight
 // rows of 128 bytes; from registers' loads 32 rows of 32 bytes, lines stay in the vector cache until their other parts are asked for, and
 // that cache, not HBM, bounds what is in flight (5 rows against 100003 x 4096 in bf16: 4.2 TB/s through registers).
@@ -190,7 +194,8 @@ __global__ __launch_bounds__(256, ring_bytes(NB, XQ, ST) > 81920 ? 1 : 2) void f
         for (int q = 0; q < XQ; ++q)
             load_lds16(px + at, piece_of(q) < left ? xoff[q] : xoff[q] - piece_of(q) * 16, l + (Q + q) * 1024);
     };
-    f32x16 acc[1][NB] = {};
+    typedef typename FewFormat<T>::Acc Acc;
+    Acc acc[1][NB] = {};
 #pragma unroll
     for (int s = 0; s < ST - 1; ++s)
         if (s < own) load(s);
@@ -212,13 +217,13 @@ __global__ __launch_bounds__(256, ring_bytes(NB, XQ, ST) > 81920 ? 1 : 2) void f
         }
         // rows beyond those of x that were brought take the last one's place; their sums are dropped
         const int xr = min(l32, 8 * XQ - 1), xswap = (xr >> 1) & 7, wswap = (l32 >> 1) & 7;
-        if constexpr (sizeof(T) == 2) {
+        if constexpr (sizeof(T) <= 2) {
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 const u32x4 x = *(const u32x4 *)(l + Q * 1024 + xr * 128 + (((2 * c + h) ^ xswap) * 16));
 #pragma unroll
                 for (int j = 0; j < NB; ++j)
-                    acc[0][j] = mfma32(*(const u32x4 *)(l + j * 4096 + l32 * 128 + (((2 * c + h) ^ wswap) * 16)), x, acc[0][j]);
+                    acc[0][j] = FewFormat<T>::mul(*(const u32x4 *)(l + j * 4096 + l32 * 128 + (((2 * c + h) ^ wswap) * 16)), x, acc[0][j]);
             }
         } else {
 #pragma unroll
@@ -234,7 +239,7 @@ __global__ __launch_bounds__(256, ring_bytes(NB, XQ, ST) > 81920 ? 1 : 2) void f
         }
     }
     __syncthreads();   // all rings are free
-    f32x16 *const sums = (f32x16 *)smem;
+    Acc *const sums = (Acc *)smem;
     if (wave) {
 #pragma unroll
         for (int j = 0; j < NB; ++j) sums[((wave - 1) * NB + j) * 64 + lane] = acc[0][j];
@@ -260,8 +265,12 @@ int launch_blocks(const char *name, const FewOperand<T> &A, const FewOperand<T> 
     LC_PLAN_REQUIRE(p, FB == PAIR ? Nn == 32 * ceil_div(B.rows, 16) : B.rows >= Nn);
     LC_PLAN_REQUIRE(p, A.ld <= (1 << 20) && B.ld <= (1 << 20));   // 64 rows' offsets stay below 2^31 bytes
     LC_PLAN_REQUIRE(p, ptr_aligned16(A.p0) && ptr_aligned16(B.p0) && ptr_aligned16(B.p1));
-    if (!ring) LC_LAUNCH(p, name, (few_kernel<T, FB, NB, Epi>), s, A, B, M, rows_dev, Nn, K, epi);
-    else if (M <= 8) LC_LAUNCH(p, name, (few_ring_kernel<T, FB, NB, 1, 4, Epi>), s, A, B, M, rows_dev, Nn, K, epi);
+    if constexpr (sizeof(T) == 1) LC_PLAN_REQUIRE(p, ring);
+    else if (!ring) {
+        LC_LAUNCH(p, name, (few_kernel<T, FB, NB, Epi>), s, A, B, M, rows_dev, Nn, K, epi);
+        return LC_OK;
+    }
+    if (M <= 8) LC_LAUNCH(p, name, (few_ring_kernel<T, FB, NB, 1, 4, Epi>), s, A, B, M, rows_dev, Nn, K, epi);
     else LC_LAUNCH(p, name, (few_ring_kernel<T, FB, NB, 4, 3, Epi>), s, A, B, M, rows_dev, Nn, K, epi);
     return LC_OK;
 }

@@ -30,6 +30,43 @@ __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
+// Number formats of a product, the first template parameter of what follows.  1, 2, 3: bf16 planes, as above.  HALF: one fp16 plane.  HALF2:
+// two fp16 planes, a value and what its rounding to the first leaves, of which three products of four are formed (the fourth is below 2^-22
+// of the result).  BYTES: 8-bit whole numbers, two in the place of one 16-bit value, sums in 32-bit whole numbers: the matrix instruction
+// takes the same 16 bytes of a row as those for 16-bit values, so nothing else changes, and sizes along the contraction count pairs.
+enum { HALF = 4, HALF2 = 5, BYTES = 6 };
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x16 __attribute__((ext_vector_type(16)));
+// PAIRS: products of planes; A, B: the plane of each operand in them, four bits a product.  STACK: products of a stack of matrices.
+template <int PL> struct Format {
+    typedef f32x16 Acc;
+    static constexpr int PAIRS = 1;
+    static constexpr unsigned A = 0, B = 0;
+    static constexpr bool STACK = false;
+    static __device__ __forceinline__ Acc mul(u32x4 a, u32x4 b, Acc c) { return mfma32(a, b, c); }
+};
+template <> struct Format<3> : Format<1> {   // 00 10 01 11 02 20
+    static constexpr int PAIRS = 6;
+    static constexpr unsigned A = 0x201010, B = 0x021100;
+};
+template <> struct Format<HALF> : Format<1> {
+    static constexpr bool STACK = true;
+    static __device__ __forceinline__ Acc mul(u32x4 a, u32x4 b, Acc c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    }
+};
+template <> struct Format<HALF2> : Format<HALF> {   // 00 10 01
+    static constexpr int PAIRS = 3;
+    static constexpr unsigned A = 0x010, B = 0x100;
+};
+template <> struct Format<BYTES> : Format<1> {
+    typedef i32x16 Acc;
+    static __device__ __forceinline__ Acc mul(u32x4 a, u32x4 b, Acc c) {
+        return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
+    }
+};
+
 // fn(0), fn(1), .. with the numbers as types: the accumulators may only be indexed by constants, however long fn is
 template <int N, int I = 0, typename Fn>
 __device__ __forceinline__ void for_blocks(const Fn &fn) {
@@ -48,6 +85,8 @@ struct Shape {
     const int *k_dev;
     int k_first;
     int times = 1;
+    int stack = 1;      // products of this shape, one item of a stack each
+    int sym = 0;        // the result is symmetric: only tiles on and below the diagonal are formed
 };
 __device__ __forceinline__ int live(int most, const int *dev, int first, int times = 1) {
     return dev ? max(0, min(most, times * (*dev - first))) : most;
@@ -123,6 +162,24 @@ __device__ __forceinline__ bool tile_of(int wg, int mt, int nt, int splits, int 
     return true;
 }
 
+// Tiles of one product of a shape, and in a stack: all tiles of a part of an item one after the other, so that an XCD has few items at a time;
+// of a symmetric result row by row.  item: of the stack, times the parts, plus the part.
+__device__ __host__ __forceinline__ long long tiles_in(const Shape &sh, int mt, int nt) { return sh.sym ? (long long)mt * (mt + 1) / 2 : (long long)mt * nt; }
+__device__ __forceinline__ void tile_in_stack(const Shape &sh, int wg, int mt, int nt, int splits, int *tm, int *tn, int *item) {
+    const int tiles = (int)tiles_in(sh, mt, nt), id = remap_xcd(wg, gridDim.x);
+    *item = id / tiles;
+    const int t = id - *item * tiles;
+    if (sh.sym) {
+        int r = (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
+        r -= r * (r + 1) / 2 > t;
+        r += (r + 1) * (r + 2) / 2 <= t;
+        *tm = r, *tn = t - r * (r + 1) / 2;
+    } else {
+        const int group = t / (kGroup * nt), first = group * kGroup, size = min(kGroup, mt - first), in = t - group * kGroup * nt;
+        *tm = first + in % size, *tn = in / size;
+    }
+}
+
 // ---------------------------------------------------------------------------------------------------------------------------
 // The tiled product.  BM x BN of the result per workgroup of 2 x 2 waves, steps of 64 along the contraction, through LDS buffers that
 // are filled by loads which go straight there: NA for A, NB for B (three and two are all 160 KB for 256 x 256).  A long contraction over
@@ -152,7 +209,7 @@ template <int FORM, int N, int PL>
 struct Stager {
     static constexpr bool COLS = FORM == COL || FORM == COLPAIR;
     static constexpr int Q = N / 8 / kWaves;   // load instructions of a wave a step, 1024 bytes each
-    static constexpr int PAIRS = PL == 3 ? 6 : 1;
+    static constexpr int PAIRS = Format<PL>::PAIRS;
     unsigned off[Q];
     gbyte_ptr base, base2;                     // of the current kStep indices; the second matrix (PAIR: of these indices, COLPAIR: its start)
     long long move, plane, at;                 // bytes: to the next kStep indices, to the next plane, to the current plane
@@ -215,7 +272,7 @@ struct Stager {
         }
     }
     __device__ __forceinline__ void next() {   // on to the next step: the next pair of planes, or the next indices
-        if constexpr (PL == 3) {
+        if constexpr (PAIRS > 1) {
             if (++pair < PAIRS) {
                 const unsigned q = planes >> (4 * pair);
                 at = q & 1 ? plane : q & 2 ? 2 * plane : 0;
@@ -232,7 +289,7 @@ struct Stager {
     template <int q>
     __device__ __forceinline__ void load(unsigned lds) const {
         const gbyte_ptr p = FORM == PAIR && q % 2 ? base2 : base;
-        load_lds16(PL == 1 ? p : p + at, off[q], lds + q * kWaves * 1024);
+        load_lds16(PAIRS == 1 && PL != 2 ? p : p + at, off[q], lds + q * kWaves * 1024);
     }
     // zeros for what is beyond the `n` indices left of a step (the same bytes this lane brought)
     __device__ __forceinline__ void clear(char *lds, int n) const {
@@ -287,13 +344,21 @@ template <int NT> constexpr int kEpiBytes = 32 * (NT * 32 * 4 + 16);
 
 template <int PL, int FA, int FB, int BM, int BN, int NA, int NB, typename Epi>
 __global__ __launch_bounds__(64 * kWaves, (NA * BM + NB * BN) * 128 > 81920 ? 1 : 2) void gemm_kernel(Operand A, Operand B, Shape sh, int nt, int splits, Epi epi) {
-    constexpr int MT = BM / 64, NT = BN / 64, PAIRS = PL == 3 ? 6 : 1;
+    constexpr int MT = BM / 64, NT = BN / 64, PAIRS = Format<PL>::PAIRS;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int M = live(sh.M, sh.rows_dev, sh.rows_first, sh.times);
     const int K = live(sh.K, sh.k_dev, sh.k_first, sh.times);
     int tm, tn, split;
-    if (!tile_of(blockIdx.x, (M + BM - 1) / BM, nt, splits, &tm, &tn, &split)) return;
+    if constexpr (Format<PL>::STACK) {
+        int item;
+        tile_in_stack(sh, blockIdx.x, (M + BM - 1) / BM, nt, splits, &tm, &tn, &item);
+        split = item % splits;
+        A.p0 += item / splits * A.each, B.p0 += item / splits * B.each;
+        epi.item(item);
+    } else {
+        if (!tile_of(blockIdx.x, (M + BM - 1) / BM, nt, splits, &tm, &tn, &split)) return;
+    }
     const int wm = wave / 2, wn = wave % 2;
     constexpr unsigned ABYTES = BM * 128, BBYTES = BN * 128, B0 = NA * ABYTES;   // A's buffers, then B's
     const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) char *)smem;
@@ -301,15 +366,14 @@ __global__ __launch_bounds__(64 * kWaves, (NA * BM + NB * BN) * 128 > 81920 ? 1 
     Reader<FB, BN, NT> rb;
     ra.init(lds0, wm * MT * 32, lane);
     rb.init(lds0 + B0, wn * NT * 32, lane);
-    f32x16 acc[MT][NT] = {};
+    typename Format<PL>::Acc acc[MT][NT] = {};
     // parts are whole steps of the contraction at its longest; what is beyond its actual end is left out
     const int per = ((sh.K + kStep - 1) / kStep + splits - 1) / splits;
     const int kt0 = split * per, kt1 = min((K + kStep - 1) / kStep, kt0 + per), steps = max(0, kt1 - kt0) * PAIRS;
     Stager<FA, BM, PL> sa;
     Stager<FB, BN, PL> sb;
-    // planes of A and B in the six products: 00 10 01 11 02 20
-    sa.init(A, tm * BM, kt0, K, 0x201010, wave, lane);
-    sb.init(B, tn * BN, kt0, K, 0x021100, wave, lane, PL == 2 ? K / 2 : 0);
+    sa.init(A, tm * BM, kt0, K, Format<PL>::A, wave, lane);
+    sb.init(B, tn * BN, kt0, K, Format<PL>::B, wave, lane, PL == 2 ? K / 2 : 0);
     constexpr int QA = Stager<FA, BM, PL>::Q, QB = Stager<FB, BN, PL>::Q;
     const unsigned lds_wave = lds0 + wave * 1024;
     auto load_a = [&](unsigned buffer, auto number) __attribute__((always_inline)) { sa.template load<decltype(number)::value>(lds_wave + buffer); };
@@ -354,7 +418,7 @@ __global__ __launch_bounds__(64 * kWaves, (NA * BM + NB * BN) * 128 > 81920 ? 1 
                         rb.turn(bnext);
                     }
                 }
-                acc[p / NT][p % NT] = mfma32(b[c & 1][p % NT], a[c & 1][p / NT], acc[p / NT][p % NT]);
+                acc[p / NT][p % NT] = Format<PL>::mul(b[c & 1][p % NT], a[c & 1][p / NT], acc[p / NT][p % NT]);
                 if constexpr (c < 3) {
 #pragma unroll
                     for (int r = p * R / P; r < (p + 1) * R / P; ++r) fetch(c + 1, r);
@@ -424,9 +488,11 @@ int launch_tiles(const char *name, const Operand &A, const Operand &B, const Sha
     const int mt = ceil_div(sh.M, BM), nt = ceil_div(sh.Nn, BN);
     constexpr int LDS = (NA * BM + NB * BN) * 128;
     static_assert(kWaves * kEpiBytes<BN / 64> <= LDS, "the epilogue's LDS is that of the buffers");
-    const LaunchPlan p = make_plan(name, {PL, FA, FB, BM, BN, NA, NB}, {sh.M, sh.Nn, sh.K, splits}, dim3((unsigned)((long long)mt * nt * splits)),
-                                   64 * kWaves, LDS);
-    LC_PLAN_REQUIRE(p, (long long)mt * nt * splits <= 0x7fffffffLL && splits >= 1);
+    const long long wgs = tiles_in(sh, mt, nt) * splits * sh.stack;
+    const LaunchPlan p = make_plan(name, {PL, FA, FB, BM, BN, NA, NB}, {sh.M, sh.Nn, sh.K, splits, sh.stack, sh.sym}, dim3((unsigned)wgs), 64 * kWaves, LDS);
+    LC_PLAN_REQUIRE(p, wgs <= 0x7fffffffLL && splits >= 1);
+    LC_PLAN_REQUIRE(p, Format<PL>::STACK ? sh.stack >= 1 && !sh.rows_dev && !sh.k_dev && (!sh.sym || (BM == BN && sh.M == sh.Nn && mt <= 4096))
+                                         : sh.stack == 1 && !sh.sym);
     LC_PLAN_REQUIRE(p, A.ld % 8 == 0 && B.ld % 8 == 0 && A.plane % 8 == 0 && B.plane % 8 == 0);
     constexpr bool CA = FA == COL || FA == COLPAIR, CB = FB == COL || FB == COLPAIR;
     LC_PLAN_REQUIRE(p, CA ? A.rows % 8 == 0 && A.ld >= A.rows && A.rows >= sh.M : A.rows >= sh.M && A.ld >= sh.K);
@@ -621,16 +687,20 @@ struct Cut {
 // gradients of up to 8192 rows two lose by it, 0.1 % by the estimate.
 constexpr int kMostSplits = 32;
 constexpr long long kMostParts = 1LL << 26;
-inline Cut choose_cut(int M, int Nn, int K, int pairs, bool may_split) {
-    const double large = (double)ceil_div(M, 256) * ceil_div(Nn, 256), small = (double)ceil_div(M, 128) * ceil_div(Nn, 128);
+inline double tiles_of_size(int M, int Nn, int tile, int stack, bool sym) {
+    const double mt = ceil_div(M, tile);
+    return stack * (sym ? mt * (mt + 1) / 2 : mt * ceil_div(Nn, tile));
+}
+inline Cut choose_cut(int M, int Nn, int K, int pairs, bool may_split, int stack = 1, bool sym = false) {
+    const double large = tiles_of_size(M, Nn, 256, stack, sym), small = tiles_of_size(M, Nn, 128, stack, sym);
     if (large >= 4 * kComputeUnits) return Cut{Cut::LARGE, 1};
     const int steps = ceil_div(K, kStep);
     Cut best = {Cut::SMALL, 1};
     double least = 1e30;
-    const long long result = M * round_up(Nn, 4);
+    const long long result = M * round_up(Nn, 4) * stack;
     for (int s = 1; s == 1 || (may_split && s <= kMostSplits && s <= steps / 2 && s * result <= kMostParts); ++s) {
         const double part = (double)ceil_div(steps, s) * pairs;
-        const double join = s > 1 ? 4 + 8e-6 * s * (double)M * Nn / 4 : 0;
+        const double join = s > 1 ? 4 + 8e-6 * s * (double)M * Nn * stack / 4 : 0;
         const double rounds = std::ceil(large * s / kComputeUnits), wgs = small * s;
         const double tl = rounds * (part * 1.7 + 15) + join;
         const bool deep = wgs <= kComputeUnits;

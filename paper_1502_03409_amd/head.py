@@ -17,7 +17,8 @@ from .binding import LC_F32, LC_BF16
 LC_ACT_SIGMOID, LC_ACT_SILU, LC_ACT_GELU = 0, 1, 2
 
 HEAD_EXPORTS = ("glu_workspace_bytes", "glu_fwd", "glu_bwd", "xent_workspace_bytes", "xent_fwd", "xent_fwd_bwd",
-                "grad_clip_workspace_bytes", "grad_norm", "grad_clip")
+                "grad_clip_workspace_bytes", "grad_norm", "grad_clip", "q8_row_bytes", "q8_rows", "q8_workspace_bytes", "q8_matmul",
+                "q8_glu_fwd")
 
 __all__ = ["LC_ACT_SIGMOID", "LC_ACT_SILU", "LC_ACT_GELU", *HEAD_EXPORTS]
 
@@ -38,8 +39,13 @@ def _lib() -> C.CDLL:
         L.grad_clip_workspace_bytes.argtypes = [i64, i32]
         L.grad_norm.argtypes = [vp, i32, vp, vp, sz, vp]
         L.grad_clip.argtypes = [vp, i32, f32, vp, vp, sz, vp]
+        L.q8_row_bytes.argtypes = [i32]
+        L.q8_rows.argtypes = [vp] * 3 + [i32, i32, C.c_int, vp]
+        L.q8_workspace_bytes.argtypes = [i32, i32, i32, C.c_int]
+        L.q8_matmul.argtypes = [vp] * 4 + [i32, i32, i32, C.c_int, vp, sz, vp]
+        L.q8_glu_fwd.argtypes = [vp] * 6 + [i32, i32, i32, C.c_int, C.c_int, vp, sz, vp]
         for name in HEAD_EXPORTS:
-            getattr(L, name).restype = sz if name.endswith("_bytes") else C.c_int
+            getattr(L, name).restype = sz if name.endswith("workspace_bytes") else C.c_int
         _typed = True
     return L
 
@@ -134,3 +140,36 @@ def grad_clip(tensors: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tens
     wp, wb = _b._ws(ws)
     _b._check("grad_clip", _lib().grad_clip(_tensor_list(tensors, tensors if out is None else out), len(tensors), max_norm,
                                             _dev(norm, (1,), torch.float32, "norm"), wp, wb, _b._stream()))
+
+
+def q8_row_bytes(D: int) -> int:
+    return int(_lib().q8_row_bytes(D))
+
+
+def q8_rows(x, q, scale, dtype: int = LC_F32) -> None:
+    N, D = x.shape
+    _b._check("q8_rows", _lib().q8_rows(
+        _dev(x, (N, D), _b._op_dtype(dtype), "x"), _dev(q, (N, q8_row_bytes(D)), torch.int8, "q"),
+        _dev(scale, (N,), torch.float32, "scale"), N, D, dtype, _b._stream()))
+
+
+def q8_workspace_bytes(N: int, D: int, F: int, dtype: int = LC_F32) -> int:
+    return int(_lib().q8_workspace_bytes(N, D, F, dtype))
+
+
+def q8_matmul(x, q, scale, y, dtype: int = LC_F32, ws=None) -> None:
+    (N, D), F = x.shape, q.shape[0]
+    dt, qs = _b._op_dtype(dtype), (F, q8_row_bytes(D))
+    wp, wb = _b._ws(ws)
+    _b._check("q8_matmul", _lib().q8_matmul(
+        _dev(x, (N, D), dt, "x"), _dev(q, qs, torch.int8, "q"), _dev(scale, (F,), torch.float32, "scale"), _dev(y, (N, F), dt, "y"),
+        N, D, F, dtype, wp, wb, _b._stream()))
+
+
+def q8_glu_fwd(x, qg, sg, qu, su, h, act: int, dtype: int = LC_F32, ws=None) -> None:
+    (N, D), F = x.shape, qg.shape[0]
+    dt, qs = _b._op_dtype(dtype), (F, q8_row_bytes(D))
+    wp, wb = _b._ws(ws)
+    _b._check("q8_glu_fwd", _lib().q8_glu_fwd(
+        _dev(x, (N, D), dt, "x"), _dev(qg, qs, torch.int8, "qg"), _dev(sg, (F,), torch.float32, "sg"), _dev(qu, qs, torch.int8, "qu"),
+        _dev(su, (F,), torch.float32, "su"), _dev(h, (N, F), dt, "h"), N, D, F, act, dtype, wp, wb, _b._stream()))
