@@ -117,6 +117,22 @@ int q8_matmul(const void *x, const int8_t *q, const float *scale, void *y, int32
 int q8_glu_fwd(const void *x, const int8_t *qg, const float *sg, const int8_t *qu, const float *su, void *h, int32_t N,
                int32_t D, int32_t F, int act, int dtype, void *ws, size_t ws_bytes, void *hip_stream);
 
+/* Host only.  Scratch for muon_step; 0 for invalid arguments.  What is enough for a stack is enough for a shorter one.  It is bounded for
+ * any number of matrices (about 4 GiB, or what one matrix takes). */
+size_t muon_workspace_bytes(int32_t count, int32_t rows, int32_t cols, int dtype);
+
+/* A step of gradient descent on each matrix of a stack [count][rows][cols] with an orthogonalised update:
+ *   m' = momentum m + g;  u = g + momentum m' (nesterov) or m';  X = u / |u|, its 2-norm over all values of the matrix;
+ *   `steps` times: A = X X^T, X = 3.4445 X + (-4.7750 A + 2.0315 A A) X;  w_out = (1 - decay) w - rate X,  m_out = m'.
+ * w, g and w_out are of type dtype, m and m_out fp32.  w_out may be w and m_out may be m; no other overlap.  The untied filters of a
+ * layer, [LH][LW][K][F], are a stack of LH LW matrices.  A matrix u of zeros has the update 0; one with an infinite or NaN value makes all of its
+ * matrix of w_out NaN.
+ * Between products X is held in fp16 for bf16 weights (scaled, so that all of its 11 bits count), and in 22 bits for fp32 weights.
+ * count is 0 to 2^24, sides 1 to 2^20, the smaller one at most 2^15, all values at most 2^40; steps 1 to 32. */
+int muon_step(const void *w, const void *g, const float *m, void *w_out, float *m_out, int32_t count, int32_t rows,
+              int32_t cols, float rate, float decay, float momentum, int nesterov, int32_t steps, int dtype, void *ws,
+              size_t ws_bytes, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -18,7 +18,7 @@ LC_ACT_SIGMOID, LC_ACT_SILU, LC_ACT_GELU = 0, 1, 2
 
 HEAD_EXPORTS = ("glu_workspace_bytes", "glu_fwd", "glu_bwd", "xent_workspace_bytes", "xent_fwd", "xent_fwd_bwd",
                 "grad_clip_workspace_bytes", "grad_norm", "grad_clip", "q8_row_bytes", "q8_rows", "q8_workspace_bytes", "q8_matmul",
-                "q8_glu_fwd")
+                "q8_glu_fwd", "muon_workspace_bytes", "muon_step")
 
 __all__ = ["LC_ACT_SIGMOID", "LC_ACT_SILU", "LC_ACT_GELU", *HEAD_EXPORTS]
 
@@ -44,6 +44,8 @@ def _lib() -> C.CDLL:
         L.q8_workspace_bytes.argtypes = [i32, i32, i32, C.c_int]
         L.q8_matmul.argtypes = [vp] * 4 + [i32, i32, i32, C.c_int, vp, sz, vp]
         L.q8_glu_fwd.argtypes = [vp] * 6 + [i32, i32, i32, C.c_int, C.c_int, vp, sz, vp]
+        L.muon_workspace_bytes.argtypes = [i32, i32, i32, C.c_int]
+        L.muon_step.argtypes = [vp] * 5 + [i32, i32, i32, f32, f32, f32, C.c_int, i32, C.c_int, vp, sz, vp]
         for name in HEAD_EXPORTS:
             getattr(L, name).restype = sz if name.endswith("workspace_bytes") else C.c_int
         _typed = True
@@ -173,3 +175,21 @@ def q8_glu_fwd(x, qg, sg, qu, su, h, act: int, dtype: int = LC_F32, ws=None) -> 
     _b._check("q8_glu_fwd", _lib().q8_glu_fwd(
         _dev(x, (N, D), dt, "x"), _dev(qg, qs, torch.int8, "qg"), _dev(sg, (F,), torch.float32, "sg"), _dev(qu, qs, torch.int8, "qu"),
         _dev(su, (F,), torch.float32, "su"), _dev(h, (N, F), dt, "h"), N, D, F, act, dtype, wp, wb, _b._stream()))
+
+
+def muon_workspace_bytes(count: int, rows: int, cols: int, dtype: int = LC_F32) -> int:
+    return int(_lib().muon_workspace_bytes(count, rows, cols, dtype))
+
+
+def muon_step(w, g, m, w_out, m_out, rate: float, decay: float = 0.0, momentum: float = 0.95, nesterov: bool = True, steps: int = 5,
+              dtype: int = LC_F32, ws=None) -> None:
+    """``w``: a matrix, or a stack of them in all dimensions but the last two.  ``w_out``, ``m_out`` None: in place."""
+    rows, cols = w.shape[-2:]
+    count = w.numel() // max(1, rows * cols)
+    dt, shape = _b._op_dtype(dtype), tuple(w.shape)
+    w_out, m_out = w if w_out is None else w_out, m if m_out is None else m_out
+    wp, wb = _b._ws(ws)
+    _b._check("muon_step", _lib().muon_step(
+        _dev(w, shape, dt, "w"), _dev(g, shape, dt, "g"), _dev(m, shape, torch.float32, "m"), _dev(w_out, shape, dt, "w_out"),
+        _dev(m_out, shape, torch.float32, "m_out"), count, rows, cols, rate, decay, momentum, int(nesterov), steps, dtype, wp, wb,
+        _b._stream()))
