@@ -117,6 +117,33 @@ int q8_matmul(const void *x, const int8_t *q, const float *scale, void *y, int32
 int q8_glu_fwd(const void *x, const int8_t *qg, const float *sg, const int8_t *qu, const float *su, void *h, int32_t N,
                int32_t D, int32_t F, int act, int dtype, void *ws, size_t ws_bytes, void *hip_stream);
 
+/* Host only.  Scratch for logp_fwd (grads = 0), or for logp_fwd and logp_bwd (grads = 1); 0 for invalid arguments.  What is enough for N rows is
+ * enough for fewer.  T: words given with each row, 0 to 64; K: likeliest words asked for, 0 to 64 and no more than V.  It is bounded for any
+ * number of rows but for what a few numbers and, laid out, x take. */
+size_t logp_workspace_bytes(int32_t N, int32_t D, int32_t V, int32_t T, int32_t K, int dtype, int grads);
+
+/* What a softmax over V words says, projection included: with l[n][v] = sum_d x[n][d] w[v][d] and p = softmax(l),
+ *   logp[n][t] = log p[n][tags[n][t]], 0 where the tag is negative;  entropy[n] = -sum_v p log p;
+ *   top[n][0 .. K-1]: the words of the K largest scores, largest first, equal ones by their number; top_logp: their log p.
+ * x [N][D], w [V][D]; tags [N][T] int64 (8-byte aligned; NULL if T = 0), logp [N][T], entropy NULL or [N], top [N][K] int64 and top_logp [N][K]
+ * (NULL if K = 0), all fp32 but for top.  state NULL or [N][3] fp32: receives what logp_bwd needs of the softmax.
+ * Where words are given (T > 0), a row without one (all tags negative) is masked: its x is not looked at, its numbers are 0 and its top is -1.
+ * A tag >= V has logp NaN.  A row with a NaN score, a score of +inf or none above -inf has no distribution: its numbers are NaN, its top is -1.
+ * Scores of given and likeliest words are formed in 64 bits, and so is their order.  Where more words than 2048 come as near to the K-th score
+ * as the product's sums tell scores apart (some 2^-16 of it), which of these follow is decided by those sums. */
+int logp_fwd(const void *x, const void *w, const int64_t *tags, float *logp, float *entropy, int64_t *top, float *top_logp,
+             float *state, int32_t N, int32_t D, int32_t V, int32_t T, int32_t K, int dtype, void *ws, size_t ws_bytes,
+             void *hip_stream);
+
+/* Gradients of sum dlogp logp + sum dentropy entropy, for given dlogp [N][T] (not looked at where the tag is negative) and dentropy (NULL or [N]), fp32,
+ * with x, w, tags as in logp_fwd and logp and state from it:
+ *   d[n][v] = sum of dlogp[n][t] over t with tags[n][t] = v - p[n][v] (sum_t dlogp[n][t] + dentropy[n] (log p[n][v] + entropy[n])),
+ *   dx = d w (zero in masked rows), dw = d^T x, both overwritten.  dx may be NULL.
+ * A row with a tag >= V, or without a distribution, makes the gradients it enters NaN. */
+int logp_bwd(const void *x, const void *w, const int64_t *tags, const float *logp, const float *state, const float *dlogp,
+             const float *dentropy, void *dx, void *dw, int32_t N, int32_t D, int32_t V, int32_t T, int dtype, void *ws,
+             size_t ws_bytes, void *hip_stream);
+
 /* Host only.  Scratch for muon_step; 0 for invalid arguments.  What is enough for a stack is enough for a shorter one.  It is bounded for
  * any number of matrices (about 4 GiB, or what one matrix takes). */
 size_t muon_workspace_bytes(int32_t count, int32_t rows, int32_t cols, int dtype);

@@ -94,6 +94,14 @@ struct Scratch {
     }
 };
 
+// What logp_fwd leaves for each row, T given words and K likeliest ones.
+struct LogpOut {
+    float *logp, *entropy;
+    int64_t *top;
+    float *top_logp, *state;
+    int T, K;
+};
+
 // Sizes of a head's matrices: widths 1 .. 2^20, rows 0 .. 2^24, so that every index within a row or a tile has 31 bits and
 // every product of two sizes is formed in 64.
 inline bool head_width(long long v) { return v >= 1 && v <= (1 << 20); }

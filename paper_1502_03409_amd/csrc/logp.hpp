@@ -1,0 +1,661 @@
+// What a softmax over a vocabulary answers: log probabilities of given words, the entropy, the likeliest words; and the gradients of the first two.
+//
+// The scores l = x w^T are never stored.  Each tile of the product leaves, per row, its largest score, the sum of the other words' exponentials
+// relative to it, and the sum of those times the distance; and per row and group of 32 words the largest score, its place, and the second
+// largest.  A small kernel joins the tiles: with m the largest score, r the sum of exp(l - m) over all words but one that has it, and
+// U = sum exp(l - m) (m - l),
+//   log sum exp(l) = m + log(1 + r),  H = log(1 + r) + U / (1 + r),
+// neither of which cancels where one word has nearly all.
+//
+// The likeliest words are looked for among the groups: with t at most the K-th largest score, only groups whose largest reaches t hold any, and
+// only where the second reaches it too is more than one of 32 a candidate.  Candidates' scores are formed again in 64 bits, and so are those of the
+// given words; the order is that of these, equal ones in the vocabulary's order, so it does not hang on how a tile added up.
+//
+// Gradients: with a, b those of the log probabilities and the entropy, and A = sum of a row's a,
+//   d[v] = sum of a over t with word[t] = v - p[v] (A + b (log p[v] + H)),  dx = d w,  dw = d^T x;
+// the scores are formed once more, d leaves the product's tiles, given words get theirs in a kernel of its own, where with S the sum of a over a
+// word, S - p A = (S - A) - A (p - 1) does not cancel where p is near one.  d meets bf16 operands as in xent.hpp.
+#pragma once
+#include "head_few.hpp"
+#include "head_planes.hpp"
+
+namespace lc {
+namespace head {
+
+constexpr long long kKeyBytes = 512LL << 20;      // groups' scores kept at a time
+constexpr long long kGradBytes = 2LL << 30;       // of d
+constexpr int kGroupWords = 32;
+constexpr int kMostTop = 64, kMostGiven = 64;     // words asked for and given a row
+constexpr int kCandidates = kMostTop * kGroupWords;
+
+struct LogpRows {
+    int *count, *place, *index;   // as in xent.hpp; null: all rows count
+    float4 *sums;                 // by position: largest score, log(1 + r), entropy
+    float *a, *b;                 // by position: A and b
+};
+
+// Positions of the rows that have a word.  One workgroup, 1024 rows at a time.
+static __global__ __launch_bounds__(1024) void logp_rows_kernel(const int64_t *tags, int N, int T, LogpRows o) {
+    __shared__ int part[16];
+    __shared__ int total;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (threadIdx.x == 0) total = 0;
+    __syncthreads();
+    for (int n0 = 0; n0 < N; n0 += 1024) {
+        const int n = n0 + threadIdx.x;
+        bool in = false;
+        if (n < N)
+            for (int t = 0; t < T; ++t) in |= tags[(long long)n * T + t] >= 0;
+        const unsigned long long mask = __ballot(in);
+        if (lane == 0) part[wave] = __popcll(mask);
+        __syncthreads();
+        int at = total;
+        for (int w = 0; w < wave; ++w) at += part[w];
+        at += __popcll(mask & ((1ull << lane) - 1));
+        if (n < N) o.place[n] = in ? at : -1;
+        if (in) o.index[at] = n;
+        __syncthreads();
+        if (threadIdx.x == 0)
+            for (int w = 0; w < 16; ++w) total += part[w];
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) *o.count = total;
+}
+
+// The rows that count as planes, zeros in the other rows of dx (nullable); with gradients a row's A and b and what the forward pass left.
+struct LogpGiven {
+    const int64_t *tags;
+    const float *state, *dlogp, *dentropy;
+    int T, V;
+};
+template <typename T, bool GRADS>
+__global__ __launch_bounds__(256) void logp_gather_kernel(const T *x, bf16_t *dst, T *dx, LogpRows o, LogpGiven given, int N, int D, int pieces) {
+    constexpr int PL = Planes<T>::N;
+    const long long at = blockIdx.x * 256LL + threadIdx.x;
+    const int n = (int)(at / pieces), piece = (int)(at - (long long)n * pieces), c = piece * 8;
+    if (n >= N) return;
+    const int to = o.place ? o.place[n] : n;
+    if (to >= 0) {
+        if (dst) {
+            float v[8];
+            load8(x + (long long)n * D, c, D, v);
+            put_planes<PL>(dst + (long long)to * pieces * 8 + c, (long long)N * pieces * 8, v);
+        }
+        if (GRADS && piece == 0) {
+            float a = 0.f;
+            for (int t = 0; t < given.T; ++t) {
+                const long long word = given.tags[(long long)n * given.T + t];
+                if (word >= 0) a += word < given.V ? given.dlogp[(long long)n * given.T + t] : __builtin_nanf("");
+            }
+            o.a[to] = a;
+            o.b[to] = given.dentropy ? given.dentropy[n] : 0.f;
+            o.sums[to] = make_float4(given.state[3LL * n], given.state[3LL * n + 1], given.state[3LL * n + 2], 0.f);
+        }
+    } else if (dx) {
+        T *row = dx + (long long)n * D + c;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (c + e < D) row[e] = 0;
+    }
+}
+
+// A group's scores: the largest, and the second largest with the place of the largest in its last five bits.
+struct __attribute__((aligned(8))) Group {
+    float first;
+    unsigned second;
+};
+
+// Per wave and row: (largest score m, sum of exp(l - m) without one of the largest, sum of exp(l - m) (m - l)), and the groups.  A distance m - l is
+// not negative, so distances compare as whole numbers, infinite and NaN ones as the largest; its last five bits make room for the word's place
+// in the group.
+template <typename T>
+struct LogpEpi {
+    float4 *stats;       // [wave's columns][stats_ld]
+    long long stats_ld;
+    Group *groups;       // [M][groups_ld], groups_ld even
+    int groups_ld;
+    template <int MT, int NT>
+    __device__ __forceinline__ void run(f32x16 (&acc)[MT][NT], int m0, int n0, int lane, int M, int V, int, char *) const {
+        static_assert(NT == 2 || NT == 4, "half the groups of a row for each of its two lanes");
+        const int h = lane >> 5;
+        for_blocks<MT>([&](auto block) __attribute__((always_inline)) {
+            constexpr int i = decltype(block)::value;
+            const int m = m0 + 32 * i + (lane & 31);
+            int end = V - n0 - 4 * h;   // columns of this wave that exist, as this lane counts: 0 .. 3, 8 .. 11, ..
+            asm volatile("" : "+v"(end));
+            if (__any(end < NT * 32)) {
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (32 * j + 8 * (e >> 2) + (e & 3) >= end) acc[i][j][e] = -__builtin_inff();
+            }
+            float top = -__builtin_inff();
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) top = fmaxf(top, acc[i][j][e]);
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float base = top == -__builtin_inff() ? 0.f : top;   // all scores -inf: exponentials of 0, not of NaN
+            float sum = 0.f, part = 0.f, apart = 0.f;   // of exponentials, of those below one, of those times the distance
+            Group g[NT];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                unsigned near = 0xffffffffu, next = 0xffffffffu;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float d = base - acc[i][j][e];
+                    const float p = sizeof(T) == 4 ? expf(-d) : __builtin_amdgcn_exp2f(d * -1.44269504f);
+                    sum += p;
+                    part += __builtin_amdgcn_fractf(p);
+                    apart += p * fminf(d, 256.f);   // beyond, and where l = -inf, p is zero
+                    const unsigned key = (__builtin_bit_cast(unsigned, d) & ~31u) | (8 * (e >> 2) + (e & 3) + 4 * h);
+                    next = max(min(near, next), min(max(near, next), key));
+                    near = min(near, key);
+                }
+                const unsigned near2 = __shfl_xor((int)near, 32), next2 = __shfl_xor((int)next, 32);
+                next = min(min(next, next2), max(near, near2));
+                near = min(near, near2);
+                g[j].first = base - __builtin_bit_cast(float, near & ~31u);
+                const float second = fmaxf(base - __builtin_bit_cast(float, next & ~31u), -3.4028234664e38f);   // 0xffffffff, NaN and infinity: none
+                g[j].second = (__builtin_bit_cast(unsigned, second) & ~31u) | (near & 31u);
+            }
+            sum += __shfl_xor(sum, 32);
+            part += __shfl_xor(part, 32);
+            apart += __shfl_xor(apart, 32);
+            if (m >= M) return;
+            // what reaches one are the largest scores; one of them is left out
+            const float rest = top == -__builtin_inff() ? sum * 0.f : part + (rintf(sum - part) - 1.f);
+            if (h == 0) stats[(n0 / (NT * 32)) * stats_ld + m] = make_float4(top, rest, apart, 0.f);
+            Group *const to = groups + (long long)m * groups_ld + n0 / kGroupWords + h * (NT / 2);
+            if (n0 + 32 * (h * (NT / 2)) < V) {
+                if constexpr (NT == 4) {   // the pair's second may be behind the last word, where the row still has room
+                    const Group a = h ? g[2] : g[0], b = h ? g[3] : g[1];
+                    *(u32x4 *)to = (u32x4){__builtin_bit_cast(unsigned, a.first), a.second, __builtin_bit_cast(unsigned, b.first), b.second};
+                } else {
+                    *to = h ? g[1] : g[0];
+                }
+            }
+        });
+    }
+};
+
+struct Joined {
+    float top, rest, apart;
+    __device__ __forceinline__ void join(float t, float r, float u) {
+        if (t > top) {
+            float s = t;
+            t = top, top = s;
+            s = r, r = rest, rest = s;
+            s = u, u = apart, apart = s;
+        }
+        if (t != -__builtin_inff()) {
+            const float d = top - t, f = expf(-d);
+            apart += f * (u + fminf(d, 256.f) * (1.f + r));
+            rest += f * (1.f + r);
+        } else {
+            rest += r * 0.f;   // nothing, unless it is NaN
+        }
+    }
+};
+
+// Joins the tiles of R rows, as lse_kernel in xent.hpp does.
+template <int R>
+static __global__ __launch_bounds__(256) void logp_join_kernel(const float4 *stats, long long stats_ld, int tiles, LogpRows o, int first, int most) {
+    constexpr int P = 256 / R;
+    const int M = live(most, o.count, first);
+    const int row = threadIdx.x % R, part = threadIdx.x / R, m = blockIdx.x * R + row;
+    __shared__ Joined all[P][R + 1];
+    Joined s = {-__builtin_inff(), 0.f, 0.f};
+    if (m < M)
+        for (int t = part; t < tiles; t += 4 * P) {   // four loads in flight
+            float4 v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = stats[min(t + k * P, tiles - 1) * stats_ld + m];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (t + k * P < tiles) s.join(v[k].x, v[k].y, v[k].z);
+        }
+    all[part][row] = s;
+    for (int w = P / 2; w; w >>= 1) {
+        __syncthreads();
+        if (part < w) {
+            const Joined b = all[part + w][row];
+            s.join(b.top, b.rest, b.apart);
+            all[part][row] = s;
+        }
+    }
+    if (part == 0 && m < M) {
+        const float log_sum = __builtin_isfinite(s.top) ? log1pf(s.rest) : __builtin_nanf("");   // no softmax without a finite largest score
+        o.sums[first + m] = make_float4(s.top, log_sum, log_sum + s.apart / (1.f + s.rest), 0.f);
+    }
+}
+
+// sum_k x[k] w[k] in 64 bits by one wave; the same bits for the same rows, whoever asks
+template <typename T>
+__device__ __forceinline__ double wave_dot(const T *x, const T *w, int D, int lane) {
+    double s = 0.0;
+    for (int c = lane * 8; c < D; c += 512) {
+        float a[8], b[8];
+        load8(x, c, D, a);
+        load8(w, c, D, b);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s = __builtin_fma((double)a[e], (double)b[e], s);
+    }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
+    return s;
+}
+
+// One row a workgroup: its likeliest words, the log probabilities of its given words, and what the joined sums say.
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS) void logp_answer_kernel(const T *x, const T *w, const int64_t *tags, const Group *groups, int groups_ld, LogpRows o,
+                                                             LogpOut out, int first, int most, int D, int V) {
+    constexpr int WAVES = THREADS / 64;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tid = threadIdx.x;
+    __shared__ float tops[THREADS];
+    __shared__ double score[kCandidates];
+    __shared__ int word[kCandidates];
+    __shared__ float limit, best;
+    __shared__ double base64;
+    __shared__ int found;
+    __shared__ unsigned long long picked[WAVES];
+    const int m = blockIdx.x;
+    if (m >= live(most, o.count, first)) return;
+    const long long n = o.index ? o.index[first + m] : first + m;
+    const float4 sums = o.sums[first + m];
+    if (tid == 0) {
+        if (out.entropy) out.entropy[n] = sums.z;
+        if (out.state) out.state[3 * n] = sums.x, out.state[3 * n + 1] = sums.y, out.state[3 * n + 2] = sums.z;
+    }
+    if (!(sums.y == sums.y)) {   // no distribution
+        for (int k = tid; k < out.K; k += THREADS) out.top[n * out.K + k] = -1, out.top_logp[n * out.K + k] = __builtin_nanf("");
+        for (int t = tid; t < out.T; t += THREADS) out.logp[n * out.T + t] = tags[n * out.T + t] >= 0 ? __builtin_nanf("") : 0.f;
+        return;
+    }
+    const int G = (V + kGroupWords - 1) / kGroupWords, K = max(out.K, 1);
+    const Group *const row = groups + (long long)m * groups_ld;
+    float own = -__builtin_inff();
+    for (int g = tid; g < G; g += THREADS) own = fmaxf(own, row[g].first);
+    tops[tid] = own;
+    if (tid == 0) found = 0, limit = -__builtin_inff();
+    __syncthreads();
+    {   // K of these maxima are at least as large as the K-th: as many words' scores are
+        int above = 0;
+        for (int t = 0; t < THREADS; ++t) {
+            const float v = tops[t];
+            above += v > own || (v == own && t < tid);
+        }
+        if (above == 0) best = own;
+        if (above == K - 1) limit = own;
+    }
+    __syncthreads();
+    // what a product of tiles, and the places in a group, may be off by
+    const float at_least = limit - 0x1p-16f * fmaxf(fabsf(limit), fabsf(best));
+    const float cut = limit == -__builtin_inff() ? limit : at_least;
+    for (int g = tid; g < G; g += THREADS) {
+        const Group v = row[g];
+        if (!(v.first >= cut)) continue;
+        const unsigned u = v.second;
+        if (__builtin_bit_cast(float, u) >= cut) {
+            const int words = min(kGroupWords, V - g * kGroupWords), at = atomicAdd(&found, words);
+            for (int k = 0; k < words; ++k)
+                if (at + k < kCandidates) word[at + k] = g * kGroupWords + k;
+        } else {
+            const int at = atomicAdd(&found, 1);
+            if (at < kCandidates) word[at] = g * kGroupWords + (int)(u & 31u);
+        }
+    }
+    __syncthreads();
+    int candidates = found;
+    if (candidates > kCandidates) {
+        // Many words share nearly the same score.  The K groups whose largest scores come first hold the K first words, as far as
+        // the product's scores tell; all of their words are candidates.
+        unsigned long long last = ~0ull;   // a score as a whole number that orders alike, then the groups from the last to the first
+        candidates = 0;
+        for (int k = 0; k < min(K, G); ++k) {
+            unsigned long long mine = 0;
+            for (int g = tid; g < G; g += THREADS) {
+                const float f = row[g].first + 0.f;   // one zero
+                const unsigned u = __builtin_bit_cast(unsigned, f);
+                const unsigned long long key = (unsigned long long)(u & 0x80000000u ? ~u : u | 0x80000000u) << 32 | (unsigned)(0x7fffffff - g);
+                if (key < last && key > mine) mine = key;
+            }
+#pragma unroll
+            for (int d = 32; d; d >>= 1) {
+                const unsigned long long other = __shfl_xor(mine, d);
+                mine = other > mine ? other : mine;
+            }
+            __syncthreads();
+            if (lane == 0) picked[wave] = mine;
+            __syncthreads();
+            for (int v = 0; v < WAVES; ++v) mine = picked[v] > mine ? picked[v] : mine;
+            last = mine;
+            const int g = 0x7fffffff - (int)(unsigned)mine, words = min(kGroupWords, V - g * kGroupWords);
+            if (tid < words) word[candidates + tid] = g * kGroupWords + tid;
+            candidates += words;
+        }
+        __syncthreads();
+    }
+    for (int c = wave; c < candidates; c += WAVES) {
+        const double s = wave_dot(x + n * D, w + (long long)word[c] * D, D, lane);
+        if (lane == 0) score[c] = s;
+    }
+    __syncthreads();
+    for (int c = tid; c < candidates; c += THREADS) {
+        const double s = score[c];
+        const int v = word[c];
+        int rank = 0;
+        for (int k = 0; k < candidates; ++k) rank += score[k] > s || (score[k] == s && word[k] < v);
+        if (rank == 0) base64 = s;
+        if (rank < out.K) out.top[n * out.K + rank] = v;
+    }
+    __syncthreads();
+    for (int c = tid; out.K && c < candidates; c += THREADS) {
+        const double s = score[c];
+        int rank = 0;
+        for (int k = 0; k < candidates; ++k) rank += score[k] > s || (score[k] == s && word[k] < word[c]);
+        if (rank < out.K) out.top_logp[n * out.K + rank] = (float)(s - base64) - sums.y;
+    }
+    for (int t = wave; t < out.T; t += WAVES) {
+        const long long v = tags[n * out.T + t];
+        float lp = 0.f;
+        if (v >= V) lp = __builtin_nanf("");
+        else if (v >= 0) lp = (float)fmin(wave_dot(x + n * D, w + v * D, D, lane) - base64, 0.0) - sums.y;
+        if (lane == 0) out.logp[n * out.T + t] = lp;
+    }
+}
+
+// Rows without a word.
+static __global__ __launch_bounds__(256) void logp_masked_kernel(const int *place, LogpOut out, int N) {
+    const int n = blockIdx.x * 256 + threadIdx.x;
+    if (n >= N || place[n] >= 0) return;
+    if (out.entropy) out.entropy[n] = 0.f;
+    if (out.state)
+        for (int k = 0; k < 3; ++k) out.state[3LL * n + k] = 0.f;
+    for (int t = 0; t < out.T; ++t) out.logp[(long long)n * out.T + t] = 0.f;
+    for (int k = 0; k < out.K; ++k) out.top[(long long)n * out.K + k] = -1, out.top_logp[(long long)n * out.K + k] = 0.f;
+}
+
+// d of a row and word that is not given.  l - base first: the sum of both would be rounded at the scores' size
+template <typename T>
+__device__ __forceinline__ float logp_grad(float l, const float4 &sums, float a, float b) {
+    const float lp = (l - sums.x) - sums.y;
+    const float p = sizeof(T) == 4 ? expf(lp) : __builtin_amdgcn_exp2f(lp * 1.44269504f);
+    return -p * (a + b * (fmaxf(lp, -256.f) + sums.z));
+}
+
+// V: bf16_t or float, what d is stored as; [M][ld], zeros behind the last word.
+template <typename T, typename V>
+struct LogpGradEpi {
+    V *d;
+    long long ld;
+    const float4 *sums;
+    const float *a, *b;
+    template <int MT, int NT>
+    __device__ __forceinline__ void run(f32x16 (&acc)[MT][NT], int m0, int n0, int lane, int M, int words, int, char *lds) const {
+        const RowStage<V, NT * 32> stage = {lds, lane};
+        const int h = lane >> 5;
+        float4 s[MT];
+        float ra[MT], rb[MT];   // all before the first store: a load behind a store waits until that has reached memory
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            const int m = min(m0 + 32 * i + (lane & 31), M - 1);
+            s[i] = sums[m], ra[i] = a[m], rb[i] = b[m];
+        }
+        for_blocks<MT>([&](auto block) __attribute__((always_inline)) {
+            constexpr int i = decltype(block)::value;
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int c = 32 * j + 8 * q + 4 * h;
+                    V v[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float g = logp_grad<T>(acc[i][j][4 * q + r], s[i], ra[i], rb[i]);
+                        v[r] = narrow<V>(n0 + c + r < words ? g : 0.f);
+                    }
+                    stage.put(c, v);
+                }
+            stage.take([&](int r, int c, const u32x4 &w) {
+                const int to = m0 + 32 * i + r;
+                if (to < M && n0 + c < ld) *(u32x4 *)(d + to * ld + n0 + c) = w;
+            });
+        });
+    }
+};
+
+// d where words are given, once for each word of a row.
+template <typename V>
+__global__ __launch_bounds__(256) void logp_given_kernel(V *d, long long ld, LogpRows o, LogpGiven g, const float *logp, int first, int most) {
+    const long long at = blockIdx.x * 256LL + threadIdx.x;
+    const int m = (int)(at / g.T), t = (int)(at - (long long)m * g.T);
+    if (m >= live(most, o.count, first)) return;
+    const long long n = o.index ? o.index[first + m] : first + m;
+    const int64_t *const words = g.tags + n * g.T;
+    const float *const da = g.dlogp + n * g.T;
+    const long long v = words[t];
+    if (v < 0 || v >= g.V) return;
+    float s = 0.f;
+    for (int k = 0; k < g.T; ++k)
+        if (words[k] == v) {
+            if (k < t) return;
+            s += da[k];
+        }
+    const float4 sums = o.sums[first + m];
+    const float a = o.a[first + m], b = o.b[first + m], lp = logp[n * g.T + t];
+    const float p = expf(lp), own = p > 0.5f ? (s - a) - a * expm1f(lp) : s - a * p;
+    d[m * ld + v] = narrow<V>(own - b * p * (fmaxf(lp, -256.f) + sums.z));
+}
+
+// d as it is kept in fp32
+struct KeptGrad {
+    const float *d;
+    long long ld;
+    const int *count;
+    int first, most;
+    __device__ void beside() const {}
+    __device__ bool skip(int m) const { return m >= live(most, count, first); }
+    __device__ long long rows() const { return live(most, count, first); }
+    __device__ void operator()(int m, int c, float (&v)[1][8]) const {
+        const f32x4 *k = (const f32x4 *)(d + m * ld + c);
+        const f32x4 a = k[0], b = k[1];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[0][e] = a[e], v[0][4 + e] = b[e];
+    }
+};
+
+template <typename T>
+__global__ __launch_bounds__(256) void logp_zero_kernel(T *p, long long n) {
+    for (long long i = blockIdx.x * 256LL + threadIdx.x; i < n; i += gridDim.x * 256LL) p[i] = 0;
+}
+
+template <typename T>
+struct LogpScratch {
+    static constexpr int PL = Planes<T>::N;
+    int Dp, Vp, block, blocks, wave_cols, tiles, groups_ld;
+    bool direct, gathers;   // w is used where it is; rows are picked
+    LogpRows rows = {};
+    bf16_t *x = nullptr, *w = nullptr, *d = nullptr;
+    float4 *stats = nullptr;
+    Group *groups = nullptr;
+    float *kept = nullptr, *sum = nullptr;
+    Parts part = {};
+    LogpScratch(Scratch &sc, int N, int D, int V, bool given, bool grads) {
+        Dp = (int)round_up(D, 8), Vp = (int)round_up(V, 64);
+        direct = PL == 1 && D == Dp, gathers = given;
+        groups_ld = (int)round_up((V + kGroupWords - 1) / kGroupWords, 2);
+        const long long row_bytes = grads ? (long long)Vp * (long long)sizeof(T) : groups_ld * (long long)sizeof(Group);
+        block = (int)std::min<long long>(round_up(N, 8), std::max<long long>(kStep, (grads ? kGradBytes : kKeyBytes) / row_bytes / 256 * 256));
+        blocks = N ? (N + block - 1) / block : 0;
+        const bool few = N <= kFewRows;
+        wave_cols = few ? 64 : product_wave_cols(block, V, D, Planes<T>::PAIRS);
+        tiles = (V + wave_cols - 1) / wave_cols;
+        rows.count = sc.take<int>(1);
+        rows.place = sc.take<int>(N);
+        rows.index = sc.take<int>(N);
+        rows.sums = sc.take<float4>(N);
+        rows.a = sc.take<float>(N);
+        rows.b = sc.take<float>(N);
+        if (!given) rows.count = rows.place = rows.index = nullptr;
+        if (grads || !few) {
+            x = sc.take<bf16_t>((long long)PL * N * Dp);
+            w = direct ? nullptr : sc.take<bf16_t>((long long)PL * V * Dp);
+        }
+        if (!grads) {
+            stats = sc.take<float4>((V + 63) / 64 * (long long)block);
+            groups = sc.take<Group>((long long)block * groups_ld);
+            return;
+        }
+        const int twice = PL == 1 ? 2 * std::min(N, kFewRows) : 0;
+        d = sc.take<bf16_t>((long long)Vp * std::max(PL * block, twice));
+        kept = sc.take<float>((long long)Vp * (PL == 3 ? block : std::min(N, kFewRows)));
+        part.floats = std::max({part_floats(std::max(block, twice), D, V), part_floats(V, D, block), twice * round_up(D, 4)});
+        part.at = sc.take<float>(part.floats);
+        sum = blocks > 1 ? sc.take<float>((long long)V * D) : nullptr;
+    }
+    int lay_out(const T *xs, const T *ws, T *dx, const LogpGiven &given, bool grads, int N, int D, int V, hipStream_t s) const {
+        if (gathers) {
+            const LaunchPlan p = make_plan("logp_rows", {}, {N, given.T}, dim3(1), 1024, 0);
+            LC_LAUNCH(p, "logp (rows)", logp_rows_kernel, s, given.tags, N, given.T, rows);
+        }
+        if (x) {
+            const long long n = ((long long)N * (Dp / 8) + 255) / 256;
+            const LaunchPlan p = make_plan("logp_gather", {PL, grads}, {N, D}, dim3((unsigned)n), 256, 0);
+            LC_PLAN_REQUIRE(p, n <= 0x7fffffffLL);
+            if (grads) LC_LAUNCH(p, "logp (x)", (logp_gather_kernel<T, true>), s, xs, x, dx, rows, given, N, D, Dp / 8);
+            else LC_LAUNCH(p, "logp (x)", (logp_gather_kernel<T, false>), s, xs, x, dx, rows, given, N, D, Dp / 8);
+        }
+        if (w) return launch_planes<PL, 1>("logp (w)", Stored<T>{ws, V, D}, w, Dp, (long long)V * Dp, V, Dp, 0, s);
+        return LC_OK;
+    }
+};
+
+template <typename T>
+int logp_forward(const T *x, const T *w, const int64_t *tags, const LogpOut &out, int N, int D, int V, void *ws, hipStream_t s) {
+    constexpr int PL = Planes<T>::N;
+    if (N == 0) return LC_OK;
+    Scratch sc(ws);
+    const LogpScratch<T> g(sc, N, D, V, out.T > 0, false);
+    if (int rc = g.lay_out(x, w, nullptr, LogpGiven{tags, nullptr, nullptr, nullptr, out.T, V}, false, N, D, V, s)) return rc;
+    if (g.gathers) {
+        const LaunchPlan p = make_plan("logp_masked", {}, {N}, dim3(ceil_div(N, 256)), 256, 0);
+        LC_LAUNCH(p, "logp (masked)", logp_masked_kernel, s, g.rows.place, out, N);
+    }
+    const bool few = N <= kFewRows;
+    const Operand W = g.w ? Operand{g.w, g.w, g.Dp, (long long)V * g.Dp, V, 0, 0} : Operand{(const bf16_t *)w, (const bf16_t *)w, D, 0, V, 0, 0};
+    for (int b = 0; b < g.blocks; ++b) {
+        const int first = b * g.block, most = std::min(g.block, N - first);
+        const LogpEpi<T> epi = {g.stats, g.block, g.groups, g.groups_ld};
+        int rc;
+        if (few) {
+            rc = launch_few<T, ROW>("logp (few rows)", FewOperand<T>{x, x, D, N, g.rows.index}, FewOperand<T>{w, w, D, V, nullptr}, N, g.rows.count, V, D,
+                                    epi, s);
+        } else {
+            const Operand X = {g.x + (long long)first * g.Dp, g.x, g.Dp, (long long)N * g.Dp, most, 0, 0};
+            const Shape sh = {most, V, D, g.rows.count, first, nullptr, 0};
+            rc = launch_cut<PL, ROW, ROW>("logp", X, W, sh, choose_cut(g.block, V, D, Planes<T>::PAIRS, false), epi, s);
+        }
+        if (rc) return rc;
+        if (most >= 2048) {
+            const LaunchPlan p = make_plan("logp_join", {16}, {most}, dim3((most + 15) / 16), 256, 0);
+            LC_LAUNCH(p, "logp (join)", logp_join_kernel<16>, s, g.stats, (long long)g.block, g.tiles, g.rows, first, most);
+        } else {
+            const LaunchPlan p = make_plan("logp_join", {1}, {most}, dim3(most), 256, 0);
+            LC_LAUNCH(p, "logp (join)", logp_join_kernel<1>, s, g.stats, (long long)g.block, g.tiles, g.rows, first, most);
+        }
+        const LaunchPlan p = make_plan("logp_answer", {(int)sizeof(T)}, {most, D, V, out.T, out.K}, dim3(most), 256, 0);
+        LC_LAUNCH(p, "logp (answer)", (logp_answer_kernel<T, 256>), s, x, w, tags, g.groups, g.groups_ld, g.rows, out, first, most, D, V);
+    }
+    return LC_OK;
+}
+
+template <typename T>
+int logp_backward(const T *x, const T *w, const int64_t *tags, const float *logp, const float *state, const float *dlogp, const float *dentropy, T *dx,
+                  T *dw, int N, int D, int V, int given_words, void *ws, hipStream_t s) {
+    constexpr int PL = Planes<T>::N;
+    if (N == 0) {
+        const long long n = (long long)V * D;
+        const LaunchPlan p = make_plan("logp_zero", {}, {}, dim3((unsigned)std::min<long long>((n + 255) / 256, 4096)), 256, 0);
+        LC_LAUNCH(p, "logp_bwd (no rows)", (logp_zero_kernel<T>), s, dw, n);
+        return LC_OK;
+    }
+    Scratch sc(ws);
+    const LogpScratch<T> g(sc, N, D, V, given_words > 0, true);
+    const LogpGiven given = {tags, state, dlogp, dentropy, given_words, V};
+    if (int rc = g.lay_out(x, w, dx, given, true, N, D, V, s)) return rc;
+    const bool few = N <= kFewRows, fine = few && PL == 1;   // fine: d in two parts
+    Operand W = g.w ? Operand{g.w, g.w, g.Dp, (long long)V * g.Dp, V, 0, 0} : Operand{(const bf16_t *)w, (const bf16_t *)w, D, 0, V, 0, 0};
+    for (int b = 0; b < g.blocks; ++b) {
+        const int first = b * g.block, most = std::min(g.block, N - first);
+        Operand X = {g.x + (long long)first * g.Dp, g.x, g.Dp, (long long)N * g.Dp, most, 0, 0}, Wr = W;
+        const Shape sh = {most, V, D, g.rows.count, first, nullptr, 0};
+        const auto scores = [&](const auto &epi) -> int {
+            if (few)
+                return launch_few<T, ROW>("logp_bwd (few rows)", FewOperand<T>{x, x, D, N, g.rows.index}, FewOperand<T>{w, w, D, V, nullptr}, N,
+                                          g.rows.count, V, D, epi, s);
+            return launch_cut<PL, ROW, ROW>("logp_bwd", X, Wr, sh, choose_cut(g.block, V, D, Planes<T>::PAIRS, false), epi, s);
+        };
+        const auto words = [&](auto *d) -> int {
+            typedef std::remove_reference_t<decltype(*d)> Stored_t;
+            if (int rc = scores(LogpGradEpi<T, Stored_t>{d, g.Vp, g.rows.sums + first, g.rows.a + first, g.rows.b + first})) return rc;
+            if (!given_words) return LC_OK;
+            const long long n = ((long long)most * given_words + 255) / 256;
+            const LaunchPlan p = make_plan("logp_given", {}, {most, given_words}, dim3((unsigned)n), 256, 0);
+            LC_PLAN_REQUIRE(p, n <= 0x7fffffffLL);
+            LC_LAUNCH(p, "logp_bwd (given)", (logp_given_kernel<Stored_t>), s, d, (long long)g.Vp, g.rows, given, logp, first, most);
+            return LC_OK;
+        };
+        int rc;
+        const bool kept = PL == 3 || fine;
+        if ((rc = kept ? words(g.kept) : words(g.d))) return rc;
+        const int *const index = g.rows.index ? g.rows.index + first : nullptr;
+        const KeptGrad from = {g.kept, g.Vp, g.rows.count, first, most};
+        T *const to = dx && !index ? dx + (long long)first * D : dx;
+        if constexpr (PL == 1)
+            if (fine) {   // one block
+                const int two = 2 * N;
+                if ((rc = launch_planes<2, 1>("logp_bwd (d)", from, g.d, g.Vp, 0, N, g.Vp, 0, s))) return rc;
+                Operand d = {g.d, g.d, g.Vp, 0, two, 0, 0};
+                Wr.rows = X.rows = g.Dp;
+                if (dx) {
+                    const Shape shx = {two, D, V, g.rows.count, 0, nullptr, 0, 2};
+                    if ((rc = launch_product<PL, ROW, COL, true>("logp_bwd (dx)", d, Wr, shx, StoreEpi<T>{dx, nullptr, 0x7fffffff, N, 0, D, index, nullptr, nullptr},
+                                                                 g.part, s)))
+                        return rc;
+                }
+                const Shape shw = {V, D, two, nullptr, 0, g.rows.count, 0, 2};
+                d.rows = g.Vp;
+                return launch_gemm<2, COL, COL>("logp_bwd (dw)", d, X, shw, StoreEpi<T>{dw, nullptr, 0x7fffffff, V, 0, D, nullptr, nullptr, nullptr}, s);
+            }
+        const long long pd = (long long)g.block * g.Vp;
+        if (kept && (rc = launch_planes<PL, 1>("logp_bwd (d)", from, g.d, g.Vp, pd, most, g.Vp, 0, s))) return rc;
+        Operand d = {g.d, g.d, g.Vp, pd, most, 0, 0};
+        Wr.rows = X.rows = g.Dp;
+        if (dx) {
+            const Shape shx = {most, D, V, g.rows.count, first, nullptr, 0};
+            if ((rc = launch_product<PL, ROW, COL>("logp_bwd (dx)", d, Wr, shx, StoreEpi<T>{to, nullptr, 0x7fffffff, most, 0, D, index, nullptr, nullptr}, g.part, s)))
+                return rc;
+        }
+        const Shape shw = {V, D, most, nullptr, 0, g.rows.count, first};
+        d.rows = g.Vp;
+        const float *add = b ? g.sum : nullptr;
+        if (b + 1 < g.blocks)
+            rc = launch_product<PL, COL, COL>("logp_bwd (dw)", d, X, shw, StoreEpi<float>{g.sum, nullptr, 0x7fffffff, V, 0, D, nullptr, add, nullptr}, g.part, s);
+        else
+            rc = launch_product<PL, COL, COL>("logp_bwd (dw)", d, X, shw, StoreEpi<T>{dw, nullptr, 0x7fffffff, V, 0, D, nullptr, add, nullptr}, g.part, s);
+        if (rc) return rc;
+    }
+    return LC_OK;
+}
+
+template <typename T>
+size_t logp_scratch(int N, int D, int V, bool given, bool grads) {
+    Scratch sc(nullptr);
+    (void)LogpScratch<T>(sc, N, D, V, given, grads);
+    return sc.used;
+}
+
+}  // namespace head
+}  // namespace lc

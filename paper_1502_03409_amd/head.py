@@ -18,7 +18,7 @@ LC_ACT_SIGMOID, LC_ACT_SILU, LC_ACT_GELU = 0, 1, 2
 
 HEAD_EXPORTS = ("glu_workspace_bytes", "glu_fwd", "glu_bwd", "xent_workspace_bytes", "xent_fwd", "xent_fwd_bwd",
                 "grad_clip_workspace_bytes", "grad_norm", "grad_clip", "q8_row_bytes", "q8_rows", "q8_workspace_bytes", "q8_matmul",
-                "q8_glu_fwd", "muon_workspace_bytes", "muon_step")
+                "q8_glu_fwd", "muon_workspace_bytes", "muon_step", "logp_workspace_bytes", "logp_fwd", "logp_bwd")
 
 __all__ = ["LC_ACT_SIGMOID", "LC_ACT_SILU", "LC_ACT_GELU", *HEAD_EXPORTS]
 
@@ -44,6 +44,9 @@ def _lib() -> C.CDLL:
         L.q8_workspace_bytes.argtypes = [i32, i32, i32, C.c_int]
         L.q8_matmul.argtypes = [vp] * 4 + [i32, i32, i32, C.c_int, vp, sz, vp]
         L.q8_glu_fwd.argtypes = [vp] * 6 + [i32, i32, i32, C.c_int, C.c_int, vp, sz, vp]
+        L.logp_workspace_bytes.argtypes = [i32] * 5 + [C.c_int, C.c_int]
+        L.logp_fwd.argtypes = [vp] * 8 + [i32] * 5 + [C.c_int, vp, sz, vp]
+        L.logp_bwd.argtypes = [vp] * 9 + [i32] * 4 + [C.c_int, vp, sz, vp]
         L.muon_workspace_bytes.argtypes = [i32, i32, i32, C.c_int]
         L.muon_step.argtypes = [vp] * 5 + [i32, i32, i32, f32, f32, f32, C.c_int, i32, C.c_int, vp, sz, vp]
         for name in HEAD_EXPORTS:
@@ -192,4 +195,33 @@ def muon_step(w, g, m, w_out, m_out, rate: float, decay: float = 0.0, momentum: 
     _b._check("muon_step", _lib().muon_step(
         _dev(w, shape, dt, "w"), _dev(g, shape, dt, "g"), _dev(m, shape, torch.float32, "m"), _dev(w_out, shape, dt, "w_out"),
         _dev(m_out, shape, torch.float32, "m_out"), count, rows, cols, rate, decay, momentum, int(nesterov), steps, dtype, wp, wb,
+        _b._stream()))
+
+
+def logp_workspace_bytes(N: int, D: int, V: int, T: int, K: int, dtype: int = LC_F32, grads: bool = False) -> int:
+    return int(_lib().logp_workspace_bytes(N, D, V, T, K, dtype, int(grads)))
+
+
+def logp_fwd(x, w, tags, logp, entropy, top, top_logp, state, dtype: int = LC_F32, ws=None) -> None:
+    """``tags`` None: no words are given; ``top`` None: none are asked for."""
+    (N, D), V = x.shape, w.shape[0]
+    T, K = 0 if tags is None else tags.shape[1], 0 if top is None else top.shape[1]
+    dt = _b._op_dtype(dtype)
+    wp, wb = _b._ws(ws)
+    _b._check("logp_fwd", _lib().logp_fwd(
+        _dev(x, (N, D), dt, "x"), _dev(w, (V, D), dt, "w"), _dev(tags, (N, T), torch.int64, "tags"),
+        _dev(logp, (N, T), torch.float32, "logp"), _dev(entropy, (N,), torch.float32, "entropy"), _dev(top, (N, K), torch.int64, "top"),
+        _dev(top_logp, (N, K), torch.float32, "top_logp"), _dev(state, (N, 3), torch.float32, "state"), N, D, V, T, K, dtype, wp, wb,
+        _b._stream()))
+
+
+def logp_bwd(x, w, tags, logp, state, dlogp, dentropy, dx, dw, dtype: int = LC_F32, ws=None) -> None:
+    (N, D), V = x.shape, w.shape[0]
+    T = 0 if tags is None else tags.shape[1]
+    dt = _b._op_dtype(dtype)
+    wp, wb = _b._ws(ws)
+    _b._check("logp_bwd", _lib().logp_bwd(
+        _dev(x, (N, D), dt, "x"), _dev(w, (V, D), dt, "w"), _dev(tags, (N, T), torch.int64, "tags"),
+        _dev(logp, (N, T), torch.float32, "logp"), _dev(state, (N, 3), torch.float32, "state"), _dev(dlogp, (N, T), torch.float32, "dlogp"),
+        _dev(dentropy, (N,), torch.float32, "dentropy"), _dev(dx, (N, D), dt, "dx"), _dev(dw, (V, D), dt, "dw"), N, D, V, T, dtype, wp, wb,
         _b._stream()))
