@@ -25,8 +25,6 @@ namespace head {
 constexpr long long kKeyBytes = 512LL << 20;      // groups' scores kept at a time
 constexpr long long kGradBytes = 2LL << 30;       // of d
 constexpr int kGroupWords = 32;
-constexpr int kMostTop = 64, kMostGiven = 64;     // words asked for and given a row
-constexpr int kCandidates = kMostTop * kGroupWords;
 
 struct LogpRows {
     int *count, *place, *index;   // as in xent.hpp; null: all rows count
@@ -34,8 +32,18 @@ struct LogpRows {
     float *a, *b;                 // by position: A and b
 };
 
-// Positions of the rows that have a word.  One workgroup, 1024 rows at a time.
-static __global__ __launch_bounds__(1024) void logp_rows_kernel(const int64_t *tags, int N, int T, LogpRows o) {
+// What a row without a word is answered.
+__device__ __forceinline__ void answer_masked(const LogpOut &out, long long n) {
+    if (out.entropy) out.entropy[n] = 0.f;
+    if (out.state)
+        for (int k = 0; k < 3; ++k) out.state[3 * n + k] = 0.f;
+    if (out.logp)
+        for (int t = 0; t < out.T; ++t) out.logp[n * out.T + t] = 0.f;
+    for (int k = 0; k < out.K; ++k) out.top[n * out.K + k] = -1, out.top_logp[n * out.K + k] = 0.f;
+}
+
+// Positions of the rows that have a word; the answers of those that have none.  One workgroup, 1024 rows at a time.
+static __global__ __launch_bounds__(1024) void logp_rows_kernel(const int64_t *tags, int N, int T, LogpRows o, LogpOut out) {
     __shared__ int part[16];
     __shared__ int total;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -54,6 +62,7 @@ static __global__ __launch_bounds__(1024) void logp_rows_kernel(const int64_t *t
         at += __popcll(mask & ((1ull << lane) - 1));
         if (n < N) o.place[n] = in ? at : -1;
         if (in) o.index[at] = n;
+        else if (n < N) answer_masked(out, n);
         __syncthreads();
         if (threadIdx.x == 0)
             for (int w = 0; w < 16; ++w) total += part[w];
@@ -199,25 +208,34 @@ struct Joined {
     }
 };
 
-// Joins the tiles of R rows, as lse_kernel in xent.hpp does.
-template <int R>
-static __global__ __launch_bounds__(256) void logp_join_kernel(const float4 *stats, long long stats_ld, int tiles, LogpRows o, int first, int most) {
-    constexpr int P = 256 / R;
-    const int M = live(most, o.count, first);
-    const int row = threadIdx.x % R, part = threadIdx.x / R, m = blockIdx.x * R + row;
-    __shared__ Joined all[P][R + 1];
+// What joined tiles say of a row: its largest score, the logarithm of the sum relative to it, the entropy.
+__device__ __forceinline__ float4 sums_of(const Joined &s) {
+    const float log_sum = __builtin_isfinite(s.top) ? log1pf(s.rest) : __builtin_nanf("");   // no softmax without a finite largest score
+    return make_float4(s.top, log_sum, log_sum + s.apart / (1.f + s.rest), 0.f);
+}
+
+// One thread's share of a row's tiles, four loads in flight.
+__device__ __forceinline__ Joined join_some(const float4 *stats, long long stats_ld, int tiles, int m, int from, int step) {
     Joined s = {-__builtin_inff(), 0.f, 0.f};
-    if (m < M)
-        for (int t = part; t < tiles; t += 4 * P) {   // four loads in flight
-            float4 v[4];
+    for (int t = from; t < tiles; t += 4 * step) {
+        float4 v[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = stats[min(t + k * P, tiles - 1) * stats_ld + m];
+        for (int k = 0; k < 4; ++k) v[k] = stats[min(t + k * step, tiles - 1) * stats_ld + m];
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (t + k * P < tiles) s.join(v[k].x, v[k].y, v[k].z);
-        }
+        for (int k = 0; k < 4; ++k)
+            if (t + k * step < tiles) s.join(v[k].x, v[k].y, v[k].z);
+    }
+    return s;
+}
+
+// Many rows: 16 a workgroup, which reads whole lines of the statistics, 16 threads each, in a fixed order.
+static __global__ __launch_bounds__(256) void logp_join_kernel(const float4 *stats, long long stats_ld, int tiles, LogpRows o, int first, int most) {
+    __shared__ Joined all[16][17];
+    const int row = threadIdx.x % 16, part = threadIdx.x / 16, m = blockIdx.x * 16 + row;
+    const bool in = m < live(most, o.count, first);
+    Joined s = join_some(stats, stats_ld, in ? tiles : 0, m, part, 16);
     all[part][row] = s;
-    for (int w = P / 2; w; w >>= 1) {
+    for (int w = 8; w; w >>= 1) {
         __syncthreads();
         if (part < w) {
             const Joined b = all[part + w][row];
@@ -225,102 +243,194 @@ static __global__ __launch_bounds__(256) void logp_join_kernel(const float4 *sta
             all[part][row] = s;
         }
     }
-    if (part == 0 && m < M) {
-        const float log_sum = __builtin_isfinite(s.top) ? log1pf(s.rest) : __builtin_nanf("");   // no softmax without a finite largest score
-        o.sums[first + m] = make_float4(s.top, log_sum, log_sum + s.apart / (1.f + s.rest), 0.f);
-    }
+    if (part == 0 && in) o.sums[first + m] = sums_of(s);
 }
 
-// sum_k x[k] w[k] in 64 bits by one wave; the same bits for the same rows, whoever asks
-template <typename T>
-__device__ __forceinline__ double wave_dot(const T *x, const T *w, int D, int lane) {
-    double s = 0.0;
-    for (int c = lane * 8; c < D; c += 512) {
-        float a[8], b[8];
-        load8(x, c, D, a);
-        load8(w, c, D, b);
+// sum_k x[k] w_i[k] in 64 bits for W rows w_i by one wave; the same bits for a row whatever W is and whoever asks.
+template <int W, typename T>
+__device__ __forceinline__ void wave_dots(const T *x, const T *const (&w)[W], int D, int lane, double (&s)[W]) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s = __builtin_fma((double)a[e], (double)b[e], s);
-    }
+    for (int i = 0; i < W; ++i) s[i] = 0.0;
+    const auto step = [&](int c, int end) __attribute__((always_inline)) {
+        float a[8], b[W][8];
 #pragma unroll
-    for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
-    return s;
+        for (int i = 0; i < W; ++i) load8(w[i], c, end, b[i]);
+        load8(x, c, end, a);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+            for (int i = 0; i < W; ++i) s[i] = __builtin_fma((double)a[e], (double)b[i][e], s[i]);
+    };
+    const int whole = D / 512 * 512;
+#pragma unroll 4
+    for (int c = lane * 8; c < whole; c += 512) step(c, c + 8);
+    if (whole + lane * 8 < D) step(whole + lane * 8, D);
+#pragma unroll
+    for (int i = 0; i < W; ++i)
+#pragma unroll
+        for (int d = 32; d; d >>= 1) s[i] += __shfl_xor(s[i], d);
 }
 
-// One row a workgroup: its likeliest words, the log probabilities of its given words, and what the joined sums say.
-template <typename T, int THREADS>
-__global__ __launch_bounds__(THREADS) void logp_answer_kernel(const T *x, const T *w, const int64_t *tags, const Group *groups, int groups_ld, LogpRows o,
-                                                             LogpOut out, int first, int most, int D, int V) {
-    constexpr int WAVES = THREADS / 64;
+// Scores in a workgroup's list: candidates, and behind them the given words.
+constexpr int most_candidates(int K) { return K * kGroupWords > 256 ? K * kGroupWords : 256; }
+
+// One row a workgroup: its likeliest words, the log probabilities of its given words, and what the joined sums say.  JOIN: joins them too, where
+// rows are few enough for their tiles not to be read by whole lines.  Bound by latency for few rows, so what one wait can bring is asked for at once;
+// for many by the groups' scores and the candidates' weights.
+template <typename T, int THREADS, bool JOIN>
+__global__ __launch_bounds__(THREADS) void logp_answer_kernel(const T *x, const T *w, const int64_t *tags, const float4 *stats, long long stats_ld, int tiles,
+                                                             const Group *groups, int groups_ld, LogpRows o, LogpOut out, int first, int most, int D,
+                                                             int V) {
+    constexpr int WAVES = THREADS / 64, HELD = 8;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tid = threadIdx.x;
-    __shared__ float tops[THREADS];
-    __shared__ double score[kCandidates];
-    __shared__ int word[kCandidates];
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    __shared__ __attribute__((aligned(16))) float tops[THREADS];
+    __shared__ float4 joined;
+    __shared__ Joined shares[WAVES];
     __shared__ float limit, best;
     __shared__ double base64;
     __shared__ int found;
     __shared__ unsigned long long picked[WAVES];
-    const int m = blockIdx.x;
+    const int m = blockIdx.x, K = max(out.K, 1), room = most_candidates(K);
+    double *const score = (double *)smem;
+    int *const word = (int *)(score + room + out.T);
     if (m >= live(most, o.count, first)) return;
     const long long n = o.index ? o.index[first + m] : first + m;
-    const float4 sums = o.sums[first + m];
+    const int G = (V + kGroupWords - 1) / kGroupWords, pairs = (G + 1) / 2;
+    const u32x4 *const row = (const u32x4 *)(groups + (long long)m * groups_ld);   // two groups at a time; behind the last one: not looked at
+    u32x4 held[HELD];   // this thread's first pairs
+#pragma unroll
+    for (int k = 0; k < HELD; ++k) held[k] = row[min(tid + k * THREADS, pairs - 1)];
+    Joined share;
+    if constexpr (JOIN) {
+        share = join_some(stats, stats_ld, tiles, m, tid, THREADS);
+#pragma unroll
+        for (int d = 32; d; d >>= 1) {
+            const Joined b = {__shfl_xor(share.top, d), __shfl_xor(share.rest, d), __shfl_xor(share.apart, d)};
+            share.join(b.top, b.rest, b.apart);
+        }
+        if (lane == 0) shares[wave] = share;
+    }
+    // fn(group, its largest score, its second largest with the largest's place) for this thread's groups
+    const auto for_groups = [&](const auto &fn) __attribute__((always_inline)) {
+        const auto both = [&](int p, const u32x4 &v) __attribute__((always_inline)) {
+            const unsigned a = v[0], a2 = v[1], b = v[2], b2 = v[3];
+            fn(2 * p, __builtin_bit_cast(float, a), a2);
+            if (2 * p + 1 < G) fn(2 * p + 1, __builtin_bit_cast(float, b), b2);
+        };
+#pragma unroll
+        for (int k = 0; k < HELD; ++k)
+            if (tid + k * THREADS < pairs) both(tid + k * THREADS, held[k]);
+        for (int p = tid + HELD * THREADS; p < pairs; p += THREADS) both(p, row[p]);
+    };
+    float own = -__builtin_inff();
+    for_groups([&](int, float f, unsigned) __attribute__((always_inline)) { own = fmaxf(own, f); });
+    // maxima of 256 parts of the groups: few groups are parts of their own
+    const bool single = pairs <= 128;
+    if (!single) {
+        tops[tid] = own;
+    } else if (tid < 128) {
+        const unsigned a = held[0][0], b = held[0][2];
+        tops[2 * tid] = tid < pairs ? __builtin_bit_cast(float, a) : -__builtin_inff();
+        tops[2 * tid + 1] = 2 * tid + 1 < G ? __builtin_bit_cast(float, b) : -__builtin_inff();
+    }
+    if (tid == 0) found = 0, limit = -__builtin_inff();
+    for (int t = tid; t < out.T; t += THREADS) {
+        const long long v = tags[n * out.T + t];
+        word[room + t] = v < 0 ? -1 : v < V ? (int)v : -2;
+    }
+    __syncthreads();
+    if (JOIN && wave == 1) {
+        share = lane < WAVES ? shares[lane] : Joined{-__builtin_inff(), 0.f, 0.f};
+#pragma unroll
+        for (int d = 8; d; d >>= 1) {
+            const Joined b = {__shfl_xor(share.top, d), __shfl_xor(share.rest, d), __shfl_xor(share.apart, d)};
+            share.join(b.top, b.rest, b.apart);
+        }
+        if (lane == 0) joined = sums_of(share);
+    }
+    const auto part_top = [&](int i) {
+        float v = tops[i];
+        if (!single)
+#pragma unroll
+            for (int k = 256; k < THREADS; k += 256) v = fmaxf(v, tops[i + k]);
+        return v;
+    };
+    // K of any number of parts' maxima are at least as large as the K-th: as many words' scores are.  64 parts are found faster, and of up to 16 the
+    // K-th lets hardly more than K words through.
+    if (K <= 16) {
+        if (wave == 0) {
+            float v = part_top(lane);
+#pragma unroll
+            for (int k = 1; k < 4; ++k) v = fmaxf(v, part_top(lane + 64 * k));
+            int above = 0;
+#pragma unroll
+            for (int t = 0; t < 64; ++t) {
+                const float b = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), t));
+                above += b > v || (b == v && t < lane);
+            }
+            if (above == 0) best = v;
+            if (above == K - 1) limit = v;
+        }
+    } else {
+        if constexpr (THREADS > 256) {
+            const float v = tid < 256 ? part_top(tid) : 0.f;
+            __syncthreads();
+            if (tid < 256) tops[tid] = v;
+            __syncthreads();
+        }
+        if (tid < 256) {
+            const float v = tops[tid];
+            int above = 0;
+#pragma unroll 4
+            for (int t = 0; t < 256; t += 4) {
+                const f32x4 b = *(const f32x4 *)(tops + t);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) above += b[k] > v || (b[k] == v && t + k < tid);
+            }
+            if (above == 0) best = v;
+            if (above == K - 1) limit = v;
+        }
+    }
+    __syncthreads();
+    const float4 sums = JOIN ? joined : o.sums[first + m];
     if (tid == 0) {
         if (out.entropy) out.entropy[n] = sums.z;
         if (out.state) out.state[3 * n] = sums.x, out.state[3 * n + 1] = sums.y, out.state[3 * n + 2] = sums.z;
     }
     if (!(sums.y == sums.y)) {   // no distribution
         for (int k = tid; k < out.K; k += THREADS) out.top[n * out.K + k] = -1, out.top_logp[n * out.K + k] = __builtin_nanf("");
-        for (int t = tid; t < out.T; t += THREADS) out.logp[n * out.T + t] = tags[n * out.T + t] >= 0 ? __builtin_nanf("") : 0.f;
+        for (int t = tid; t < out.T; t += THREADS) out.logp[n * out.T + t] = word[room + t] != -1 ? __builtin_nanf("") : 0.f;
         return;
     }
-    const int G = (V + kGroupWords - 1) / kGroupWords, K = max(out.K, 1);
-    const Group *const row = groups + (long long)m * groups_ld;
-    float own = -__builtin_inff();
-    for (int g = tid; g < G; g += THREADS) own = fmaxf(own, row[g].first);
-    tops[tid] = own;
-    if (tid == 0) found = 0, limit = -__builtin_inff();
-    __syncthreads();
-    {   // K of these maxima are at least as large as the K-th: as many words' scores are
-        int above = 0;
-        for (int t = 0; t < THREADS; ++t) {
-            const float v = tops[t];
-            above += v > own || (v == own && t < tid);
-        }
-        if (above == 0) best = own;
-        if (above == K - 1) limit = own;
-    }
-    __syncthreads();
-    // what a product of tiles, and the places in a group, may be off by
-    const float at_least = limit - 0x1p-16f * fmaxf(fabsf(limit), fabsf(best));
-    const float cut = limit == -__builtin_inff() ? limit : at_least;
-    for (int g = tid; g < G; g += THREADS) {
-        const Group v = row[g];
-        if (!(v.first >= cut)) continue;
-        const unsigned u = v.second;
-        if (__builtin_bit_cast(float, u) >= cut) {
-            const int words = min(kGroupWords, V - g * kGroupWords), at = atomicAdd(&found, words);
-            for (int k = 0; k < words; ++k)
-                if (at + k < kCandidates) word[at + k] = g * kGroupWords + k;
-        } else {
-            const int at = atomicAdd(&found, 1);
-            if (at < kCandidates) word[at] = g * kGroupWords + (int)(u & 31u);
-        }
-    }
+    // less what a product of tiles, and the places in a group, may be off by
+    const float cut = limit == -__builtin_inff() ? limit : limit - 0x1p-16f * fmaxf(fabsf(limit), fabsf(best));
+    if (own >= cut)   // few threads
+        for_groups([&](int g, float f, unsigned second) __attribute__((always_inline)) {
+            if (!(f >= cut)) return;
+            if (__builtin_bit_cast(float, second) >= cut) {
+                const int words = min(kGroupWords, V - g * kGroupWords), at = atomicAdd(&found, words);
+                for (int i = 0; i < words; ++i)
+                    if (at + i < room) word[at + i] = g * kGroupWords + i;
+            } else {
+                const int at = atomicAdd(&found, 1);
+                if (at < room) word[at] = g * kGroupWords + (int)(second & 31u);
+            }
+        });
     __syncthreads();
     int candidates = found;
-    if (candidates > kCandidates) {
+    if (candidates > room) {
         // Many words share nearly the same score.  The K groups whose largest scores come first hold the K first words, as far as
         // the product's scores tell; all of their words are candidates.
         unsigned long long last = ~0ull;   // a score as a whole number that orders alike, then the groups from the last to the first
         candidates = 0;
         for (int k = 0; k < min(K, G); ++k) {
             unsigned long long mine = 0;
-            for (int g = tid; g < G; g += THREADS) {
-                const float f = row[g].first + 0.f;   // one zero
-                const unsigned u = __builtin_bit_cast(unsigned, f);
-                const unsigned long long key = (unsigned long long)(u & 0x80000000u ? ~u : u | 0x80000000u) << 32 | (unsigned)(0x7fffffff - g);
+            for_groups([&](int g, float f, unsigned) __attribute__((always_inline)) {
+                const unsigned b = __builtin_bit_cast(unsigned, f + 0.f);   // one zero
+                const unsigned long long key = (unsigned long long)(b & 0x80000000u ? ~b : b | 0x80000000u) << 32 | (unsigned)(0x7fffffff - g);
                 if (key < last && key > mine) mine = key;
-            }
+            });
 #pragma unroll
             for (int d = 32; d; d >>= 1) {
                 const unsigned long long other = __shfl_xor(mine, d);
@@ -337,44 +447,49 @@ __global__ __launch_bounds__(THREADS) void logp_answer_kernel(const T *x, const 
         }
         __syncthreads();
     }
-    for (int c = wave; c < candidates; c += WAVES) {
-        const double s = wave_dot(x + n * D, w + (long long)word[c] * D, D, lane);
-        if (lane == 0) score[c] = s;
-    }
+    // scores of the candidates and, behind them, of the given words
+    const int all = candidates + out.T;
+    const auto place = [&](int c) { return c < candidates ? c : room + c - candidates; };
+    const auto dots = [&](auto many) __attribute__((always_inline)) {
+        constexpr int W = decltype(many)::value;
+        for (int c = wave * W; c < all; c += WAVES * W) {
+            const T *rows[W];
+            double s[W];
+#pragma unroll
+            for (int i = 0; i < W; ++i) rows[i] = w + (long long)max(word[place(min(c + i, all - 1))], 0) * D;
+            wave_dots<W>(x + n * D, rows, D, lane, s);
+#pragma unroll
+            for (int i = 0; i < W; ++i)
+                if (lane == 0 && c + i < all) score[place(c + i)] = s[i];
+        }
+    };
+    if (all <= WAVES) dots(std::integral_constant<int, 1>());
+    else if (all <= 2 * WAVES) dots(std::integral_constant<int, 2>());
+    else dots(std::integral_constant<int, 4>());
     __syncthreads();
-    for (int c = tid; c < candidates; c += THREADS) {
+    const auto rank_of = [&](int c) {
         const double s = score[c];
         const int v = word[c];
         int rank = 0;
         for (int k = 0; k < candidates; ++k) rank += score[k] > s || (score[k] == s && word[k] < v);
-        if (rank == 0) base64 = s;
-        if (rank < out.K) out.top[n * out.K + rank] = v;
-    }
+        return rank;
+    };
+    int rank = tid < candidates ? rank_of(tid) : -1;
+    if (rank == 0) base64 = score[tid];
+    for (int c = tid + THREADS; c < candidates; c += THREADS)
+        if (rank_of(c) == 0) base64 = score[c];
     __syncthreads();
+    const double top = base64;
     for (int c = tid; out.K && c < candidates; c += THREADS) {
-        const double s = score[c];
-        int rank = 0;
-        for (int k = 0; k < candidates; ++k) rank += score[k] > s || (score[k] == s && word[k] < word[c]);
-        if (rank < out.K) out.top_logp[n * out.K + rank] = (float)(s - base64) - sums.y;
+        if (c != tid) rank = rank_of(c);
+        if (rank >= out.K) continue;
+        out.top[n * out.K + rank] = word[c];
+        out.top_logp[n * out.K + rank] = (float)(score[c] - top) - sums.y;
     }
-    for (int t = wave; t < out.T; t += WAVES) {
-        const long long v = tags[n * out.T + t];
-        float lp = 0.f;
-        if (v >= V) lp = __builtin_nanf("");
-        else if (v >= 0) lp = (float)fmin(wave_dot(x + n * D, w + v * D, D, lane) - base64, 0.0) - sums.y;
-        if (lane == 0) out.logp[n * out.T + t] = lp;
+    for (int t = tid; t < out.T; t += THREADS) {
+        const int v = word[room + t];
+        out.logp[n * out.T + t] = v == -2 ? __builtin_nanf("") : v < 0 ? 0.f : (float)fmin(score[room + t] - top, 0.0) - sums.y;
     }
-}
-
-// Rows without a word.
-static __global__ __launch_bounds__(256) void logp_masked_kernel(const int *place, LogpOut out, int N) {
-    const int n = blockIdx.x * 256 + threadIdx.x;
-    if (n >= N || place[n] >= 0) return;
-    if (out.entropy) out.entropy[n] = 0.f;
-    if (out.state)
-        for (int k = 0; k < 3; ++k) out.state[3LL * n + k] = 0.f;
-    for (int t = 0; t < out.T; ++t) out.logp[(long long)n * out.T + t] = 0.f;
-    for (int k = 0; k < out.K; ++k) out.top[(long long)n * out.K + k] = -1, out.top_logp[(long long)n * out.K + k] = 0.f;
 }
 
 // d of a row and word that is not given.  l - base first: the sum of both would be rounded at the scores' size
@@ -515,10 +630,10 @@ struct LogpScratch {
         part.at = sc.take<float>(part.floats);
         sum = blocks > 1 ? sc.take<float>((long long)V * D) : nullptr;
     }
-    int lay_out(const T *xs, const T *ws, T *dx, const LogpGiven &given, bool grads, int N, int D, int V, hipStream_t s) const {
+    int lay_out(const T *xs, const T *ws, T *dx, const LogpGiven &given, const LogpOut &out, bool grads, int N, int D, int V, hipStream_t s) const {
         if (gathers) {
             const LaunchPlan p = make_plan("logp_rows", {}, {N, given.T}, dim3(1), 1024, 0);
-            LC_LAUNCH(p, "logp (rows)", logp_rows_kernel, s, given.tags, N, given.T, rows);
+            LC_LAUNCH(p, "logp (rows)", logp_rows_kernel, s, given.tags, N, given.T, rows, out);
         }
         if (x) {
             const long long n = ((long long)N * (Dp / 8) + 255) / 256;
@@ -538,11 +653,7 @@ int logp_forward(const T *x, const T *w, const int64_t *tags, const LogpOut &out
     if (N == 0) return LC_OK;
     Scratch sc(ws);
     const LogpScratch<T> g(sc, N, D, V, out.T > 0, false);
-    if (int rc = g.lay_out(x, w, nullptr, LogpGiven{tags, nullptr, nullptr, nullptr, out.T, V}, false, N, D, V, s)) return rc;
-    if (g.gathers) {
-        const LaunchPlan p = make_plan("logp_masked", {}, {N}, dim3(ceil_div(N, 256)), 256, 0);
-        LC_LAUNCH(p, "logp (masked)", logp_masked_kernel, s, g.rows.place, out, N);
-    }
+    if (int rc = g.lay_out(x, w, nullptr, LogpGiven{tags, nullptr, nullptr, nullptr, out.T, V}, out, false, N, D, V, s)) return rc;
     const bool few = N <= kFewRows;
     const Operand W = g.w ? Operand{g.w, g.w, g.Dp, (long long)V * g.Dp, V, 0, 0} : Operand{(const bf16_t *)w, (const bf16_t *)w, D, 0, V, 0, 0};
     for (int b = 0; b < g.blocks; ++b) {
@@ -558,15 +669,23 @@ int logp_forward(const T *x, const T *w, const int64_t *tags, const LogpOut &out
             rc = launch_cut<PL, ROW, ROW>("logp", X, W, sh, choose_cut(g.block, V, D, Planes<T>::PAIRS, false), epi, s);
         }
         if (rc) return rc;
-        if (most >= 2048) {
-            const LaunchPlan p = make_plan("logp_join", {16}, {most}, dim3((most + 15) / 16), 256, 0);
-            LC_LAUNCH(p, "logp (join)", logp_join_kernel<16>, s, g.stats, (long long)g.block, g.tiles, g.rows, first, most);
-        } else {
-            const LaunchPlan p = make_plan("logp_join", {1}, {most}, dim3(most), 256, 0);
-            LC_LAUNCH(p, "logp (join)", logp_join_kernel<1>, s, g.stats, (long long)g.block, g.tiles, g.rows, first, most);
+        const bool apart = most >= 2048;
+        if (apart) {
+            const LaunchPlan p = make_plan("logp_join", {}, {most}, dim3((most + 15) / 16), 256, 0);
+            LC_LAUNCH(p, "logp (join)", logp_join_kernel, s, g.stats, (long long)g.block, g.tiles, g.rows, first, most);
         }
-        const LaunchPlan p = make_plan("logp_answer", {(int)sizeof(T)}, {most, D, V, out.T, out.K}, dim3(most), 256, 0);
-        LC_LAUNCH(p, "logp (answer)", (logp_answer_kernel<T, 256>), s, x, w, tags, g.groups, g.groups_ld, g.rows, out, first, most, D, V);
+        const int threads = most <= kComputeUnits ? 1024 : 256;
+        const LaunchPlan p = make_plan("logp_answer", {(int)sizeof(T), apart}, {most, D, V, out.T, out.K}, dim3(most), threads,
+                                       12 * (size_t)(most_candidates(std::max(out.K, 1)) + out.T));
+        if (apart)
+            LC_LAUNCH(p, "logp (answer)", (logp_answer_kernel<T, 256, false>), s, x, w, tags, g.stats, (long long)g.block, g.tiles, g.groups, g.groups_ld, g.rows,
+                      out, first, most, D, V);
+        else if (threads == 256)
+            LC_LAUNCH(p, "logp (answer)", (logp_answer_kernel<T, 256, true>), s, x, w, tags, g.stats, (long long)g.block, g.tiles, g.groups, g.groups_ld, g.rows,
+                      out, first, most, D, V);
+        else
+            LC_LAUNCH(p, "logp (answer)", (logp_answer_kernel<T, 1024, true>), s, x, w, tags, g.stats, (long long)g.block, g.tiles, g.groups, g.groups_ld, g.rows,
+                      out, first, most, D, V);
     }
     return LC_OK;
 }
@@ -584,7 +703,7 @@ int logp_backward(const T *x, const T *w, const int64_t *tags, const float *logp
     Scratch sc(ws);
     const LogpScratch<T> g(sc, N, D, V, given_words > 0, true);
     const LogpGiven given = {tags, state, dlogp, dentropy, given_words, V};
-    if (int rc = g.lay_out(x, w, dx, given, true, N, D, V, s)) return rc;
+    if (int rc = g.lay_out(x, w, dx, given, LogpOut{}, true, N, D, V, s)) return rc;
     const bool few = N <= kFewRows, fine = few && PL == 1;   // fine: d in two parts
     Operand W = g.w ? Operand{g.w, g.w, g.Dp, (long long)V * g.Dp, V, 0, 0} : Operand{(const bf16_t *)w, (const bf16_t *)w, D, 0, V, 0, 0};
     for (int b = 0; b < g.blocks; ++b) {
