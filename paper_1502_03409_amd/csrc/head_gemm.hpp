@@ -687,20 +687,16 @@ struct Cut {
 // gradients of up to 8192 rows two lose by it, 0.1 % by the estimate.
 constexpr int kMostSplits = 32;
 constexpr long long kMostParts = 1LL << 26;
-inline double tiles_of_size(int M, int Nn, int tile, int stack, bool sym) {
-    const double mt = ceil_div(M, tile);
-    return stack * (sym ? mt * (mt + 1) / 2 : mt * ceil_div(Nn, tile));
-}
-inline Cut choose_cut(int M, int Nn, int K, int pairs, bool may_split, int stack = 1, bool sym = false) {
-    const double large = tiles_of_size(M, Nn, 256, stack, sym), small = tiles_of_size(M, Nn, 128, stack, sym);
+inline Cut choose_cut(int M, int Nn, int K, int pairs, bool may_split) {
+    const double large = (double)ceil_div(M, 256) * ceil_div(Nn, 256), small = (double)ceil_div(M, 128) * ceil_div(Nn, 128);
     if (large >= 4 * kComputeUnits) return Cut{Cut::LARGE, 1};
     const int steps = ceil_div(K, kStep);
     Cut best = {Cut::SMALL, 1};
     double least = 1e30;
-    const long long result = M * round_up(Nn, 4) * stack;
+    const long long result = M * round_up(Nn, 4);
     for (int s = 1; s == 1 || (may_split && s <= kMostSplits && s <= steps / 2 && s * result <= kMostParts); ++s) {
         const double part = (double)ceil_div(steps, s) * pairs;
-        const double join = s > 1 ? 4 + 8e-6 * s * (double)M * Nn * stack / 4 : 0;
+        const double join = s > 1 ? 4 + 8e-6 * s * (double)M * Nn / 4 : 0;
         const double rounds = std::ceil(large * s / kComputeUnits), wgs = small * s;
         const double tl = rounds * (part * 1.7 + 15) + join;
         const bool deep = wgs <= kComputeUnits;

@@ -3,13 +3,18 @@
 //   m' = mu m + g;  u = g + mu m' (looking ahead) or m';  X = u / |u|;  steps times  X <- a X + b (X X^T) X + c (X X^T)^2 X;
 //   w' = (1 - decay) w - rate X.
 //
-// With S = X X^T + b / (2 c) I (or X^T X, whichever is smaller) the polynomial is P = c S S + (a - b^2 / (4 c)) I, and a step X <- P X:
-// three products and nothing to add but on a diagonal.  S and P are symmetric: tiles below the diagonal are formed and stored twice.
+// With A = X X^T (or X^T X, whichever is smaller) and S = A + b / (2 c) I the polynomial is P = c S S + (a - b^2 / (4 c)) I, and a step X <- P X:
+// products, and nothing to add but on a diagonal.  A, S and P are symmetric: tiles below the diagonal are formed and stored twice.
 //
-// Between products X, S and P are held in fp16, times powers of two.  Singular values of X lie in [0, 1.203] throughout, because |u| bounds the
-// largest and a s + b s^3 + c s^5 maps [0, 1.203] into itself, so no value of X, S, P exceeds 1.203, 1.176, 3.445 in magnitude and the powers
-// put all of them at the upper end of fp16's range: what a rounding costs is 2^-12 of values that count, an eighth of bf16's, and small ones lose
-// nothing below 2^-24 of the largest.  For bf16 weights one fp16 value is held; for fp32 weights two, a value and what its rounding leaves, 22 bits,
+// Products with the longer side are the long ones, so up to three steps go by on the short side alone: all of their A and P are polynomials of the
+// first A and commute, the next A is (P A) P, and X takes the product Q of the group's P at once.  No more than three, because a rounding of the
+// first A, r of |A| at most, grows with the square of what Q does to it: r 3.4445^4 by the third step, where it meets singular values of 0.08 and
+// more of the largest, and 3.4445^8 by the fifth.
+//
+// Between products X, A, S, P and Q are held in fp16, times powers of two.  Singular values of X lie in [0, 1.203] throughout, because |u| bounds
+// the largest and a s + b s^3 + c s^5 maps [0, 1.203] into itself, so no value of X, A, S, P exceeds 1.203, 1.447, 1.176, 3.445 in magnitude, nor
+// one of Q a power of 3.445, and the powers of two put all of them at the upper end of fp16's range: what a rounding costs is 2^-12 of values that
+// count, an eighth of bf16's, and small ones lose nothing below 2^-24 of the largest.  For bf16 weights one fp16 value is held; for fp32 weights two, a value and what its rounding leaves, 22 bits,
 // and three products of them are formed.  Sums, norms and the momentum are fp32 and more.
 #pragma once
 #include "head_planes.hpp"
@@ -20,7 +25,9 @@ namespace head {
 
 constexpr float kMuonA = 3.4445f, kMuonB = -4.7750f, kMuonC = 2.0315f;
 constexpr float kShift = kMuonB / (2.f * kMuonC), kRest = (float)(3.4445 - 4.7750 * 4.7750 / (4 * 2.0315));
-constexpr float kScaleX = 0x1p14f, kScaleS = 0x1p14f, kScaleP = 0x1p13f;   // 1.203, 1.176 and 3.445 times these stay below 2^15
+constexpr float kScaleX = 0x1p14f, kScaleA = 0x1p14f;                 // 1.203 and 1.447 times these, and 3.4445, 3.4445^2, 3.4445^3 times
+constexpr float kScaleQ[4] = {0.f, 0x1p13f, 0x1p12f, 0x1p10f};        // those, stay below 2^16 (P is the first Q)
+constexpr int kGroupSteps = 3;
 constexpr int kMostParts256 = 256;   // partial sums of a matrix's squares
 
 typedef _Float16 half_t;
@@ -117,14 +124,18 @@ __global__ __launch_bounds__(256) void muon_start_kernel(const T *g, const float
 }
 
 // A product as planes of fp16: times `factor`, `diag` added on the diagonal; zeros in the columns behind the last one up to ld.  MIRROR: the
-// result is symmetric, tiles beside the diagonal go to their mirrored place as well.
+// result is symmetric, tiles beside the diagonal go to their mirrored place as well; and where there is a second place, all goes there too, with
+// `diag2` added on the diagonal.
 template <int PLANES, bool MIRROR>
 struct PlaneEpi {
-    bf16_t *out;
+    bf16_t *out, *out2;
     long long plane, each;
     int ld;
-    float factor, diag;
-    __device__ __forceinline__ void item(int i) { out += i * each; }
+    float factor, diag, diag2;
+    __device__ __forceinline__ void item(int i) {
+        out += i * each;
+        if (MIRROR && out2) out2 += i * each;
+    }
     template <int MT, int NT>
     __device__ __forceinline__ void run(f32x16 (&acc)[MT][NT], int m0, int n0, int lane, int M, int Nn, int, char *lds) const {
         const int h = lane >> 5, l32 = lane & 31;
@@ -138,6 +149,23 @@ struct PlaneEpi {
                     const float v = acc[i][j][e] * factor + (m == n ? diag : 0.f);
                     acc[i][j][e] = n < Nn && m < M ? v : 0.f;
                 }
+        send(acc, m0, n0, lane, M, Nn, out, lds);
+        if (MIRROR && out2) {
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int m = m0 + 32 * i + l32, n = n0 + 32 * j + 8 * (e >> 2) + 4 * h + (e & 3);
+                        if (m == n && m < M) acc[i][j][e] += diag2 - diag;
+                    }
+            send(acc, m0, n0, lane, M, Nn, out2, lds);
+        }
+    }
+    template <int MT, int NT>
+    __device__ __forceinline__ void send(f32x16 (&acc)[MT][NT], int m0, int n0, int lane, int M, int Nn, bf16_t *to, char *lds) const {
+        const int h = lane >> 5, l32 = lane & 31;
         const RowStage<bf16_t, NT * 32> stage = {lds, lane};
         for_blocks<MT>([&](auto block) __attribute__((always_inline)) {
             constexpr int i = decltype(block)::value;
@@ -154,7 +182,7 @@ struct PlaneEpi {
                     }
                 stage.take([&](int r, int c, const u32x4 &w) {
                     const int m = m0 + 32 * i + r;
-                    if (m < M && n0 + c < ld) *(u32x4 *)(out + p * plane + (long long)m * ld + n0 + c) = w;
+                    if (m < M && n0 + c < ld) *(u32x4 *)(to + p * plane + (long long)m * ld + n0 + c) = w;
                 });
             }
         });
@@ -172,7 +200,7 @@ struct PlaneEpi {
                         *(bf16_t *)(lds + (8 * (e >> 2) + 4 * h + (e & 3)) * Across::PITCH + (32 * i + l32) * 2) = part(acc[i][j][e], p);
                 across.take([&](int r, int c, const u32x4 &w) {
                     const int n = n0 + 32 * j + r;
-                    if (n < Nn && m0 + c < ld) *(u32x4 *)(out + p * plane + (long long)n * ld + m0 + c) = w;
+                    if (n < Nn && m0 + c < ld) *(u32x4 *)(to + p * plane + (long long)n * ld + m0 + c) = w;
                 });
             }
         });
@@ -245,14 +273,134 @@ struct UpdateEpi {
     }
 };
 
+// The sums of a part, as PartEpi stores them: [item][part][M][ld].
+struct StackPartEpi : PartEpi {
+    int at;
+    __device__ __forceinline__ void item(int i) { at = i; }
+    template <int MT, int NT>
+    __device__ __forceinline__ void run(f32x16 (&acc)[MT][NT], int m0, int n0, int lane, int live_rows, int nn, int, char *lds) const {
+        PartEpi::run(acc, m0, n0, lane, live_rows, nn, at, lds);
+    }
+};
+
+// Adds up the parts of a symmetric product, tiles of 64 x 64 on and below the diagonal, and stores them as PlaneEpi does.  Bound by the parts.
+template <int PLANES>
+__global__ __launch_bounds__(256) void muon_join_kernel(const float *part, int splits, int n, int ldp, PlaneEpi<PLANES, true> epi) {
+    __shared__ float tile[64][65];
+    const Shape sh = {n, n, 0, nullptr, 0, nullptr, 0, 1, 1, 1};
+    int tm, tn, item;
+    tile_in_stack(sh, blockIdx.x, (n + 63) / 64, 0, 1, &tm, &tn, &item);
+    epi.item(item);
+    const int r0 = threadIdx.x / 16, c = threadIdx.x % 16 * 4;
+    f32x4 s[4] = {};
+    for (int p = 0; p < splits; ++p)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int m = min(tm * 64 + r0 + 16 * i, n - 1), at = min(tn * 64 + c, ldp - 4);
+            s[i] += *(const f32x4 *)(part + (((long long)item * splits + p) * n + m) * ldp + at);
+        }
+    const auto put = [&](bf16_t *to, int m, int k, const float (&v)[4]) {
+        typedef bf16_t V4 __attribute__((ext_vector_type(4)));
+        if (m >= n || k >= epi.ld) return;
+#pragma unroll
+        for (int p = 0; p < PLANES; ++p)
+            *(V4 *)(to + p * epi.plane + (long long)m * epi.ld + k) = (V4){epi.part(v[0], p), epi.part(v[1], p), epi.part(v[2], p), epi.part(v[3], p)};
+    };
+    const auto both = [&](int m, int k, float (&v)[4]) {   // four columns k .. k + 3 of row m
+        put(epi.out, m, k, v);
+        if (!epi.out2) return;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (m == k + e) v[e] += epi.diag2 - epi.diag;
+        put(epi.out2, m, k, v);
+    };
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int m = tm * 64 + r0 + 16 * i;
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int k = tn * 64 + c + e;
+            v[e] = m < n && k < n ? s[i][e] * epi.factor + (m == k ? epi.diag : 0.f) : 0.f;
+            tile[r0 + 16 * i][c + e] = v[e];
+        }
+        both(m, tn * 64 + c, v);
+    }
+    if (tm == tn) return;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = tile[c + e][r0 + 16 * i];
+        both(tn * 64 + r0 + 16 * i, tm * 64 + c, v);
+    }
+}
+
+// How products of a stack are cut: into tiles of 256, 192, 128 (two on a compute unit, or with more buffers one) or 64, their contraction into parts.
+struct StackCut {
+    int tile, deep, splits;
+};
+// The cut that takes least by an estimate in microseconds: rounds of workgroups, each a step for each 64 indices and pair of planes, and what begins
+// and ends a tile.  Tiles of 192 read rows only.
+inline double stack_tiles(const Shape &sh, int tile) { return (double)tiles_in(sh, ceil_div(sh.M, tile), ceil_div(sh.Nn, tile)) * sh.stack; }
+constexpr double kSplitTiles = 512;   // no product of more tiles of 128 is cut along its contraction
+inline StackCut choose_stack_cut(const Shape &sh, int pairs, bool rows_only, bool may_split) {
+    struct { int tile, deep; double slots, step, ends; } const kinds[] = {{256, 0, kComputeUnits, 1.7, 15}, {192, 0, kComputeUnits, 1.0, 10},
+                                                                          {128, 0, 2 * kComputeUnits, 0.82, 6}, {128, 1, kComputeUnits, 0.5, 4},
+                                                                          {64, 0, 4 * kComputeUnits, 0.5, 4}};
+    const int steps = ceil_div(sh.K, kStep);
+    StackCut best = {128, 0, 1};
+    double least = 1e30;
+    if (stack_tiles(sh, 128) > kSplitTiles) may_split = false;
+    const long long result = sh.M * round_up(sh.Nn, 4) * sh.stack;
+    for (int s = 1; s == 1 || (may_split && s <= kMostSplits && s <= steps / 2 && s * result <= kMostParts); ++s)
+        for (const auto &k : kinds) {
+            if (k.tile == 192 && !rows_only) continue;
+            const double t = std::ceil(stack_tiles(sh, k.tile) * s / k.slots) * ((double)ceil_div(steps, s) * pairs * k.step + k.ends) +
+                             (s > 1 ? 6 + 4e-6 * s * (double)result / 4 : 0);
+            if (t < least) best = {k.tile, k.deep, s}, least = t;
+        }
+    return best;
+}
+
+template <int PL, int FA, int FB, typename Epi>
+int launch_stack(const char *name, const Operand &A, const Operand &B, const Shape &sh, const StackCut &c, const Epi &epi, hipStream_t s) {
+    if (c.tile == 256) return launch_tiles<PL, FA, FB, 256, 256, 3, 2>(name, A, B, sh, c.splits, epi, s);
+    if constexpr (FA == ROW && FB == ROW)
+        if (c.tile == 192) return launch_tiles<PL, FA, FB, 192, 192, 3, 2>(name, A, B, sh, c.splits, epi, s);
+    if (c.tile == 64) return launch_tiles<PL, FA, FB, 64, 64, 3, 2>(name, A, B, sh, c.splits, epi, s);
+    if (c.deep) return launch_tiles<PL, FA, FB, 128, 128, 5, 5>(name, A, B, sh, c.splits, epi, s);
+    return launch_tiles<PL, FA, FB, 128, 128, 3, 2>(name, A, B, sh, c.splits, epi, s);
+}
+
+// A symmetric product of a stack.
+template <int PL, int FA, int FB, int PLANES>
+int launch_symmetric(const char *name, const Operand &A, const Operand &B, const Shape &sh, const PlaneEpi<PLANES, true> &epi, const Parts &part,
+                     hipStream_t s) {
+    const StackCut c = choose_stack_cut(sh, Format<PL>::PAIRS, FA == ROW && FB == ROW, true);
+    if (c.splits == 1) return launch_stack<PL, FA, FB>(name, A, B, sh, c, epi, s);
+    const int ldp = (int)round_up(sh.Nn, 4);
+    const long long wgs = (long long)stack_tiles(sh, 64);
+    const LaunchPlan p = make_plan("muon_join", {PLANES}, {sh.M, c.splits, sh.stack}, dim3((unsigned)wgs), 256, 0);
+    LC_PLAN_REQUIRE(p, wgs <= 0x7fffffffLL && (long long)c.splits * sh.stack * sh.M * ldp <= part.floats && ldp >= 4);
+    if (int rc = launch_stack<PL, FA, FB>(name, A, B, sh, c, StackPartEpi{{part.at, ldp, sh.M}, 0}, s)) return rc;
+    LC_LAUNCH(p, name, (muon_join_kernel<PLANES>), s, part.at, c.splits, sh.M, ldp, epi);
+    return LC_OK;
+}
+
 constexpr long long kStackBytes = 1LL << 30;   // of X's planes at a time
+
+// Steps that go by on the short side: all alike where the matrix is square.
+inline int group_of(int rows, int cols) { return rows == cols ? 1 : kGroupSteps; }
 
 template <typename T>
 struct MuonScratch {
     static constexpr int PLANES = MuonFormat<T>::N;
-    int small, ld, lds, most, parts;   // the smaller side; values of a row of X, of S and P; items at a time; partial sums of a matrix
+    int small, ld, lds, most, parts;   // the smaller side; values of a row of X, of what is small x small; items at a time; partial sums of a matrix
     double *partial;
-    bf16_t *x[2], *s, *p;
+    bf16_t *x[2], *s, *a = nullptr, *t = nullptr, *q[3] = {};
+    Parts part = {};
     MuonScratch(Scratch &sc, int count, int rows, int cols) {
         small = std::min(rows, cols);
         ld = (int)round_up(cols, 8), lds = (int)round_up(small, 8);
@@ -260,55 +408,87 @@ struct MuonScratch {
         most = (int)std::max<long long>(1, std::min<long long>(count, kStackBytes / (2 * PLANES * values)));
         parts = (int)std::min<long long>(kMostParts256, ((long long)rows * cols + 8191) / 8192);
         partial = sc.take<double>((long long)most * parts);
-        for (int i = 0; i < 2; ++i) x[i] = sc.take<bf16_t>(PLANES * most * values);
-        s = sc.take<bf16_t>(PLANES * most * (long long)small * lds);
-        p = sc.take<bf16_t>(PLANES * most * (long long)small * lds);
+        for (auto &p : x) p = sc.take<bf16_t>(PLANES * most * values);
+        const long long square = PLANES * most * (long long)small * lds;
+        s = sc.take<bf16_t>(square);
+        q[0] = sc.take<bf16_t>(square);
+        if (group_of(rows, cols) > 1)
+            for (bf16_t **p : {&a, &t, &q[1], &q[2]}) *p = sc.take<bf16_t>(square);
+        // of as many matrices as are cut along the contraction; a shorter stack may be cut into more parts
+        const Shape one = {small, small, std::max(rows, cols), nullptr, 0, nullptr, 0, 1, 1, 1};
+        const long long cut = std::min<long long>(most, (long long)(kSplitTiles / stack_tiles(one, 128)));
+        part.floats = std::min(kMostParts, kMostSplits * cut * small * round_up(small, 4));
+        part.at = sc.take<float>(part.floats);
     }
 };
 
 template <typename T>
 int muon(const T *w, const T *g, const float *m, T *w_out, float *m_out, int count, int rows, int cols, float rate, float decay, float mu, bool ahead,
          int steps, void *ws, hipStream_t st) {
-    constexpr int PL = MuonFormat<T>::PL, PLANES = MuonFormat<T>::N;
+    constexpr int PL = MuonFormat<T>::PL, PLANES = MuonFormat<T>::N, PAIRS = Format<PL>::PAIRS;
     Scratch sc(ws);
     const MuonScratch<T> k(sc, count, rows, cols);
     const bool tall = rows > cols;
-    const long long n = (long long)rows * cols;
+    const long long n = (long long)rows * cols, each = (long long)k.small * k.lds;
+    const int groups = ceil_div(steps, group_of(rows, cols));
     for (int first = 0; first < count; first += k.most) {
         const int items = std::min(k.most, count - first);
-        const long long skip = first * n, plane = (long long)k.most * rows * k.ld, splane = (long long)k.most * k.small * k.lds;
+        const long long skip = first * n, plane = (long long)k.most * rows * k.ld, splane = k.most * each;
         const LaunchPlan pm = make_plan("muon_momentum", {(int)sizeof(T)}, {items, rows, cols, k.parts}, dim3((unsigned)((long long)items * k.parts)), 256, 0);
         LC_PLAN_REQUIRE(pm, (long long)items * k.parts <= 0x7fffffffLL);
         LC_LAUNCH(pm, "muon_step (momentum)", (muon_momentum_kernel<T>), st, g + skip, m + skip, m_out + skip, k.partial, n, k.parts, mu, (int)ahead);
-        const long long groups = ((long long)rows * (k.ld / 8) + 255) / 256;
-        const LaunchPlan ps = make_plan("muon_start", {(int)sizeof(T)}, {items, rows, cols, k.ld}, dim3((unsigned)(items * groups)), 256, 0);
-        LC_PLAN_REQUIRE(ps, items * groups <= 0x7fffffffLL);
+        const long long wgs = ((long long)rows * (k.ld / 8) + 255) / 256;
+        const LaunchPlan ps = make_plan("muon_start", {(int)sizeof(T)}, {items, rows, cols, k.ld}, dim3((unsigned)(items * wgs)), 256, 0);
+        LC_PLAN_REQUIRE(ps, items * wgs <= 0x7fffffffLL);
         LC_LAUNCH(ps, "muon_step (start)", (muon_start_kernel<T, PLANES>), st, g + skip, m_out + skip, k.partial, k.x[0], plane, rows, cols, k.ld, k.parts,
-                  (int)groups, mu, (int)ahead);
-        const auto cut = [&](const Shape &sh) { return choose_cut(sh.M, sh.Nn, sh.K, Format<PL>::PAIRS, false, sh.stack, sh.sym); };
-        const Operand S = {k.s, k.s, k.lds, splane, k.small, 0, 0, (long long)k.small * k.lds};
-        const Operand P = {k.p, k.p, k.lds, splane, k.small, 0, 0, (long long)k.small * k.lds};
+                  (int)wgs, mu, (int)ahead);
+        const auto square = [&](const bf16_t *p) { return Operand{p, p, k.lds, splane, k.small, 0, 0, each}; };
         const Shape sq = {k.small, k.small, k.small, nullptr, 0, nullptr, 0, 1, items, 1};
         Shape sx = sq;
         sx.K = tall ? rows : cols;
-        Shape up = {rows, cols, k.small, nullptr, 0, nullptr, 0, 1, items, 0};
-        for (int i = 0; i < steps; ++i) {
-            const Operand X = {k.x[i & 1], k.x[i & 1], k.ld, plane, rows, 0, 0, (long long)rows * k.ld};
+        const Shape up = {rows, cols, k.small, nullptr, 0, nullptr, 0, 1, items, 0};
+        // `to` = left right / (scales of both), at the scale `scale`
+        const auto multiply = [&](const char *name, const bf16_t *left, const bf16_t *right, bf16_t *to, bf16_t *to2, float factor, float diag, float diag2) {
+            return launch_symmetric<PL, ROW, ROW>(name, square(left), square(right), sq, PlaneEpi<PLANES, true>{to, to2, splane, each, k.lds, factor, diag, diag2},
+                                                  k.part, st);
+        };
+        int at = 0, rc;   // X's place
+        for (int group = 0, done = 0; group < groups; ++group) {
+            const int len = (steps - done) / (groups - group);
+            const Operand X = {k.x[at], k.x[at], k.ld, plane, rows, 0, 0, (long long)rows * k.ld};
             Operand Xc = X;
             Xc.rows = k.ld;   // by columns
-            const PlaneEpi<PLANES, true> es = {k.s, splane, S.each, k.lds, kScaleS / (kScaleX * kScaleX), kShift * kScaleS};
-            const PlaneEpi<PLANES, true> ep = {k.p, splane, P.each, k.lds, kMuonC * kScaleP / (kScaleS * kScaleS), kRest * kScaleP};
-            int rc = tall ? launch_cut<PL, COL, COL>("muon_step (S)", Xc, Xc, sx, cut(sx), es, st) : launch_cut<PL, ROW, ROW>("muon_step (S)", X, X, sx, cut(sx), es, st);
+            const float fa = kScaleA / (kScaleX * kScaleX), fs = kShift * kScaleA;
+            const PlaneEpi<PLANES, true> ea = {len > 1 ? k.a : k.s, len > 1 ? k.s : nullptr, splane, each, k.lds, fa, len > 1 ? 0.f : fs, fs};
+            rc = tall ? launch_symmetric<PL, COL, COL>("muon_step (A)", Xc, Xc, sx, ea, k.part, st)
+                      : launch_symmetric<PL, ROW, ROW>("muon_step (A)", X, X, sx, ea, k.part, st);
             if (rc) return rc;
-            if ((rc = launch_cut<PL, ROW, ROW>("muon_step (P)", S, S, sq, cut(sq), ep, st))) return rc;
+            int q = 0;   // place of Q, the product of the group's P
+            for (int i = 0; i < len; ++i) {
+                const int p = i ? (q + 1) % 3 : 0;
+                if ((rc = multiply("muon_step (P)", k.s, k.s, k.q[p], nullptr, kMuonC * kScaleQ[1] / (kScaleA * kScaleA), kRest * kScaleQ[1], 0.f))) return rc;
+                if (i + 1 < len) {
+                    if ((rc = multiply("muon_step (P A)", k.q[p], k.a, k.t, nullptr, 1.f / kScaleQ[1], 0.f, 0.f))) return rc;
+                    if ((rc = multiply("muon_step (P A P)", k.t, k.q[p], k.a, k.s, 1.f / kScaleQ[1], 0.f, fs))) return rc;
+                }
+                if (i) {
+                    const int to = (q + 2) % 3;
+                    if ((rc = multiply("muon_step (Q)", k.q[p], k.q[q], k.q[to], nullptr, kScaleQ[i + 1] / (kScaleQ[1] * kScaleQ[i]), 0.f, 0.f))) return rc;
+                    q = to;
+                }
+            }
+            done += len;
+            const Operand Q = square(k.q[q]);
+            const StackCut cut = choose_stack_cut(up, PAIRS, tall, false);
             const auto apply = [&](const auto &epi) {
-                return tall ? launch_cut<PL, ROW, ROW>("muon_step (X)", X, P, up, cut(up), epi, st) : launch_cut<PL, ROW, COL>("muon_step (X)", P, Xc, up, cut(up), epi, st);
+                return tall ? launch_stack<PL, ROW, ROW>("muon_step (X)", X, Q, up, cut, epi, st) : launch_stack<PL, ROW, COL>("muon_step (X)", Q, Xc, up, cut, epi, st);
             };
-            if (i + 1 < steps)
-                rc = apply(PlaneEpi<PLANES, false>{k.x[~i & 1], plane, X.each, k.ld, 1.f / kScaleP, 0.f});
+            if (done < steps)
+                rc = apply(PlaneEpi<PLANES, false>{k.x[1 - at], nullptr, plane, X.each, k.ld, 1.f / kScaleQ[len], 0.f, 0.f});
             else
-                rc = apply(UpdateEpi<T>{w + skip, w_out + skip, n, cols, 1.f - decay, rate / (kScaleP * kScaleX)});
+                rc = apply(UpdateEpi<T>{w + skip, w_out + skip, n, cols, 1.f - decay, rate / (kScaleQ[len] * kScaleX)});
             if (rc) return rc;
+            at = 1 - at;
         }
     }
     return LC_OK;
