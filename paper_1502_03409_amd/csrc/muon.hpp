@@ -128,6 +128,7 @@ __global__ __launch_bounds__(256) void muon_start_kernel(const T *g, const float
 // `diag2` added on the diagonal.
 template <int PLANES, bool MIRROR>
 struct PlaneEpi {
+    static constexpr bool UPDATES = false;
     bf16_t *out, *out2;
     long long plane, each;
     int ld;
@@ -214,6 +215,7 @@ struct PlaneEpi {
 // The last product: w' = keep w - rate X.
 template <typename T>
 struct UpdateEpi {
+    static constexpr bool UPDATES = true;
     const T *w;
     T *w_out;
     long long each;
@@ -275,6 +277,7 @@ struct UpdateEpi {
 
 // The sums of a part, as PartEpi stores them: [item][part][M][ld].
 struct StackPartEpi : PartEpi {
+    static constexpr bool UPDATES = false;
     int at;
     __device__ __forceinline__ void item(int i) { at = i; }
     template <int MT, int NT>
@@ -337,40 +340,46 @@ __global__ __launch_bounds__(256) void muon_join_kernel(const float *part, int s
     }
 }
 
-// How products of a stack are cut: into tiles of 256, 192, 128 (two on a compute unit, or with more buffers one) or 64, their contraction into parts.
+// How products of a stack are cut: into tiles of 256, 192, 128 or 64, their contraction into parts.
 struct StackCut {
-    int tile, deep, splits;
+    int tile, splits;
+    double us;   // by the estimate
 };
-// The cut that takes least by an estimate in microseconds: rounds of workgroups, each a step for each 64 indices and pair of planes, and what begins
-// and ends a tile.  Tiles of 192 read rows only.
+// The cut that takes least by an estimate in microseconds from measured times: what begins and ends a tile, and for each 64 indices and pair of
+// planes a step of the tiles that share the fullest compute unit.  fp16, n x n times its like, the half below the diagonal, tiles of 64 / 128 /
+// 192 / 256: n = 256 5.5 / 7.0 / 12.6 / 15.6 us, 1024 11.3 / 13.3 / 22.6 / 34, 2048 22.1 / 22.8 / 34.8 / 52.5, 4096 145 / 104 / 86 / 97, two of 4096
+// 281 / 182 / 157 / 204.  Parts cost a kernel and their bytes: 1021 x 20011 times its transpose 152 us whole and 33 + 7 in 14.
+// Tiles of 192 read rows only, and tiles of 256 have no room to load what they update (8192 x 4096, both: 670 us, 621 with tiles of 128).
 inline double stack_tiles(const Shape &sh, int tile) { return (double)tiles_in(sh, ceil_div(sh.M, tile), ceil_div(sh.Nn, tile)) * sh.stack; }
 constexpr double kSplitTiles = 512;   // no product of more tiles of 128 is cut along its contraction
-inline StackCut choose_stack_cut(const Shape &sh, int pairs, bool rows_only, bool may_split) {
-    struct { int tile, deep; double slots, step, ends; } const kinds[] = {{256, 0, kComputeUnits, 1.7, 15}, {192, 0, kComputeUnits, 1.0, 10},
-                                                                          {128, 0, 2 * kComputeUnits, 0.82, 6}, {128, 1, kComputeUnits, 0.5, 4},
-                                                                          {64, 0, 4 * kComputeUnits, 0.5, 4}};
+enum { ROWS_ONLY = 1, MAY_SPLIT = 2, UPDATES = 4 };
+inline StackCut choose_stack_cut(const Shape &sh, int pairs, int how) {
     const int steps = ceil_div(sh.K, kStep);
-    StackCut best = {128, 0, 1};
-    double least = 1e30;
-    if (stack_tiles(sh, 128) > kSplitTiles) may_split = false;
+    StackCut best = {128, 1, 1e30};
+    const bool may_split = (how & MAY_SPLIT) && stack_tiles(sh, 128) <= kSplitTiles;
     const long long result = sh.M * round_up(sh.Nn, 4) * sh.stack;
     for (int s = 1; s == 1 || (may_split && s <= kMostSplits && s <= steps / 2 && s * result <= kMostParts); ++s)
-        for (const auto &k : kinds) {
-            if (k.tile == 192 && !rows_only) continue;
-            const double t = std::ceil(stack_tiles(sh, k.tile) * s / k.slots) * ((double)ceil_div(steps, s) * pairs * k.step + k.ends) +
-                             (s > 1 ? 6 + 4e-6 * s * (double)result / 4 : 0);
-            if (t < least) best = {k.tile, k.deep, s}, least = t;
+        for (const int tile : {64, 128, 192, 256}) {
+            if ((tile == 192 && !(how & ROWS_ONLY)) || (tile == 256 && (how & UPDATES))) continue;
+            const double load = stack_tiles(sh, tile) * s / kComputeUnits, most = std::ceil(load);
+            double ends, step;
+            if (tile == 64) ends = 3.4, step = std::max(0.5, 0.28 * load);
+            else if (tile == 128) ends = 4.5, step = most <= 1 ? 0.57 : most <= 2 ? 0.92 : 0.55 * most;
+            else if (tile == 192) ends = 9, step = load <= 0.5 ? 0.9 : 1.15 * most;
+            else ends = 14, step = most <= 1 ? 1.3 : most <= 2 ? 3.0 : 1.8 * most;
+            const double us = ends + (double)ceil_div(steps, s) * pairs * step + (s > 1 ? 6 + 4e-6 * s * (double)result / 4 : 0);
+            if (us < best.us) best = {tile, s, us};
         }
     return best;
 }
 
 template <int PL, int FA, int FB, typename Epi>
 int launch_stack(const char *name, const Operand &A, const Operand &B, const Shape &sh, const StackCut &c, const Epi &epi, hipStream_t s) {
-    if (c.tile == 256) return launch_tiles<PL, FA, FB, 256, 256, 3, 2>(name, A, B, sh, c.splits, epi, s);
+    if constexpr (!Epi::UPDATES)
+        if (c.tile == 256) return launch_tiles<PL, FA, FB, 256, 256, 3, 2>(name, A, B, sh, c.splits, epi, s);
     if constexpr (FA == ROW && FB == ROW)
         if (c.tile == 192) return launch_tiles<PL, FA, FB, 192, 192, 3, 2>(name, A, B, sh, c.splits, epi, s);
     if (c.tile == 64) return launch_tiles<PL, FA, FB, 64, 64, 3, 2>(name, A, B, sh, c.splits, epi, s);
-    if (c.deep) return launch_tiles<PL, FA, FB, 128, 128, 5, 5>(name, A, B, sh, c.splits, epi, s);
     return launch_tiles<PL, FA, FB, 128, 128, 3, 2>(name, A, B, sh, c.splits, epi, s);
 }
 
@@ -378,7 +387,7 @@ int launch_stack(const char *name, const Operand &A, const Operand &B, const Sha
 template <int PL, int FA, int FB, int PLANES>
 int launch_symmetric(const char *name, const Operand &A, const Operand &B, const Shape &sh, const PlaneEpi<PLANES, true> &epi, const Parts &part,
                      hipStream_t s) {
-    const StackCut c = choose_stack_cut(sh, Format<PL>::PAIRS, FA == ROW && FB == ROW, true);
+    const StackCut c = choose_stack_cut(sh, Format<PL>::PAIRS, (FA == ROW && FB == ROW ? ROWS_ONLY : 0) | MAY_SPLIT);
     if (c.splits == 1) return launch_stack<PL, FA, FB>(name, A, B, sh, c, epi, s);
     const int ldp = (int)round_up(sh.Nn, 4);
     const long long wgs = (long long)stack_tiles(sh, 64);
@@ -391,13 +400,35 @@ int launch_symmetric(const char *name, const Operand &A, const Operand &B, const
 
 constexpr long long kStackBytes = 1LL << 30;   // of X's planes at a time
 
-// Steps that go by on the short side: all alike where the matrix is square.
-inline int group_of(int rows, int cols) { return rows == cols ? 1 : kGroupSteps; }
+// Products of `items` matrices: short sides, the long side, the update of X.
+struct MuonShapes {
+    Shape sq, sx, up;
+    MuonShapes(int items, int rows, int cols) {
+        const int small = std::min(rows, cols);
+        sq = sx = Shape{small, small, small, nullptr, 0, nullptr, 0, 1, items, 1};
+        sx.K = std::max(rows, cols);
+        up = {rows, cols, small, nullptr, 0, nullptr, 0, 1, items, 0};
+    }
+};
+// Steps that go by on the short side at a time: kGroupSteps, or one where the products with the long side cost no more by the estimate (no
+// less than their bytes at 4.5 TB/s).  Both: two of 256 x 400 in fp32 155 us with one, 841 of 2048 x 128 in fp32 4.4 ms with one and 2.9 with
+// three, two of 8192 x 4096 in bf16 5.3 and 4.2.
+inline double stack_us(const Shape &sh, int planes, int pairs, int how) {
+    const double bytes = 2.0 * planes * sh.stack * ((double)sh.M * sh.K + (sh.sym ? 0.0 : (double)sh.Nn * sh.K) + (double)sh.M * sh.Nn);
+    return std::max(choose_stack_cut(sh, pairs, how).us, bytes / 4.5e6);
+}
+inline int group_of(int items, int rows, int cols, int planes, int pairs) {
+    const MuonShapes k(items, rows, cols);
+    const int rows_only = rows > cols ? 0 : ROWS_ONLY;
+    const double sq = stack_us(k.sq, planes, pairs, ROWS_ONLY | MAY_SPLIT), sx = stack_us(k.sx, planes, pairs, rows_only | MAY_SPLIT),
+                 up = stack_us(k.up, planes, pairs, rows > cols ? ROWS_ONLY : 0);
+    return sx + up > 3 * sq ? kGroupSteps : 1;
+}
 
 template <typename T>
 struct MuonScratch {
     static constexpr int PLANES = MuonFormat<T>::N;
-    int small, ld, lds, most, parts;   // the smaller side; values of a row of X, of what is small x small; items at a time; partial sums of a matrix
+    int small, ld, lds, most, parts, group;   // the smaller side; values of a row of X, of what is small x small; items at a time; partial sums of a matrix
     double *partial;
     bf16_t *x[2], *s, *a = nullptr, *t = nullptr, *q[3] = {};
     Parts part = {};
@@ -412,11 +443,11 @@ struct MuonScratch {
         const long long square = PLANES * most * (long long)small * lds;
         s = sc.take<bf16_t>(square);
         q[0] = sc.take<bf16_t>(square);
-        if (group_of(rows, cols) > 1)
+        group = group_of(most, rows, cols, PLANES, Format<MuonFormat<T>::PL>::PAIRS);
+        if (rows != cols)   // whatever the stack's length says
             for (bf16_t **p : {&a, &t, &q[1], &q[2]}) *p = sc.take<bf16_t>(square);
         // of as many matrices as are cut along the contraction; a shorter stack may be cut into more parts
-        const Shape one = {small, small, std::max(rows, cols), nullptr, 0, nullptr, 0, 1, 1, 1};
-        const long long cut = std::min<long long>(most, (long long)(kSplitTiles / stack_tiles(one, 128)));
+        const long long cut = std::min<long long>(most, (long long)(kSplitTiles / stack_tiles(MuonShapes(1, rows, cols).sx, 128)));
         part.floats = std::min(kMostParts, kMostSplits * cut * small * round_up(small, 4));
         part.at = sc.take<float>(part.floats);
     }
@@ -430,7 +461,7 @@ int muon(const T *w, const T *g, const float *m, T *w_out, float *m_out, int cou
     const MuonScratch<T> k(sc, count, rows, cols);
     const bool tall = rows > cols;
     const long long n = (long long)rows * cols, each = (long long)k.small * k.lds;
-    const int groups = ceil_div(steps, group_of(rows, cols));
+    const int groups = ceil_div(steps, k.group);
     for (int first = 0; first < count; first += k.most) {
         const int items = std::min(k.most, count - first);
         const long long skip = first * n, plane = (long long)k.most * rows * k.ld, splane = k.most * each;
@@ -443,13 +474,10 @@ int muon(const T *w, const T *g, const float *m, T *w_out, float *m_out, int cou
         LC_LAUNCH(ps, "muon_step (start)", (muon_start_kernel<T, PLANES>), st, g + skip, m_out + skip, k.partial, k.x[0], plane, rows, cols, k.ld, k.parts,
                   (int)wgs, mu, (int)ahead);
         const auto square = [&](const bf16_t *p) { return Operand{p, p, k.lds, splane, k.small, 0, 0, each}; };
-        const Shape sq = {k.small, k.small, k.small, nullptr, 0, nullptr, 0, 1, items, 1};
-        Shape sx = sq;
-        sx.K = tall ? rows : cols;
-        const Shape up = {rows, cols, k.small, nullptr, 0, nullptr, 0, 1, items, 0};
+        const MuonShapes of(items, rows, cols);
         // `to` = left right / (scales of both), at the scale `scale`
         const auto multiply = [&](const char *name, const bf16_t *left, const bf16_t *right, bf16_t *to, bf16_t *to2, float factor, float diag, float diag2) {
-            return launch_symmetric<PL, ROW, ROW>(name, square(left), square(right), sq, PlaneEpi<PLANES, true>{to, to2, splane, each, k.lds, factor, diag, diag2},
+            return launch_symmetric<PL, ROW, ROW>(name, square(left), square(right), of.sq, PlaneEpi<PLANES, true>{to, to2, splane, each, k.lds, factor, diag, diag2},
                                                   k.part, st);
         };
         int at = 0, rc;   // X's place
@@ -460,8 +488,8 @@ int muon(const T *w, const T *g, const float *m, T *w_out, float *m_out, int cou
             Xc.rows = k.ld;   // by columns
             const float fa = kScaleA / (kScaleX * kScaleX), fs = kShift * kScaleA;
             const PlaneEpi<PLANES, true> ea = {len > 1 ? k.a : k.s, len > 1 ? k.s : nullptr, splane, each, k.lds, fa, len > 1 ? 0.f : fs, fs};
-            rc = tall ? launch_symmetric<PL, COL, COL>("muon_step (A)", Xc, Xc, sx, ea, k.part, st)
-                      : launch_symmetric<PL, ROW, ROW>("muon_step (A)", X, X, sx, ea, k.part, st);
+            rc = tall ? launch_symmetric<PL, COL, COL>("muon_step (A)", Xc, Xc, of.sx, ea, k.part, st)
+                      : launch_symmetric<PL, ROW, ROW>("muon_step (A)", X, X, of.sx, ea, k.part, st);
             if (rc) return rc;
             int q = 0;   // place of Q, the product of the group's P
             for (int i = 0; i < len; ++i) {
@@ -479,9 +507,10 @@ int muon(const T *w, const T *g, const float *m, T *w_out, float *m_out, int cou
             }
             done += len;
             const Operand Q = square(k.q[q]);
-            const StackCut cut = choose_stack_cut(up, PAIRS, tall, false);
             const auto apply = [&](const auto &epi) {
-                return tall ? launch_stack<PL, ROW, ROW>("muon_step (X)", X, Q, up, cut, epi, st) : launch_stack<PL, ROW, COL>("muon_step (X)", Q, Xc, up, cut, epi, st);
+                const StackCut cut = choose_stack_cut(of.up, PAIRS, (tall ? ROWS_ONLY : 0) | (epi.UPDATES ? UPDATES : 0));
+                return tall ? launch_stack<PL, ROW, ROW>("muon_step (X)", X, Q, of.up, cut, epi, st)
+                            : launch_stack<PL, ROW, COL>("muon_step (X)", Q, Xc, of.up, cut, epi, st);
             };
             if (done < steps)
                 rc = apply(PlaneEpi<PLANES, false>{k.x[1 - at], nullptr, plane, X.each, k.ld, 1.f / kScaleQ[len], 0.f, 0.f});
