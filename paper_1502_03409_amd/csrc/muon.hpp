@@ -28,7 +28,7 @@ constexpr float kShift = kMuonB / (2.f * kMuonC), kRest = (float)(3.4445 - 4.775
 constexpr float kScaleX = 0x1p14f, kScaleA = 0x1p14f;                 // 1.203 and 1.447 times these, and 3.4445, 3.4445^2, 3.4445^3 times
 constexpr float kScaleQ[4] = {0.f, 0x1p13f, 0x1p12f, 0x1p10f};        // those, stay below 2^16 (P is the first Q)
 constexpr int kGroupSteps = 3;
-constexpr int kMostParts256 = 256;   // partial sums of a matrix's squares
+constexpr int kMostSums = 1024;   // partial sums of a matrix's squares
 
 typedef _Float16 half_t;
 __device__ __forceinline__ bf16_t half_bits(float v) { return __builtin_bit_cast(bf16_t, (half_t)v); }
@@ -68,11 +68,7 @@ __global__ __launch_bounds__(256) void muon_momentum_kernel(const T *g, const fl
     const int part = blockIdx.x % parts;
     g += item * n, m += item * n, m_out += item * n;
     double s = 0.0;
-    for (long long i = (part * 256LL + threadIdx.x) * 8; i < n; i += parts * 2048LL) {
-        const int left = (int)min(n - i, 8LL);
-        float a[8], b[8];
-        load8(g + i, 0, left, a);
-        load8(m + i, 0, left, b);
+    const auto some = [&](long long i, int left, float (&a)[8], float (&b)[8]) __attribute__((always_inline)) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             b[e] = next_momentum(b[e], a[e], mu);
@@ -80,6 +76,25 @@ __global__ __launch_bounds__(256) void muon_momentum_kernel(const T *g, const fl
             if (e < left) s += u * u;
         }
         store8(m_out + i, b, left);
+    };
+    const long long step = parts * 2048LL;
+    long long i = (part * 256LL + threadIdx.x) * 8;
+    for (; i + step + 8 <= n; i += 2 * step) {   // two at a time
+        float a[2][8], b[2][8];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            load8(g + i + k * step, 0, 8, a[k]);
+            load8(m + i + k * step, 0, 8, b[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) some(i + k * step, 8, a[k], b[k]);
+    }
+    for (; i < n; i += step) {
+        const int left = (int)min(n - i, 8LL);
+        float a[8], b[8];
+        load8(g + i, 0, left, a);
+        load8(m + i, 0, left, b);
+        some(i, left, a, b);
     }
     s = workgroup_sum(s);
     if (threadIdx.x == 0) partial[blockIdx.x] = s;
@@ -100,6 +115,7 @@ __device__ __forceinline__ void put_halves(bf16_t *to, long long plane, const fl
     for (int q = 0; q < PLANES; ++q) *(u32x4 *)(to + q * plane) = w[q];
 }
 
+constexpr int kStartPieces = 2;   // of eight values, a thread
 // X = u / |u| as planes [item][rows][ld], zeros behind a row.  A matrix of zeros stays one; one with an infinite or NaN value becomes NaN.
 template <typename T, int PLANES>
 __global__ __launch_bounds__(256) void muon_start_kernel(const T *g, const float *m, const double *partial, bf16_t *x, long long plane, int rows, int cols,
@@ -110,17 +126,26 @@ __global__ __launch_bounds__(256) void muon_start_kernel(const T *g, const float
     s = sqrt(workgroup_sum(s));
     const double f = !__builtin_isfinite(s) ? __builtin_nan("") : s > 0.0 ? (double)kScaleX / s : 0.0;
     const int pieces = ld / 8;
-    const long long at = (blockIdx.x - item * groups) * 256LL + threadIdx.x;
-    const int r = (int)(at / pieces), c = (int)(at - (long long)r * pieces) * 8;
-    if (r >= rows) return;
-    float a[8], b[8];
-    load8(g + item * n + (long long)r * cols, c, cols, a);
-    load8(m + item * n + (long long)r * cols, c, cols, b);
+    const long long all = (long long)rows * pieces, from = (blockIdx.x - item * groups) * (256LL * kStartPieces) + threadIdx.x;
+    const T *const gi = g + item * n;
+    const float *const mi = m + item * n;
+    float a[kStartPieces][8], b[kStartPieces][8];
+    int r[kStartPieces], c[kStartPieces];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        b[e] = c + e < cols ? (float)((double)looked_ahead(b[e], a[e], mu, ahead) * f) : 0.f;   // 1 / |u| may be beyond fp32
+    for (int k = 0; k < kStartPieces; ++k) {
+        const long long at = min(from + 256 * k, all - 1);
+        r[k] = (int)(at / pieces), c[k] = (int)(at - (long long)r[k] * pieces) * 8;
+        load8(gi + (long long)r[k] * cols, c[k], cols, a[k]);
+        load8(mi + (long long)r[k] * cols, c[k], cols, b[k]);
     }
-    put_halves<PLANES>(x + (item * rows + r) * ld + c, plane, b);
+#pragma unroll
+    for (int k = 0; k < kStartPieces; ++k) {
+        if (from + 256 * k >= all) break;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)   // 1 / |u| may be beyond fp32
+            b[k][e] = c[k] + e < cols ? (float)((double)looked_ahead(b[k][e], a[k][e], mu, ahead) * f) : 0.f;
+        put_halves<PLANES>(x + (item * rows + r[k]) * ld + c[k], plane, b[k]);
+    }
 }
 
 // A product as planes of fp16: times `factor`, `diag` added on the diagonal; zeros in the columns behind the last one up to ld.  MIRROR: the
@@ -437,7 +462,7 @@ struct MuonScratch {
         ld = (int)round_up(cols, 8), lds = (int)round_up(small, 8);
         const long long values = (long long)rows * ld;
         most = (int)std::max<long long>(1, std::min<long long>(count, kStackBytes / (2 * PLANES * values)));
-        parts = (int)std::min<long long>(kMostParts256, ((long long)rows * cols + 8191) / 8192);
+        parts = (int)std::min<long long>(kMostSums, ((long long)rows * cols + 8191) / 8192);
         partial = sc.take<double>((long long)most * parts);
         for (auto &p : x) p = sc.take<bf16_t>(PLANES * most * values);
         const long long square = PLANES * most * (long long)small * lds;
@@ -468,7 +493,7 @@ int muon(const T *w, const T *g, const float *m, T *w_out, float *m_out, int cou
         const LaunchPlan pm = make_plan("muon_momentum", {(int)sizeof(T)}, {items, rows, cols, k.parts}, dim3((unsigned)((long long)items * k.parts)), 256, 0);
         LC_PLAN_REQUIRE(pm, (long long)items * k.parts <= 0x7fffffffLL);
         LC_LAUNCH(pm, "muon_step (momentum)", (muon_momentum_kernel<T>), st, g + skip, m + skip, m_out + skip, k.partial, n, k.parts, mu, (int)ahead);
-        const long long wgs = ((long long)rows * (k.ld / 8) + 255) / 256;
+        const long long wgs = ((long long)rows * (k.ld / 8) + 256 * kStartPieces - 1) / (256 * kStartPieces);
         const LaunchPlan ps = make_plan("muon_start", {(int)sizeof(T)}, {items, rows, cols, k.ld}, dim3((unsigned)(items * wgs)), 256, 0);
         LC_PLAN_REQUIRE(ps, items * wgs <= 0x7fffffffLL);
         LC_LAUNCH(ps, "muon_step (start)", (muon_start_kernel<T, PLANES>), st, g + skip, m_out + skip, k.partial, k.x[0], plane, rows, cols, k.ld, k.parts,
