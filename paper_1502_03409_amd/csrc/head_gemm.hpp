@@ -724,6 +724,16 @@ int launch_gemm(const char *name, const Operand &A, const Operand &B, const Shap
     return launch_cut<PL, FA, FB>(name, A, B, sh, choose_cut(sh.M, sh.Nn, sh.K, PL == 3 ? 6 : 1, false), epi, s);
 }
 
+// A product of up to kNarrow rows, as mini-batches that are answered have, with tiles of 64 rows: what waits for weights from HBM is more
+// workgroups, and no row is padded to 128 (8-bit, 4096 long, tiles of 64 x 128 and 128 x 128: 192 rows times 8192 26 and 37 us, in fewer steps at a
+// time 30, times 100003 158 and 173; 64 rows times 100003 107 and 113, 101 with 64 x 64).
+constexpr int kNarrow = 192;
+template <int PL, int FB, int BN, typename Epi>
+int launch_narrow(const char *name, const Operand &A, const Operand &B, const Shape &sh, const Epi &epi, hipStream_t s) {
+    constexpr int NB = BN == 64 ? 4 : 3;
+    return launch_tiles<PL, ROW, FB, 64, BN, NB, NB>(name, A, B, sh, 1, epi, s);
+}
+
 // Floats that are enough for the parts of any product of up to M rows and up to K indices that is cut: a shorter product may be cut into more
 // parts.
 inline long long part_floats(int M, int Nn, int K) {

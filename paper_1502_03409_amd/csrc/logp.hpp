@@ -590,7 +590,7 @@ template <typename T>
 struct LogpScratch {
     static constexpr int PL = Planes<T>::N;
     int Dp, Vp, block, blocks, wave_cols, tiles, groups_ld;
-    bool direct, gathers;   // w is used where it is; rows are picked
+    bool direct, gathers, narrow;   // w is used where it is; rows are picked; tiles of 64 rows
     LogpRows rows = {};
     bf16_t *x = nullptr, *w = nullptr, *d = nullptr;
     float4 *stats = nullptr;
@@ -605,7 +605,8 @@ struct LogpScratch {
         block = (int)std::min<long long>(round_up(N, 8), std::max<long long>(kStep, (grads ? kGradBytes : kKeyBytes) / row_bytes / 256 * 256));
         blocks = N ? (N + block - 1) / block : 0;
         const bool few = N <= kFewRows;
-        wave_cols = few ? 64 : product_wave_cols(block, V, D, Planes<T>::PAIRS);
+        narrow = !few && N <= kNarrow;
+        wave_cols = few || narrow ? 64 : product_wave_cols(block, V, D, Planes<T>::PAIRS);
         tiles = (V + wave_cols - 1) / wave_cols;
         rows.count = sc.take<int>(1);
         rows.place = sc.take<int>(N);
@@ -666,7 +667,8 @@ int logp_forward(const T *x, const T *w, const int64_t *tags, const LogpOut &out
         } else {
             const Operand X = {g.x + (long long)first * g.Dp, g.x, g.Dp, (long long)N * g.Dp, most, 0, 0};
             const Shape sh = {most, V, D, g.rows.count, first, nullptr, 0};
-            rc = launch_cut<PL, ROW, ROW>("logp", X, W, sh, choose_cut(g.block, V, D, Planes<T>::PAIRS, false), epi, s);
+            rc = g.narrow ? launch_narrow<PL, ROW, 128>("logp", X, W, sh, epi, s)
+                          : launch_cut<PL, ROW, ROW>("logp", X, W, sh, choose_cut(g.block, V, D, Planes<T>::PAIRS, false), epi, s);
         }
         if (rc) return rc;
         const bool apart = most >= 2048;
@@ -714,6 +716,7 @@ int logp_backward(const T *x, const T *w, const int64_t *tags, const float *logp
             if (few)
                 return launch_few<T, ROW>("logp_bwd (few rows)", FewOperand<T>{x, x, D, N, g.rows.index}, FewOperand<T>{w, w, D, V, nullptr}, N,
                                           g.rows.count, V, D, epi, s);
+            if (g.narrow) return launch_narrow<PL, ROW, 128>("logp_bwd", X, Wr, sh, epi, s);
             return launch_cut<PL, ROW, ROW>("logp_bwd", X, Wr, sh, choose_cut(g.block, V, D, Planes<T>::PAIRS, false), epi, s);
         };
         const auto words = [&](auto *d) -> int {

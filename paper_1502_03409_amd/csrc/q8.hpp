@@ -123,7 +123,10 @@ int q8_matmul(const T *x, const int8_t *qw, const float *sw, T *y, int N, int D,
         return launch_few<int8_t, ROW>("q8_matmul (few rows)", FewOperand<int8_t>{g.q, g.q, ld, N, nullptr}, FewOperand<int8_t>{qw, qw, ld, F, nullptr}, N,
                                        nullptr, F, ld, epi, s);
     const Shape sh = {N, F, ld / 2, nullptr, 0, nullptr, 0};
-    return launch_gemm<BYTES, ROW, ROW>("q8_matmul", bytes_operand(g.q, g.q, ld, N), bytes_operand(qw, qw, ld, F), sh, epi, s);
+    const Operand X = bytes_operand(g.q, g.q, ld, N), W = bytes_operand(qw, qw, ld, F);
+    if (N <= 64) return launch_narrow<BYTES, ROW, 64>("q8_matmul", X, W, sh, epi, s);
+    if (N <= kNarrow) return launch_narrow<BYTES, ROW, 128>("q8_matmul", X, W, sh, epi, s);
+    return launch_gemm<BYTES, ROW, ROW>("q8_matmul", X, W, sh, epi, s);
 }
 
 template <typename T, int ACT>
@@ -137,8 +140,10 @@ int q8_glu(const T *x, const int8_t *qg, const float *sg, const int8_t *qu, cons
                                         nullptr, 2 * (int)round_up(F, 16), ld,
                                         ScaledEpi<GluEpi<T, ACT, 16>, 16>{GluEpi<T, ACT, 16>{h, nullptr, F}, g.scale, sg, su, F}, s);
     const Shape sh = {N, 2 * (int)round_up(F, 32), ld / 2, nullptr, 0, nullptr, 0};
-    return launch_gemm<BYTES, ROW, PAIR>("q8_glu_fwd", bytes_operand(g.q, g.q, ld, N), bytes_operand(qg, qu, ld, F), sh,
-                                         ScaledEpi<GluEpi<T, ACT>, 32>{GluEpi<T, ACT>{h, nullptr, F}, g.scale, sg, su, F}, s);
+    const Operand X = bytes_operand(g.q, g.q, ld, N), W = bytes_operand(qg, qu, ld, F);
+    const ScaledEpi<GluEpi<T, ACT>, 32> epi = {GluEpi<T, ACT>{h, nullptr, F}, g.scale, sg, su, F};
+    if (N <= kNarrow) return launch_narrow<BYTES, PAIR, 128>("q8_glu_fwd", X, W, sh, epi, s);
+    return launch_gemm<BYTES, ROW, PAIR>("q8_glu_fwd", X, W, sh, epi, s);
 }
 template <typename T>
 int q8_glu(int act, const T *x, const int8_t *qg, const float *sg, const int8_t *qu, const float *su, T *h, int N, int D, int F, void *ws,
