@@ -3,13 +3,15 @@
  *
  * The data set of Sec. 2 comes with its users' tags, a vocabulary of tens of thousands of words.  A head turns the
  * learned features into scores for them: a gated hidden layer (glu), a softmax over the vocabulary with its cross
- * entropy and gradients (xent), and the clipping of all gradients by their common norm (grad_clip).
+ * entropy and gradients (xent), and the clipping of all gradients by their common norm (grad_clip).  Beside these: what the
+ * softmax answers, log probabilities of given words, entropies and likeliest words, with gradients (logp); steps along the
+ * orthogonalised momentum of a matrix (muon); and products and the gated layer with weights of 8 bits (q8).
  *
  * Conventions: those of lc.h (status codes, caller-owned device memory, scratch passed in as ws / ws_bytes, work only
  * enqueued on hip_stream, arguments checked on the host before anything is launched), with these of its own:
  *  - Matrices are row-major and contiguous.  Weights are [outputs][inputs], one output's weights contiguous.
  *  - `dtype` is the type of every matrix of a call, results and gradients included: each is an operand of the next
- *    call.  Sums are formed in fp32 and rounded once.  Losses, costs and norms are fp32.
+ *    call.  Sums are formed in fp32 and rounded once.  Losses, costs, norms, log probabilities, entropies and momenta are fp32.
  *  - With bf16 operands three numbers inside a call are rounded as well.  g and u are kept for glu_bwd in 16 bits (see
  *    glu_fwd), the softmax's exponentials in ten significant bits; and dg, du and the softmax's d meet the bf16 operands of
  *    the last products as bf16, for up to 32 rows as sixteen bits, because the roundings of few numbers do not average out.

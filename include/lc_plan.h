@@ -46,7 +46,12 @@ int l2pool_lcn_plan_query(int32_t B, int32_t H, int32_t W, int32_t C, int32_t po
                           int32_t lcn_ksize, float gauss_sigma, lc_launch_t *out, int32_t max_out, int32_t *n_out);
 
 /* Operators of lc_head.h, for head_plan_query. */
-enum lc_head_op { LC_HEAD_GLU_FWD = 0, LC_HEAD_GLU_BWD = 1, LC_HEAD_XENT_FWD = 2, LC_HEAD_XENT_FWD_BWD = 3 };
+enum lc_head_op {
+    LC_HEAD_GLU_FWD = 0, LC_HEAD_GLU_BWD = 1, LC_HEAD_XENT_FWD = 2, LC_HEAD_XENT_FWD_BWD = 3,
+    LC_HEAD_LOGP_FWD = 4, LC_HEAD_LOGP_BWD = 5,   /* two given words a row and the likeliest one */
+    LC_HEAD_Q8_MATMUL = 6, LC_HEAD_Q8_GLU_FWD = 7,
+    LC_HEAD_MUON = 8                              /* a stack of N matrices of D rows and `width` columns, five steps */
+};
 
 /* Host only.  The launches of an operator of lc_head.h for N rows of D values and `width` outputs (F or V), planned and
  * checked as in a call that has every optional argument and exactly the scratch that the operator's workspace function

@@ -22,6 +22,7 @@ LC_OK, LC_EINVAL, LC_ENULL, LC_EALIGN, LC_EWORKSPACE, LC_EUNSUPPORTED, LC_EHIP, 
 LC_F32, LC_BF16 = 0, 1
 LC_OP_FORWARD, LC_OP_BACKWARD_DATA, LC_OP_BACKWARD_WEIGHTS, LC_OP_SAE_STEP = 0, 1, 2, 3
 LC_HEAD_GLU_FWD, LC_HEAD_GLU_BWD, LC_HEAD_XENT_FWD, LC_HEAD_XENT_FWD_BWD = 0, 1, 2, 3
+LC_HEAD_LOGP_FWD, LC_HEAD_LOGP_BWD, LC_HEAD_Q8_MATMUL, LC_HEAD_Q8_GLU_FWD, LC_HEAD_MUON = 4, 5, 6, 7, 8
 LC_SAE_PROJECT_ROWS, LC_SAE_LEARN_ALPHA = 1, 2
 _STATUS = {0: "LC_OK", -1: "LC_EINVAL", -2: "LC_ENULL", -3: "LC_EALIGN", -4: "LC_EWORKSPACE",
            -5: "LC_EUNSUPPORTED", -6: "LC_EHIP", -7: "LC_EINTERNAL"}

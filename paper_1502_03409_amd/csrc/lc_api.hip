@@ -212,6 +212,19 @@ int head_plan_query(int op, int32_t N, int32_t D, int32_t width, int dtype, lc_l
         const size_t ws = xent_workspace_bytes(N, D, width, dtype, grads);
         rc = grads ? xent_fwd_bwd(f, f, t, cf, ff, ff, f, f, N, D, width, dtype, f, ws, nullptr)
                    : xent_fwd(f, f, t, cf, ff, ff, N, D, width, dtype, f, ws, nullptr);
+    } else if (op == LC_HEAD_LOGP_FWD || op == LC_HEAD_LOGP_BWD) {
+        const bool back = op == LC_HEAD_LOGP_BWD;
+        const size_t ws = logp_workspace_bytes(N, D, width, 2, back ? 0 : 1, dtype, back);
+        rc = back ? logp_bwd(f, f, t, cf, cf, cf, cf, f, f, N, D, width, 2, dtype, f, ws, nullptr)
+                  : logp_fwd(f, f, t, ff, ff, (int64_t *)f, ff, ff, N, D, width, 2, 1, dtype, f, ws, nullptr);
+    } else if (op == LC_HEAD_Q8_MATMUL || op == LC_HEAD_Q8_GLU_FWD) {
+        const size_t ws = q8_workspace_bytes(N, D, width, dtype);
+        const int8_t *q = (const int8_t *)f;
+        rc = op == LC_HEAD_Q8_MATMUL ? q8_matmul(f, q, cf, f, N, D, width, dtype, f, ws, nullptr)
+                                     : q8_glu_fwd(f, q, cf, q, cf, f, N, D, width, LC_ACT_SILU, dtype, f, ws, nullptr);
+    } else if (op == LC_HEAD_MUON) {
+        const size_t ws = muon_workspace_bytes(N, D, width, dtype);
+        rc = muon_step(f, f, cf, f, ff, N, D, width, 0.1f, 0.f, 0.9f, 1, 5, dtype, f, ws, nullptr);
     }
     g_capture = nullptr;
     if (rc != LC_OK) return rc;
