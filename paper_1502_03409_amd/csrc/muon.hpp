@@ -423,6 +423,168 @@ int launch_symmetric(const char *name, const Operand &A, const Operand &B, const
     return LC_OK;
 }
 
+// ---------------------------------------------------------------------------------------------------------------------------
+// A group's steps on the short side where that is at most kChain: one workgroup a matrix, everything in LDS and registers.  A and Q stay in fp32
+// between products, in the layout of the accumulators; operands go through two places of LDS as planes, which the fragments are read from as
+// in a tile of the other products.  2 x 2 waves, each B / 2 x B / 2.
+//
+// 841 matrices of 128 x 128 in fp32: two and three steps 35 us a product with a kernel each, 14 of them; bound by the matrix unit, LDS reads
+// beside it and the barriers between products, as a workgroup has a compute unit for itself.
+constexpr int kChain = 128;
+template <int PL, int B>
+struct Chain {
+    static constexpr int PLANES = PL == HALF2 ? 2 : 1, MT = B / 64, PLANE = B * B * 2;   // bytes of a plane
+    static constexpr int PLACE = PLANES * PLANE;
+    typedef f32x16 Square[MT][MT];
+    char *lds;
+    int lane, m0, n0;
+    // where four values from column n on of row m lie in a plane: steps of 64 columns, rows of 128 bytes whose 16-byte pieces are exchanged by the row
+    static __device__ __forceinline__ int at(int m, int n) { return (n / 64 * B + m) * 128 + ((((n & 63) / 8) ^ ((m >> 1) & 7)) * 16) + (n & 7) * 2; }
+    // fn(block row, block column, component, row, column of the component's four)
+    template <typename Fn>
+    __device__ __forceinline__ void each4(const Fn &fn) const {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < MT; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) fn(i, j, 4 * q, m0 + 32 * i + (lane & 31), n0 + 32 * j + 8 * q + 4 * (lane >> 5));
+    }
+    __device__ __forceinline__ void put(int place, const Square &v) const {   // as planes
+        each4([&](int i, int j, int e, int m, int n) __attribute__((always_inline)) {
+            typedef bf16_t V4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+            for (int p = 0; p < PLANES; ++p) {
+                V4 w;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) w[r] = PlaneEpi<PLANES, true>::part(v[i][j][e + r], p);
+                *(V4 *)(lds + place * PLACE + p * PLANE + at(m, n)) = w;
+            }
+        });
+    }
+    // left times right, which is symmetric: rows of both
+    __device__ __forceinline__ void multiply(int left, int right, Square &acc) const {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < MT; ++j) acc[i][j] = (f32x16){};
+#pragma unroll
+        for (int k = 0; k < B; k += 16) {
+            u32x4 a[PLANES][MT], b[PLANES][MT];
+#pragma unroll
+            for (int p = 0; p < PLANES; ++p)
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    a[p][i] = *(const u32x4 *)(lds + left * PLACE + p * PLANE + at(m0 + 32 * i + (lane & 31), k + 8 * (lane >> 5)));
+                    b[p][i] = *(const u32x4 *)(lds + right * PLACE + p * PLANE + at(n0 + 32 * i + (lane & 31), k + 8 * (lane >> 5)));
+                }
+#pragma unroll
+            for (int q = 0; q < Format<PL>::PAIRS; ++q)
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int j = 0; j < MT; ++j)
+                        acc[i][j] = Format<PL>::mul(b[Format<PL>::B >> (4 * q) & 1][j], a[Format<PL>::A >> (4 * q) & 1][i], acc[i][j]);
+        }
+    }
+};
+
+template <int PL, int B>
+__global__ __launch_bounds__(256) void muon_chain_kernel(const bf16_t *a, bf16_t *out, long long plane, long long each, int n, int ld, int len) {
+    typedef Chain<PL, B> C;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int wave = threadIdx.x >> 6;
+    const C c = {smem, (int)threadIdx.x & 63, wave / 2 * (B / 2), wave % 2 * (B / 2)};
+    a += blockIdx.x * each, out += blockIdx.x * each;
+    typename C::Square held, q, acc;   // A, Q
+    c.each4([&](int i, int j, int e, int m, int k) __attribute__((always_inline)) {
+        typedef bf16_t V4 __attribute__((ext_vector_type(4)));
+        const bool in = m < n && k < ld;   // columns up to ld are zeros behind the last one
+#pragma unroll
+        for (int r = 0; r < 4; ++r) held[i][j][e + r] = 0.f;
+#pragma unroll
+        for (int p = 0; p < C::PLANES; ++p) {
+            V4 w = {0, 0, 0, 0};
+            if (in) w = *(const V4 *)(a + p * plane + (long long)m * ld + k);
+            *(V4 *)(smem + p * C::PLANE + C::at(m, k)) = w;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const bf16_t h = w[r];
+                held[i][j][e + r] += (float)__builtin_bit_cast(half_t, h);
+            }
+        }
+    });
+    __syncthreads();
+    for (int step = 0; step < len; ++step) {
+        // place 0 holds A
+        c.multiply(0, 0, acc);
+        c.each4([&](int i, int j, int e, int m, int k) __attribute__((always_inline)) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                acc[i][j][e + r] = acc[i][j][e + r] * (kMuonC * kScaleQ[1] / (kScaleA * kScaleA)) + held[i][j][e + r] * (kMuonB * kScaleQ[1] / kScaleA) +
+                                   (m == k + r && m < n ? kMuonA * kScaleQ[1] : 0.f);
+        });
+        const bool more = step + 1 < len;
+        if (step || more) c.put(1, acc);   // P
+        if (step == 0)
+#pragma unroll
+            for (int i = 0; i < C::MT; ++i)
+#pragma unroll
+                for (int j = 0; j < C::MT; ++j) q[i][j] = acc[i][j];
+        __syncthreads();
+        if (more) {
+            c.multiply(1, 0, acc);   // P A
+#pragma unroll
+            for (int i = 0; i < C::MT; ++i)
+#pragma unroll
+                for (int j = 0; j < C::MT; ++j) acc[i][j] *= 1.f / kScaleQ[1];
+            __syncthreads();
+            c.put(0, acc);
+            __syncthreads();
+            c.multiply(0, 1, held);   // P A P
+#pragma unroll
+            for (int i = 0; i < C::MT; ++i)
+#pragma unroll
+                for (int j = 0; j < C::MT; ++j) held[i][j] *= 1.f / kScaleQ[1];
+            __syncthreads();
+        }
+        if (step) {   // Q
+            c.put(0, q);
+            __syncthreads();
+            c.multiply(1, 0, q);
+            const float f = step == 1 ? kScaleQ[2] / (kScaleQ[1] * kScaleQ[1]) : kScaleQ[3] / (kScaleQ[1] * kScaleQ[2]);
+#pragma unroll
+            for (int i = 0; i < C::MT; ++i)
+#pragma unroll
+                for (int j = 0; j < C::MT; ++j) q[i][j] *= f;
+            __syncthreads();
+        }
+        if (more) {
+            c.put(0, held);
+            __syncthreads();
+        }
+    }
+    c.each4([&](int i, int j, int e, int m, int k) __attribute__((always_inline)) {
+        typedef bf16_t V4 __attribute__((ext_vector_type(4)));
+        if (m >= n || k >= ld) return;
+#pragma unroll
+        for (int p = 0; p < C::PLANES; ++p) {
+            V4 w;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) w[r] = PlaneEpi<C::PLANES, true>::part(q[i][j][e + r], p);
+            *(V4 *)(out + p * plane + (long long)m * ld + k) = w;
+        }
+    });
+}
+
+template <int PL, int B>
+int launch_chain(const bf16_t *a, bf16_t *q, long long plane, long long each, int n, int ld, int len, int items, hipStream_t s) {
+    const LaunchPlan p = make_plan("muon_chain", {PL, B}, {n, ld, len, items}, dim3((unsigned)items), 256, 2 * Chain<PL, B>::PLACE);
+    LC_PLAN_REQUIRE(p, n <= B && ld % 8 == 0 && ld >= n && ld < n + 8 && len >= 1 && len <= kGroupSteps);
+    LC_LAUNCH(p, "muon_step (Q)", (muon_chain_kernel<PL, B>), s, a, q, plane, each, n, ld, len);
+    return LC_OK;
+}
+
 constexpr long long kStackBytes = 1LL << 30;   // of X's planes at a time
 
 // Products of `items` matrices: short sides, the long side, the update of X.
@@ -443,6 +605,7 @@ inline double stack_us(const Shape &sh, int planes, int pairs, int how) {
     return std::max(choose_stack_cut(sh, pairs, how).us, bytes / 4.5e6);
 }
 inline int group_of(int items, int rows, int cols, int planes, int pairs) {
+    if (std::min(rows, cols) <= kChain) return kGroupSteps;
     const MuonShapes k(items, rows, cols);
     const int rows_only = rows > cols ? 0 : ROWS_ONLY;
     const double sq = stack_us(k.sq, planes, pairs, ROWS_ONLY | MAY_SPLIT), sx = stack_us(k.sx, planes, pairs, rows_only | MAY_SPLIT),
@@ -469,7 +632,8 @@ struct MuonScratch {
         s = sc.take<bf16_t>(square);
         q[0] = sc.take<bf16_t>(square);
         group = group_of(most, rows, cols, PLANES, Format<MuonFormat<T>::PL>::PAIRS);
-        if (rows != cols)   // whatever the stack's length says
+        if (small <= kChain) a = sc.take<bf16_t>(square);
+        else if (rows != cols)   // whatever the stack's length says
             for (bf16_t **p : {&a, &t, &q[1], &q[2]}) *p = sc.take<bf16_t>(square);
         // of as many matrices as are cut along the contraction; a shorter stack may be cut into more parts
         const long long cut = std::min<long long>(most, (long long)(kSplitTiles / stack_tiles(MuonShapes(1, rows, cols).sx, 128)));
@@ -512,12 +676,18 @@ int muon(const T *w, const T *g, const float *m, T *w_out, float *m_out, int cou
             Operand Xc = X;
             Xc.rows = k.ld;   // by columns
             const float fa = kScaleA / (kScaleX * kScaleX), fs = kShift * kScaleA;
-            const PlaneEpi<PLANES, true> ea = {len > 1 ? k.a : k.s, len > 1 ? k.s : nullptr, splane, each, k.lds, fa, len > 1 ? 0.f : fs, fs};
+            const bool chain = k.small <= kChain, plain = chain || len > 1;   // A itself, S, or both
+            const PlaneEpi<PLANES, true> ea = {plain ? k.a : k.s, plain && !chain ? k.s : nullptr, splane, each, k.lds, fa, plain ? 0.f : fs, fs};
             rc = tall ? launch_symmetric<PL, COL, COL>("muon_step (A)", Xc, Xc, of.sx, ea, k.part, st)
                       : launch_symmetric<PL, ROW, ROW>("muon_step (A)", X, X, of.sx, ea, k.part, st);
             if (rc) return rc;
             int q = 0;   // place of Q, the product of the group's P
-            for (int i = 0; i < len; ++i) {
+            if (chain) {
+                rc = k.small <= 64 ? launch_chain<PL, 64>(k.a, k.q[0], splane, each, k.small, k.lds, len, items, st)
+                                   : launch_chain<PL, 128>(k.a, k.q[0], splane, each, k.small, k.lds, len, items, st);
+                if (rc) return rc;
+            }
+            for (int i = 0; i < len && !chain; ++i) {
                 const int p = i ? (q + 1) % 3 : 0;
                 if ((rc = multiply("muon_step (P)", k.s, k.s, k.q[p], nullptr, kMuonC * kScaleQ[1] / (kScaleA * kScaleA), kRest * kScaleQ[1], 0.f))) return rc;
                 if (i + 1 < len) {
