@@ -26,11 +26,19 @@ constexpr long long kKeyBytes = 512LL << 20;      // groups' scores kept at a ti
 constexpr long long kGradBytes = 2LL << 30;       // of d
 constexpr int kGroupWords = 32;
 
+// Masked rows of large batches are left out: the others are gathered (count, place and index as in xent.hpp).  Up to kNarrow rows that would cost more
+// than it saves, and each row stays where it is: where x is laid out, a masked row of it becomes zeros, so
+// that what it holds makes no tile of fp32 planes form its sums again, and backward its d too, and its index -1.
 struct LogpRows {
-    int *count, *place, *index;   // as in xent.hpp; null: all rows count
-    float4 *sums;                 // by position: largest score, log(1 + r), entropy
+    int *count, *place, *index;   // null: all rows count, where they are
+    float4 *sums;                 // by position: largest score, log(1 + r), entropy; 1 where masked
     float *a, *b;                 // by position: A and b
 };
+__device__ __forceinline__ bool any_given(const int64_t *words, int T) {
+    bool any = false;
+    for (int t = 0; t < T; ++t) any |= words[t] >= 0;
+    return any;
+}
 
 // What a row without a word is answered.
 __device__ __forceinline__ void answer_masked(const LogpOut &out, long long n) {
@@ -51,9 +59,7 @@ static __global__ __launch_bounds__(1024) void logp_rows_kernel(const int64_t *t
     __syncthreads();
     for (int n0 = 0; n0 < N; n0 += 1024) {
         const int n = n0 + threadIdx.x;
-        bool in = false;
-        if (n < N)
-            for (int t = 0; t < T; ++t) in |= tags[(long long)n * T + t] >= 0;
+        const bool in = n < N && any_given(tags + (long long)n * T, T);
         const unsigned long long mask = __ballot(in);
         if (lane == 0) part[wave] = __popcll(mask);
         __syncthreads();
@@ -83,13 +89,12 @@ __global__ __launch_bounds__(256) void logp_gather_kernel(const T *x, bf16_t *ds
     const long long at = blockIdx.x * 256LL + threadIdx.x;
     const int n = (int)(at / pieces), piece = (int)(at - (long long)n * pieces), c = piece * 8;
     if (n >= N) return;
+    const bool masked = o.place ? o.place[n] < 0 : given.T && !any_given(given.tags + (long long)n * given.T, given.T);
     const int to = o.place ? o.place[n] : n;
     if (to >= 0) {
-        if (dst) {
-            float v[8];
-            load8(x + (long long)n * D, c, D, v);
-            put_planes<PL>(dst + (long long)to * pieces * 8 + c, (long long)N * pieces * 8, v);
-        }
+        float v[8] = {};
+        if (!masked) load8(x + (long long)n * D, c, D, v);
+        put_planes<PL>(dst + (long long)to * pieces * 8 + c, (long long)N * pieces * 8, v);
         if (GRADS && piece == 0) {
             float a = 0.f;
             for (int t = 0; t < given.T; ++t) {
@@ -97,10 +102,12 @@ __global__ __launch_bounds__(256) void logp_gather_kernel(const T *x, bf16_t *ds
                 if (word >= 0) a += word < given.V ? given.dlogp[(long long)n * given.T + t] : __builtin_nanf("");
             }
             o.a[to] = a;
-            o.b[to] = given.dentropy ? given.dentropy[n] : 0.f;
-            o.sums[to] = make_float4(given.state[3LL * n], given.state[3LL * n + 1], given.state[3LL * n + 2], 0.f);
+            o.b[to] = given.dentropy && !masked ? given.dentropy[n] : 0.f;
+            o.sums[to] = make_float4(given.state[3LL * n], given.state[3LL * n + 1], given.state[3LL * n + 2], masked ? 1.f : 0.f);
+            if (o.index && !o.place) o.index[n] = masked ? -1 : n;
         }
-    } else if (dx) {
+    }
+    if (masked && dx) {
         T *row = dx + (long long)n * D + c;
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -335,11 +342,20 @@ __global__ __launch_bounds__(THREADS) void logp_answer_kernel(const T *x, const 
         tops[2 * tid + 1] = 2 * tid + 1 < G ? __builtin_bit_cast(float, b) : -__builtin_inff();
     }
     if (tid == 0) found = 0, limit = -__builtin_inff();
+    bool given = false;
     for (int t = tid; t < out.T; t += THREADS) {
         const long long v = tags[n * out.T + t];
+        given |= v >= 0;
         word[room + t] = v < 0 ? -1 : v < V ? (int)v : -2;
     }
-    __syncthreads();
+    if (out.T && !o.place) {
+        if (!__syncthreads_or(given)) {
+            if (tid == 0) answer_masked(out, n);
+            return;
+        }
+    } else {
+        __syncthreads();
+    }
     if (JOIN && wave == 1) {
         share = lane < WAVES ? shares[lane] : Joined{-__builtin_inff(), 0.f, 0.f};
 #pragma unroll
@@ -529,7 +545,7 @@ struct LogpGradEpi {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const float g = logp_grad<T>(acc[i][j][4 * q + r], s[i], ra[i], rb[i]);
-                        v[r] = narrow<V>(n0 + c + r < words ? g : 0.f);
+                        v[r] = narrow<V>(n0 + c + r < words && s[i].w == 0.f ? g : 0.f);
                     }
                     stage.put(c, v);
                 }
@@ -548,6 +564,7 @@ __global__ __launch_bounds__(256) void logp_given_kernel(V *d, long long ld, Log
     const int m = (int)(at / g.T), t = (int)(at - (long long)m * g.T);
     if (m >= live(most, o.count, first)) return;
     const long long n = o.index ? o.index[first + m] : first + m;
+    if (n < 0) return;
     const int64_t *const words = g.tags + n * g.T;
     const float *const da = g.dlogp + n * g.T;
     const long long v = words[t];
@@ -599,7 +616,7 @@ struct LogpScratch {
     Parts part = {};
     LogpScratch(Scratch &sc, int N, int D, int V, bool given, bool grads) {
         Dp = (int)round_up(D, 8), Vp = (int)round_up(V, 64);
-        direct = PL == 1 && D == Dp, gathers = given;
+        direct = PL == 1 && D == Dp, gathers = given && N > kNarrow;
         groups_ld = (int)round_up((V + kGroupWords - 1) / kGroupWords, 2);
         const long long row_bytes = grads ? (long long)Vp * (long long)sizeof(T) : groups_ld * (long long)sizeof(Group);
         block = (int)std::min<long long>(round_up(N, 8), std::max<long long>(kStep, (grads ? kGradBytes : kKeyBytes) / row_bytes / 256 * 256));
@@ -614,11 +631,10 @@ struct LogpScratch {
         rows.sums = sc.take<float4>(N);
         rows.a = sc.take<float>(N);
         rows.b = sc.take<float>(N);
-        if (!given) rows.count = rows.place = rows.index = nullptr;
-        if (grads || !few) {
-            x = sc.take<bf16_t>((long long)PL * N * Dp);
-            w = direct ? nullptr : sc.take<bf16_t>((long long)PL * V * Dp);
-        }
+        if (!gathers) rows.count = rows.place = nullptr;
+        if (!gathers && !(given && grads)) rows.index = nullptr;
+        if (grads || (!few && (gathers || !direct))) x = sc.take<bf16_t>((long long)PL * N * Dp);
+        if ((grads || !few) && !direct) w = sc.take<bf16_t>((long long)PL * V * Dp);
         if (!grads) {
             stats = sc.take<float4>((V + 63) / 64 * (long long)block);
             groups = sc.take<Group>((long long)block * groups_ld);
@@ -662,10 +678,10 @@ int logp_forward(const T *x, const T *w, const int64_t *tags, const LogpOut &out
         const LogpEpi<T> epi = {g.stats, g.block, g.groups, g.groups_ld};
         int rc;
         if (few) {
-            rc = launch_few<T, ROW>("logp (few rows)", FewOperand<T>{x, x, D, N, g.rows.index}, FewOperand<T>{w, w, D, V, nullptr}, N, g.rows.count, V, D,
-                                    epi, s);
+            rc = launch_few<T, ROW>("logp (few rows)", FewOperand<T>{x, x, D, N, nullptr}, FewOperand<T>{w, w, D, V, nullptr}, N, nullptr, V, D, epi, s);
         } else {
-            const Operand X = {g.x + (long long)first * g.Dp, g.x, g.Dp, (long long)N * g.Dp, most, 0, 0};
+            const bf16_t *const xs = g.x ? g.x : (const bf16_t *)x;   // as it lies, where rows are neither picked nor laid out
+            const Operand X = {xs + (long long)first * g.Dp, xs, g.Dp, (long long)N * g.Dp, most, 0, 0};
             const Shape sh = {most, V, D, g.rows.count, first, nullptr, 0};
             rc = g.narrow ? launch_narrow<PL, ROW, 128>("logp", X, W, sh, epi, s)
                           : launch_cut<PL, ROW, ROW>("logp", X, W, sh, choose_cut(g.block, V, D, Planes<T>::PAIRS, false), epi, s);
@@ -714,8 +730,8 @@ int logp_backward(const T *x, const T *w, const int64_t *tags, const float *logp
         const Shape sh = {most, V, D, g.rows.count, first, nullptr, 0};
         const auto scores = [&](const auto &epi) -> int {
             if (few)
-                return launch_few<T, ROW>("logp_bwd (few rows)", FewOperand<T>{x, x, D, N, g.rows.index}, FewOperand<T>{w, w, D, V, nullptr}, N,
-                                          g.rows.count, V, D, epi, s);
+                return launch_few<T, ROW>("logp_bwd (few rows)", FewOperand<T>{x, x, D, N, nullptr}, FewOperand<T>{w, w, D, V, nullptr}, N, nullptr,
+                                          V, D, epi, s);
             if (g.narrow) return launch_narrow<PL, ROW, 128>("logp_bwd", X, Wr, sh, epi, s);
             return launch_cut<PL, ROW, ROW>("logp_bwd", X, Wr, sh, choose_cut(g.block, V, D, Planes<T>::PAIRS, false), epi, s);
         };
