@@ -132,7 +132,7 @@ struct LogpEpi {
     int groups_ld;
     template <int MT, int NT>
     __device__ __forceinline__ void run(f32x16 (&acc)[MT][NT], int m0, int n0, int lane, int M, int V, int, char *) const {
-        static_assert(NT == 2 || NT == 4, "half the groups of a row for each of its two lanes");
+        static_assert(NT == 1 || NT == 2 || NT == 4, "half the groups of a row for each of its two lanes, or one");
         const int h = lane >> 5;
         for_blocks<MT>([&](auto block) __attribute__((always_inline)) {
             constexpr int i = decltype(block)::value;
@@ -188,8 +188,10 @@ struct LogpEpi {
                 if constexpr (NT == 4) {   // the pair's second may be behind the last word, where the row still has room
                     const Group a = h ? g[2] : g[0], b = h ? g[3] : g[1];
                     *(u32x4 *)to = (u32x4){__builtin_bit_cast(unsigned, a.first), a.second, __builtin_bit_cast(unsigned, b.first), b.second};
-                } else {
+                } else if constexpr (NT == 2) {
                     *to = h ? g[1] : g[0];
+                } else if (h == 0) {
+                    *to = g[0];
                 }
             }
         });
@@ -603,6 +605,11 @@ __global__ __launch_bounds__(256) void logp_zero_kernel(T *p, long long n) {
     for (long long i = blockIdx.x * 256LL + threadIdx.x; i < n; i += gridDim.x * 256LL) p[i] = 0;
 }
 
+// Few rows' scores are formed by single blocks of 32 words: workgroups of half the size fill the compute units more evenly, and x is small (7 x
+// 1021 times 20011 in fp32 57.7 us with two blocks, 47.3 with one; 1 x 4096 in bf16 51.5 and 46.5, times 50000 103 and 96, times 128000 214
+// and 214).
+constexpr int kFewCols = 32;
+
 template <typename T>
 struct LogpScratch {
     static constexpr int PL = Planes<T>::N;
@@ -623,7 +630,7 @@ struct LogpScratch {
         blocks = N ? (N + block - 1) / block : 0;
         const bool few = N <= kFewRows;
         narrow = !few && N <= kNarrow;
-        wave_cols = few || narrow ? 64 : product_wave_cols(block, V, D, Planes<T>::PAIRS);
+        wave_cols = few ? kFewCols : narrow ? 64 : product_wave_cols(block, V, D, Planes<T>::PAIRS);
         tiles = (V + wave_cols - 1) / wave_cols;
         rows.count = sc.take<int>(1);
         rows.place = sc.take<int>(N);
@@ -636,7 +643,7 @@ struct LogpScratch {
         if (grads || (!few && (gathers || !direct))) x = sc.take<bf16_t>((long long)PL * N * Dp);
         if ((grads || !few) && !direct) w = sc.take<bf16_t>((long long)PL * V * Dp);
         if (!grads) {
-            stats = sc.take<float4>((V + 63) / 64 * (long long)block);
+            stats = sc.take<float4>(std::max((V + 63) / 64 * (long long)block, (V + kFewCols - 1) / kFewCols * std::min(round_up(N, 8), (long long)kFewRows)));
             groups = sc.take<Group>((long long)block * groups_ld);
             return;
         }
@@ -678,7 +685,7 @@ int logp_forward(const T *x, const T *w, const int64_t *tags, const LogpOut &out
         const LogpEpi<T> epi = {g.stats, g.block, g.groups, g.groups_ld};
         int rc;
         if (few) {
-            rc = launch_few<T, ROW>("logp (few rows)", FewOperand<T>{x, x, D, N, nullptr}, FewOperand<T>{w, w, D, V, nullptr}, N, nullptr, V, D, epi, s);
+            rc = launch_blocks<T, ROW, 1>("logp (few rows)", FewOperand<T>{x, x, D, N, nullptr}, FewOperand<T>{w, w, D, V, nullptr}, N, nullptr, V, D, epi, s);
         } else {
             const bf16_t *const xs = g.x ? g.x : (const bf16_t *)x;   // as it lies, where rows are neither picked nor laid out
             const Operand X = {xs + (long long)first * g.Dp, xs, g.Dp, (long long)N * g.Dp, most, 0, 0};
@@ -730,7 +737,7 @@ int logp_backward(const T *x, const T *w, const int64_t *tags, const float *logp
         const Shape sh = {most, V, D, g.rows.count, first, nullptr, 0};
         const auto scores = [&](const auto &epi) -> int {
             if (few)
-                return launch_few<T, ROW>("logp_bwd (few rows)", FewOperand<T>{x, x, D, N, nullptr}, FewOperand<T>{w, w, D, V, nullptr}, N, nullptr,
+                return launch_blocks<T, ROW, 1>("logp_bwd (few rows)", FewOperand<T>{x, x, D, N, nullptr}, FewOperand<T>{w, w, D, V, nullptr}, N, nullptr,
                                           V, D, epi, s);
             if (g.narrow) return launch_narrow<PL, ROW, 128>("logp_bwd", X, Wr, sh, epi, s);
             return launch_cut<PL, ROW, ROW>("logp_bwd", X, Wr, sh, choose_cut(g.block, V, D, Planes<T>::PAIRS, false), epi, s);
