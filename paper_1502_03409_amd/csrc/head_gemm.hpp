@@ -345,6 +345,7 @@ template <int NT> constexpr int kEpiBytes = 32 * (NT * 32 * 4 + 16);
 template <int PL, int FA, int FB, int BM, int BN, int NA, int NB, typename Epi>
 __global__ __launch_bounds__(64 * kWaves, (NA * BM + NB * BN) * 128 > 81920 ? 1 : 2) void gemm_kernel(Operand A, Operand B, Shape sh, int nt, int splits, Epi epi) {
     constexpr int MT = BM / 64, NT = BN / 64, PAIRS = Format<PL>::PAIRS;
+    static_assert(NA >= 3 && NB >= 2 && NB <= NA, "what may stay in flight at a step's barrier is counted for these");
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int M = live(sh.M, sh.rows_dev, sh.rows_first, sh.times);

@@ -585,6 +585,116 @@ int launch_chain(const bf16_t *a, bf16_t *q, long long plane, long long each, in
     return LC_OK;
 }
 
+// ---------------------------------------------------------------------------------------------------------------------------
+// X Q where rows are short, at most kShort values: a wave keeps Q and lets rows of X stream by, 32 at a time, from memory to registers and back.  Tiles
+// through LDS begin and end once for each 64 rows and are wide for nobody (3249 of 768 x 16 in fp32: 198 us, and 298 where w is
+// updated; 1485 of 5248 x 19 in bf16 506 and 1893).
+constexpr int kShort = 64, kShortBlocks = 4;   // blocks of 32 rows a wave
+template <typename T, int PL, int PLANES, int NT, bool UPDATE>
+__global__ __launch_bounds__(256) void muon_short_kernel(const bf16_t *x, long long plane, const bf16_t *q, long long qplane, int rows, int cols, int ld,
+                                                         int groups, PlaneEpi<PLANES, false> to, UpdateEpi<T> up) {
+    constexpr int KC = NT * 2;   // steps of 16 values of a row
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, h = lane >> 5;
+    const long long item = blockIdx.x / groups;
+    const int first = ((int)(blockIdx.x - item * groups) * 4 + wave) * (32 * kShortBlocks);
+    x += item * rows * ld, q += item * cols * ld;
+    if constexpr (UPDATE) up.item((int)item);
+    else to.item((int)item);
+    const u32x4 none = {0, 0, 0, 0};
+    u32x4 b[PLANES][KC][NT];
+#pragma unroll
+    for (int p = 0; p < PLANES; ++p)
+#pragma unroll
+        for (int c = 0; c < KC; ++c)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const int n = 32 * j + l32, k = 16 * c + 8 * h;
+                b[p][c][j] = n < cols && k < ld ? *(const u32x4 *)(q + p * qplane + n * ld + k) : none;
+            }
+#pragma unroll 2
+    for (int i = 0; i < kShortBlocks; ++i) {
+        const int m = first + 32 * i + l32;
+        if (first + 32 * i >= rows) break;
+        const long long row = min(m, rows - 1);
+        u32x4 a[PLANES][KC];
+#pragma unroll
+        for (int p = 0; p < PLANES; ++p)
+#pragma unroll
+            for (int c = 0; c < KC; ++c) {
+                const int k = 16 * c + 8 * h;
+                a[p][c] = k < ld ? *(const u32x4 *)(x + p * plane + row * ld + k) : none;
+            }
+        float old[NT][4][4];
+        if constexpr (UPDATE) {
+            const T *const w = up.w + row * cols;
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int n = 32 * j + 8 * e + 4 * h;
+                    T v[4];
+                    if (n + 4 <= cols) {
+                        __builtin_memcpy(v, w + n, sizeof(v));
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) v[r] = w[min(n + r, cols - 1)];
+                    }
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) old[j][e][r] = widen<T>(v[r]);
+                }
+        }
+        f32x16 acc[NT] = {};
+#pragma unroll
+        for (int c = 0; c < KC; ++c)
+#pragma unroll
+            for (int t = 0; t < Format<PL>::PAIRS; ++t)
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+                    acc[j] = Format<PL>::mul(b[Format<PL>::B >> (4 * t) & 1][c][j], a[Format<PL>::A >> (4 * t) & 1][c], acc[j]);
+        if (m >= rows) continue;
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int n = 32 * j + 8 * e + 4 * h;
+                if constexpr (UPDATE) {
+                    T *const w = up.w_out + row * cols;
+                    T o[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[r] = narrow<T>(up.keep * old[j][e][r] - up.rate * acc[j][4 * e + r]);
+                    if (n + 4 <= cols) {
+                        __builtin_memcpy(w + n, o, sizeof(o));
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (n + r < cols) w[n + r] = o[r];
+                    }
+                } else if (n < ld) {   // zeros behind the last column: Q has none there
+                    typedef bf16_t V4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+                    for (int p = 0; p < PLANES; ++p) {
+                        V4 w;
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) w[r] = to.part(acc[j][4 * e + r] * to.factor, p);
+                        *(V4 *)(to.out + p * to.plane + row * ld + n) = w;
+                    }
+                }
+            }
+    }
+}
+
+template <typename T, int PL, bool UPDATE, int PLANES>
+int launch_short(const Operand &X, const Operand &Q, int rows, int cols, int items, const PlaneEpi<PLANES, false> &to, const UpdateEpi<T> &up, hipStream_t s) {
+    const int groups = ceil_div(rows, 4 * 32 * kShortBlocks);
+    const LaunchPlan p = make_plan("muon_short", {PL, UPDATE}, {rows, cols, (int)X.ld, items}, dim3((unsigned)((long long)items * groups)), 256, 0);
+    LC_PLAN_REQUIRE(p, cols <= kShort && X.ld == Q.ld && X.ld % 8 == 0 && X.ld >= cols && X.ld < cols + 8 && (long long)items * groups <= 0x7fffffffLL);
+    if (cols <= 32)
+        LC_LAUNCH(p, "muon_step (X)", (muon_short_kernel<T, PL, PLANES, 1, UPDATE>), s, X.p0, X.plane, Q.p0, Q.plane, rows, cols, (int)X.ld, groups, to, up);
+    else
+        LC_LAUNCH(p, "muon_step (X)", (muon_short_kernel<T, PL, PLANES, 2, UPDATE>), s, X.p0, X.plane, Q.p0, Q.plane, rows, cols, (int)X.ld, groups, to, up);
+    return LC_OK;
+}
+
 constexpr long long kStackBytes = 1LL << 30;   // of X's planes at a time
 
 // Products of `items` matrices: short sides, the long side, the update of X.
@@ -702,15 +812,18 @@ int muon(const T *w, const T *g, const float *m, T *w_out, float *m_out, int cou
             }
             done += len;
             const Operand Q = square(k.q[q]);
+            const PlaneEpi<PLANES, false> next = {k.x[1 - at], nullptr, plane, X.each, k.ld, 1.f / kScaleQ[len], 0.f, 0.f};
+            const UpdateEpi<T> update = {w + skip, w_out + skip, n, cols, 1.f - decay, rate / (kScaleQ[len] * kScaleX)};
             const auto apply = [&](const auto &epi) {
                 const StackCut cut = choose_stack_cut(of.up, PAIRS, (tall ? ROWS_ONLY : 0) | (epi.UPDATES ? UPDATES : 0));
                 return tall ? launch_stack<PL, ROW, ROW>("muon_step (X)", X, Q, of.up, cut, epi, st)
                             : launch_stack<PL, ROW, COL>("muon_step (X)", Q, Xc, of.up, cut, epi, st);
             };
-            if (done < steps)
-                rc = apply(PlaneEpi<PLANES, false>{k.x[1 - at], nullptr, plane, X.each, k.ld, 1.f / kScaleQ[len], 0.f, 0.f});
+            const bool last = done == steps;
+            if (tall && cols <= kShort)
+                rc = last ? launch_short<T, PL, true>(X, Q, rows, cols, items, next, update, st) : launch_short<T, PL, false>(X, Q, rows, cols, items, next, update, st);
             else
-                rc = apply(UpdateEpi<T>{w + skip, w_out + skip, n, cols, 1.f - decay, rate / (kScaleQ[len] * kScaleX)});
+                rc = last ? apply(update) : apply(next);
             if (rc) return rc;
             at = 1 - at;
         }

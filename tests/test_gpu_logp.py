@@ -148,7 +148,7 @@ def test_values_and_gradients(N, D, V, T, K, dtype):
 
 
 @dtypes
-@pytest.mark.parametrize("N", [3, 90])
+@pytest.mark.parametrize("N", [3, 90, 260])      # few rows, rows that stay where they are, rows that are gathered
 def test_masked_rows_are_not_looked_at(N, dtype):
     x, w, tags = inputs(N, 70, 260, 2, dtype, seed=3, masked=0.5)
     tags[1] = -1
@@ -169,7 +169,7 @@ def test_masked_rows_are_not_looked_at(N, dtype):
 
 
 @dtypes
-@pytest.mark.parametrize("N", [1, 70])
+@pytest.mark.parametrize("N", [1, 70, 193])
 def test_no_row_left(N, dtype):
     x, w, tags = inputs(N, 33, 40, 2, dtype)
     tags.fill_(-1)
@@ -191,7 +191,7 @@ def test_no_rows(dtype):
 
 
 @dtypes
-@pytest.mark.parametrize("N", [20, 50])
+@pytest.mark.parametrize("N", [20, 50, 200])
 def test_a_tag_outside_the_vocabulary_is_loud(N, dtype):
     x, w, tags = inputs(N, 40, 100, 2, dtype, masked=0.0)
     tags[7, 1], tags[8, 0] = 100, 1 << 40

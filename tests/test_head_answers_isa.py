@@ -28,3 +28,10 @@ def test_loads_into_lds_carry_their_wait_states(assembly, source):
 @pytest.mark.parametrize("source", SOURCES)
 def test_a_barrier_of_the_loads_waits_for_them(assembly, source):
     isa.test_a_barrier_of_the_loads_waits_for_them(assembly, source)
+
+
+@pytest.mark.parametrize("source", SOURCES)
+def test_kernels_have_names_that_both_passes_agree_on(assembly, source):
+    """An unnamed type in a kernel's signature is numbered by the host's and the device's pass apart, and its launch finds no kernel."""
+    names = [l.split()[1] for l in assembly[source].splitlines() if l.strip().startswith(".amdhsa_kernel")]
+    assert len(names) > 5 and not [n for n in names if "$" in n]
