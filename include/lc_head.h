@@ -120,7 +120,7 @@ int q8_glu_fwd(const void *x, const int8_t *qg, const float *sg, const int8_t *q
                int32_t D, int32_t F, int act, int dtype, void *ws, size_t ws_bytes, void *hip_stream);
 
 /* Host only.  Scratch for logp_fwd (grads = 0), or for logp_fwd and logp_bwd (grads = 1); 0 for invalid arguments.  What is enough for N rows is
- * enough for fewer.  T: words given with each row, 0 to 64; K: likeliest words asked for, 0 to 64 and no more than V.  It is bounded for any
+ * enough for fewer, and what is for K words for fewer.  T: words given with each row, 0 to 64; K: likeliest words asked for, 0 to 64 and no more than V.  It is bounded for any
  * number of rows but for what a few numbers and, laid out, x take. */
 size_t logp_workspace_bytes(int32_t N, int32_t D, int32_t V, int32_t T, int32_t K, int dtype, int grads);
 

@@ -10,7 +10,7 @@ template <typename T>
 int logp_backward(const T *x, const T *w, const int64_t *tags, const float *logp, const float *state, const float *dlogp, const float *dentropy, T *dx,
                   T *dw, int N, int D, int V, int T_, void *ws, hipStream_t s);
 template <typename T>
-size_t logp_scratch(int N, int D, int V, bool given, bool grads);
+size_t logp_scratch(int N, int D, int V, int K, bool given, bool grads);
 
 namespace {
 
@@ -29,8 +29,9 @@ extern "C" {
 
 size_t logp_workspace_bytes(int32_t N, int32_t D, int32_t V, int32_t T, int32_t K, int dtype, int grads) {
     if (!logp_sizes(N, D, V, T, K, dtype)) return 0;
-    const auto bytes = [&](bool g) { return dtype == LC_BF16 ? logp_scratch<bf16_t>(N, D, V, T > 0, g) : logp_scratch<float>(N, D, V, T > 0, g); };
-    return grads ? std::max(bytes(false), bytes(true)) : bytes(false);
+    const auto bytes = [&](int k, bool g) { return dtype == LC_BF16 ? logp_scratch<bf16_t>(N, D, V, k, T > 0, g) : logp_scratch<float>(N, D, V, k, T > 0, g); };
+    const size_t forward = std::max(bytes(K, false), bytes(0, false));   // fewer words may be looked for in another way
+    return grads ? std::max(forward, bytes(0, true)) : forward;
 }
 
 int logp_fwd(const void *x, const void *w, const int64_t *tags, float *logp, float *entropy, int64_t *top, float *top_logp, float *state, int32_t N,

@@ -123,15 +123,15 @@ struct __attribute__((aligned(8))) Group {
 
 // Per wave and row: (largest score m, sum of exp(l - m) without one of the largest, sum of exp(l - m) (m - l)), and the groups.  A distance m - l is
 // not negative, so distances compare as whole numbers, infinite and NaN ones as the largest; its last five bits make room for the word's place
-// in the group.
-template <typename T>
+// in the group.  WORDS: the scores themselves in the place of the groups, -inf behind the last word.
+template <typename T, bool WORDS>
 struct LogpEpi {
     float4 *stats;       // [wave's columns][stats_ld]
     long long stats_ld;
-    Group *groups;       // [M][groups_ld], groups_ld even
+    void *groups;        // [M][groups_ld] Group or float, rows of whole 16 bytes
     int groups_ld;
     template <int MT, int NT>
-    __device__ __forceinline__ void run(f32x16 (&acc)[MT][NT], int m0, int n0, int lane, int M, int V, int, char *) const {
+    __device__ __forceinline__ void run(f32x16 (&acc)[MT][NT], int m0, int n0, int lane, int M, int V, int, char *lds) const {
         static_assert(NT == 1 || NT == 2 || NT == 4, "half the groups of a row for each of its two lanes, or one");
         const int h = lane >> 5;
         for_blocks<MT>([&](auto block) __attribute__((always_inline)) {
@@ -165,10 +165,12 @@ struct LogpEpi {
                     sum += p;
                     part += __builtin_amdgcn_fractf(p);
                     apart += p * fminf(d, 256.f);   // beyond, and where l = -inf, p is zero
+                    if constexpr (WORDS) continue;
                     const unsigned key = (__builtin_bit_cast(unsigned, d) & ~31u) | (8 * (e >> 2) + (e & 3) + 4 * h);
                     next = max(min(near, next), min(max(near, next), key));
                     near = min(near, key);
                 }
+                if constexpr (WORDS) continue;
                 const unsigned near2 = __shfl_xor((int)near, 32), next2 = __shfl_xor((int)next, 32);
                 next = min(min(next, next2), max(near, near2));
                 near = min(near, near2);
@@ -179,11 +181,26 @@ struct LogpEpi {
             sum += __shfl_xor(sum, 32);
             part += __shfl_xor(part, 32);
             apart += __shfl_xor(apart, 32);
+            if constexpr (WORDS) {
+                const RowStage<float, NT * 32> stage = {lds, lane};
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                        stage.put(32 * j + 8 * q + 4 * h, v);
+                    }
+                stage.take([&](int r, int c, const u32x4 &w) {
+                    const int to = m0 + 32 * i + r;
+                    if (to < M && n0 + c < groups_ld) *(u32x4 *)((float *)groups + (long long)to * groups_ld + n0 + c) = w;
+                });
+            }
             if (m >= M) return;
             // what reaches one are the largest scores; one of them is left out
             const float rest = top == -__builtin_inff() ? sum * 0.f : part + (rintf(sum - part) - 1.f);
             if (h == 0) stats[(n0 / (NT * 32)) * stats_ld + m] = make_float4(top, rest, apart, 0.f);
-            Group *const to = groups + (long long)m * groups_ld + n0 / kGroupWords + h * (NT / 2);
+            if constexpr (WORDS) return;
+            Group *const to = (Group *)groups + (long long)m * groups_ld + n0 / kGroupWords + h * (NT / 2);
             if (n0 + 32 * (h * (NT / 2)) < V) {
                 if constexpr (NT == 4) {   // the pair's second may be behind the last word, where the row still has room
                     const Group a = h ? g[2] : g[0], b = h ? g[3] : g[1];
@@ -286,11 +303,12 @@ constexpr int most_candidates(int K) { return K * kGroupWords > 256 ? K * kGroup
 // One row a workgroup: its likeliest words, the log probabilities of its given words, and what the joined sums say.  JOIN: joins them too, where
 // rows are few enough for their tiles not to be read by whole lines.  Bound by latency for few rows, so what one wait can bring is asked for at once;
 // for many by the groups' scores and the candidates' weights.
-template <typename T, int THREADS, bool JOIN>
+// A workgroup looks at groups, or at words where their scores have been kept: PER of them in 16 bytes.
+template <typename T, int THREADS, bool JOIN, bool WORDS>
 __global__ __launch_bounds__(THREADS) void logp_answer_kernel(const T *x, const T *w, const int64_t *tags, const float4 *stats, long long stats_ld, int tiles,
-                                                             const Group *groups, int groups_ld, LogpRows o, LogpOut out, int first, int most, int D,
+                                                             const void *groups, int groups_ld, LogpRows o, LogpOut out, int first, int most, int D,
                                                              int V) {
-    constexpr int WAVES = THREADS / 64, HELD = 8;
+    constexpr int WAVES = THREADS / 64, HELD = 8, PER = WORDS ? 4 : 2, SIZE = WORDS ? 1 : kGroupWords;   // words of a group
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tid = threadIdx.x;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     __shared__ __attribute__((aligned(16))) float tops[THREADS];
@@ -305,11 +323,11 @@ __global__ __launch_bounds__(THREADS) void logp_answer_kernel(const T *x, const 
     int *const word = (int *)(score + room + out.T);
     if (m >= live(most, o.count, first)) return;
     const long long n = o.index ? o.index[first + m] : first + m;
-    const int G = (V + kGroupWords - 1) / kGroupWords, pairs = (G + 1) / 2;
-    const u32x4 *const row = (const u32x4 *)(groups + (long long)m * groups_ld);   // two groups at a time; behind the last one: not looked at
-    u32x4 held[HELD];   // this thread's first pairs
+    const int G = (V + SIZE - 1) / SIZE, pieces = (G + PER - 1) / PER;
+    const u32x4 *const row = (const u32x4 *)((const char *)groups + (long long)m * groups_ld * (16 / PER));   // behind the last group: not looked at
+    u32x4 held[HELD];   // this thread's first pieces
 #pragma unroll
-    for (int k = 0; k < HELD; ++k) held[k] = row[min(tid + k * THREADS, pairs - 1)];
+    for (int k = 0; k < HELD; ++k) held[k] = row[min(tid + k * THREADS, pieces - 1)];
     Joined share;
     if constexpr (JOIN) {
         share = join_some(stats, stats_ld, tiles, m, tid, THREADS);
@@ -322,26 +340,30 @@ __global__ __launch_bounds__(THREADS) void logp_answer_kernel(const T *x, const 
     }
     // fn(group, its largest score, its second largest with the largest's place) for this thread's groups
     const auto for_groups = [&](const auto &fn) __attribute__((always_inline)) {
-        const auto both = [&](int p, const u32x4 &v) __attribute__((always_inline)) {
-            const unsigned a = v[0], a2 = v[1], b = v[2], b2 = v[3];
-            fn(2 * p, __builtin_bit_cast(float, a), a2);
-            if (2 * p + 1 < G) fn(2 * p + 1, __builtin_bit_cast(float, b), b2);
+        const auto each = [&](int p, const u32x4 &v) __attribute__((always_inline)) {
+#pragma unroll
+            for (int k = 0; k < PER; ++k) {
+                const unsigned f = v[WORDS ? k : 2 * k], second = v[WORDS ? k : 2 * k + 1];
+                if (k == 0 || PER * p + k < G) fn(PER * p + k, __builtin_bit_cast(float, f), second);
+            }
         };
 #pragma unroll
         for (int k = 0; k < HELD; ++k)
-            if (tid + k * THREADS < pairs) both(tid + k * THREADS, held[k]);
-        for (int p = tid + HELD * THREADS; p < pairs; p += THREADS) both(p, row[p]);
+            if (tid + k * THREADS < pieces) each(tid + k * THREADS, held[k]);
+        for (int p = tid + HELD * THREADS; p < pieces; p += THREADS) each(p, row[p]);
     };
     float own = -__builtin_inff();
     for_groups([&](int, float f, unsigned) __attribute__((always_inline)) { own = fmaxf(own, f); });
     // maxima of 256 parts of the groups: few groups are parts of their own
-    const bool single = pairs <= 128;
+    const bool single = pieces <= 256 / PER;
     if (!single) {
         tops[tid] = own;
-    } else if (tid < 128) {
-        const unsigned a = held[0][0], b = held[0][2];
-        tops[2 * tid] = tid < pairs ? __builtin_bit_cast(float, a) : -__builtin_inff();
-        tops[2 * tid + 1] = 2 * tid + 1 < G ? __builtin_bit_cast(float, b) : -__builtin_inff();
+    } else if (tid < 256 / PER) {
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const unsigned f = held[0][WORDS ? k : 2 * k];
+            tops[PER * tid + k] = PER * tid + k < G ? __builtin_bit_cast(float, f) : -__builtin_inff();
+        }
     }
     if (tid == 0) found = 0, limit = -__builtin_inff();
     bool given = false;
@@ -426,13 +448,13 @@ __global__ __launch_bounds__(THREADS) void logp_answer_kernel(const T *x, const 
     if (own >= cut)   // few threads
         for_groups([&](int g, float f, unsigned second) __attribute__((always_inline)) {
             if (!(f >= cut)) return;
-            if (__builtin_bit_cast(float, second) >= cut) {
+            if (!WORDS && __builtin_bit_cast(float, second) >= cut) {
                 const int words = min(kGroupWords, V - g * kGroupWords), at = atomicAdd(&found, words);
                 for (int i = 0; i < words; ++i)
                     if (at + i < room) word[at + i] = g * kGroupWords + i;
             } else {
                 const int at = atomicAdd(&found, 1);
-                if (at < room) word[at] = g * kGroupWords + (int)(second & 31u);
+                if (at < room) word[at] = WORDS ? g : g * kGroupWords + (int)(second & 31u);
             }
         });
     __syncthreads();
@@ -459,8 +481,8 @@ __global__ __launch_bounds__(THREADS) void logp_answer_kernel(const T *x, const 
             __syncthreads();
             for (int v = 0; v < WAVES; ++v) mine = picked[v] > mine ? picked[v] : mine;
             last = mine;
-            const int g = 0x7fffffff - (int)(unsigned)mine, words = min(kGroupWords, V - g * kGroupWords);
-            if (tid < words) word[candidates + tid] = g * kGroupWords + tid;
+            const int g = 0x7fffffff - (int)(unsigned)mine, words = min(SIZE, V - g * SIZE);
+            if (tid < words) word[candidates + tid] = g * SIZE + tid;
             candidates += words;
         }
         __syncthreads();
@@ -609,6 +631,9 @@ __global__ __launch_bounds__(256) void logp_zero_kernel(T *p, long long n) {
 // 1021 times 20011 in fp32 57.7 us with two blocks, 47.3 with one; 1 x 4096 in bf16 51.5 and 46.5, times 50000 103 and 96, times 128000 214
 // and 214).
 constexpr int kFewCols = 32;
+// Whether scores are kept as they are: for small vocabularies of which many words are asked for, about 16 K^2 / V groups hold two of them or more,
+// and all their words' scores would be formed again (4046 x 256 over 2760 words, 30 likeliest: 391 us with groups).
+inline bool keeps_words(int V, int K) { return V <= 8192 && 8LL * K * K > V; }
 
 template <typename T>
 struct LogpScratch {
@@ -618,14 +643,16 @@ struct LogpScratch {
     LogpRows rows = {};
     bf16_t *x = nullptr, *w = nullptr, *d = nullptr;
     float4 *stats = nullptr;
-    Group *groups = nullptr;
+    void *groups = nullptr;
     float *kept = nullptr, *sum = nullptr;
     Parts part = {};
-    LogpScratch(Scratch &sc, int N, int D, int V, bool given, bool grads) {
+    bool words;   // scores are kept, and not those of groups
+    LogpScratch(Scratch &sc, int N, int D, int V, int K, bool given, bool grads) {
         Dp = (int)round_up(D, 8), Vp = (int)round_up(V, 64);
         direct = PL == 1 && D == Dp, gathers = given && N > kNarrow;
-        groups_ld = (int)round_up((V + kGroupWords - 1) / kGroupWords, 2);
-        const long long row_bytes = grads ? (long long)Vp * (long long)sizeof(T) : groups_ld * (long long)sizeof(Group);
+        words = keeps_words(V, K);
+        groups_ld = words ? (int)round_up(V, 4) : (int)round_up((V + kGroupWords - 1) / kGroupWords, 2);
+        const long long row_bytes = grads ? (long long)Vp * (long long)sizeof(T) : groups_ld * (words ? 4LL : (long long)sizeof(Group));
         block = (int)std::min<long long>(round_up(N, 8), std::max<long long>(kStep, (grads ? kGradBytes : kKeyBytes) / row_bytes / 256 * 256));
         blocks = N ? (N + block - 1) / block : 0;
         const bool few = N <= kFewRows;
@@ -644,7 +671,7 @@ struct LogpScratch {
         if ((grads || !few) && !direct) w = sc.take<bf16_t>((long long)PL * V * Dp);
         if (!grads) {
             stats = sc.take<float4>(std::max((V + 63) / 64 * (long long)block, (V + kFewCols - 1) / kFewCols * std::min(round_up(N, 8), (long long)kFewRows)));
-            groups = sc.take<Group>((long long)block * groups_ld);
+            groups = sc.take<char>(block * row_bytes);
             return;
         }
         const int twice = PL == 1 ? 2 * std::min(N, kFewRows) : 0;
@@ -676,24 +703,24 @@ int logp_forward(const T *x, const T *w, const int64_t *tags, const LogpOut &out
     constexpr int PL = Planes<T>::N;
     if (N == 0) return LC_OK;
     Scratch sc(ws);
-    const LogpScratch<T> g(sc, N, D, V, out.T > 0, false);
+    const LogpScratch<T> g(sc, N, D, V, out.K, out.T > 0, false);
     if (int rc = g.lay_out(x, w, nullptr, LogpGiven{tags, nullptr, nullptr, nullptr, out.T, V}, out, false, N, D, V, s)) return rc;
     const bool few = N <= kFewRows;
     const Operand W = g.w ? Operand{g.w, g.w, g.Dp, (long long)V * g.Dp, V, 0, 0} : Operand{(const bf16_t *)w, (const bf16_t *)w, D, 0, V, 0, 0};
     for (int b = 0; b < g.blocks; ++b) {
         const int first = b * g.block, most = std::min(g.block, N - first);
-        const LogpEpi<T> epi = {g.stats, g.block, g.groups, g.groups_ld};
-        int rc;
-        if (few) {
-            rc = launch_blocks<T, ROW, 1>("logp (few rows)", FewOperand<T>{x, x, D, N, nullptr}, FewOperand<T>{w, w, D, V, nullptr}, N, nullptr, V, D, epi, s);
-        } else {
+        const auto scores = [&](const auto &epi) -> int {
+            if (few)
+                return launch_blocks<T, ROW, 1>("logp (few rows)", FewOperand<T>{x, x, D, N, nullptr}, FewOperand<T>{w, w, D, V, nullptr}, N, nullptr, V, D,
+                                                epi, s);
             const bf16_t *const xs = g.x ? g.x : (const bf16_t *)x;   // as it lies, where rows are neither picked nor laid out
             const Operand X = {xs + (long long)first * g.Dp, xs, g.Dp, (long long)N * g.Dp, most, 0, 0};
             const Shape sh = {most, V, D, g.rows.count, first, nullptr, 0};
-            rc = g.narrow ? launch_narrow<PL, ROW, 128>("logp", X, W, sh, epi, s)
-                          : launch_cut<PL, ROW, ROW>("logp", X, W, sh, choose_cut(g.block, V, D, Planes<T>::PAIRS, false), epi, s);
-        }
-        if (rc) return rc;
+            return g.narrow ? launch_narrow<PL, ROW, 128>("logp", X, W, sh, epi, s)
+                            : launch_cut<PL, ROW, ROW>("logp", X, W, sh, choose_cut(g.block, V, D, Planes<T>::PAIRS, false), epi, s);
+        };
+        if (int rc = g.words ? scores(LogpEpi<T, true>{g.stats, g.block, g.groups, g.groups_ld}) : scores(LogpEpi<T, false>{g.stats, g.block, g.groups, g.groups_ld}))
+            return rc;
         const bool apart = most >= 2048;
         if (apart) {
             const LaunchPlan p = make_plan("logp_join", {}, {most}, dim3((most + 15) / 16), 256, 0);
@@ -702,15 +729,17 @@ int logp_forward(const T *x, const T *w, const int64_t *tags, const LogpOut &out
         const int threads = most <= kComputeUnits ? 1024 : 256;
         const LaunchPlan p = make_plan("logp_answer", {(int)sizeof(T), apart}, {most, D, V, out.T, out.K}, dim3(most), threads,
                                        12 * (size_t)(most_candidates(std::max(out.K, 1)) + out.T));
-        if (apart)
-            LC_LAUNCH(p, "logp (answer)", (logp_answer_kernel<T, 256, false>), s, x, w, tags, g.stats, (long long)g.block, g.tiles, g.groups, g.groups_ld, g.rows,
-                      out, first, most, D, V);
-        else if (threads == 256)
-            LC_LAUNCH(p, "logp (answer)", (logp_answer_kernel<T, 256, true>), s, x, w, tags, g.stats, (long long)g.block, g.tiles, g.groups, g.groups_ld, g.rows,
-                      out, first, most, D, V);
-        else
-            LC_LAUNCH(p, "logp (answer)", (logp_answer_kernel<T, 1024, true>), s, x, w, tags, g.stats, (long long)g.block, g.tiles, g.groups, g.groups_ld, g.rows,
-                      out, first, most, D, V);
+        const auto answer = [&](auto kernel) -> int {
+            LC_LAUNCH(p, "logp (answer)", kernel, s, x, w, tags, g.stats, (long long)g.block, g.tiles, g.groups, g.groups_ld, g.rows, out, first, most, D, V);
+            return LC_OK;
+        };
+        if (int rc = g.words ? apart            ? answer(logp_answer_kernel<T, 256, false, true>)
+                               : threads == 256 ? answer(logp_answer_kernel<T, 256, true, true>)
+                                                : answer(logp_answer_kernel<T, 1024, true, true>)
+                     : apart          ? answer(logp_answer_kernel<T, 256, false, false>)
+                     : threads == 256 ? answer(logp_answer_kernel<T, 256, true, false>)
+                                      : answer(logp_answer_kernel<T, 1024, true, false>))
+            return rc;
     }
     return LC_OK;
 }
@@ -726,7 +755,7 @@ int logp_backward(const T *x, const T *w, const int64_t *tags, const float *logp
         return LC_OK;
     }
     Scratch sc(ws);
-    const LogpScratch<T> g(sc, N, D, V, given_words > 0, true);
+    const LogpScratch<T> g(sc, N, D, V, 0, given_words > 0, true);
     const LogpGiven given = {tags, state, dlogp, dentropy, given_words, V};
     if (int rc = g.lay_out(x, w, dx, given, LogpOut{}, true, N, D, V, s)) return rc;
     const bool few = N <= kFewRows, fine = few && PL == 1;   // fine: d in two parts
@@ -796,9 +825,9 @@ int logp_backward(const T *x, const T *w, const int64_t *tags, const float *logp
 }
 
 template <typename T>
-size_t logp_scratch(int N, int D, int V, bool given, bool grads) {
+size_t logp_scratch(int N, int D, int V, int K, bool given, bool grads) {
     Scratch sc(nullptr);
-    (void)LogpScratch<T>(sc, N, D, V, given, grads);
+    (void)LogpScratch<T>(sc, N, D, V, K, given, grads);
     return sc.used;
 }
 

@@ -50,7 +50,7 @@ class TagHead:
         self.top = torch.empty(batch * likeliest, dtype=torch.int64, device=device)
         self.entropy, self.state = torch.empty(batch, device=device), torch.empty(batch, 3, device=device)
         need = max(H.glu_workspace_bytes(batch, D, F, self.code, True), H.xent_workspace_bytes(batch, F, V, self.code, True),
-                   H.grad_clip_workspace_bytes(self.grads), *(H.logp_workspace_bytes(batch, F, V, t, 0, self.code, True) for t in (0, tags)),
+                   H.grad_clip_workspace_bytes(self.grads), *(H.logp_workspace_bytes(batch, F, V, t, likeliest, self.code, True) for t in (0, tags)),
                    *(H.muon_workspace_bytes(1, *w.shape, self.code) for w in self.params if momentum is not None))
         self.ws = torch.empty(need, dtype=torch.uint8, device=device)
 

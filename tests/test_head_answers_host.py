@@ -167,6 +167,7 @@ def test_scratch_for_many_is_enough_for_fewer(dtype):
         for T in (0, 2):
             fwd, both = (lc.logp_workspace_bytes(N, D, V, T, 1, dtype, g) for g in (False, True))
             assert fwd <= both
+            assert all(lc.logp_workspace_bytes(N, D, V, T, k, dtype) <= lc.logp_workspace_bytes(N, D, V, T, min(V, 40), dtype) for k in range(min(V, 40)))
             for n in {rng.randrange(N) for _ in range(40)} | set(range(min(N, 40))):
                 assert lc.logp_workspace_bytes(n, D, V, T, 1, dtype) <= fwd and lc.logp_workspace_bytes(n, D, V, T, 1, dtype, True) <= both, (n, N, D, V)
         assert all(lc.q8_workspace_bytes(n, D, V, dtype) <= lc.q8_workspace_bytes(N, D, V, dtype) for n in range(0, N, 37))
