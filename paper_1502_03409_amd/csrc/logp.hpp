@@ -40,38 +40,58 @@ __device__ __forceinline__ bool any_given(const int64_t *words, int T) {
     return any;
 }
 
-// What a row without a word is answered.
+// What a row without a word is answered, by a workgroup.
 __device__ __forceinline__ void answer_masked(const LogpOut &out, long long n) {
-    if (out.entropy) out.entropy[n] = 0.f;
-    if (out.state)
-        for (int k = 0; k < 3; ++k) out.state[3 * n + k] = 0.f;
-    if (out.logp)
-        for (int t = 0; t < out.T; ++t) out.logp[n * out.T + t] = 0.f;
-    for (int k = 0; k < out.K; ++k) out.top[n * out.K + k] = -1, out.top_logp[n * out.K + k] = 0.f;
+    if (threadIdx.x == 0) {
+        if (out.entropy) out.entropy[n] = 0.f;
+        if (out.state) out.state[3 * n] = out.state[3 * n + 1] = out.state[3 * n + 2] = 0.f;
+    }
+    for (int t = threadIdx.x; t < out.T; t += blockDim.x) out.logp[n * out.T + t] = 0.f;
+    for (int k = threadIdx.x; k < out.K; k += blockDim.x) out.top[n * out.K + k] = -1, out.top_logp[n * out.K + k] = 0.f;
 }
 
-// Positions of the rows that have a word; the answers of those that have none.  One workgroup, 1024 rows at a time.
-static __global__ __launch_bounds__(1024) void logp_rows_kernel(const int64_t *tags, int N, int T, LogpRows o, LogpOut out) {
-    __shared__ int part[16];
-    __shared__ int total;
+// Positions of the rows that have a word; behind them in the index, from its end, those that have none.  One workgroup, 8192 rows at a time, eight a
+// thread.
+static __global__ __launch_bounds__(1024) void logp_rows_kernel(const int64_t *tags, int N, int T, LogpRows o) {
+    constexpr int EACH = 8;
+    __shared__ int part[EACH * 16 + 1];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if (threadIdx.x == 0) total = 0;
-    __syncthreads();
-    for (int n0 = 0; n0 < N; n0 += 1024) {
-        const int n = n0 + threadIdx.x;
-        const bool in = n < N && any_given(tags + (long long)n * T, T);
-        const unsigned long long mask = __ballot(in);
-        if (lane == 0) part[wave] = __popcll(mask);
+    int total = 0;
+    for (int n0 = 0; n0 < N; n0 += 1024 * EACH) {
+        unsigned long long mask[EACH];
+        bool in[EACH] = {};
+        for (int t = 0; t < T; ++t)
+#pragma unroll
+            for (int k = 0; k < EACH; ++k) {
+                const int n = n0 + k * 1024 + (int)threadIdx.x;
+                in[k] |= n < N && tags[(long long)min(n, N - 1) * T + t] >= 0;
+            }
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+            mask[k] = __ballot(in[k]);
+            if (lane == 0) part[k * 16 + wave] = __popcll(mask[k]);
+        }
         __syncthreads();
-        int at = total;
-        for (int w = 0; w < wave; ++w) at += part[w];
-        at += __popcll(mask & ((1ull << lane) - 1));
-        if (n < N) o.place[n] = in ? at : -1;
-        if (in) o.index[at] = n;
-        else if (n < N) answer_masked(out, n);
+        if (wave == 0) {   // sums of all before, 128 of them
+            const int a = part[2 * lane], b = part[2 * lane + 1];
+            int s = a + b;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const int other = __shfl_up(s, d);
+                if (lane >= d) s += other;
+            }
+            part[2 * lane] = s - a - b, part[2 * lane + 1] = s - b;
+            if (lane == 63) part[EACH * 16] = s;
+        }
         __syncthreads();
-        if (threadIdx.x == 0)
-            for (int w = 0; w < 16; ++w) total += part[w];
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+            const int n = n0 + k * 1024 + threadIdx.x, at = total + part[k * 16 + wave] + __popcll(mask[k] & ((1ull << lane) - 1));
+            if (n >= N) continue;
+            o.place[n] = in[k] ? at : -1;
+            o.index[in[k] ? at : N - 1 - (n - at)] = n;
+        }
+        total += part[EACH * 16];
         __syncthreads();
     }
     if (threadIdx.x == 0) *o.count = total;
@@ -321,8 +341,11 @@ __global__ __launch_bounds__(THREADS) void logp_answer_kernel(const T *x, const 
     const int m = blockIdx.x, K = max(out.K, 1), room = most_candidates(K);
     double *const score = (double *)smem;
     int *const word = (int *)(score + room + out.T);
-    if (m >= live(most, o.count, first)) return;
     const long long n = o.index ? o.index[first + m] : first + m;
+    if (m >= live(most, o.count, first)) {
+        answer_masked(out, n);
+        return;
+    }
     const int G = (V + SIZE - 1) / SIZE, pieces = (G + PER - 1) / PER;
     const u32x4 *const row = (const u32x4 *)((const char *)groups + (long long)m * groups_ld * (16 / PER));   // behind the last group: not looked at
     u32x4 held[HELD];   // this thread's first pieces
@@ -374,7 +397,7 @@ __global__ __launch_bounds__(THREADS) void logp_answer_kernel(const T *x, const 
     }
     if (out.T && !o.place) {
         if (!__syncthreads_or(given)) {
-            if (tid == 0) answer_masked(out, n);
+            answer_masked(out, n);
             return;
         }
     } else {
@@ -681,10 +704,10 @@ struct LogpScratch {
         part.at = sc.take<float>(part.floats);
         sum = blocks > 1 ? sc.take<float>((long long)V * D) : nullptr;
     }
-    int lay_out(const T *xs, const T *ws, T *dx, const LogpGiven &given, const LogpOut &out, bool grads, int N, int D, int V, hipStream_t s) const {
+    int lay_out(const T *xs, const T *ws, T *dx, const LogpGiven &given, bool grads, int N, int D, int V, hipStream_t s) const {
         if (gathers) {
             const LaunchPlan p = make_plan("logp_rows", {}, {N, given.T}, dim3(1), 1024, 0);
-            LC_LAUNCH(p, "logp (rows)", logp_rows_kernel, s, given.tags, N, given.T, rows, out);
+            LC_LAUNCH(p, "logp (rows)", logp_rows_kernel, s, given.tags, N, given.T, rows);
         }
         if (x) {
             const long long n = ((long long)N * (Dp / 8) + 255) / 256;
@@ -704,7 +727,7 @@ int logp_forward(const T *x, const T *w, const int64_t *tags, const LogpOut &out
     if (N == 0) return LC_OK;
     Scratch sc(ws);
     const LogpScratch<T> g(sc, N, D, V, out.K, out.T > 0, false);
-    if (int rc = g.lay_out(x, w, nullptr, LogpGiven{tags, nullptr, nullptr, nullptr, out.T, V}, out, false, N, D, V, s)) return rc;
+    if (int rc = g.lay_out(x, w, nullptr, LogpGiven{tags, nullptr, nullptr, nullptr, out.T, V}, false, N, D, V, s)) return rc;
     const bool few = N <= kFewRows;
     const Operand W = g.w ? Operand{g.w, g.w, g.Dp, (long long)V * g.Dp, V, 0, 0} : Operand{(const bf16_t *)w, (const bf16_t *)w, D, 0, V, 0, 0};
     for (int b = 0; b < g.blocks; ++b) {
@@ -757,7 +780,7 @@ int logp_backward(const T *x, const T *w, const int64_t *tags, const float *logp
     Scratch sc(ws);
     const LogpScratch<T> g(sc, N, D, V, 0, given_words > 0, true);
     const LogpGiven given = {tags, state, dlogp, dentropy, given_words, V};
-    if (int rc = g.lay_out(x, w, dx, given, LogpOut{}, true, N, D, V, s)) return rc;
+    if (int rc = g.lay_out(x, w, dx, given, true, N, D, V, s)) return rc;
     const bool few = N <= kFewRows, fine = few && PL == 1;   // fine: d in two parts
     Operand W = g.w ? Operand{g.w, g.w, g.Dp, (long long)V * g.Dp, V, 0, 0} : Operand{(const bf16_t *)w, (const bf16_t *)w, D, 0, V, 0, 0};
     for (int b = 0; b < g.blocks; ++b) {

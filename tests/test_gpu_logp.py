@@ -435,3 +435,14 @@ def test_tags_may_start_at_any_row_of_a_list(dtype):
     a, b = answers(x, w, tags, 2), answers(x, w, longer[1:22], 2)
     for k in a:
         assert torch.equal(a[k], b[k]), k
+
+
+def test_more_rows_than_are_counted_at_a_time():
+    """Rows with and without words, well beyond 8192, in an order that has no pattern."""
+    N, D, V = 20000, 16, 40
+    x, w, tags = inputs(N, D, V, 2, torch.float32, seed=21, masked=0.4)
+    got = answers(x, w, tags, 2)
+    check_answers(x, w, tags, 2, got)
+    dlogp, dentropy = upstream(N, 2)
+    want = definition(x, w, tags, 2)
+    check_gradients(x, w, tags, dlogp, dentropy, gradients(x, w, tags, got, dlogp, dentropy), score_bound(want["x"], w), want)
