@@ -181,7 +181,8 @@ __device__ __forceinline__ void tile_in_stack(const Shape &sh, int wg, int mt, i
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------
-// The tiled product.  BM x BN of the result per workgroup of 2 x 2 waves, steps of 64 along the contraction, through LDS buffers that
+// The tiled product.  BM x BN of the result per workgroup of 2 x 2 waves, or 4 x 2 (W 8) where tiles are large: two waves on a SIMD wait for
+// different things (8192 x 4096 times 128000 6.97 ms with four, 6.65 with eight, the same bits), steps of 64 along the contraction, through LDS buffers that
 // are filled by loads which go straight there: NA for A, NB for B (three and two are all 160 KB for 256 x 256).  A long contraction over
 // few tiles is cut into `splits` parts, whose sums are added up by a kernel of their own.
 //
@@ -205,10 +206,10 @@ constexpr int kWaves = 4;
 
 // Brings an operand's tile of N rows, one step after the other.  A wave can issue about six other instructions per matrix instruction, so
 // what a step needs is kept running: one base for all of a wave's loads, which moves along, and one offset per load.
-template <int FORM, int N, int PL>
+template <int FORM, int N, int PL, int W = kWaves>
 struct Stager {
     static constexpr bool COLS = FORM == COL || FORM == COLPAIR;
-    static constexpr int Q = N / 8 / kWaves;   // load instructions of a wave a step, 1024 bytes each
+    static constexpr int Q = N / 8 / W;   // load instructions of a wave a step, 1024 bytes each
     static constexpr int PAIRS = Format<PL>::PAIRS;
     unsigned off[Q];
     gbyte_ptr base, base2;                     // of the current kStep indices; the second matrix (PAIR: of these indices, COLPAIR: its start)
@@ -223,7 +224,8 @@ struct Stager {
         ld2 = (unsigned)ld, plane = o.plane * 2;
         depth = o.depth, half = o.half;
         move = COLS ? kStep * ld : kStep * 2;
-        // load q of this wave brings rows 8 (q kWaves + wave) on: of a pair, those of the first matrix for even q
+        // load q of this wave brings rows 8 (q W + wave) on: of a pair, with four waves, those of the first matrix for even q; with eight, those
+        // of one matrix
         int second;
         const int top = min(FORM == PAIR ? pair_row(r0, 32, &second) : r0, o.rows - 1);
 #pragma unroll
@@ -234,13 +236,14 @@ struct Stager {
                 const int k = first_k(q) >= again && first_k(q) < 2 * again ? first_k(q) - again : first_k(q);
                 off[q] = (unsigned)k * ld2 + (unsigned)(min(r0 + 8 * c, o.rows - 8) - r0) * 2;
             } else {
-                int f = r0 + 8 * (q * kWaves + wave), s;
+                int f = r0 + 8 * (q * W + wave), s;
                 if constexpr (FORM == PAIR) f = pair_row(f, 32, &s);
                 off[q] = (unsigned)(min(f + lane / 8, o.rows - 1) - top) * ld2 + first_k(q) * 2;
             }
         }
         if constexpr (COLS) base = (gbyte_ptr)(o.p0 + r0), base2 = (gbyte_ptr)(o.p1 + r0);
         else base = (gbyte_ptr)(o.p0 + (long long)top * o.ld), base2 = (gbyte_ptr)(o.p1 + (long long)top * o.ld) + kt * move;
+        if (FORM == PAIR && W == 8 && wave >= 4) base = base2;
         if (FORM == COLPAIR && kt * kStep >= half) base = base2, base += (kt - half / kStep) * move;
         else base += kt * move;
         trimmed = false;
@@ -248,7 +251,7 @@ struct Stager {
     }
     // the index within the step of the first value (by columns: of all values) of this lane's 16 bytes of load q
     __device__ __forceinline__ int first_k(int q) const {
-        if constexpr (COLS) return (q * kWaves + wave) * (512 / N) + lane / (N / 8);
+        if constexpr (COLS) return (q * W + wave) * (512 / N) + lane / (N / 8);
         else return ((lane % 8) ^ (4 * (wave & 1) + lane / 16)) * 8;
     }
     // indices from this step on that exist (by rows: in whole 16-byte pieces)
@@ -288,14 +291,14 @@ struct Stager {
     }
     template <int q>
     __device__ __forceinline__ void load(unsigned lds) const {
-        const gbyte_ptr p = FORM == PAIR && q % 2 ? base2 : base;
-        load_lds16(PAIRS == 1 && PL != 2 ? p : p + at, off[q], lds + q * kWaves * 1024);
+        const gbyte_ptr p = FORM == PAIR && W == 4 && q % 2 ? base2 : base;
+        load_lds16(PAIRS == 1 && PL != 2 ? p : p + at, off[q], lds + q * W * 1024);
     }
     // zeros for what is beyond the `n` indices left of a step (the same bytes this lane brought)
     __device__ __forceinline__ void clear(char *lds, int n) const {
 #pragma unroll
         for (int q = 0; q < Q; ++q)
-            if (first_k(q) >= n) *(u32x4 *)(lds + (q * kWaves + wave) * 1024 + lane * 16) = (u32x4){0, 0, 0, 0};
+            if (first_k(q) >= n) *(u32x4 *)(lds + (q * W + wave) * 1024 + lane * 16) = (u32x4){0, 0, 0, 0};
     }
 };
 
@@ -342,9 +345,9 @@ struct Reader {
 // LDS of a wave's epilogue: one block of 32 rows on its way to whole 16-byte pieces.
 template <int NT> constexpr int kEpiBytes = 32 * (NT * 32 * 4 + 16);
 
-template <int PL, int FA, int FB, int BM, int BN, int NA, int NB, typename Epi>
-__global__ __launch_bounds__(64 * kWaves, (NA * BM + NB * BN) * 128 > 81920 ? 1 : 2) void gemm_kernel(Operand A, Operand B, Shape sh, int nt, int splits, Epi epi) {
-    constexpr int MT = BM / 64, NT = BN / 64, PAIRS = Format<PL>::PAIRS;
+template <int PL, int FA, int FB, int BM, int BN, int NA, int NB, int W, typename Epi>
+__global__ __launch_bounds__(64 * W, W > kWaves || (NA * BM + NB * BN) * 128 <= 81920 ? 2 : 1) void gemm_kernel(Operand A, Operand B, Shape sh, int nt, int splits, Epi epi) {
+    constexpr int MT = BM / (16 * W), NT = BN / 64, PAIRS = Format<PL>::PAIRS;
     static_assert(NA >= 3 && NB >= 2 && NB <= NA, "what may stay in flight at a step's barrier is counted for these");
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -371,11 +374,11 @@ __global__ __launch_bounds__(64 * kWaves, (NA * BM + NB * BN) * 128 > 81920 ? 1 
     // parts are whole steps of the contraction at its longest; what is beyond its actual end is left out
     const int per = ((sh.K + kStep - 1) / kStep + splits - 1) / splits;
     const int kt0 = split * per, kt1 = min((K + kStep - 1) / kStep, kt0 + per), steps = max(0, kt1 - kt0) * PAIRS;
-    Stager<FA, BM, PL> sa;
-    Stager<FB, BN, PL> sb;
+    Stager<FA, BM, PL, W> sa;
+    Stager<FB, BN, PL, W> sb;
     sa.init(A, tm * BM, kt0, K, Format<PL>::A, wave, lane);
     sb.init(B, tn * BN, kt0, K, Format<PL>::B, wave, lane, PL == 2 ? K / 2 : 0);
-    constexpr int QA = Stager<FA, BM, PL>::Q, QB = Stager<FB, BN, PL>::Q;
+    constexpr int QA = Stager<FA, BM, PL, W>::Q, QB = Stager<FB, BN, PL, W>::Q;
     const unsigned lds_wave = lds0 + wave * 1024;
     auto load_a = [&](unsigned buffer, auto number) __attribute__((always_inline)) { sa.template load<decltype(number)::value>(lds_wave + buffer); };
     auto load_b = [&](unsigned buffer, auto number) __attribute__((always_inline)) { sb.template load<decltype(number)::value>(lds_wave + B0 + buffer); };
@@ -484,13 +487,13 @@ __global__ __launch_bounds__(64 * kWaves, (NA * BM + NB * BN) * 128 > 81920 ? 1 
     epi.run(acc, m0, n0, lane, M, sh.Nn, split, smem + wave * kEpiBytes<NT>);
 }
 
-template <int PL, int FA, int FB, int BM, int BN, int NA, int NB, typename Epi>
+template <int PL, int FA, int FB, int BM, int BN, int NA, int NB, int W = kWaves, typename Epi>
 int launch_tiles(const char *name, const Operand &A, const Operand &B, const Shape &sh, int splits, const Epi &epi, hipStream_t s) {
     const int mt = ceil_div(sh.M, BM), nt = ceil_div(sh.Nn, BN);
     constexpr int LDS = (NA * BM + NB * BN) * 128;
-    static_assert(kWaves * kEpiBytes<BN / 64> <= LDS, "the epilogue's LDS is that of the buffers");
+    static_assert(W * kEpiBytes<BN / 64> <= LDS, "the epilogue's LDS is that of the buffers");
     const long long wgs = tiles_in(sh, mt, nt) * splits * sh.stack;
-    const LaunchPlan p = make_plan(name, {PL, FA, FB, BM, BN, NA, NB}, {sh.M, sh.Nn, sh.K, splits, sh.stack, sh.sym}, dim3((unsigned)wgs), 64 * kWaves, LDS);
+    const LaunchPlan p = make_plan(name, {PL, FA, FB, BM, BN, NA, NB, W}, {sh.M, sh.Nn, sh.K, splits, sh.stack, sh.sym}, dim3((unsigned)wgs), 64 * W, LDS);
     LC_PLAN_REQUIRE(p, wgs <= 0x7fffffffLL && splits >= 1);
     LC_PLAN_REQUIRE(p, Format<PL>::STACK ? sh.stack >= 1 && !sh.rows_dev && !sh.k_dev && (!sh.sym || (BM == BN && sh.M == sh.Nn && mt <= 4096))
                                          : sh.stack == 1 && !sh.sym);
@@ -504,7 +507,7 @@ int launch_tiles(const char *name, const Operand &A, const Operand &B, const Sha
                                          sh.K == B.half + B.depth));
     LC_PLAN_REQUIRE(p, A.ld <= (1 << 22) && B.ld <= (1 << 22));   // 256 rows' offsets stay below 2^31 bytes
     LC_PLAN_REQUIRE(p, ptr_aligned16(A.p0) && ptr_aligned16(B.p0) && ptr_aligned16(B.p1));
-    LC_LAUNCH(p, name, (gemm_kernel<PL, FA, FB, BM, BN, NA, NB, Epi>), s, A, B, sh, nt, splits, epi);
+    LC_LAUNCH(p, name, (gemm_kernel<PL, FA, FB, BM, BN, NA, NB, W, Epi>), s, A, B, sh, nt, splits, epi);
     return LC_OK;
 }
 
@@ -708,9 +711,10 @@ inline Cut choose_cut(int M, int Nn, int K, int pairs, bool may_split) {
     return best;
 }
 
-template <int PL, int FA, int FB, typename Epi>
+// W: waves of a large tile.
+template <int PL, int FA, int FB, int W = kWaves, typename Epi>
 int launch_cut(const char *name, const Operand &A, const Operand &B, const Shape &sh, const Cut &c, const Epi &epi, hipStream_t s) {
-    if (c.tile == Cut::LARGE) return launch_tiles<PL, FA, FB, 256, 256, 3, 2>(name, A, B, sh, c.splits, epi, s);
+    if (c.tile == Cut::LARGE) return launch_tiles<PL, FA, FB, 256, 256, 3, 2, W>(name, A, B, sh, c.splits, epi, s);
     if (c.tile == Cut::SMALL) return launch_tiles<PL, FA, FB, 128, 128, 3, 2>(name, A, B, sh, c.splits, epi, s);
     return launch_tiles<PL, FA, FB, 128, 128, 5, 5>(name, A, B, sh, c.splits, epi, s);
 }
@@ -719,10 +723,10 @@ int launch_cut(const char *name, const Operand &A, const Operand &B, const Shape
 inline int product_wave_cols(int M, int Nn, int K, int pairs) { return choose_cut(M, Nn, K, pairs, false).tile == Cut::LARGE ? 128 : 64; }
 
 // A product whose epilogue needs whole sums.
-template <int PL, int FA, int FB, typename Epi>
+template <int PL, int FA, int FB, int W = kWaves, typename Epi>
 int launch_gemm(const char *name, const Operand &A, const Operand &B, const Shape &sh, const Epi &epi, hipStream_t s) {
     if (sh.M == 0 || sh.Nn == 0) return LC_OK;
-    return launch_cut<PL, FA, FB>(name, A, B, sh, choose_cut(sh.M, sh.Nn, sh.K, PL == 3 ? 6 : 1, false), epi, s);
+    return launch_cut<PL, FA, FB, W>(name, A, B, sh, choose_cut(sh.M, sh.Nn, sh.K, PL == 3 ? 6 : 1, false), epi, s);
 }
 
 // A product of up to kNarrow rows, as mini-batches that are answered have, with tiles of 64 rows: what waits for weights from HBM is more
@@ -749,16 +753,16 @@ struct Parts {
 };
 
 // A product that is stored, cut along its contraction where that helps; FOLD: always through its parts.
-template <int PL, int FA, int FB, bool FOLD = false, typename T>
+template <int PL, int FA, int FB, bool FOLD = false, int W = kWaves, typename T>
 int launch_product(const char *name, const Operand &A, const Operand &B, const Shape &sh, const StoreEpi<T> &epi, const Parts &part, hipStream_t s) {
     if (sh.M == 0 || sh.Nn == 0) return LC_OK;
     const Cut c = choose_cut(sh.M, sh.Nn, sh.K, PL == 3 ? 6 : 1, true);
-    if (!FOLD && c.splits == 1) return launch_cut<PL, FA, FB>(name, A, B, sh, c, epi, s);
+    if (!FOLD && c.splits == 1) return launch_cut<PL, FA, FB, W>(name, A, B, sh, c, epi, s);
     const long long ld = round_up(sh.Nn, 4);
     const long long blocks = ((long long)(FOLD ? sh.M / 2 : sh.M) * (ld / 4) + 255) / 256;
     const LaunchPlan p = make_plan(name, {}, {sh.M, sh.Nn, c.splits}, dim3((unsigned)blocks), 256, 0);
     LC_PLAN_REQUIRE(p, blocks <= 0x7fffffffLL && part.at && c.splits * sh.M * ld <= part.floats);
-    if (int rc = launch_cut<PL, FA, FB>(name, A, B, sh, c, PartEpi{part.at, ld, sh.M}, s)) return rc;
+    if (int rc = launch_cut<PL, FA, FB, W>(name, A, B, sh, c, PartEpi{part.at, ld, sh.M}, s)) return rc;
     LC_LAUNCH(p, name, (join_parts_kernel<T, FOLD>), s, part.at, ld, c.splits, sh, epi);
     return LC_OK;
 }

@@ -740,7 +740,7 @@ int logp_forward(const T *x, const T *w, const int64_t *tags, const LogpOut &out
             const Operand X = {xs + (long long)first * g.Dp, xs, g.Dp, (long long)N * g.Dp, most, 0, 0};
             const Shape sh = {most, V, D, g.rows.count, first, nullptr, 0};
             return g.narrow ? launch_narrow<PL, ROW, 128>("logp", X, W, sh, epi, s)
-                            : launch_cut<PL, ROW, ROW>("logp", X, W, sh, choose_cut(g.block, V, D, Planes<T>::PAIRS, false), epi, s);
+                            : launch_cut<PL, ROW, ROW, 8>("logp", X, W, sh, choose_cut(g.block, V, D, Planes<T>::PAIRS, false), epi, s);
         };
         if (int rc = g.words ? scores(LogpEpi<T, true>{g.stats, g.block, g.groups, g.groups_ld}) : scores(LogpEpi<T, false>{g.stats, g.block, g.groups, g.groups_ld}))
             return rc;
@@ -792,7 +792,7 @@ int logp_backward(const T *x, const T *w, const int64_t *tags, const float *logp
                 return launch_blocks<T, ROW, 1>("logp_bwd (few rows)", FewOperand<T>{x, x, D, N, nullptr}, FewOperand<T>{w, w, D, V, nullptr}, N, nullptr,
                                           V, D, epi, s);
             if (g.narrow) return launch_narrow<PL, ROW, 128>("logp_bwd", X, Wr, sh, epi, s);
-            return launch_cut<PL, ROW, ROW>("logp_bwd", X, Wr, sh, choose_cut(g.block, V, D, Planes<T>::PAIRS, false), epi, s);
+            return launch_cut<PL, ROW, ROW, 8>("logp_bwd", X, Wr, sh, choose_cut(g.block, V, D, Planes<T>::PAIRS, false), epi, s);
         };
         const auto words = [&](auto *d) -> int {
             typedef std::remove_reference_t<decltype(*d)> Stored_t;
@@ -818,13 +818,13 @@ int logp_backward(const T *x, const T *w, const int64_t *tags, const float *logp
                 Wr.rows = X.rows = g.Dp;
                 if (dx) {
                     const Shape shx = {two, D, V, g.rows.count, 0, nullptr, 0, 2};
-                    if ((rc = launch_product<PL, ROW, COL, true>("logp_bwd (dx)", d, Wr, shx, StoreEpi<T>{dx, nullptr, 0x7fffffff, N, 0, D, index, nullptr, nullptr},
+                    if ((rc = launch_product<PL, ROW, COL, true, 8>("logp_bwd (dx)", d, Wr, shx, StoreEpi<T>{dx, nullptr, 0x7fffffff, N, 0, D, index, nullptr, nullptr},
                                                                  g.part, s)))
                         return rc;
                 }
                 const Shape shw = {V, D, two, nullptr, 0, g.rows.count, 0, 2};
                 d.rows = g.Vp;
-                return launch_gemm<2, COL, COL>("logp_bwd (dw)", d, X, shw, StoreEpi<T>{dw, nullptr, 0x7fffffff, V, 0, D, nullptr, nullptr, nullptr}, s);
+                return launch_gemm<2, COL, COL, 8>("logp_bwd (dw)", d, X, shw, StoreEpi<T>{dw, nullptr, 0x7fffffff, V, 0, D, nullptr, nullptr, nullptr}, s);
             }
         const long long pd = (long long)g.block * g.Vp;
         if (kept && (rc = launch_planes<PL, 1>("logp_bwd (d)", from, g.d, g.Vp, pd, most, g.Vp, 0, s))) return rc;
@@ -832,16 +832,16 @@ int logp_backward(const T *x, const T *w, const int64_t *tags, const float *logp
         Wr.rows = X.rows = g.Dp;
         if (dx) {
             const Shape shx = {most, D, V, g.rows.count, first, nullptr, 0};
-            if ((rc = launch_product<PL, ROW, COL>("logp_bwd (dx)", d, Wr, shx, StoreEpi<T>{to, nullptr, 0x7fffffff, most, 0, D, index, nullptr, nullptr}, g.part, s)))
+            if ((rc = launch_product<PL, ROW, COL, false, 8>("logp_bwd (dx)", d, Wr, shx, StoreEpi<T>{to, nullptr, 0x7fffffff, most, 0, D, index, nullptr, nullptr}, g.part, s)))
                 return rc;
         }
         const Shape shw = {V, D, most, nullptr, 0, g.rows.count, first};
         d.rows = g.Vp;
         const float *add = b ? g.sum : nullptr;
         if (b + 1 < g.blocks)
-            rc = launch_product<PL, COL, COL>("logp_bwd (dw)", d, X, shw, StoreEpi<float>{g.sum, nullptr, 0x7fffffff, V, 0, D, nullptr, add, nullptr}, g.part, s);
+            rc = launch_product<PL, COL, COL, false, 8>("logp_bwd (dw)", d, X, shw, StoreEpi<float>{g.sum, nullptr, 0x7fffffff, V, 0, D, nullptr, add, nullptr}, g.part, s);
         else
-            rc = launch_product<PL, COL, COL>("logp_bwd (dw)", d, X, shw, StoreEpi<T>{dw, nullptr, 0x7fffffff, V, 0, D, nullptr, add, nullptr}, g.part, s);
+            rc = launch_product<PL, COL, COL, false, 8>("logp_bwd (dw)", d, X, shw, StoreEpi<T>{dw, nullptr, 0x7fffffff, V, 0, D, nullptr, add, nullptr}, g.part, s);
         if (rc) return rc;
     }
     return LC_OK;

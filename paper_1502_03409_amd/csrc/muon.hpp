@@ -401,7 +401,7 @@ inline StackCut choose_stack_cut(const Shape &sh, int pairs, int how) {
 template <int PL, int FA, int FB, typename Epi>
 int launch_stack(const char *name, const Operand &A, const Operand &B, const Shape &sh, const StackCut &c, const Epi &epi, hipStream_t s) {
     if constexpr (!Epi::UPDATES)
-        if (c.tile == 256) return launch_tiles<PL, FA, FB, 256, 256, 3, 2>(name, A, B, sh, c.splits, epi, s);
+        if (c.tile == 256) return launch_tiles<PL, FA, FB, 256, 256, 3, 2, 8>(name, A, B, sh, c.splits, epi, s);
     if constexpr (FA == ROW && FB == ROW)
         if (c.tile == 192) return launch_tiles<PL, FA, FB, 192, 192, 3, 2>(name, A, B, sh, c.splits, epi, s);
     if (c.tile == 64) return launch_tiles<PL, FA, FB, 64, 64, 3, 2>(name, A, B, sh, c.splits, epi, s);

@@ -129,7 +129,7 @@ int q8_matmul(const T *x, const int8_t *qw, const float *sw, T *y, int N, int D,
     const Operand X = bytes_operand(g.q, g.q, ld, N), W = bytes_operand(qw, qw, ld, F);
     if (N <= 64) return launch_narrow<BYTES, ROW, 64>("q8_matmul", X, W, sh, epi, s);
     if (N <= kNarrow) return launch_narrow<BYTES, ROW, 128>("q8_matmul", X, W, sh, epi, s);
-    return launch_gemm<BYTES, ROW, ROW>("q8_matmul", X, W, sh, epi, s);
+    return launch_gemm<BYTES, ROW, ROW, 8>("q8_matmul", X, W, sh, epi, s);
 }
 
 template <typename T, int ACT>
@@ -146,7 +146,7 @@ int q8_glu(const T *x, const int8_t *qg, const float *sg, const int8_t *qu, cons
     const Operand X = bytes_operand(g.q, g.q, ld, N), W = bytes_operand(qg, qu, ld, F);
     const ScaledEpi<GluEpi<T, ACT>, 32> epi = {GluEpi<T, ACT>{h, nullptr, F}, g.scale, sg, su, F};
     if (N <= kNarrow) return launch_narrow<BYTES, PAIR, 128>("q8_glu_fwd", X, W, sh, epi, s);
-    return launch_gemm<BYTES, ROW, PAIR>("q8_glu_fwd", X, W, sh, epi, s);
+    return launch_gemm<BYTES, ROW, PAIR, 8>("q8_glu_fwd", X, W, sh, epi, s);
 }
 template <typename T>
 int q8_glu(int act, const T *x, const int8_t *qg, const float *sg, const int8_t *qu, const float *su, T *h, int N, int D, int F, void *ws,
