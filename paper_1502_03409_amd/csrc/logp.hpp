@@ -542,16 +542,19 @@ __global__ __launch_bounds__(THREADS) void logp_answer_kernel(const T *x, const 
     for (int c = tid + THREADS; c < candidates; c += THREADS)
         if (rank_of(c) == 0) base64 = score[c];
     __syncthreads();
-    const double top = base64;
+    // The largest score has 64 bits here and 32 in the sum, where it stands for exp of itself: what the others' sum is relative to it moves by the
+    // difference, times their share.
+    const double top = base64, moved = (top - (double)sums.x) * (double)-expm1f(-sums.y);
+    const auto log_p = [&](double s) { return (float)((s - top) + moved - (double)sums.y); };
     for (int c = tid; out.K && c < candidates; c += THREADS) {
         if (c != tid) rank = rank_of(c);
         if (rank >= out.K) continue;
         out.top[n * out.K + rank] = word[c];
-        out.top_logp[n * out.K + rank] = (float)(score[c] - top) - sums.y;
+        out.top_logp[n * out.K + rank] = log_p(score[c]);
     }
     for (int t = tid; t < out.T; t += THREADS) {
         const int v = word[room + t];
-        out.logp[n * out.T + t] = v == -2 ? __builtin_nanf("") : v < 0 ? 0.f : (float)fmin(score[room + t] - top, 0.0) - sums.y;
+        out.logp[n * out.T + t] = v == -2 ? __builtin_nanf("") : v < 0 ? 0.f : log_p(fmin(score[room + t], top));
     }
 }
 

@@ -9,7 +9,9 @@
 // Products with the longer side are the long ones, so up to three steps go by on the short side alone: all of their A and P are polynomials of the
 // first A and commute, the next A is (P A) P, and X takes the product Q of the group's P at once.  No more than three, because a rounding of the
 // first A, r of |A| at most, grows with the square of what Q does to it: r 3.4445^4 by the third step, where it meets singular values of 0.08 and
-// more of the largest, and 3.4445^8 by the fifth.
+// more of the largest, and 3.4445^8 by the fifth.  What a group's later A is off by counts where it brings singular values near one, which start at
+// about one over the root of the short side: within three steps of few and not before the fourth of thousands, so short groups come first on short
+// sides and last on long ones (fp32, 41 x 1280 0.46 and 0.1 10^-5 off with groups of 3, 2 and of 2, 3; bf16, 8192 x 4096 0.19 % and 0.28 %).
 //
 // Between products X, A, S, P and Q are held in fp16, times powers of two.  Singular values of X lie in [0, 1.203] throughout, because |u| bounds
 // the largest and a s + b s^3 + c s^5 maps [0, 1.203] into itself, so no value of X, A, S, P exceeds 1.203, 1.447, 1.176, 3.445 in magnitude, nor
@@ -27,7 +29,7 @@ constexpr float kMuonA = 3.4445f, kMuonB = -4.7750f, kMuonC = 2.0315f;
 constexpr float kShift = kMuonB / (2.f * kMuonC), kRest = (float)(3.4445 - 4.7750 * 4.7750 / (4 * 2.0315));
 constexpr float kScaleX = 0x1p14f, kScaleA = 0x1p14f;                 // 1.203 and 1.447 times these, and 3.4445, 3.4445^2, 3.4445^3 times
 constexpr float kScaleQ[4] = {0.f, 0x1p13f, 0x1p12f, 0x1p10f};        // those, stay below 2^16 (P is the first Q)
-constexpr int kGroupSteps = 3;
+constexpr int kGroupSteps = 3, kLateSide = 1024;
 constexpr int kMostSums = 1024;   // partial sums of a matrix's squares
 
 typedef _Float16 half_t;
@@ -153,7 +155,6 @@ __global__ __launch_bounds__(256) void muon_start_kernel(const T *g, const float
 // `diag2` added on the diagonal.
 template <int PLANES, bool MIRROR>
 struct PlaneEpi {
-    static constexpr bool UPDATES = false;
     bf16_t *out, *out2;
     long long plane, each;
     int ld;
@@ -240,7 +241,6 @@ struct PlaneEpi {
 // The last product: w' = keep w - rate X.
 template <typename T>
 struct UpdateEpi {
-    static constexpr bool UPDATES = true;
     const T *w;
     T *w_out;
     long long each;
@@ -302,7 +302,6 @@ struct UpdateEpi {
 
 // The sums of a part, as PartEpi stores them: [item][part][M][ld].
 struct StackPartEpi : PartEpi {
-    static constexpr bool UPDATES = false;
     int at;
     __device__ __forceinline__ void item(int i) { at = i; }
     template <int MT, int NT>
@@ -372,12 +371,12 @@ struct StackCut {
 };
 // The cut that takes least by an estimate in microseconds from measured times: what begins and ends a tile, and for each 64 indices and pair of
 // planes a step of the tiles that share the fullest compute unit.  fp16, n x n times its like, the half below the diagonal, tiles of 64 / 128 /
-// 192 / 256: n = 256 5.5 / 7.0 / 12.6 / 15.6 us, 1024 11.3 / 13.3 / 22.6 / 34, 2048 22.1 / 22.8 / 34.8 / 52.5, 4096 145 / 104 / 86 / 97, two of 4096
-// 281 / 182 / 157 / 204.  Parts cost a kernel and their bytes: 1021 x 20011 times its transpose 152 us whole and 33 + 7 in 14.
-// Tiles of 192 read rows only, and tiles of 256 have no room to load what they update (8192 x 4096, both: 670 us, 621 with tiles of 128).
+// 192 / 256: n = 256 5.5 / 7.0 / 12.6 / 15.6 us, 1024 11.3 / 13.3 / 22.6 / 34, 2048 22.1 / 22.8 / 34.8 / 46, 4096 145 / 104 / 86 / 102, two of 4096
+// 281 / 182 / 157 / 201; two of 8192 x 4096 times 4096 x 4096 with tiles of 128 / 256 563 / 473, with the update 621 / 547.  Parts cost a kernel and
+// their bytes: 1021 x 20011 times its transpose 152 us whole and 33 + 7 in 14.  Tiles of 192 read rows only.
 inline double stack_tiles(const Shape &sh, int tile) { return (double)tiles_in(sh, ceil_div(sh.M, tile), ceil_div(sh.Nn, tile)) * sh.stack; }
 constexpr double kSplitTiles = 512;   // no product of more tiles of 128 is cut along its contraction
-enum { ROWS_ONLY = 1, MAY_SPLIT = 2, UPDATES = 4 };
+enum { ROWS_ONLY = 1, MAY_SPLIT = 2 };
 inline StackCut choose_stack_cut(const Shape &sh, int pairs, int how) {
     const int steps = ceil_div(sh.K, kStep);
     StackCut best = {128, 1, 1e30};
@@ -385,7 +384,7 @@ inline StackCut choose_stack_cut(const Shape &sh, int pairs, int how) {
     const long long result = sh.M * round_up(sh.Nn, 4) * sh.stack;
     for (int s = 1; s == 1 || (may_split && s <= kMostSplits && s <= steps / 2 && s * result <= kMostParts); ++s)
         for (const int tile : {64, 128, 192, 256}) {
-            if ((tile == 192 && !(how & ROWS_ONLY)) || (tile == 256 && (how & UPDATES))) continue;
+            if (tile == 192 && !(how & ROWS_ONLY)) continue;
             const double load = stack_tiles(sh, tile) * s / kComputeUnits, most = std::ceil(load);
             double ends, step;
             if (tile == 64) ends = 3.4, step = std::max(0.5, 0.28 * load);
@@ -400,8 +399,7 @@ inline StackCut choose_stack_cut(const Shape &sh, int pairs, int how) {
 
 template <int PL, int FA, int FB, typename Epi>
 int launch_stack(const char *name, const Operand &A, const Operand &B, const Shape &sh, const StackCut &c, const Epi &epi, hipStream_t s) {
-    if constexpr (!Epi::UPDATES)
-        if (c.tile == 256) return launch_tiles<PL, FA, FB, 256, 256, 3, 2, 8>(name, A, B, sh, c.splits, epi, s);
+    if (c.tile == 256) return launch_tiles<PL, FA, FB, 256, 256, 3, 2, 8>(name, A, B, sh, c.splits, epi, s);
     if constexpr (FA == ROW && FB == ROW)
         if (c.tile == 192) return launch_tiles<PL, FA, FB, 192, 192, 3, 2>(name, A, B, sh, c.splits, epi, s);
     if (c.tile == 64) return launch_tiles<PL, FA, FB, 64, 64, 3, 2>(name, A, B, sh, c.splits, epi, s);
@@ -426,14 +424,16 @@ int launch_symmetric(const char *name, const Operand &A, const Operand &B, const
 // ---------------------------------------------------------------------------------------------------------------------------
 // A group's steps on the short side where that is at most kChain: one workgroup a matrix, everything in LDS and registers.  A and Q stay in fp32
 // between products, in the layout of the accumulators; operands go through two places of LDS as planes, which the fragments are read from as
-// in a tile of the other products.  2 x 2 waves, each B / 2 x B / 2.
+// in a tile of the other products.  2 x 2 waves, each B / 2 x B / 2.  Two planes inside whatever the weights' type: on a short side singular values
+// are near one after few steps, where one plane of A showed (64 x 1408 in bf16: off by 0.57 % with one, 0.18 % with two, of which the weights' own
+// rounding is 0.17 %), and all of it costs little.
 //
 // 841 matrices of 128 x 128 in fp32: two and three steps 35 us a product with a kernel each, 14 of them; bound by the matrix unit, LDS reads
 // beside it and the barriers between products, as a workgroup has a compute unit for itself.
 constexpr int kChain = 128;
-template <int PL, int B>
+template <int B>
 struct Chain {
-    static constexpr int PLANES = PL == HALF2 ? 2 : 1, MT = B / 64, PLANE = B * B * 2;   // bytes of a plane
+    static constexpr int PL = HALF2, PLANES = 2, MT = B / 64, PLANE = B * B * 2;   // bytes of a plane
     static constexpr int PLACE = PLANES * PLANE;
     typedef f32x16 Square[MT][MT];
     char *lds;
@@ -489,9 +489,9 @@ struct Chain {
     }
 };
 
-template <int PL, int B>
+template <int OUT, int B>
 __global__ __launch_bounds__(256) void muon_chain_kernel(const bf16_t *a, bf16_t *out, long long plane, long long each, int n, int ld, int len) {
-    typedef Chain<PL, B> C;
+    typedef Chain<B> C;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int wave = threadIdx.x >> 6;
     const C c = {smem, (int)threadIdx.x & 63, wave / 2 * (B / 2), wave % 2 * (B / 2)};
@@ -568,20 +568,20 @@ __global__ __launch_bounds__(256) void muon_chain_kernel(const bf16_t *a, bf16_t
         typedef bf16_t V4 __attribute__((ext_vector_type(4)));
         if (m >= n || k >= ld) return;
 #pragma unroll
-        for (int p = 0; p < C::PLANES; ++p) {
+        for (int p = 0; p < OUT; ++p) {
             V4 w;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) w[r] = PlaneEpi<C::PLANES, true>::part(q[i][j][e + r], p);
+            for (int r = 0; r < 4; ++r) w[r] = PlaneEpi<OUT, true>::part(q[i][j][e + r], p);
             *(V4 *)(out + p * plane + (long long)m * ld + k) = w;
         }
     });
 }
 
-template <int PL, int B>
+template <int OUT, int B>
 int launch_chain(const bf16_t *a, bf16_t *q, long long plane, long long each, int n, int ld, int len, int items, hipStream_t s) {
-    const LaunchPlan p = make_plan("muon_chain", {PL, B}, {n, ld, len, items}, dim3((unsigned)items), 256, 2 * Chain<PL, B>::PLACE);
+    const LaunchPlan p = make_plan("muon_chain", {OUT, B}, {n, ld, len, items}, dim3((unsigned)items), 256, 2 * Chain<B>::PLACE);
     LC_PLAN_REQUIRE(p, n <= B && ld % 8 == 0 && ld >= n && ld < n + 8 && len >= 1 && len <= kGroupSteps);
-    LC_LAUNCH(p, "muon_step (Q)", (muon_chain_kernel<PL, B>), s, a, q, plane, each, n, ld, len);
+    LC_LAUNCH(p, "muon_step (Q)", (muon_chain_kernel<OUT, B>), s, a, q, plane, each, n, ld, len);
     return LC_OK;
 }
 
@@ -742,7 +742,7 @@ struct MuonScratch {
         s = sc.take<bf16_t>(square);
         q[0] = sc.take<bf16_t>(square);
         group = group_of(most, rows, cols, PLANES, Format<MuonFormat<T>::PL>::PAIRS);
-        if (small <= kChain) a = sc.take<bf16_t>(square);
+        if (small <= kChain) a = sc.take<bf16_t>(2LL * most * small * lds);
         else if (rows != cols)   // whatever the stack's length says
             for (bf16_t **p : {&a, &t, &q[1], &q[2]}) *p = sc.take<bf16_t>(square);
         // of as many matrices as are cut along the contraction; a shorter stack may be cut into more parts
@@ -781,20 +781,23 @@ int muon(const T *w, const T *g, const float *m, T *w_out, float *m_out, int cou
         };
         int at = 0, rc;   // X's place
         for (int group = 0, done = 0; group < groups; ++group) {
-            const int len = (steps - done) / (groups - group);
+            const int len = k.small > kLateSide ? ceil_div(steps - done, groups - group) : (steps - done) / (groups - group);
             const Operand X = {k.x[at], k.x[at], k.ld, plane, rows, 0, 0, (long long)rows * k.ld};
             Operand Xc = X;
             Xc.rows = k.ld;   // by columns
             const float fa = kScaleA / (kScaleX * kScaleX), fs = kShift * kScaleA;
-            const bool chain = k.small <= kChain, plain = chain || len > 1;   // A itself, S, or both
-            const PlaneEpi<PLANES, true> ea = {plain ? k.a : k.s, plain && !chain ? k.s : nullptr, splane, each, k.lds, fa, plain ? 0.f : fs, fs};
-            rc = tall ? launch_symmetric<PL, COL, COL>("muon_step (A)", Xc, Xc, of.sx, ea, k.part, st)
-                      : launch_symmetric<PL, ROW, ROW>("muon_step (A)", X, X, of.sx, ea, k.part, st);
+            const bool chain = k.small <= kChain;
+            const PlaneEpi<PLANES, true> ea = {len > 1 ? k.a : k.s, len > 1 ? k.s : nullptr, splane, each, k.lds, fa, len > 1 ? 0.f : fs, fs};
+            const auto gram = [&](const auto &epi) {
+                return tall ? launch_symmetric<PL, COL, COL>("muon_step (A)", Xc, Xc, of.sx, epi, k.part, st)
+                            : launch_symmetric<PL, ROW, ROW>("muon_step (A)", X, X, of.sx, epi, k.part, st);
+            };
+            rc = chain ? gram(PlaneEpi<2, true>{k.a, nullptr, splane, each, k.lds, fa, 0.f, 0.f}) : gram(ea);
             if (rc) return rc;
             int q = 0;   // place of Q, the product of the group's P
             if (chain) {
-                rc = k.small <= 64 ? launch_chain<PL, 64>(k.a, k.q[0], splane, each, k.small, k.lds, len, items, st)
-                                   : launch_chain<PL, 128>(k.a, k.q[0], splane, each, k.small, k.lds, len, items, st);
+                rc = k.small <= 64 ? launch_chain<PLANES, 64>(k.a, k.q[0], splane, each, k.small, k.lds, len, items, st)
+                                   : launch_chain<PLANES, 128>(k.a, k.q[0], splane, each, k.small, k.lds, len, items, st);
                 if (rc) return rc;
             }
             for (int i = 0; i < len && !chain; ++i) {
@@ -815,7 +818,7 @@ int muon(const T *w, const T *g, const float *m, T *w_out, float *m_out, int cou
             const PlaneEpi<PLANES, false> next = {k.x[1 - at], nullptr, plane, X.each, k.ld, 1.f / kScaleQ[len], 0.f, 0.f};
             const UpdateEpi<T> update = {w + skip, w_out + skip, n, cols, 1.f - decay, rate / (kScaleQ[len] * kScaleX)};
             const auto apply = [&](const auto &epi) {
-                const StackCut cut = choose_stack_cut(of.up, PAIRS, (tall ? ROWS_ONLY : 0) | (epi.UPDATES ? UPDATES : 0));
+                const StackCut cut = choose_stack_cut(of.up, PAIRS, tall ? ROWS_ONLY : 0);
                 return tall ? launch_stack<PL, ROW, ROW>("muon_step (X)", X, Q, of.up, cut, epi, st)
                             : launch_stack<PL, ROW, COL>("muon_step (X)", Q, Xc, of.up, cut, epi, st);
             };
