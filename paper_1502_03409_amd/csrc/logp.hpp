@@ -15,6 +15,10 @@
 //   d[v] = sum of a over t with word[t] = v - p[v] (A + b (log p[v] + H)),  dx = d w,  dw = d^T x;
 // the scores are formed once more, d leaves the product's tiles, given words get theirs in a kernel of its own, where with S the sum of a over a
 // word, S - p A = (S - A) - A (p - 1) does not cancel where p is near one.  d meets bf16 operands as in xent.hpp.
+//
+// 8192 rows of 4096 over 128000 words in bf16, a tenth masked, one word given and ten asked for: scores 6.7 ms, joining 0.03, answers 0.31 (keys of
+// 0.24 GB and candidates' weights of 0.9 GB, by workgroups that wait in 83 % of their cycles), d 6.8, dx and dw 6.7 each: four products of 7.7
+// TFLOP each, bound as large products are.  One row: scores 201 us, the 1.05 GB of weights at 5.2 TB/s, answers 23.
 #pragma once
 #include "head_few.hpp"
 #include "head_planes.hpp"

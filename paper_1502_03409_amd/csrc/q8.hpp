@@ -5,7 +5,9 @@
 // numbers and their sums are exact (32 bits hold 2^17 products of 127 x 127); the sums become fp32 and take both scales before what
 // follows the product, and are rounded once.
 //
-// The matrix instruction multiplies twice as many 8-bit as 16-bit numbers in the same time and from the same bytes.
+// The matrix instruction multiplies twice as many 8-bit as 16-bit numbers in the same time and from the same bytes.  8192 rows of 4096 -> 8192, gated,
+// bf16: 36 us for the rows (100 MB) and 0.46 to 0.5 ms for the products, 2.2 to 2.4 POP/s, with the matrix unit busy 64 % of the cycles at 1.65 GHz.
+// 192 rows over 100003 words: 153 us, where the weights' bytes take 88 and the products about 75; loads are waited for while tiles begin and end.
 //
 // Up to kFewRows rows: single blocks of 32 columns a workgroup, which fill the compute units more evenly than pairs and wait for more loads at
 // once (1 x 4096 times 8192 16.5 us with two blocks, 14.9 with one; times 50000 60 and 47; gated, 4096 -> 20011, 47 and 37).
