@@ -711,13 +711,14 @@ struct MuonShapes {
 };
 // Steps that go by on the short side at a time: kGroupSteps, or one where the products with the long side cost no more by the estimate (no
 // less than their bytes at 4.5 TB/s).  Both: two of 256 x 400 in fp32 155 us with one, 841 of 2048 x 128 in fp32 4.4 ms with one and 2.9 with
-// three, two of 8192 x 4096 in bf16 5.3 and 4.2.
+// three, two of 8192 x 4096 in bf16 5.3 and 4.2.  Square matrices have no longer side: as many products either way, and single steps round less.
 inline double stack_us(const Shape &sh, int planes, int pairs, int how) {
     const double bytes = 2.0 * planes * sh.stack * ((double)sh.M * sh.K + (sh.sym ? 0.0 : (double)sh.Nn * sh.K) + (double)sh.M * sh.Nn);
     return std::max(choose_stack_cut(sh, pairs, how).us, bytes / 4.5e6);
 }
 inline int group_of(int items, int rows, int cols, int planes, int pairs) {
     if (std::min(rows, cols) <= kChain) return kGroupSteps;
+    if (rows == cols) return 1;
     const MuonShapes k(items, rows, cols);
     const int rows_only = rows > cols ? 0 : ROWS_ONLY;
     const double sq = stack_us(k.sq, planes, pairs, ROWS_ONLY | MAY_SPLIT), sx = stack_us(k.sx, planes, pairs, rows_only | MAY_SPLIT),
@@ -745,7 +746,7 @@ struct MuonScratch {
         q[0] = sc.take<bf16_t>(square);
         group = group_of(most, rows, cols, PLANES, Format<MuonFormat<T>::PL>::PAIRS);
         if (small <= kChain) a = sc.take<bf16_t>(2LL * most * small * lds);
-        else if (rows != cols)   // whatever the stack's length says
+        else if (rows != cols)   // whatever group_of says of a stack of this length
             for (bf16_t **p : {&a, &t, &q[1], &q[2]}) *p = sc.take<bf16_t>(square);
         // of as many matrices as are cut along the contraction; a shorter stack may be cut into more parts
         const long long cut = std::min<long long>(most, (long long)(kSplitTiles / stack_tiles(MuonShapes(1, rows, cols).sx, 128)));
@@ -767,7 +768,7 @@ int muon(const T *w, const T *g, const float *m, T *w_out, float *m_out, int cou
         const int items = std::min(k.most, count - first);
         const long long skip = first * n, plane = (long long)k.most * rows * k.ld, splane = k.most * each;
         const LaunchPlan pm = make_plan("muon_momentum", {(int)sizeof(T)}, {items, rows, cols, k.parts}, dim3((unsigned)((long long)items * k.parts)), 256, 0);
-        LC_PLAN_REQUIRE(pm, (long long)items * k.parts <= 0x7fffffffLL);
+        LC_PLAN_REQUIRE(pm, (long long)items * k.parts <= 0x7fffffffLL && (k.group == 1 || (k.group <= kGroupSteps && k.a)));
         LC_LAUNCH(pm, "muon_step (momentum)", (muon_momentum_kernel<T>), st, g + skip, m + skip, m_out + skip, k.partial, n, k.parts, mu, (int)ahead);
         const long long wgs = ((long long)rows * (k.ld / 8) + 256 * kStartPieces - 1) / (256 * kStartPieces);
         const LaunchPlan ps = make_plan("muon_start", {(int)sizeof(T)}, {items, rows, cols, k.ld}, dim3((unsigned)(items * wgs)), 256, 0);

@@ -29,8 +29,9 @@ def code(t):
     return lc.LC_BF16 if t == torch.bfloat16 else lc.LC_F32
 
 
-def orthogonalised(u, steps, dtype):
-    """The result for each matrix and a bound on the 2-norm of its error."""
+def orthogonalised(u, steps, dtype, bounds=False):
+    """The result for each matrix and a bound on the 2-norm of its error.  `bounds`: the largest singular values of X and S by their bounds, 1.203
+    and 1.18, where finding them would take long."""
     r = 2.0 ** -11 if dtype == torch.bfloat16 else 2.0 ** -22
     small = min(u.shape[-2:])
     size = u.square().sum(dim=(1, 2), keepdim=True).sqrt()
@@ -44,7 +45,7 @@ def orthogonalised(u, steps, dtype):
         return t.square().sum(dim=(1, 2)).sqrt()
 
     def largest(t):
-        return torch.linalg.matrix_norm(t, 2)
+        return torch.linalg.matrix_norm(t, 2) if not bounds else 1.18 if t is s else 1.203
 
     err = (r + 2.0 ** -22) * fro(x)
     for _ in range(steps):
@@ -59,11 +60,11 @@ def orthogonalised(u, steps, dtype):
     return (x.mT if u.shape[1] > u.shape[2] else x), err
 
 
-def definition(w, g, m, rate, decay, mu, nesterov, steps):
+def definition(w, g, m, rate, decay, mu, nesterov, steps, bounds=False):
     rate, decay, mu = (float(torch.tensor(v, dtype=torch.float32)) for v in (rate, decay, mu))   # the entry point takes fp32 numbers
     m1 = mu * m.double() + g.double()
     u = g.double() + mu * m1 if nesterov else m1
-    o, err = orthogonalised(u, steps, w.dtype)
+    o, err = orthogonalised(u, steps, w.dtype, bounds)
     return m1, o, err, (1 - decay) * w.double() - rate * o
 
 
@@ -87,8 +88,8 @@ def step(w, g, m, rate=0.3, decay=0.01, mu=0.9, nesterov=True, steps=5, in_place
     return (w, m) if in_place else (wo, mo)
 
 
-def check(got, w, g, m, rate=0.3, decay=0.01, mu=0.9, nesterov=True, steps=5):
-    m1, o, err, w1 = definition(w, g, m, rate, decay, mu, nesterov, steps)
+def check(got, w, g, m, rate=0.3, decay=0.01, mu=0.9, nesterov=True, steps=5, bounds=False):
+    m1, o, err, w1 = definition(w, g, m, rate, decay, mu, nesterov, steps, bounds)
     assert ((got[1].double() - m1).abs() <= 2.0 ** -24 * m1.abs() + 2.0 ** -149).all()
     half = 2.0 ** -8 if w.dtype == torch.bfloat16 else 2.0 ** -24
     off = (got[0].double() - w1).square().sum(dim=(1, 2)).sqrt()
@@ -197,3 +198,12 @@ def test_captured_and_replayed(dtype):
         call()
         torch.cuda.synchronize()
         assert torch.equal(got[0], wo) and torch.equal(got[1], mo)
+
+
+@pytest.mark.parametrize("dtype,shape", [(torch.float32, (1, 4291, 4291)), (torch.bfloat16, (9, 2436, 2436)), (torch.bfloat16, (2, 1024, 1024))], ids=str)
+def test_large_square_matrices(shape, dtype):
+    """Sides so long that a product with one costs more than two symmetric ones: no other order of products is taken, there is no shorter side."""
+    print(f"case muon square {shape} {dtype}", flush=True)
+    w, g, m = (torch.empty(shape, device="cuda").normal_(0, std, generator=torch.Generator("cuda").manual_seed(k)) for k, std in enumerate((0.5, 1.0, 4.0)))
+    w, g = w.to(dtype), g.to(dtype)
+    check(step(w, g, m), w, g, m, bounds=True)

@@ -182,3 +182,13 @@ def test_scratch_is_bounded():
     a, b = (lc.logp_workspace_bytes(n, 64, 100000, 0, 5, lc.LC_BF16, True) for n in (1 << 17, 1 << 18))
     assert b - a < 1 << 30 and a < 5 << 30
     assert lc.muon_workspace_bytes(1 << 20, 128, 128) < 12 << 30
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
+def test_square_matrices_take_one_step_at_a_time(dtype):
+    """Neither side is the shorter one: the products and places of several steps on the short side alone (P A, P A P, Q) are for others."""
+    for count, n in [(c, n) for c in (1, 2, 3, 5, 7, 9, 24, 100) for n in (129, 256, 513, 1281, 1477, 2048, 2499, 2816, 2950, 3270, 4096, 4291, 5120, 7680, 8192)]:
+        if count * n * n > 1 << 31:
+            continue
+        names = [p["kernel"] for p in lc.head_plan_query(B.LC_HEAD_MUON, count, n, n, dtype)]
+        assert "muon_step (X)" in names and not {"muon_step (P A)", "muon_step (P A P)", "muon_step (Q)"} & set(names), (count, n)
