@@ -104,6 +104,7 @@ struct LogpOut {
 
 // Sizes of a head's matrices: widths 1 .. 2^20, rows 0 .. 2^24, so that every index within a row or a tile has 31 bits and
 // every product of two sizes is formed in 64.
+constexpr long long kMostGroups = 1 << 23;   // workgroups of 256 threads a launch, which takes fewer than 2^32 threads
 inline bool head_width(long long v) { return v >= 1 && v <= (1 << 20); }
 inline bool head_rows(long long v) { return v >= 0 && v <= (1 << 24); }
 

@@ -683,7 +683,7 @@ struct LogpScratch {
         words = keeps_words(V, K);
         groups_ld = words ? (int)round_up(V, 4) : (int)round_up((V + kGroupWords - 1) / kGroupWords, 2);
         const long long row_bytes = grads ? (long long)Vp * (long long)sizeof(T) : groups_ld * (words ? 4LL : (long long)sizeof(Group));
-        block = (int)std::min<long long>(round_up(N, 8), std::max<long long>(kStep, (grads ? kGradBytes : kKeyBytes) / row_bytes / 256 * 256));
+        block = (int)std::min<long long>({round_up(N, 8), kMostGroups, std::max<long long>(kStep, (grads ? kGradBytes : kKeyBytes) / row_bytes / 256 * 256)});
         blocks = N ? (N + block - 1) / block : 0;
         const bool few = N <= kFewRows;
         narrow = !few && N <= kNarrow;

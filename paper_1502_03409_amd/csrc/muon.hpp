@@ -737,7 +737,7 @@ struct MuonScratch {
         small = std::min(rows, cols);
         ld = (int)round_up(cols, 8), lds = (int)round_up(small, 8);
         const long long values = (long long)rows * ld;
-        most = (int)std::max<long long>(1, std::min<long long>(count, kStackBytes / (2 * PLANES * values)));
+        most = (int)std::max<long long>(1, std::min<long long>({count, kMostGroups, kStackBytes / (2 * PLANES * values)}));
         parts = (int)std::min<long long>(kMostSums, ((long long)rows * cols + 8191) / 8192);
         partial = sc.take<double>((long long)most * parts);
         for (auto &p : x) p = sc.take<bf16_t>(PLANES * most * values);

@@ -65,9 +65,12 @@ __global__ __launch_bounds__(256) void q8_rows_kernel(const T *x, int8_t *q, flo
 
 template <typename T>
 int q8_rows(const T *x, int8_t *q, float *scale, int N, int D, hipStream_t s) {
-    if (N == 0) return LC_OK;
-    const LaunchPlan p = make_plan("q8_rows", {(int)sizeof(T)}, {N, D, q8_ld(D)}, dim3(N), 256, 0);
-    LC_LAUNCH(p, "q8_rows", (q8_rows_kernel<T>), s, x, q, scale, D, q8_ld(D));
+    const int ld = q8_ld(D);
+    for (long long first = 0; first < N; first += kMostGroups) {
+        const int some = (int)std::min(N - first, kMostGroups);
+        const LaunchPlan p = make_plan("q8_rows", {(int)sizeof(T)}, {some, D, ld}, dim3(some), 256, 0);
+        LC_LAUNCH(p, "q8_rows", (q8_rows_kernel<T>), s, x + first * D, q + first * ld, scale + first, D, ld);
+    }
     return LC_OK;
 }
 

@@ -72,3 +72,27 @@ def test_stacks_of_more_than_2_31_values(dtype, shape):
     old = [t[at].clone() for t in (w, g, m)]
     lc.muon_step(w, g, m, None, None, 0.3, 0.01, 0.9, True, 5, muon.code(dtype), muon.scratch(shape, dtype))
     muon.check((w[at], m[at]), *old, bounds=True)
+
+
+def test_the_most_rows_and_matrices():
+    """2^24, of one value each: more workgroups of 256 threads than a launch takes."""
+    N = 1 << 24
+    x, w = normal((N, 1), torch.float32, 1.0, 8), normal((2, 1), torch.float32, 1.0, 9)
+    q, s = q8.rows(x)
+    assert torch.equal(s, (x.abs()[:, 0] / torch.full_like(s, 127)).clamp(min=2.0 ** -126))
+    assert torch.equal(q[:, 0].float(), 127 * torch.sign(x[:, 0])) and not q[:, 1:].any()
+    del q, s
+    tags = torch.arange(N, device="cuda")[:, None] % 3 - 1
+    got, want = logp.answers(x, w, tags, 1), logp.definition(x, w, tags, 1)
+    b = logp.check_answers(x, w, tags, 1, got, want)
+    dlogp, dentropy = normal((N, 1), torch.float32, 1.0, 10), normal((N,), torch.float32, 1.0, 11)
+    dx = logp.gradients(x, w, tags, got, dlogp, dentropy)[0].double()
+    d = logp.d_of(want, tags, dlogp, dentropy) @ w.double()
+    assert float((dx - d).norm()) <= 8 * b * float(d.norm())
+    del got, want, d, dx
+    u, g, m = torch.zeros(N, 1, 1, device="cuda"), x[:, :, None].contiguous(), torch.zeros(N, 1, 1, device="cuda")
+    lc.muon_step(u, g, m, None, None, 1.0, 0.0, 0.9, True, 1, lc.LC_F32, muon.scratch((N, 1, 1), torch.float32))
+    assert torch.equal(m, g)
+    one = muon.A + muon.B + muon.C       # a matrix of one value becomes its sign
+    # three products of values with 22 bits, each at most 4.8, one on the way to S and two to P X
+    assert ((u[:, 0, 0].double() + one * torch.sign(x[:, 0])).abs() <= 6 * 4.8 * 2.0 ** -22).all()

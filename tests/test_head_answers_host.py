@@ -192,3 +192,13 @@ def test_square_matrices_take_one_step_at_a_time(dtype):
             continue
         names = [p["kernel"] for p in lc.head_plan_query(B.LC_HEAD_MUON, count, n, n, dtype)]
         assert "muon_step (X)" in names and not {"muon_step (P A)", "muon_step (P A P)", "muon_step (Q)"} & set(names), (count, n)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
+def test_most_rows_and_matrices_can_be_launched(dtype):
+    """A launch takes fewer than 2^32 threads."""
+    for N in (1 << 23, (1 << 23) + 1, (1 << 24) - 1, 1 << 24):
+        plans = [lc.head_plan_query(op, N, 1, 2, dtype) for op in (B.LC_HEAD_LOGP_FWD, B.LC_HEAD_LOGP_BWD, B.LC_HEAD_Q8_MATMUL, B.LC_HEAD_Q8_GLU_FWD)]
+        plans += [lc.head_plan_query(B.LC_HEAD_MUON, N, r, c, dtype) for r, c in ((1, 1), (3, 8), (9, 5))]
+        for p in sum(plans, []):
+            assert p["grid"][0] * p["grid"][1] * p["grid"][2] * p["block"] < 1 << 32, (N, p)
