@@ -238,6 +238,21 @@ struct PlaneEpi {
         const half_t a = (half_t)v;
         return p == 0 ? __builtin_bit_cast(bf16_t, a) : half_bits(v - (float)a);
     }
+    // four columns k .. k + 3 of row m, of n rows
+    __device__ __forceinline__ void put4(int m, int k, float (&v)[4], int n) const {
+        put4_at(out, m, k, v, n);
+        if (!MIRROR || !out2) return;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (m == k + e) v[e] += diag2 - diag;
+        put4_at(out2, m, k, v, n);
+    }
+    __device__ __forceinline__ void put4_at(bf16_t *to, int m, int k, const float (&v)[4], int n) const {
+        typedef bf16_t V4 __attribute__((ext_vector_type(4)));
+        if (m >= n || k >= ld) return;
+#pragma unroll
+        for (int p = 0; p < PLANES; ++p) *(V4 *)(to + p * plane + (long long)m * ld + k) = (V4){part(v[0], p), part(v[1], p), part(v[2], p), part(v[3], p)};
+    }
 };
 
 // The last product: w' = keep w - rate X.
@@ -328,21 +343,6 @@ __global__ __launch_bounds__(256) void muon_join_kernel(const float *part, int s
             const int m = min(tm * 64 + r0 + 16 * i, n - 1), at = min(tn * 64 + c, ldp - 4);
             s[i] += *(const f32x4 *)(part + (((long long)item * splits + p) * n + m) * ldp + at);
         }
-    const auto put = [&](bf16_t *to, int m, int k, const float (&v)[4]) {
-        typedef bf16_t V4 __attribute__((ext_vector_type(4)));
-        if (m >= n || k >= epi.ld) return;
-#pragma unroll
-        for (int p = 0; p < PLANES; ++p)
-            *(V4 *)(to + p * epi.plane + (long long)m * epi.ld + k) = (V4){epi.part(v[0], p), epi.part(v[1], p), epi.part(v[2], p), epi.part(v[3], p)};
-    };
-    const auto both = [&](int m, int k, float (&v)[4]) {   // four columns k .. k + 3 of row m
-        put(epi.out, m, k, v);
-        if (!epi.out2) return;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (m == k + e) v[e] += epi.diag2 - epi.diag;
-        put(epi.out2, m, k, v);
-    };
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int m = tm * 64 + r0 + 16 * i;
@@ -353,7 +353,7 @@ __global__ __launch_bounds__(256) void muon_join_kernel(const float *part, int s
             v[e] = m < n && k < n ? s[i][e] * epi.factor + (m == k ? epi.diag : 0.f) : 0.f;
             tile[r0 + 16 * i][c + e] = v[e];
         }
-        both(m, tn * 64 + c, v);
+        epi.put4(m, tn * 64 + c, v, n);
     }
     if (tm == tn) return;
     __syncthreads();
@@ -362,11 +362,90 @@ __global__ __launch_bounds__(256) void muon_join_kernel(const float *part, int s
         float v[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = tile[c + e][r0 + 16 * i];
-        both(tn * 64 + r0 + 16 * i, tm * 64 + c, v);
+        epi.put4(tn * 64 + r0 + 16 * i, tm * 64 + c, v, n);
     }
 }
 
-// How products of a stack are cut: into tiles of 256, 192, 128 or 64, their contraction into parts.
+// A symmetric product with short sides and rows, a tile of 32 x 32 a workgroup: each wave takes 64 of every 256 indices, from memory straight to
+// registers, all at once for up to 512, and the waves' sums are added up in LDS.  What the product before has just written comes from beyond this
+// XCD's L2 cache, and a compute unit has only so many lines on their way at a time: neither more buffers nor earlier reads of LDS make tiles of 64 x
+// 64 faster, more and smaller workgroups do.  Two of 256 x 256 times their like in fp32 10.8 and 6.1 us a product, two steps of 256 x 400
+// 155 and 108 us.
+template <int PL, int PLANES>
+__global__ __launch_bounds__(256) void muon_block_kernel(Operand A, Operand B, Shape sh, PlaneEpi<PLANES, true> epi) {
+    __shared__ __attribute__((aligned(16))) float sums[4][32][36];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, h = lane >> 5, n = sh.M, K = (int)A.ld;   // zeros from sh.K on
+    int tm, tn, item;
+    tile_in_stack(sh, blockIdx.x, (n + 31) / 32, 0, 1, &tm, &tn, &item);
+    epi.item(item);
+    const bf16_t *const a = A.p0 + item * A.each + min(tm * 32 + l32, n - 1) * A.ld, *const b = B.p0 + item * B.each + min(tn * 32 + l32, n - 1) * B.ld;
+    u32x4 va[2][PLANES][4], vb[2][PLANES][4];
+    const auto load = [&](auto slot, int k0) __attribute__((always_inline)) {
+        constexpr int s = decltype(slot)::value;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int p = 0; p < PLANES; ++p) {
+                const int k = k0 + 16 * c + 8 * h;
+                va[s][p][c] = vb[s][p][c] = (u32x4){0, 0, 0, 0};
+                if (k < K) va[s][p][c] = *(const u32x4 *)(a + p * A.plane + k), vb[s][p][c] = *(const u32x4 *)(b + p * B.plane + k);
+            }
+    };
+    f32x16 acc = {};
+    const auto multiply = [&](auto slot) __attribute__((always_inline)) {
+        constexpr int s = decltype(slot)::value;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int t = 0; t < Format<PL>::PAIRS; ++t)
+                acc = Format<PL>::mul(vb[s][Format<PL>::B >> (4 * t) & 1][c], va[s][Format<PL>::A >> (4 * t) & 1][c], acc);
+    };
+    const std::integral_constant<int, 0> even;
+    const std::integral_constant<int, 1> odd;
+    int k = wave * 64;
+    load(even, k);
+    for (; k < K; k += 512) {
+        load(odd, k + 256);
+        multiply(even);
+        load(even, k + 512);
+        multiply(odd);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) *(f32x4 *)&sums[wave][l32][8 * q + 4 * h] = (f32x4){acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
+    __syncthreads();
+    const int r = threadIdx.x / 8, c = threadIdx.x % 8 * 4, m = tm * 32 + r;
+    f32x4 *const own = (f32x4 *)&sums[0][r][c];   // of all waves' sums a thread has four places to itself
+    f32x4 s = *own;
+#pragma unroll
+    for (int w = 1; w < 4; ++w) s += *(const f32x4 *)&sums[w][r][c];
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int col = tn * 32 + c + e;
+        s[e] = v[e] = m < n && col < n ? s[e] * epi.factor + (m == col ? epi.diag : 0.f) : 0.f;
+    }
+    *own = s;
+    epi.put4(m, tn * 32 + c, v, n);
+    if (tm == tn) return;
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = sums[0][c + e][r];
+    epi.put4(tn * 32 + r, tm * 32 + c, v, n);
+}
+
+template <int PL, int PLANES>
+int launch_block(const char *name, const Operand &A, const Operand &B, const Shape &sh, const PlaneEpi<PLANES, true> &epi, hipStream_t s) {
+    const int t = ceil_div(sh.M, 32);
+    const long long wgs = tiles_in(sh, t, t) * sh.stack;
+    const LaunchPlan p = make_plan(name, {PL, ROW, ROW, 32, 32}, {sh.M, sh.Nn, sh.K, 1, sh.stack, sh.sym}, dim3((unsigned)wgs), 256, 0);
+    LC_PLAN_REQUIRE(p, wgs <= 0x7fffffffLL && sh.sym && sh.M == sh.Nn && t <= 4096 && sh.stack >= 1);
+    LC_PLAN_REQUIRE(p, A.ld == B.ld && A.ld % 8 == 0 && A.ld >= sh.K && A.ld < sh.K + 8 && A.plane % 8 == 0 && B.plane % 8 == 0 && A.each % 8 == 0 && B.each % 8 == 0);
+    LC_PLAN_REQUIRE(p, A.rows >= sh.M && B.rows >= sh.M && epi.ld % 8 == 0 && ptr_aligned16(A.p0) && ptr_aligned16(B.p0));
+    LC_LAUNCH(p, name, (muon_block_kernel<PL, PLANES>), s, A, B, sh, epi);
+    return LC_OK;
+}
+
+// How products of a stack are cut: into tiles of 256, 192, 128, 64 or 32, their contraction into parts.
 struct StackCut {
     int tile, splits;
     double us;   // by the estimate
@@ -376,11 +455,18 @@ struct StackCut {
 // 192 / 256: n = 256 5.5 / 7.0 / 12.6 / 15.6 us, 1024 11.3 / 13.3 / 22.6 / 34, 2048 22.1 / 22.8 / 34.8 / 46, 4096 145 / 104 / 86 / 102, two of 4096
 // 281 / 182 / 157 / 201; two of 8192 x 4096 times 4096 x 4096 with tiles of 128 / 256 563 / 473, with the update 621 / 547.  Parts cost a kernel and
 // their bytes: 1021 x 20011 times its transpose 152 us whole and 33 + 7 in 14.  Tiles of 192 read rows only.
+//
+// Symmetric products of rows whose workgroups of 32 x 32 hardly share compute units take those (five steps in fp32 with and without: 512 x 512 154 and
+// 181 us, 768 x 768 260 and 253, eight of 256 x 400 123 and 149, 32 of 256 x 256 199 and 166; 256 x 4000 with all products so 258, with A in parts
+// of tiles of 64 134).
 inline double stack_tiles(const Shape &sh, int tile) { return (double)tiles_in(sh, ceil_div(sh.M, tile), ceil_div(sh.Nn, tile)) * sh.stack; }
 constexpr double kSplitTiles = 512;   // no product of more tiles of 128 is cut along its contraction
-enum { ROWS_ONLY = 1, MAY_SPLIT = 2 };
+enum { ROWS_ONLY = 1, MAY_SPLIT = 2 };   // ROWS_ONLY: both operands by rows
+constexpr int kBlockSide = 512, kBlockLong = 1024;   // of products in tiles of 32
 inline StackCut choose_stack_cut(const Shape &sh, int pairs, int how) {
     const int steps = ceil_div(sh.K, kStep);
+    if ((how & ROWS_ONLY) && sh.sym && sh.M <= kBlockSide && sh.K <= kBlockLong && stack_tiles(sh, 32) <= 2 * kComputeUnits)
+        return {32, 1, 3 + 0.4 * steps * (pairs > 1 ? 2 : 1)};
     StackCut best = {128, 1, 1e30};
     const bool may_split = (how & MAY_SPLIT) && stack_tiles(sh, 128) <= kSplitTiles;
     const long long result = sh.M * round_up(sh.Nn, 4) * sh.stack;
@@ -413,6 +499,8 @@ template <int PL, int FA, int FB, int PLANES>
 int launch_symmetric(const char *name, const Operand &A, const Operand &B, const Shape &sh, const PlaneEpi<PLANES, true> &epi, const Parts &part,
                      hipStream_t s) {
     const StackCut c = choose_stack_cut(sh, Format<PL>::PAIRS, (FA == ROW && FB == ROW ? ROWS_ONLY : 0) | MAY_SPLIT);
+    if constexpr (FA == ROW && FB == ROW)
+        if (c.tile == 32) return launch_block<PL, PLANES>(name, A, B, sh, epi, s);
     if (c.splits == 1) return launch_stack<PL, FA, FB>(name, A, B, sh, c, epi, s);
     const int ldp = (int)round_up(sh.Nn, 4);
     const long long wgs = (long long)stack_tiles(sh, 64);
@@ -710,8 +798,8 @@ struct MuonShapes {
     }
 };
 // Steps that go by on the short side at a time: kGroupSteps, or one where the products with the long side cost no more by the estimate (no
-// less than their bytes at 4.5 TB/s).  Both: two of 256 x 400 in fp32 155 us with one, 841 of 2048 x 128 in fp32 4.4 ms with one and 2.9 with
-// three, two of 8192 x 4096 in bf16 5.3 and 4.2.  Square matrices have no longer side: as many products either way, and single steps round less.
+// less than their bytes at 4.5 TB/s).  Both: 841 of 2048 x 128 in fp32 4.4 ms with one and 2.9 with three, two of 8192 x 4096 in bf16 5.3 and 4.2,
+// 256 x 2000 in fp32 153 us and 134; two of 256 x 400 would take as many launches either way.  Square matrices have no longer side: as many products either way, and single steps round less.
 inline double stack_us(const Shape &sh, int planes, int pairs, int how) {
     const double bytes = 2.0 * planes * sh.stack * ((double)sh.M * sh.K + (sh.sym ? 0.0 : (double)sh.Nn * sh.K) + (double)sh.M * sh.Nn);
     return std::max(choose_stack_cut(sh, pairs, how).us, bytes / 4.5e6);

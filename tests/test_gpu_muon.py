@@ -207,3 +207,16 @@ def test_large_square_matrices(shape, dtype):
     w, g, m = (torch.empty(shape, device="cuda").normal_(0, std, generator=torch.Generator("cuda").manual_seed(k)) for k, std in enumerate((0.5, 1.0, 4.0)))
     w, g = w.to(dtype), g.to(dtype)
     check(step(w, g, m), w, g, m, bounds=True)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+@pytest.mark.parametrize("steps", [1, 2, 3, 4, 7])
+@pytest.mark.parametrize("shape", [(1, 200, 2000), (1, 3000, 150), (2, 513, 4100), (9, 257, 300), (3, 512, 512), (40, 140, 130)], ids=str)
+def test_groups_of_steps_and_small_tiles(shape, steps, dtype):
+    """Sides beyond what one workgroup keeps: steps by groups and one by one, products in tiles of 32 and of more, sides that none of them divides."""
+    print(f"case muon {shape} {steps} steps {dtype}", flush=True)
+    w, g, m = draw(shape, dtype, 8, 2.0 ** -12), draw(shape, dtype, 9), draw(shape, torch.float32, 10, 4.0)
+    got = step(w, g, m, steps=steps)
+    check(got, w, g, m, steps=steps, bounds=True)
+    again = step(w, g, m, steps=steps, in_place=True)
+    assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
