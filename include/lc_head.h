@@ -131,8 +131,9 @@ size_t logp_workspace_bytes(int32_t N, int32_t D, int32_t V, int32_t T, int32_t 
  * (NULL if K = 0), all fp32 but for top.  state NULL or [N][3] fp32: receives what logp_bwd needs of the softmax.
  * Where words are given (T > 0), a row without one (all tags negative) is masked: its x is not looked at, its numbers are 0 and its top is -1.
  * A tag >= V has logp NaN.  A row with a NaN score, a score of +inf or none above -inf has no distribution: its numbers are NaN, its top is -1.
- * Scores of given and likeliest words are formed in 64 bits, and so is their order.  Where more words than 2048 come as near to the K-th score
- * as the product's sums tell scores apart (some 2^-16 of it), which of these follow is decided by those sums. */
+ * Scores of given and likeliest words are formed in 64 bits, and so is their order.  Where more than 256 words, and more than 32 K, come
+ * as near to the K-th score as the product's sums tell scores apart (some 2^-16 of it), which of these follow is decided by those sums; and so it is
+ * where the terms of scores cancel so far that their fp32 sums are off by more than that. */
 int logp_fwd(const void *x, const void *w, const int64_t *tags, float *logp, float *entropy, int64_t *top, float *top_logp,
              float *state, int32_t N, int32_t D, int32_t V, int32_t T, int32_t K, int dtype, void *ws, size_t ws_bytes,
              void *hip_stream);
