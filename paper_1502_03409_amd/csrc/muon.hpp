@@ -238,6 +238,8 @@ struct PlaneEpi {
         const half_t a = (half_t)v;
         return p == 0 ? __builtin_bit_cast(bf16_t, a) : half_bits(v - (float)a);
     }
+    static constexpr bool SYM = MIRROR;
+    __device__ __forceinline__ float result(float v, int m, int n) const { return v * factor + (m == n ? diag : 0.f); }
     // four columns k .. k + 3 of row m, of n rows
     __device__ __forceinline__ void put4(int m, int k, float (&v)[4], int n) const {
         put4_at(out, m, k, v, n);
@@ -315,6 +317,24 @@ struct UpdateEpi {
             });
         });
     }
+    static constexpr bool SYM = false;
+    __device__ __forceinline__ float result(float v, int, int) const { return v; }
+    __device__ __forceinline__ void put4(int m, int k, float (&v)[4], int n) const {
+        if (m >= n) return;
+        const T *const p = w + (long long)m * cols + k;
+        T *const to = w_out + (long long)m * cols + k;
+        T o[4];
+        if (k + 4 <= cols) {
+            __builtin_memcpy(o, p, sizeof(o));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = narrow<T>(keep * widen<T>(o[e]) - rate * v[e]);
+            __builtin_memcpy(to, o, sizeof(o));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (k + e < cols) to[e] = narrow<T>(keep * widen<T>(p[e]) - rate * v[e]);
+        }
+    }
 };
 
 // The sums of a part, as PartEpi stores them: [item][part][M][ld].
@@ -366,34 +386,64 @@ __global__ __launch_bounds__(256) void muon_join_kernel(const float *part, int s
     }
 }
 
-// A symmetric product with short sides and rows, a tile of 32 x 32 a workgroup: each wave takes 64 of every 256 indices, from memory straight to
+// A product with a short side and a short contraction, a tile of 32 x 32 a workgroup: each wave takes 64 of every 256 indices, from memory straight to
 // registers, all at once for up to 512, and the waves' sums are added up in LDS.  What the product before has just written comes from beyond this
 // XCD's L2 cache, and a compute unit has only so many lines on their way at a time: neither more buffers nor earlier reads of LDS make tiles of 64 x
-// 64 faster, more and smaller workgroups do.  Two of 256 x 256 times their like in fp32 10.8 and 6.1 us a product, two steps of 256 x 400
-// 155 and 108 us.
-template <int PL, int PLANES>
-__global__ __launch_bounds__(256) void muon_block_kernel(Operand A, Operand B, Shape sh, PlaneEpi<PLANES, true> epi) {
+// 64 faster, more and smaller workgroups do.  Two of 256 x 256 times their like in fp32 10.8 us and 6.4, times 256 x 400 8.7 us and 6.5, a step of
+// two of 256 x 400 155 us and 101.
+//
+// FB COL: what lies by columns takes its turn through LDS of the wave's own, to be read by the transposing load.
+template <int PL, int PLANES, int FB, typename Epi>
+__global__ __launch_bounds__(256) void muon_block_kernel(Operand A, Operand B, Shape sh, Epi epi) {
+    constexpr int STEP = 64 * 32 * 2;   // bytes of 64 indices of 32 columns
     __shared__ __attribute__((aligned(16))) float sums[4][32][36];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, h = lane >> 5, n = sh.M, K = (int)A.ld;   // zeros from sh.K on
+    __shared__ __attribute__((aligned(1024))) char turned[FB == COL ? 4 * PLANES * STEP : 16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, h = lane >> 5, K = (int)A.ld;   // zeros from sh.K on
     int tm, tn, item;
-    tile_in_stack(sh, blockIdx.x, (n + 31) / 32, 0, 1, &tm, &tn, &item);
+    tile_in_stack(sh, blockIdx.x, (sh.M + 31) / 32, (sh.Nn + 31) / 32, 1, &tm, &tn, &item);
     epi.item(item);
-    const bf16_t *const a = A.p0 + item * A.each + min(tm * 32 + l32, n - 1) * A.ld, *const b = B.p0 + item * B.each + min(tn * 32 + l32, n - 1) * B.ld;
+    const bf16_t *const a = A.p0 + item * A.each + min(tm * 32 + l32, sh.M - 1) * A.ld, *const b0 = B.p0 + item * B.each;
+    const int col = tn * 32 + lane % 4 * 8;
     u32x4 va[2][PLANES][4], vb[2][PLANES][4];
     const auto load = [&](auto slot, int k0) __attribute__((always_inline)) {
         constexpr int s = decltype(slot)::value;
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
+        for (int c = 0; c < 4; ++c) {
+            const int k = k0 + 16 * c + 8 * h, r = k0 + 16 * c + lane / 4;
+            const bool in = FB == COL ? r < sh.K && col < B.ld : k < K;
+            const bf16_t *const b = FB == COL ? b0 + r * B.ld + col : b0 + min(tn * 32 + l32, sh.Nn - 1) * B.ld + k;
 #pragma unroll
             for (int p = 0; p < PLANES; ++p) {
-                const int k = k0 + 16 * c + 8 * h;
                 va[s][p][c] = vb[s][p][c] = (u32x4){0, 0, 0, 0};
-                if (k < K) va[s][p][c] = *(const u32x4 *)(a + p * A.plane + k), vb[s][p][c] = *(const u32x4 *)(b + p * B.plane + k);
+                if (k < K) va[s][p][c] = *(const u32x4 *)(a + p * A.plane + k);
+                if (in) vb[s][p][c] = *(const u32x4 *)(b + p * B.plane);
             }
+        }
     };
+    char *const mine = turned + (FB == COL ? wave * PLANES * STEP : 0);
+    Reader<COL, 32, 1> reader;
+    if constexpr (FB == COL) {
+        reader.init((unsigned)(size_t)(__attribute__((address_space(3))) char *)mine, 0, lane);
+        reader.turn(0);
+    }
     f32x16 acc = {};
     const auto multiply = [&](auto slot) __attribute__((always_inline)) {
         constexpr int s = decltype(slot)::value;
+        if constexpr (FB == COL) {   // a wave's LDS accesses are done in their order
+#pragma unroll
+            for (int p = 0; p < PLANES; ++p)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) *(u32x4 *)(mine + p * STEP + c * 1024 + lane * 16) = vb[s][p][c];
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+            for (int p = 0; p < PLANES; ++p) {
+                Reader<COL, 32, 1> at = reader;
+                at.at[0] += p * STEP;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) vb[s][p][c] = at.read(c, 0);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
 #pragma unroll
         for (int c = 0; c < 4; ++c)
 #pragma unroll
@@ -420,28 +470,28 @@ __global__ __launch_bounds__(256) void muon_block_kernel(Operand A, Operand B, S
     for (int w = 1; w < 4; ++w) s += *(const f32x4 *)&sums[w][r][c];
     float v[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const int col = tn * 32 + c + e;
-        s[e] = v[e] = m < n && col < n ? s[e] * epi.factor + (m == col ? epi.diag : 0.f) : 0.f;
-    }
-    *own = s;
-    epi.put4(m, tn * 32 + c, v, n);
-    if (tm == tn) return;
-    __syncthreads();
+    for (int e = 0; e < 4; ++e) s[e] = v[e] = m < sh.M && tn * 32 + c + e < sh.Nn ? epi.result(s[e], m, tn * 32 + c + e) : 0.f;
+    if constexpr (Epi::SYM) *own = s;
+    epi.put4(m, tn * 32 + c, v, sh.M);
+    if constexpr (Epi::SYM) {
+        if (tm == tn) return;
+        __syncthreads();
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = sums[0][c + e][r];
-    epi.put4(tn * 32 + r, tm * 32 + c, v, n);
+        for (int e = 0; e < 4; ++e) v[e] = sums[0][c + e][r];
+        epi.put4(tn * 32 + r, tm * 32 + c, v, sh.M);
+    }
 }
 
-template <int PL, int PLANES>
-int launch_block(const char *name, const Operand &A, const Operand &B, const Shape &sh, const PlaneEpi<PLANES, true> &epi, hipStream_t s) {
-    const int t = ceil_div(sh.M, 32);
-    const long long wgs = tiles_in(sh, t, t) * sh.stack;
-    const LaunchPlan p = make_plan(name, {PL, ROW, ROW, 32, 32}, {sh.M, sh.Nn, sh.K, 1, sh.stack, sh.sym}, dim3((unsigned)wgs), 256, 0);
-    LC_PLAN_REQUIRE(p, wgs <= 0x7fffffffLL && sh.sym && sh.M == sh.Nn && t <= 4096 && sh.stack >= 1);
-    LC_PLAN_REQUIRE(p, A.ld == B.ld && A.ld % 8 == 0 && A.ld >= sh.K && A.ld < sh.K + 8 && A.plane % 8 == 0 && B.plane % 8 == 0 && A.each % 8 == 0 && B.each % 8 == 0);
-    LC_PLAN_REQUIRE(p, A.rows >= sh.M && B.rows >= sh.M && epi.ld % 8 == 0 && ptr_aligned16(A.p0) && ptr_aligned16(B.p0));
-    LC_LAUNCH(p, name, (muon_block_kernel<PL, PLANES>), s, A, B, sh, epi);
+template <int PL, int FB, typename Epi>
+int launch_block(const char *name, const Operand &A, const Operand &B, const Shape &sh, const Epi &epi, hipStream_t s) {
+    const int mt = ceil_div(sh.M, 32), nt = ceil_div(sh.Nn, 32);
+    const long long wgs = tiles_in(sh, mt, nt) * sh.stack;
+    const LaunchPlan p = make_plan(name, {PL, ROW, FB, 32, 32}, {sh.M, sh.Nn, sh.K, 1, sh.stack, sh.sym}, dim3((unsigned)wgs), 256, 0);
+    LC_PLAN_REQUIRE(p, wgs <= 0x7fffffffLL && sh.stack >= 1 && sh.sym == (int)Epi::SYM && (!sh.sym || (sh.M == sh.Nn && mt <= 4096)));
+    LC_PLAN_REQUIRE(p, A.ld % 8 == 0 && A.ld >= sh.K && A.ld < sh.K + 8 && B.ld % 8 == 0 && (FB == COL ? B.ld >= sh.Nn : B.ld == A.ld));
+    LC_PLAN_REQUIRE(p, A.plane % 8 == 0 && B.plane % 8 == 0 && A.each % 8 == 0 && B.each % 8 == 0 && A.rows >= sh.M && B.rows >= sh.Nn);
+    LC_PLAN_REQUIRE(p, ptr_aligned16(A.p0) && ptr_aligned16(B.p0));
+    LC_LAUNCH(p, name, (muon_block_kernel<PL, PL == HALF2 ? 2 : 1, FB, Epi>), s, A, B, sh, epi);
     return LC_OK;
 }
 
@@ -456,16 +506,16 @@ struct StackCut {
 // 281 / 182 / 157 / 201; two of 8192 x 4096 times 4096 x 4096 with tiles of 128 / 256 563 / 473, with the update 621 / 547.  Parts cost a kernel and
 // their bytes: 1021 x 20011 times its transpose 152 us whole and 33 + 7 in 14.  Tiles of 192 read rows only.
 //
-// Symmetric products of rows whose workgroups of 32 x 32 hardly share compute units take those (five steps in fp32 with and without: 512 x 512 154 and
-// 181 us, 768 x 768 260 and 253, eight of 256 x 400 123 and 149, 32 of 256 x 256 199 and 166; 256 x 4000 with all products so 258, with A in parts
-// of tiles of 64 134).
+// Products whose workgroups of 32 x 32 hardly share compute units take those (five steps in fp32, symmetric products in tiles of 32 and of 64:
+// 512 x 512 154 and 181 us, 768 x 768 260 and 253, eight of 256 x 400 123 and 149, 32 of 256 x 256 199 and 166; 256 x 4000 with A so 258, with A in
+// parts of tiles of 64 134; products with X in tiles of 32 and of 64: 512 x 512 131 and 157, 400 x 700 138 and 157, 256 x 2000 the same).
 inline double stack_tiles(const Shape &sh, int tile) { return (double)tiles_in(sh, ceil_div(sh.M, tile), ceil_div(sh.Nn, tile)) * sh.stack; }
 constexpr double kSplitTiles = 512;   // no product of more tiles of 128 is cut along its contraction
-enum { ROWS_ONLY = 1, MAY_SPLIT = 2 };   // ROWS_ONLY: both operands by rows
+enum { ROWS_ONLY = 1, MAY_SPLIT = 2, BLOCKS = 4 };   // ROWS_ONLY: both operands by rows; BLOCKS: the first is, tiles of 32 may be
 constexpr int kBlockSide = 512, kBlockLong = 1024;   // of products in tiles of 32
 inline StackCut choose_stack_cut(const Shape &sh, int pairs, int how) {
     const int steps = ceil_div(sh.K, kStep);
-    if ((how & ROWS_ONLY) && sh.sym && sh.M <= kBlockSide && sh.K <= kBlockLong && stack_tiles(sh, 32) <= 2 * kComputeUnits)
+    if ((how & BLOCKS) && std::min(sh.M, sh.Nn) <= kBlockSide && sh.K <= kBlockLong && stack_tiles(sh, 32) <= 2 * kComputeUnits)
         return {32, 1, 3 + 0.4 * steps * (pairs > 1 ? 2 : 1)};
     StackCut best = {128, 1, 1e30};
     const bool may_split = (how & MAY_SPLIT) && stack_tiles(sh, 128) <= kSplitTiles;
@@ -487,6 +537,8 @@ inline StackCut choose_stack_cut(const Shape &sh, int pairs, int how) {
 
 template <int PL, int FA, int FB, typename Epi>
 int launch_stack(const char *name, const Operand &A, const Operand &B, const Shape &sh, const StackCut &c, const Epi &epi, hipStream_t s) {
+    if constexpr (FA == ROW && !std::is_same<Epi, StackPartEpi>::value)
+        if (c.tile == 32) return launch_block<PL, FB>(name, A, B, sh, epi, s);
     if (c.tile == 256) return launch_tiles<PL, FA, FB, 256, 256, 3, 2, 8>(name, A, B, sh, c.splits, epi, s);
     if constexpr (FA == ROW && FB == ROW)
         if (c.tile == 192) return launch_tiles<PL, FA, FB, 192, 192, 3, 2>(name, A, B, sh, c.splits, epi, s);
@@ -498,9 +550,7 @@ int launch_stack(const char *name, const Operand &A, const Operand &B, const Sha
 template <int PL, int FA, int FB, int PLANES>
 int launch_symmetric(const char *name, const Operand &A, const Operand &B, const Shape &sh, const PlaneEpi<PLANES, true> &epi, const Parts &part,
                      hipStream_t s) {
-    const StackCut c = choose_stack_cut(sh, Format<PL>::PAIRS, (FA == ROW && FB == ROW ? ROWS_ONLY : 0) | MAY_SPLIT);
-    if constexpr (FA == ROW && FB == ROW)
-        if (c.tile == 32) return launch_block<PL, PLANES>(name, A, B, sh, epi, s);
+    const StackCut c = choose_stack_cut(sh, Format<PL>::PAIRS, (FA == ROW && FB == ROW ? ROWS_ONLY | BLOCKS : 0) | MAY_SPLIT);
     if (c.splits == 1) return launch_stack<PL, FA, FB>(name, A, B, sh, c, epi, s);
     const int ldp = (int)round_up(sh.Nn, 4);
     const long long wgs = (long long)stack_tiles(sh, 64);
@@ -808,9 +858,9 @@ inline int group_of(int items, int rows, int cols, int planes, int pairs) {
     if (std::min(rows, cols) <= kChain) return kGroupSteps;
     if (rows == cols) return 1;
     const MuonShapes k(items, rows, cols);
-    const int rows_only = rows > cols ? 0 : ROWS_ONLY;
-    const double sq = stack_us(k.sq, planes, pairs, ROWS_ONLY | MAY_SPLIT), sx = stack_us(k.sx, planes, pairs, rows_only | MAY_SPLIT),
-                 up = stack_us(k.up, planes, pairs, rows > cols ? ROWS_ONLY : 0);
+    const int by_rows = rows > cols ? 0 : ROWS_ONLY | BLOCKS;
+    const double sq = stack_us(k.sq, planes, pairs, ROWS_ONLY | BLOCKS | MAY_SPLIT), sx = stack_us(k.sx, planes, pairs, by_rows | MAY_SPLIT),
+                 up = stack_us(k.up, planes, pairs, rows > cols ? ROWS_ONLY | BLOCKS : BLOCKS);
     return sx + up > 3 * sq ? kGroupSteps : 1;
 }
 
@@ -909,7 +959,7 @@ int muon(const T *w, const T *g, const float *m, T *w_out, float *m_out, int cou
             const PlaneEpi<PLANES, false> next = {k.x[1 - at], nullptr, plane, X.each, k.ld, 1.f / kScaleQ[len], 0.f, 0.f};
             const UpdateEpi<T> update = {w + skip, w_out + skip, n, cols, 1.f - decay, rate / (kScaleQ[len] * kScaleX)};
             const auto apply = [&](const auto &epi) {
-                const StackCut cut = choose_stack_cut(of.up, PAIRS, tall ? ROWS_ONLY : 0);
+                const StackCut cut = choose_stack_cut(of.up, PAIRS, tall ? ROWS_ONLY | BLOCKS : BLOCKS);
                 return tall ? launch_stack<PL, ROW, ROW>("muon_step (X)", X, Q, of.up, cut, epi, st)
                             : launch_stack<PL, ROW, COL>("muon_step (X)", Q, Xc, of.up, cut, epi, st);
             };
