@@ -215,7 +215,10 @@ struct PlaneEpi {
                 });
             }
         });
-        if (!MIRROR || m0 / (MT * 64) == n0 / (NT * 64)) return;
+        // On the diagonal the tile has both places itself, and other waves store what would be the mirrored ones.  Symmetric tiles are square and two
+        // waves wide, whether two or four waves share their height.
+        constexpr int SIDE = NT * 64;
+        if (!MIRROR || m0 / SIDE == n0 / SIDE) return;
         typedef RowStage<bf16_t, MT * 32> Across;
         const Across across = {lds, lane};
         for_blocks<NT>([&](auto block) __attribute__((always_inline)) {
