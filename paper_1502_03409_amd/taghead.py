@@ -53,9 +53,11 @@ class TagHead:
                    H.grad_clip_workspace_bytes(self.grads), *(H.logp_workspace_bytes(batch, F, V, t, likeliest, self.code, True) for t in (0, tags)),
                    *(H.muon_workspace_bytes(1, *w.shape, self.code) for w in self.params if momentum is not None))
         self.ws = torch.empty(need, dtype=torch.uint8, device=device)
+        self.learning = None   # images and tags an image of the answer that gradients_of may follow
 
     def gradients(self, x: torch.Tensor, target: torch.Tensor) -> None:
         """Cost, loss of every row and gradients of a batch (targets below 0: rows without a tag)."""
+        self.learning = None
         n = x.shape[0]
         h, gu, dh = self.h[:n], self.gu[:n], self.dh[:n]
         H.glu_fwd(x, self.wg, self.wu, h, gu, self.act, self.code, self.ws)
@@ -69,6 +71,7 @@ class TagHead:
 
     def update(self, lr: float) -> None:
         """Clips the gradients that are there and steps.  With a momentum each value moves by about 0.2 ``lr``, whatever its matrix's sides."""
+        self.learning = None
         H.grad_clip(self.grads, None, self.max_norm, self.norm, self.ws)
         if self.momentum is None:
             for w, g in zip(self.params, self.grads):
@@ -82,18 +85,22 @@ class TagHead:
         the ``likeliest`` tags and their log probabilities or None, and the entropies.  The results are the head's own buffers.  ``learn``:
         `gradients_of` follows."""
         n, T, K = x.shape[0], 0 if tags is None else tags.shape[1], likeliest
-        h = self.h[:n]
+        h, self.learning = self.h[:n], None
         if n * T > self.logp.numel() or n * K > self.top.numel():
             raise ValueError(f"the head was made for fewer tags than {T} given and {K} likeliest ones of {n} images")
         logp = self.logp[:n * T].view(n, T) if T else None
         top, top_logp = (self.top[:n * K].view(n, K), self.top_logp[:n * K].view(n, K)) if K else (None, None)
         H.glu_fwd(x, self.wg, self.wu, h, self.gu[:n] if learn else None, self.act, self.code, self.ws)
         H.logp_fwd(h, self.wv, tags if T else None, logp, self.entropy[:n], top, top_logp, self.state[:n] if learn else None, self.code, self.ws)
+        self.learning = (n, T) if learn else None
         return logp, top, top_logp, self.entropy[:n]
 
     def gradients_of(self, x: torch.Tensor, tags: Optional[torch.Tensor], dlogp: Optional[torch.Tensor], dentropy: Optional[torch.Tensor] = None) -> None:
-        """Gradients for given ones of the log probabilities [n, T] and entropies [n] of the batch that `answer` saw last."""
+        """Gradients for given ones of the log probabilities [n, T] and entropies [n] of the batch and tags that `answer` saw last, with ``learn`` and
+        the weights as they are: nothing else that computes with the head may lie between."""
         n, T = x.shape[0], 0 if tags is None else tags.shape[1]
+        if self.learning != (n, T):
+            raise ValueError(f"gradients of {T} tags each of {n} images follow their answer with learn=True, without another call between")
         h, gu, dh = self.h[:n], self.gu[:n], self.dh[:n]
         H.logp_bwd(h, self.wv, tags if T else None, self.logp[:n * T].view(n, T) if T else None, self.state[:n], dlogp, dentropy, dh, self.grads[2],
                    self.code, self.ws)
@@ -101,6 +108,7 @@ class TagHead:
 
     def evaluate(self, x: torch.Tensor, target: torch.Tensor) -> None:
         """Cost and loss of every row, nothing else."""
+        self.learning = None
         n = x.shape[0]
         H.glu_fwd(x, self.wg, self.wu, self.h[:n], None, self.act, self.code, self.ws)
         H.xent_fwd(self.h[:n], self.wv, target, None, self.loss[:n], self.cost, self.code, self.ws)
