@@ -105,6 +105,13 @@ struct LogpOut {
 // Sizes of a head's matrices: widths 1 .. 2^20, rows 0 .. 2^24, so that every index within a row or a tile has 31 bits and
 // every product of two sizes is formed in 64.
 constexpr long long kMostGroups = 1 << 23;   // workgroups of 256 threads a launch, which takes fewer than 2^32 threads
+// fn(first thread, workgroups) for as many workgroups of 256 threads as a launch takes at a time
+template <typename Fn>
+int in_launches(long long threads, const Fn &fn) {
+    for (long long from = 0; from < threads; from += 256 * kMostGroups)
+        if (int rc = fn(from, (unsigned)std::min(kMostGroups, (threads - from + 255) / 256))) return rc;
+    return LC_OK;
+}
 inline bool head_width(long long v) { return v >= 1 && v <= (1 << 20); }
 inline bool head_rows(long long v) { return v >= 0 && v <= (1 << 24); }
 

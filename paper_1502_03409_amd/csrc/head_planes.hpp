@@ -31,9 +31,9 @@ __device__ __forceinline__ void put_planes(bf16_t *to, long long plane, const fl
 // the right.  skip(r): rows that nobody reads.  beside(): something small that the first workgroup does as well.  Two planes: the second
 // lies get.rows() rows behind the first, a number that the device may know alone.
 template <int PL, int OUT, typename Get>
-__global__ __launch_bounds__(256) void planes_kernel(Get get, bf16_t *dst, long long ld, long long plane, int rows, int pieces, int apart) {
-    if (blockIdx.x == 0) get.beside();
-    const long long at = blockIdx.x * 256LL + threadIdx.x;
+__global__ __launch_bounds__(256) void planes_kernel(Get get, bf16_t *dst, long long ld, long long plane, int rows, int pieces, int apart, long long from) {
+    if (blockIdx.x == 0 && from == 0) get.beside();
+    const long long at = from + blockIdx.x * 256LL + threadIdx.x;
     const int r = (int)(at / pieces), c = (int)(at - (long long)r * pieces) * 8;
     if (r >= rows || get.skip(r)) return;
     if constexpr (PL == 2) plane = get.rows() * ld;
@@ -77,13 +77,14 @@ struct Stored {
 // rows x cols (cols: of one output, padded to whole pieces) at dst
 template <int PL, int OUT, typename Get>
 int launch_planes(const char *name, const Get &get, bf16_t *dst, long long ld, long long plane, int rows, int cols, int apart, hipStream_t s) {
-    const long long pieces = cols / 8, n = ((long long)rows * pieces + 255) / 256;
-    if (n == 0) return LC_OK;
-    const LaunchPlan p = make_plan(name, {PL, OUT}, {rows, cols, apart}, dim3((unsigned)n), 256, 0);
-    LC_PLAN_REQUIRE(p, n <= 0x7fffffffLL && cols % 8 == 0 && ld % 8 == 0 && plane % 8 == 0 && apart % 8 == 0);
-    LC_PLAN_REQUIRE(p, (long long)apart * (OUT - 1) + cols <= ld);
-    LC_LAUNCH(p, name, (planes_kernel<PL, OUT, Get>), s, get, dst, ld, plane, rows, (int)pieces, apart);
-    return LC_OK;
+    const long long pieces = cols / 8;
+    return in_launches(rows * pieces, [&](long long from, unsigned n) -> int {
+        const LaunchPlan p = make_plan(name, {PL, OUT}, {rows, cols, apart}, dim3(n), 256, 0);
+        LC_PLAN_REQUIRE(p, cols % 8 == 0 && ld % 8 == 0 && plane % 8 == 0 && apart % 8 == 0);
+        LC_PLAN_REQUIRE(p, (long long)apart * (OUT - 1) + cols <= ld);
+        LC_LAUNCH(p, name, (planes_kernel<PL, OUT, Get>), s, get, dst, ld, plane, rows, (int)pieces, apart, from);
+        return LC_OK;
+    });
 }
 
 }  // namespace head
