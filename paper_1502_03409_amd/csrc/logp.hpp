@@ -108,9 +108,10 @@ struct LogpGiven {
     int T, V;
 };
 template <typename T, bool GRADS>
-__global__ __launch_bounds__(256) void logp_gather_kernel(const T *x, bf16_t *dst, T *dx, LogpRows o, LogpGiven given, int N, int D, int pieces) {
+__global__ __launch_bounds__(256) void logp_gather_kernel(const T *x, bf16_t *dst, T *dx, LogpRows o, LogpGiven given, int N, int D, int pieces,
+                                                         long long from) {
     constexpr int PL = Planes<T>::N;
-    const long long at = blockIdx.x * 256LL + threadIdx.x;
+    const long long at = from + blockIdx.x * 256LL + threadIdx.x;
     const int n = (int)(at / pieces), piece = (int)(at - (long long)n * pieces), c = piece * 8;
     if (n >= N) return;
     const bool masked = o.place ? o.place[n] < 0 : given.T && !any_given(given.tags + (long long)n * given.T, given.T);
@@ -717,11 +718,14 @@ struct LogpScratch {
             LC_LAUNCH(p, "logp (rows)", logp_rows_kernel, s, given.tags, N, given.T, rows);
         }
         if (x) {
-            const long long n = ((long long)N * (Dp / 8) + 255) / 256;
-            const LaunchPlan p = make_plan("logp_gather", {PL, grads}, {N, D}, dim3((unsigned)n), 256, 0);
-            LC_PLAN_REQUIRE(p, n <= 0x7fffffffLL);
-            if (grads) LC_LAUNCH(p, "logp (x)", (logp_gather_kernel<T, true>), s, xs, x, dx, rows, given, N, D, Dp / 8);
-            else LC_LAUNCH(p, "logp (x)", (logp_gather_kernel<T, false>), s, xs, x, dx, rows, given, N, D, Dp / 8);
+            const auto gather = [&](auto kernel) -> int {
+                return in_launches((long long)N * (Dp / 8), [&](long long from, unsigned n) -> int {
+                    const LaunchPlan p = make_plan("logp_gather", {PL, grads}, {N, D}, dim3(n), 256, 0);
+                    LC_LAUNCH(p, "logp (x)", kernel, s, xs, x, dx, rows, given, N, D, Dp / 8, from);
+                    return LC_OK;
+                });
+            };
+            if (int rc = grads ? gather(logp_gather_kernel<T, true>) : gather(logp_gather_kernel<T, false>)) return rc;
         }
         if (w) return launch_planes<PL, 1>("logp (w)", Stored<T>{ws, V, D}, w, Dp, (long long)V * Dp, V, Dp, 0, s);
         return LC_OK;

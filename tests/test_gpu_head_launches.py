@@ -5,6 +5,7 @@ import torch
 
 import head_ref as ref
 import test_gpu_glu as G
+import test_gpu_logp as logp
 
 pytestmark = pytest.mark.gpu
 
@@ -26,3 +27,20 @@ def test_rows_of_the_gated_layer():
     h, _ = G.forward(x, wg, wu, "silu", save=False)
     at = rows_to_look_at(N, 257)
     ref.check("h", h[at], ref.glu(x[at], wg, wu, "silu")[0], ref.tol(torch.bfloat16, D, 1))
+
+
+def test_rows_of_the_answers_and_their_gradients():
+    N, D, V = 1 << 24, 1030, 5
+    print(f"case logp {N} x {D} over {V} words", flush=True)
+    x, w = normal((N, D), 1.0, 3), normal((V, D), 2 * D ** -0.5, 4)
+    tags = torch.arange(N, device="cuda")[:, None] % (V + 1) - 1
+    at = rows_to_look_at(N, 129)
+    got = logp.answers(x, w, tags, 2)
+    few = {k: v[at] for k, v in got.items()}
+    want = logp.definition(x[at], w, tags[at], 2)
+    b = logp.check_answers(x[at], w, tags[at], 2, few, want)
+    dlogp, dentropy = normal((N, 1), 1.0, 5).float(), normal((N,), 1.0, 6).float()
+    dx, _ = logp.gradients(x, w, tags, got, dlogp, dentropy)
+    assert not dx[at][~want["live"]].any()
+    d = logp.d_of(want, tags[at], dlogp[at], dentropy[at])
+    ref.check("dx", dx[at], d @ w.double(), ref.tol(torch.bfloat16, V, 2.25) + 4 * b)   # roundings and scores as in the tests of small sizes

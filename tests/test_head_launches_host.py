@@ -31,3 +31,15 @@ def test_rows_weights_and_gradients_of_the_gated_layer(dtype):
         plans = lc.head_plan_query(B.LC_HEAD_GLU_BWD, N, D, F, dtype)
         assert 0 <= laid_out(plans, "glu (x, w)") - (N + 2 * F) * (-(-D // 8)) < 256
         assert 0 <= laid_out(plans, "glu_bwd (gradients)") - N * (-(-F // 64) * 8) < 256
+
+
+# 2^32 and 2^33 threads; just below, at and behind what one launch takes
+SIZES = [(1 << 24, 2048), (1 << 24, 4096), (1 << 24, 1024), ((1 << 24) - 1, 1024), ((1 << 24) - 77, 1032)]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("N,D", SIZES)
+def test_gathered_rows_of_the_answers(N, D, dtype):
+    for op in (B.LC_HEAD_LOGP_FWD, B.LC_HEAD_LOGP_BWD):
+        threads = laid_out(lc.head_plan_query(op, N, D, 5, dtype), "logp_gather")
+        assert 0 <= threads - N * (D // 8) < 256
