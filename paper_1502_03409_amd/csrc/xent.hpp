@@ -235,9 +235,9 @@ static __global__ __launch_bounds__(256) void cost_kernel(Rows o, float *cost) {
 // The rows that count, gathered as planes; zeros in the masked rows of dx (nullable).  Eight columns a thread; bound by
 // HBM: 8192 rows of 4096 in bf16, 134 MB, 25 us.
 template <typename T>
-__global__ __launch_bounds__(256) void gather_kernel(const T *x, bf16_t *dst, T *dx, Rows o, int N, int D, int pieces) {
+__global__ __launch_bounds__(256) void gather_kernel(const T *x, bf16_t *dst, T *dx, Rows o, int N, int D, int pieces, long long from) {
     constexpr int PL = Planes<T>::N;
-    const long long at = blockIdx.x * 256LL + threadIdx.x;
+    const long long at = from + blockIdx.x * 256LL + threadIdx.x;
     const int n = (int)(at / pieces), c = (int)(at - (long long)n * pieces) * 8;
     if (n >= N) return;
     const int to = o.place[n];
@@ -362,10 +362,12 @@ int xent(const T *x, const T *w, const int64_t *target, const float *scale, floa
     const bool fine = few && grads && PL == 1;   // d in two parts
     if (!few || grads) {
         const int pieces = g.Dp / 8;
-        const long long blocks = ((long long)N * pieces + 255) / 256;
-        const LaunchPlan p = make_plan("xent_gather", {PL}, {N, D}, dim3((unsigned)blocks), 256, 0);
-        LC_PLAN_REQUIRE(p, blocks <= 0x7fffffffLL);
-        LC_LAUNCH(p, "xent (x)", (gather_kernel<T>), s, x, g.x, grads ? dx : nullptr, g.rows, N, D, pieces);
+        const int rc = in_launches((long long)N * pieces, [&](long long from, unsigned n) -> int {
+            const LaunchPlan p = make_plan("xent_gather", {PL}, {N, D}, dim3(n), 256, 0);
+            LC_LAUNCH(p, "xent (x)", (gather_kernel<T>), s, x, g.x, grads ? dx : nullptr, g.rows, N, D, pieces, from);
+            return LC_OK;
+        });
+        if (rc) return rc;
     }
     if (!g.direct && (!few || grads))
         if (int rc = launch_planes<PL, 1>("xent (w)", Stored<T>{w, V, D}, g.w, g.Dp, pw, V, g.Dp, 0, s)) return rc;

@@ -6,6 +6,7 @@ import torch
 import head_ref as ref
 import test_gpu_glu as G
 import test_gpu_logp as logp
+import test_gpu_xent as X
 
 pytestmark = pytest.mark.gpu
 
@@ -44,3 +45,17 @@ def test_rows_of_the_answers_and_their_gradients():
     assert not dx[at][~want["live"]].any()
     d = logp.d_of(want, tags[at], dlogp[at], dentropy[at])
     ref.check("dx", dx[at], d @ w.double(), ref.tol(torch.bfloat16, V, 2.25) + 4 * b)   # roundings and scores as in the tests of small sizes
+
+
+def test_rows_of_the_loss():
+    N, D, V = 1 << 24, 1030, 5
+    print(f"case xent {N} x {D} over {V} words", flush=True)
+    x, w = normal((N, D), 1.0, 7), normal((V, D), 2 * D ** -0.5, 8)
+    target, scale = torch.arange(N, device="cuda") % (V + 1) - 1, torch.ones(N, device="cuda")
+    at = rows_to_look_at(N, 129)
+    loss, _, dx, _ = X.run(x, w, target, scale)
+    want, _, want_dx, _ = ref.xent(x[at], w, target[at], scale[at])
+    b = X.loss_bound(x[at], w)
+    assert float((loss[at].double() - want).abs().max()) <= b + 2.0 ** -23 * float(want.max())
+    assert not dx[at][target[at] < 0].any()
+    ref.check("dx", dx[at], want_dx, ref.tol(torch.bfloat16, V, 2.25) + b)   # as at small sizes

@@ -43,3 +43,11 @@ def test_gathered_rows_of_the_answers(N, D, dtype):
     for op in (B.LC_HEAD_LOGP_FWD, B.LC_HEAD_LOGP_BWD):
         threads = laid_out(lc.head_plan_query(op, N, D, 5, dtype), "logp_gather")
         assert 0 <= threads - N * (D // 8) < 256
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("N,D", SIZES)
+def test_gathered_rows_of_the_loss(N, D, dtype):
+    for op in (B.LC_HEAD_XENT_FWD, B.LC_HEAD_XENT_FWD_BWD):
+        threads = laid_out(lc.head_plan_query(op, N, D, 5, dtype), "xent_gather")
+        assert 0 <= threads - N * (D // 8) < 256
