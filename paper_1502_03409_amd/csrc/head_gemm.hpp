@@ -243,10 +243,11 @@ struct Stager {
             }
         }
         if constexpr (COLS) base = (gbyte_ptr)(o.p0 + r0), base2 = (gbyte_ptr)(o.p1 + r0);
-        else base = (gbyte_ptr)(o.p0 + (long long)top * o.ld), base2 = (gbyte_ptr)(o.p1 + (long long)top * o.ld) + kt * move;
+        else base = (gbyte_ptr)(o.p0 + (long long)top * o.ld), base2 = (gbyte_ptr)(o.p1 + (long long)top * o.ld);
         if (FORM == PAIR && W == 8 && wave >= 4) base = base2;
         if (FORM == COLPAIR && kt * kStep >= half) base = base2, base += (kt - half / kStep) * move;
         else base += kt * move;
+        if (FORM == PAIR) base2 += kt * move;
         trimmed = false;
         trim();
     }

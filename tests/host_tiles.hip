@@ -71,7 +71,28 @@ static void walk_blocks(int n) {
     printf("symmetric 32 4 %d %d 0 %d %d\n", PLANES, n, *std::min_element(writers.begin(), writers.end()), *std::max_element(writers.begin(), writers.end()));
 }
 
+// Where a wave's loads of a tile of N rows begin, in bytes from where they do in a contraction that begins at index 0, for one that begins at step kt;
+// of both matrices, where a pair is read.  Every load moves by whole rows' bytes of kt steps.
+template <int FORM, int N, int PL, int W>
+static void walk_starts(int kt) {
+    static bf16_t a[512 * 512], b[512 * 512];
+    const bool pair = FORM == PAIR;
+    Operand o = {a, pair ? b : a, 512, 0, 64, 0, 0};
+    for (int wave = 0; wave < W; ++wave) {
+        Stager<FORM, N, PL, W> first, later;
+        first.init(o, 0, 0, 512, Format<PL>::B, wave, 5), later.init(o, 0, kt, 512, Format<PL>::B, wave, 5);
+        const long long moved = later.base - first.base, moved2 = pair && W == 4 ? later.base2 - first.base2 : moved;
+        const bool second = pair && W == 8 && wave >= 4;
+        const bool inside = (const char *)later.base >= (const char *)(second ? b : a) && (const char *)later.base < (const char *)((second ? b : a) + 512 * 512);
+        printf("start %d %d %d %d %lld %lld %lld %d\n", FORM, W, wave, kt, moved, moved2, (FORM == COL ? kt * kStep * o.ld : kt * kStep) * 2, inside);
+    }
+}
+
 int main() {
+    for (int kt : {0, 1, 3}) {
+        walk_starts<ROW, 256, 1, 4>(kt), walk_starts<ROW, 256, 1, 8>(kt), walk_starts<PAIR, 256, 1, 4>(kt), walk_starts<PAIR, 128, 1, 4>(kt);
+        walk_starts<PAIR, 256, BYTES, 8>(kt), walk_starts<COL, 256, 1, 4>(kt), walk_starts<COL, 256, 1, 8>(kt);
+    }
     for (int n : {7, 32, 75}) walk_blocks<1>(n), walk_blocks<2>(n);
     for (int n : {64, 200, 256, 333, 520, 712}) {
         walk_symmetric<64, 4, 1>(n, false), walk_symmetric<64, 4, 2>(n, true);

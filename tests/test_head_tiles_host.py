@@ -51,3 +51,11 @@ def test_the_walk_has_all_layouts(walked, dtype):
     assert seen <= have and {s for s, _ in seen} == {32, 64, 128, 192, 256}
     for shape in LARGE:
         assert (256, 8) in symmetric_layouts(*shape, dtype), shape
+
+
+def test_loads_of_a_later_part_begin_where_it_does(walked):
+    """Of a contraction in parts, for every wave and both matrices of a pair."""
+    rows = [list(map(int, w[1:])) for w in walked if w[0] == "start"]
+    assert len(rows) == 3 * (4 + 8 + 4 + 4 + 8 + 4 + 8)
+    for form, waves, wave, step, moved, moved2, want, inside in rows:
+        assert moved == moved2 == want and inside, f"form {form}, wave {wave} of {waves}: step {step} begins {moved} and {moved2} bytes on, not {want}"
