@@ -148,7 +148,7 @@ int logp_bwd(const void *x, const void *w, const int64_t *tags, const float *log
              size_t ws_bytes, void *hip_stream);
 
 /* Host only.  Scratch for muon_step; 0 for invalid arguments.  What is enough for a stack is enough for a shorter one.  It is bounded for
- * any number of matrices (about 4 GiB, or what one matrix takes). */
+ * any number of matrices (4 GiB, or what one matrix takes). */
 size_t muon_workspace_bytes(int32_t count, int32_t rows, int32_t cols, int dtype);
 
 /* A step of gradient descent on each matrix of a stack [count][rows][cols] with an orthogonalised update:

@@ -839,6 +839,7 @@ int launch_short(const Operand &X, const Operand &Q, int rows, int cols, int ite
 }
 
 constexpr long long kStackBytes = 1LL << 30;   // of X's planes at a time
+constexpr long long kScratchBytes = 4LL << 30, kRestBytes = 4 * kMostParts + 4096;   // of all that several matrices take; of parts, and of what rounds pieces up
 
 // Products of `items` matrices: short sides, the long side, the update of X.
 struct MuonShapes {
@@ -877,17 +878,19 @@ struct MuonScratch {
     MuonScratch(Scratch &sc, int count, int rows, int cols) {
         small = std::min(rows, cols);
         ld = (int)round_up(cols, 8), lds = (int)round_up(small, 8);
-        const long long values = (long long)rows * ld;
-        most = (int)std::max<long long>(1, std::min<long long>({count, kMostGroups, kStackBytes / (2 * PLANES * values)}));
+        const long long values = (long long)rows * ld, each = (long long)small * lds;
+        const bool chain = small <= kChain, grouped = !chain && rows != cols;   // whatever group_of says of a stack of this length
         parts = (int)std::min<long long>(kMostSums, ((long long)rows * cols + 8191) / 8192);
+        const long long bytes = 8 * parts + 2 * (PLANES * (2 * values + (grouped ? 6 : 2) * each) + (chain ? 2 * each : 0));
+        most = (int)std::max<long long>(1, std::min<long long>({count, kMostGroups, kStackBytes / (2 * PLANES * values), (kScratchBytes - kRestBytes) / bytes}));
         partial = sc.take<double>((long long)most * parts);
         for (auto &p : x) p = sc.take<bf16_t>(PLANES * most * values);
-        const long long square = PLANES * most * (long long)small * lds;
+        const long long square = PLANES * most * each;
         s = sc.take<bf16_t>(square);
         q[0] = sc.take<bf16_t>(square);
         group = group_of(most, rows, cols, PLANES, Format<MuonFormat<T>::PL>::PAIRS);
-        if (small <= kChain) a = sc.take<bf16_t>(2LL * most * small * lds);
-        else if (rows != cols)   // whatever group_of says of a stack of this length
+        if (chain) a = sc.take<bf16_t>(2 * most * each);
+        if (grouped)
             for (bf16_t **p : {&a, &t, &q[1], &q[2]}) *p = sc.take<bf16_t>(square);
         // of as many matrices as are cut along the contraction; a shorter stack may be cut into more parts
         const long long cut = std::min<long long>(most, (long long)(kSplitTiles / stack_tiles(MuonShapes(1, rows, cols).sx, 128)));

@@ -1,4 +1,8 @@
-"""Rows and weights of the head's largest sizes, planned on the host: they are laid out by launches of fewer than 2^32 threads."""
+"""Rows, weights and stacks of the head's largest sizes, planned on the host: they are laid out by launches of fewer than 2^32 threads, and scratch
+is no more than is said."""
+import math
+import random
+
 import pytest
 
 import paper_1502_03409_amd as lc
@@ -51,3 +55,17 @@ def test_gathered_rows_of_the_loss(N, D, dtype):
     for op in (B.LC_HEAD_XENT_FWD, B.LC_HEAD_XENT_FWD_BWD):
         threads = laid_out(lc.head_plan_query(op, N, D, 5, dtype), "xent_gather")
         assert 0 <= threads - N * (D // 8) < 256
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
+def test_scratch_of_a_stack_is_bounded(dtype):
+    """4 GiB, or what one matrix takes; sides that differ little have the most places of the short side's square beside X's."""
+    rng = random.Random(10)
+    shapes = [(5000, 1000, 1001), (100000, 130, 131), (65536, 600, 601), (1 << 20, 128, 128), (1 << 24, 1, 1), (1 << 24, 3, 300), (40, 5000, 4500)]
+    for _ in range(400):
+        rows, cols = (int(round(math.exp(rng.uniform(0, math.log(30000))))) for _ in range(2))
+        shapes.append((rng.randrange(1, 1 << 24), rows, rng.choice([cols, rows, rows + 1])))
+    for count, rows, cols in shapes:
+        count = min(count, (1 << 40) // (rows * cols))
+        one, all_of_them = (lc.muon_workspace_bytes(n, rows, cols, dtype) for n in (1, count))
+        assert 0 < all_of_them <= max(one, 4 << 30), (count, rows, cols, all_of_them / 2 ** 30)
