@@ -540,10 +540,14 @@ inline StackCut choose_stack_cut(const Shape &sh, int pairs, int how) {
 
 template <int PL, int FA, int FB, typename Epi>
 int launch_stack(const char *name, const Operand &A, const Operand &B, const Shape &sh, const StackCut &c, const Epi &epi, hipStream_t s) {
+    // Two planes from operands of one are the first A of a short side up to kChain, one tile of 128 or larger: larger ones begin, end and step
+    // longer, so the estimate takes none.
+    constexpr bool LARGE = !(PL == HALF && std::is_same<Epi, PlaneEpi<2, true>>::value);
     if constexpr (FA == ROW && !std::is_same<Epi, StackPartEpi>::value)
         if (c.tile == 32) return launch_block<PL, FB>(name, A, B, sh, epi, s);
-    if (c.tile == 256) return launch_tiles<PL, FA, FB, 256, 256, 3, 2, 8>(name, A, B, sh, c.splits, epi, s);
-    if constexpr (FA == ROW && FB == ROW)
+    if constexpr (LARGE)
+        if (c.tile == 256) return launch_tiles<PL, FA, FB, 256, 256, 3, 2, 8>(name, A, B, sh, c.splits, epi, s);
+    if constexpr (LARGE && FA == ROW && FB == ROW)
         if (c.tile == 192) return launch_tiles<PL, FA, FB, 192, 192, 3, 2>(name, A, B, sh, c.splits, epi, s);
     if (c.tile == 64) return launch_tiles<PL, FA, FB, 64, 64, 3, 2>(name, A, B, sh, c.splits, epi, s);
     return launch_tiles<PL, FA, FB, 128, 128, 3, 2>(name, A, B, sh, c.splits, epi, s);

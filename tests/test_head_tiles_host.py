@@ -1,5 +1,7 @@
 """Tiles of the head's products, walked on the host: the sources' own device functions, compiled for the CPU (host_tiles.hip)."""
 import os
+import random
+import re
 import subprocess
 from pathlib import Path
 
@@ -59,3 +61,19 @@ def test_loads_of_a_later_part_begin_where_it_does(walked):
     assert len(rows) == 3 * (4 + 8 + 4 + 4 + 8 + 4 + 8)
     for form, waves, wave, step, moved, moved2, want, inside in rows:
         assert moved == moved2 == want and inside, f"form {form}, wave {wave} of {waves}: step {step} begins {moved} and {moved2} bytes on, not {want}"
+
+
+def test_short_sides_have_the_tiles_that_they_take():
+    """Sides of up to 128 take no tile of more than 128 for their first product, and with one plane an operand, where its two planes make
+    it a kernel of its own, there are no others."""
+    rng = random.Random(11)
+    for dtype in TYPES:
+        for _ in range(1500):
+            short, long = rng.randrange(1, 129), int(2 ** rng.uniform(0, 20))
+            count = min(1 << 24, int(2 ** rng.uniform(0, 24)), max(1, (1 << 34) // (short * long)))
+            rows, cols = (short, long) if rng.random() < 0.5 else (long, short)
+            plans = lc.head_plan_query(B.LC_HEAD_MUON, count, rows, cols, dtype)
+            tiles = {p["tparam"][3] for p in plans if p["kernel"] == "muon_step (A)" and p["arg"][5] == 1 and p["tparam"][3]}
+            assert tiles <= {32, 64, 128}, (count, rows, cols, tiles)
+    kernels = set(re.findall(rb"gemm_kernelILi4ELi\dELi\dELi(\d+)E\w*?PlaneEpiILi2ELb1EE", build.LIB.read_bytes()))
+    assert kernels == {b"64", b"128"}
