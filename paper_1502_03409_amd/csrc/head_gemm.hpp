@@ -733,7 +733,9 @@ int launch_gemm(const char *name, const Operand &A, const Operand &B, const Shap
 
 // A product of up to kNarrow rows, as mini-batches that are answered have, with tiles of 64 rows: what waits for weights from HBM is more
 // workgroups, and no row is padded to 128 (8-bit, 4096 long, tiles of 64 x 128 and 128 x 128: 192 rows times 8192 26 and 37 us, in fewer steps at a
-// time 30, times 100003 158 and 173; 64 rows times 100003 107 and 113, 101 with 64 x 64).
+// time 30, times 100003 158 and 173; 64 rows times 100003 107 and 113, 101 with 64 x 64).  A fourth tile ends what is gained: 8-bit, 192, 193 and 256
+// rows times 100003 145, 168 and 181 us so and 153, 154 and 163 in the others, bf16, 1024 long, times 20011 14.5, 21.8 and 22.0 so and 18.6, 18.6 and
+// 18.9 in the others; short of that only bf16 times 100003 loses (192 rows 263 and 247), and times 8192 up to 256 rows would gain (29 and 35).
 constexpr int kNarrow = 192;
 template <int PL, int FB, int BN, typename Epi>
 int launch_narrow(const char *name, const Operand &A, const Operand &B, const Shape &sh, const Epi &epi, hipStream_t s) {

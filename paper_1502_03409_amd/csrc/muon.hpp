@@ -505,8 +505,10 @@ struct StackCut {
 };
 // The cut that takes least by an estimate in microseconds from measured times: what begins and ends a tile, and for each 64 indices and pair of
 // planes a step of the tiles that share the fullest compute unit.  fp16, n x n times its like, the half below the diagonal, tiles of 64 / 128 /
-// 192 / 256: n = 256 5.5 / 7.0 / 12.6 / 15.6 us, 1024 11.3 / 13.3 / 22.6 / 34, 2048 22.1 / 22.8 / 34.8 / 46, 4096 145 / 104 / 86 / 102, two of 4096
-// 281 / 182 / 157 / 201; two of 8192 x 4096 times 4096 x 4096 with tiles of 128 / 256 563 / 473, with the update 621 / 547.  Parts cost a kernel and
+// 192 / 256: n = 256 4.9 / 7.0 / 12.4 / 12.0 us, 1024 9.0 / 12.7 / 21.9 / 27, 2048 21.9 / 24.4 / 34.8 / 45, 4096 149 / 99 / 77 / 92, two of 4096
+// 260 / 167 / 150 / 188, 5120 295 / 168 / 159 / 128; two of 8192 x 4096 times 4096 x 4096 with tiles of 128 / 256 563 / 473, with the update 621 / 547.
+// Two planes: 4096 367 / 283 / 212 / 296, 5120 671 / 420 / 454 / 392, four of 2048 177 / 151 / 203 / 191; what tiles of 256 lose there is not in the
+// estimate (191 us taken for 139): their epilogue keeps 203 registers of a lane in scratch.  Parts cost a kernel and
 // their bytes: 1021 x 20011 times its transpose 152 us whole and 33 + 7 in 14.  Tiles of 192 read rows only.
 //
 // Products whose workgroups of 32 x 32 hardly share compute units take those (five steps in fp32, symmetric products in tiles of 32 and of 64:
@@ -735,7 +737,8 @@ int launch_chain(const bf16_t *a, bf16_t *q, long long plane, long long each, in
 // ---------------------------------------------------------------------------------------------------------------------------
 // X Q where rows are short, at most kShort values: a wave keeps Q and lets rows of X stream by, 32 at a time, from memory to registers and back.  Tiles
 // through LDS begin and end once for each 64 rows and are wide for nobody (3249 of 768 x 16 in fp32: 198 us, and 298 where w is
-// updated; 1485 of 5248 x 19 in bf16 506 and 1893).
+// updated; 1485 of 5248 x 19 in bf16 506 and 1893).  Tall matrices only: few rows of many columns take tiles (1485 of 19 x 5248 in bf16 2.17 ms a step, 1.41
+// lying the other way).
 constexpr int kShort = 64, kShortBlocks = 4;   // blocks of 32 rows a wave
 template <typename T, int PL, int PLANES, int NT, bool UPDATE>
 __global__ __launch_bounds__(256) void muon_short_kernel(const bf16_t *x, long long plane, const bf16_t *q, long long qplane, int rows, int cols, int ld,
